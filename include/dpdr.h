@@ -48,9 +48,11 @@ typedef enum {
     DPDR_INT32 = 0,      /* int32, sum wraps mod 2^32                       */
     DPDR_FLOAT32 = 1,    /* IEEE float32, sum rounded to nearest even        */
     DPDR_MAT2X2_U32 = 2, /* 2x2 uint32 matrix, row-major a,b,c,d (16 bytes) */
-    DPDR_MAT2X2_F32 = 3  /* 2x2 float32 matrix, row-major (16 bytes); each
+    DPDR_MAT2X2_F32 = 3, /* 2x2 float32 matrix, row-major (16 bytes); each
                             product entry is two rounded products and one
                             rounded sum, never fused                        */
+    DPDR_BFLOAT16 = 4,   /* operands of the projections below only           */
+    DPDR_FLOAT16 = 5     /* (IEEE binary16), not of a reduction              */
 } dpdr_dtype;
 
 typedef enum {
@@ -383,6 +385,103 @@ int dpdr_plan_sync(dpdr_plan_t plan, dpdr_stream_t stream);
 int dpdr_allreduce_schedule_noalloc(int p, int64_t m, dpdr_dtype dtype,
                                     dpdr_op op, int b, const void* const* x,
                                     void* const* y, dpdr_stream_t stream);
+
+/* ------------------------------------------------------- projections
+ * What the ranks of a split model compute on both sides of a reduction: the
+ * matrix products whose partial results (a row-parallel product, the input
+ * gradient of a column-parallel one, the weight gradients of data-parallel
+ * ranks) dpdr_allreduce adds up in float32.  Two operators, each with its
+ * gradients.  Operands are bfloat16 or float16; products are summed in
+ * float32 on the tensor cores.
+ *
+ *   linear   z = x w^T + bias,  y = act(z) + residual
+ *            dz = dy * act'(z);  dx = dz w, dw = dz^T x, dbias = sum of the
+ *            rows of dz (the residual's gradient is dy itself)
+ *   gated    g = x w_gate^T, u = x w_up^T,  h = act(g) * u
+ *            dg = dh * u * act'(g), du = dh * act(g);
+ *            dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x
+ *
+ * x: rows by n_in; w: n_out (n_hidden) by n_in; bias: n_out, contiguous.
+ * Every value but three is held in float32 until it is stored: dz, dg and du
+ * are rounded to the operand type before the products that take them (they
+ * are operands of the tensor cores), and results are rounded to their type.
+ *
+ * Matrices are given by address and strides in elements, so a transposed or
+ * sliced array is passed as it lies.  Operands may have any strides >= 0
+ * (zero: broadcast); those with one stride of 1, the other a multiple of 8
+ * and a 16-byte aligned address are read in place, others are first copied
+ * into the plan's scratch.  Results need col_stride 1 and rows that do not
+ * overlap.  A result overlaps nothing else, except that y may be the
+ * residual itself (same address and strides). */
+typedef enum {
+    DPDR_ACT_NONE = 0,
+    DPDR_ACT_RELU = 1,
+    DPDR_ACT_GELU = 2,       /* z Phi(z), Phi the normal distribution       */
+    DPDR_ACT_GELU_TANH = 3,  /* its tanh form, with the cubic term 0.044715 */
+    DPDR_ACT_SILU = 4,       /* z / (1 + exp(-z))                           */
+    DPDR_ACT_SIGMOID = 5     /* 1 / (1 + exp(-z))                           */
+} dpdr_act;
+
+typedef struct {
+    void* data;              /* device memory, aligned to its element       */
+    int64_t row_stride;      /* elements                                    */
+    int64_t col_stride;
+} dpdr_matrix;
+
+/* Opaque plan of a projection: its sizes and types, and the device scratch
+ * that some calls need (made by the first such call, of the size that
+ * max_rows rows need; make that call before any stream capture). */
+typedef struct dpdr_proj_s* dpdr_proj_t;
+
+/* Plans on the current CUDA device.  max_rows >= 0, the other sizes >= 1,
+ * each below 2^31.  operands: DPDR_BFLOAT16 or DPDR_FLOAT16; result (y, h,
+ * the residual, and dy, dh) and gradients (dx, dw, dbias): the operands'
+ * type or DPDR_FLOAT32.  The bias has the operands' type.  NULL on error. */
+dpdr_proj_t dpdr_linear_plan(int64_t max_rows, int64_t n_in, int64_t n_out,
+                             dpdr_dtype operands, dpdr_dtype result,
+                             dpdr_dtype gradients, dpdr_act act);
+dpdr_proj_t dpdr_gated_plan(int64_t max_rows, int64_t n_in, int64_t n_hidden,
+                            dpdr_dtype operands, dpdr_dtype result,
+                            dpdr_dtype gradients, dpdr_act act);
+
+/* Forward calls, 0 <= rows <= max_rows.  bias, residual and pre may be NULL.
+ * pre (float32; z as rows by n_out, or g and u side by side as rows by
+ * 2 n_hidden) keeps the projections for the backward call.  Asynchronous on
+ * stream.  Two calls on one plan that overlap on the GPU (two streams) race
+ * on its scratch. */
+int dpdr_linear(dpdr_proj_t plan, int64_t rows, const dpdr_matrix* x,
+                const dpdr_matrix* w, const void* bias,
+                const dpdr_matrix* residual, const dpdr_matrix* y,
+                const dpdr_matrix* pre, dpdr_stream_t stream);
+int dpdr_gated(dpdr_proj_t plan, int64_t rows, const dpdr_matrix* x,
+               const dpdr_matrix* w_gate, const dpdr_matrix* w_up,
+               const dpdr_matrix* h, const dpdr_matrix* pre,
+               dpdr_stream_t stream);
+
+/* Backward calls.  Any gradient may be NULL and is then not computed (of the
+ * two weight gradients of a gated plan, both or neither).  With pre, what
+ * the forward call kept there is used, and w and bias serve dx only; without
+ * it the projections are computed again.  rows == 0 writes zero weight and
+ * bias gradients. */
+int dpdr_linear_backward(dpdr_proj_t plan, int64_t rows, const dpdr_matrix* x,
+                         const dpdr_matrix* w, const void* bias,
+                         const dpdr_matrix* dy, const dpdr_matrix* pre,
+                         const dpdr_matrix* dx, const dpdr_matrix* dw,
+                         void* dbias, dpdr_stream_t stream);
+int dpdr_gated_backward(dpdr_proj_t plan, int64_t rows, const dpdr_matrix* x,
+                        const dpdr_matrix* w_gate, const dpdr_matrix* w_up,
+                        const dpdr_matrix* dh, const dpdr_matrix* pre,
+                        const dpdr_matrix* dx, const dpdr_matrix* dw_gate,
+                        const dpdr_matrix* dw_up, dpdr_stream_t stream);
+
+/* Waits for stream, then reports and clears any device-side error of the
+ * plan's kernels: DPDR_ERR_TIMEOUT when one of their bounded waits expired,
+ * after which the results of the calls since the last report are unknown. */
+int dpdr_proj_sync(dpdr_proj_t plan, dpdr_stream_t stream);
+
+/* Releases the plan's memory; no call on it may still be running.  NULL is a
+ * no-op. */
+void dpdr_proj_destroy(dpdr_proj_t plan);
 
 /* ------------------------------------------------------------ errors */
 int dpdr_last_error(void);

@@ -19,5 +19,6 @@ from ._native import (DPDR_ERR_CUDA, DPDR_ERR_INVALID,  # noqa: F401
                       OPT_SKIP_RANK, OPT_SPLIT_DEPTH, OPT_WAIT_LIMIT_NS, DpdrError,
                       Plan,
                       block_count_rule, blocks, lib, tree)
+from .projections import Gated, Linear  # noqa: F401
 
-__all__ = ["Plan", "DpdrError", "tree", "blocks", "block_count_rule", "lib"]
+__all__ = ["Plan", "Linear", "Gated", "DpdrError", "tree", "blocks", "block_count_rule", "lib"]

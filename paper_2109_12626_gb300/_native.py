@@ -13,6 +13,7 @@ from typing import Sequence
 import numpy as np
 
 DPDR_INT32, DPDR_FLOAT32, DPDR_MAT2X2_U32, DPDR_MAT2X2_F32 = 0, 1, 2, 3
+DPDR_BFLOAT16, DPDR_FLOAT16 = 4, 5
 DPDR_OP_SUM, DPDR_OP_MATMUL = 0, 1
 (DPDR_OK, DPDR_ERR_INVALID, DPDR_ERR_CUDA, DPDR_ERR_TIMEOUT,
  DPDR_ERR_NOT_COOPERATIVE, DPDR_ERR_OOM) = range(6)
@@ -49,6 +50,14 @@ SIGNATURES = {
     "dpdr_allreduce_schedule_noalloc": (ctypes.c_int, [ctypes.c_int, ctypes.c_int64,
                                                        ctypes.c_int, ctypes.c_int,
                                                        ctypes.c_int, _P, _P, _P]),
+    "dpdr_linear_plan": (_P, [ctypes.c_int64] * 3 + [ctypes.c_int] * 4),
+    "dpdr_gated_plan": (_P, [ctypes.c_int64] * 3 + [ctypes.c_int] * 4),
+    "dpdr_linear": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 7),
+    "dpdr_gated": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 6),
+    "dpdr_linear_backward": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 9),
+    "dpdr_gated_backward": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 9),
+    "dpdr_proj_sync": (ctypes.c_int, [_P, _P]),
+    "dpdr_proj_destroy": (None, [_P]),
     "dpdr_last_error": (ctypes.c_int, []),
     "dpdr_last_error_message": (ctypes.c_char_p, []),
     "dpdr_status_string": (ctypes.c_char_p, [ctypes.c_int]),

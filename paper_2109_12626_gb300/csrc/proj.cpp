@@ -1,0 +1,450 @@
+// proj.cpp -- host side of the projections: plans, argument checks, scratch
+// and the sequence of kernels of each call.
+#include <algorithm>
+#include <cstdint>
+#include <cstdio>
+#include <new>
+#include <utility>
+
+#include "proj.h"
+
+namespace dpdr {
+namespace proj {
+
+namespace {
+
+constexpr int64_t kMost = (int64_t(1) << 31) - 1;
+
+// A refusal as "who: what", without allocating.
+int refuse(const char* who, const char* what, const char* more = "")
+{
+    char msg[200];
+    std::snprintf(msg, sizeof msg, "%s: %s%s%s", who, what, *more ? " " : "", more);
+    return fail_c(DPDR_ERR_INVALID, msg);
+}
+
+bool is_half_kind(int t) { return t == DPDR_BFLOAT16 || t == DPDR_FLOAT16; }
+
+Proj* make(bool gated, int64_t max_rows, int64_t n_in, int64_t n_out, int operands, int result, int gradients,
+           int act, const char* who)
+{
+    auto bad = [&](const char* what) {
+        refuse(who, what);
+        return nullptr;
+    };
+    if (max_rows < 0 || max_rows > kMost || n_in < 1 || n_in > kMost || n_out < 1 || n_out > kMost)
+        return bad("need 0 <= max_rows and 1 <= sizes, below 2^31");
+    if (!is_half_kind(operands)) return bad("operands are bfloat16 or float16");
+    if ((result != operands && result != DPDR_FLOAT32) || (gradients != operands && gradients != DPDR_FLOAT32))
+        return bad("result and gradients have the operands' type or float32");
+    if (act < DPDR_ACT_NONE || act > DPDR_ACT_SIGMOID) return bad("unknown activation");
+    Proj* P = new (std::nothrow) Proj;
+    if (!P) {
+        fail_c(DPDR_ERR_OOM, "projection plan: host allocation");
+        return nullptr;
+    }
+    P->gated = gated;
+    P->max_rows = max_rows;
+    P->n_in = n_in;
+    P->n_out = n_out;
+    P->half = operands == DPDR_FLOAT16;
+    P->out_f32 = result == DPDR_FLOAT32;
+    P->grad_f32 = gradients == DPDR_FLOAT32;
+    P->act = act;
+    cudaError_t e = cudaGetDevice(&P->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&P->num_sms, cudaDevAttrMultiProcessorCount, P->device);
+    if (e == cudaSuccess) e = cudaMalloc(&P->err, 256);
+    if (e == cudaSuccess) e = cudaMemset(P->err, 0, 256);
+    if (e != cudaSuccess) {
+        cuda_fail_c(e, who);
+        cudaFree(P->err);
+        delete P;
+        return nullptr;
+    }
+    return P;
+}
+
+// A matrix argument in bytes: which range of memory it touches, and which
+// part of each row of its pitch.
+struct Span {
+    uintptr_t lo = 0, hi = 0, pitch = 0, width = 0;
+};
+
+Span span_of(const dpdr_matrix& m, int64_t rows, int64_t cols, int esize)
+{
+    Span s;
+    if (rows == 0 || cols == 0) return s;
+    s.lo = reinterpret_cast<uintptr_t>(m.data);
+    s.hi = s.lo + (uintptr_t(rows - 1) * uintptr_t(m.row_stride) + uintptr_t(cols - 1) * uintptr_t(m.col_stride) + 1) * esize;
+    s.pitch = uintptr_t(m.row_stride) * esize;
+    s.width = m.col_stride == 1 ? uintptr_t(cols) * esize : s.pitch;
+    return s;
+}
+
+// Whether two arguments may share a byte.  Column slices of one wider array
+// (equal pitch, disjoint parts of it) do not.
+bool overlap(const Span& a, const Span& b)
+{
+    if (a.lo == a.hi || b.lo == b.hi || a.hi <= b.lo || b.hi <= a.lo) return false;
+    if (a.pitch == b.pitch && a.pitch > 0 && a.width <= a.pitch && b.width <= b.pitch) {
+        const uintptr_t d = b.lo >= a.lo ? (b.lo - a.lo) % a.pitch : (a.pitch - (a.lo - b.lo) % a.pitch) % a.pitch;
+        if (d >= a.width && d + b.width <= a.pitch) return false;
+    }
+    return true;
+}
+
+// The arguments of one call, checked as they are added.
+struct Args {
+    const char* who;
+    Span in[6], out[4];
+    int nin = 0, nout = 0;
+    int rc = DPDR_OK;
+
+    void refuse(const char* name, const char* what)
+    {
+        if (rc == DPDR_OK) rc = proj::refuse(who, name, what);
+    }
+    void input(const char* name, const dpdr_matrix* m, int64_t rows, int64_t cols, int esize)
+    {
+        if (!m) return refuse(name, "is NULL");
+        check(name, *m, rows, cols, esize);
+        if (m->row_stride < 0 || m->col_stride < 0) return refuse(name, "has a negative stride");
+        in[nin++] = span_of(*m, rows, cols, esize);
+    }
+    void output(const char* name, const dpdr_matrix* m, int64_t rows, int64_t cols, int esize)
+    {
+        if (!m) return refuse(name, "is NULL");
+        check(name, *m, rows, cols, esize);
+        if (cols > 1 && m->col_stride != 1) return refuse(name, "needs col_stride 1");
+        if (rows > 1 && m->row_stride < cols) return refuse(name, "has rows that overlap");
+        dpdr_matrix unit = *m;
+        unit.col_stride = 1;
+        out[nout++] = span_of(unit, rows, cols, esize);
+    }
+    void check(const char* name, const dpdr_matrix& m, int64_t rows, int64_t cols, int esize)
+    {
+        if (rows == 0 || cols == 0) return;
+        if (!m.data) return refuse(name, "has no address");
+        if (reinterpret_cast<uintptr_t>(m.data) % uintptr_t(esize)) refuse(name, "is not aligned to its element");
+        // byte offsets stay within 2^62
+        const __int128 far = (__int128)(rows - 1) * m.row_stride + (__int128)(cols - 1) * m.col_stride;
+        if (far > (__int128(1) << 59)) refuse(name, "reaches too far");
+    }
+    void vector(const char* name, const void* p, int64_t n, int esize, bool result)
+    {
+        const dpdr_matrix m{const_cast<void*>(p), n, 1};
+        if (result) output(name, &m, 1, n, esize);
+        else input(name, &m, 1, n, esize);
+    }
+    // no result may touch another argument (but the residual, which is checked
+    // on its own)
+    int done()
+    {
+        for (int i = 0; i < nout && rc == DPDR_OK; i++) {
+            for (int k = 0; k < nin; k++)
+                if (overlap(out[i], in[k])) return rc = proj::refuse(who, "a result overlaps an input");
+            for (int k = 0; k < i; k++)
+                if (overlap(out[i], out[k])) return rc = proj::refuse(who, "two results overlap");
+        }
+        return rc;
+    }
+};
+
+int check_plan(const Proj* P, bool gated, int64_t rows, const char* who)
+{
+    if (!P) return refuse(who, "NULL plan");
+    if (P->gated != gated) return refuse(who, "a plan of the other operator");
+    if (rows < 0 || rows > P->max_rows) return refuse(who, "need 0 <= rows <= max_rows");
+    return DPDR_OK;
+}
+
+// Device scratch of at least `bytes`; grown by a plain allocation, before
+// which the old one's last use has finished (cudaFree waits for it).
+int reserve(Proj* P, size_t bytes)
+{
+    if (bytes <= P->scratch_bytes) return DPDR_OK;
+    cudaFree(P->scratch);
+    P->scratch = nullptr;
+    P->scratch_bytes = 0;
+    const cudaError_t e = cudaMalloc(&P->scratch, bytes);
+    if (e != cudaSuccess) return cuda_fail_c(e, "projection scratch");
+    P->scratch_bytes = bytes;
+    return DPDR_OK;
+}
+
+Operand rows_of(const dpdr_matrix& m) { return {static_cast<const char*>(m.data), m.row_stride, m.col_stride}; }
+Operand cols_of(const dpdr_matrix& m) { return {static_cast<const char*>(m.data), m.col_stride, m.row_stride}; }
+
+Epilogue epilogue_of(const Proj* P)
+{
+    Epilogue e;
+    e.act = P->act;
+    e.half = P->half;
+    return e;
+}
+
+void set_other(Epilogue& e, const dpdr_matrix& m, int f32)
+{
+    e.other = static_cast<const char*>(m.data);
+    e.other_rs = m.row_stride;
+    e.other_cs = m.col_stride;
+    e.other_f32 = f32;
+}
+
+int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+size_t upto256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+// The forward product, or with slope the same product finished as dz (dg, du).
+static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix* w0, const dpdr_matrix* w1,
+                   const void* bias, const Epilogue& e, cudaStream_t s)
+{
+    Product p;
+    p.kind = P->gated ? kPair : kSingle;
+    p.M = rows;
+    p.N = P->n_out;
+    p.K = P->n_in;
+    p.a[0] = rows_of(x);
+    p.b[0] = rows_of(*w0);
+    if (w1) p.b[1] = rows_of(*w1);
+    p.e = e;
+    p.e.bias = bias;
+    return product_launch(P, p, s);
+}
+
+struct Backward {
+    const dpdr_matrix *x, *w0, *w1, *dy, *pre, *dx, *dw0, *dw1;
+    const void* bias;
+    void* dbias;
+};
+
+static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
+{
+    const int n = P->gated ? 2 : 1;
+    const int64_t N = P->n_out, K = P->n_in;
+    if (!c.dx && !c.dw0 && !c.dbias) return DPDR_OK;
+    // dz as operands: dy itself where it already is (no activation, 16 bits)
+    const bool as_is = !P->gated && P->act == DPDR_ACT_NONE && !P->out_f32;
+    const int64_t ld = padded(N);
+    const size_t dz_bytes = as_is ? 0 : upto256(size_t(P->max_rows) * size_t(ld) * 2);
+    const size_t sum_bytes = c.dbias ? upto256(size_t(column_sum_parts(P->max_rows)) * size_t(N) * 4) : 0;
+    int rc = reserve(P, n * dz_bytes + sum_bytes);
+    if (rc) return rc;
+    dpdr_matrix dz[2] = {{P->scratch, ld, 1}, {P->scratch + dz_bytes, ld, 1}};
+    float* sums = reinterpret_cast<float*>(P->scratch + n * dz_bytes);
+    Epilogue e = epilogue_of(P);
+    if (as_is) {
+        dz[0] = *c.dy;
+    } else {
+        e.finish = kSlope;
+        set_other(e, *c.dy, P->out_f32);
+        e.out = static_cast<char*>(dz[0].data);
+        e.out2 = static_cast<char*>(dz[1].data);
+        e.out_rs = e.out2_rs = ld;
+        if (c.pre) {
+            e.pre = static_cast<float*>(c.pre->data);
+            e.pre_rs = c.pre->row_stride;
+            e.pre_up = N;
+            rc = slope_launch(e, P->gated, rows, N, s);
+        } else if (!P->gated && P->act == DPDR_ACT_NONE) {
+            rc = slope_launch(e, false, rows, N, s);   // dy rounded to the operand type
+        } else {
+            rc = forward(P, rows, *c.x, c.w0, c.w1, c.bias, e, s);
+        }
+        if (rc) return rc;
+    }
+    if (c.dx) {
+        Product p;
+        p.kind = P->gated ? kChain : kSingle;
+        p.M = rows;
+        p.N = K;
+        p.K = N;
+        for (int i = 0; i < n; i++) {
+            p.a[i] = rows_of(dz[i]);
+            p.b[i] = cols_of(i ? *c.w1 : *c.w0);
+        }
+        p.e.half = P->half;
+        p.e.out = static_cast<char*>(c.dx->data);
+        p.e.out_rs = c.dx->row_stride;
+        p.e.out_f32 = P->grad_f32;
+        rc = product_launch(P, p, s);
+        if (rc) return rc;
+    }
+    if (c.dw0) {
+        Product p;
+        p.kind = P->gated ? kTwin : kSingle;
+        p.M = N;
+        p.N = K;
+        p.K = rows;
+        for (int i = 0; i < n; i++) p.a[i] = cols_of(dz[i]);
+        p.b[0] = cols_of(*c.x);
+        p.e.half = P->half;
+        p.e.out = static_cast<char*>(c.dw0->data);
+        p.e.out_rs = c.dw0->row_stride;
+        p.e.out_f32 = P->grad_f32;
+        if (P->gated) {
+            p.e.out2 = static_cast<char*>(c.dw1->data);
+            p.e.out2_rs = c.dw1->row_stride;
+        }
+        rc = product_launch(P, p, s);
+        if (rc) return rc;
+    }
+    if (c.dbias)
+        rc = column_sums_launch(static_cast<const char*>(dz[0].data), dz[0].row_stride, dz[0].col_stride, 0, P->half,
+                                rows, N, c.dbias, P->grad_f32, sums, s);
+    return rc;
+}
+
+}  // namespace proj
+}  // namespace dpdr
+
+using namespace dpdr;
+using namespace dpdr::proj;
+
+static Proj* plan_of(dpdr_proj_t h) { return reinterpret_cast<Proj*>(h); }
+
+extern "C" dpdr_proj_t dpdr_linear_plan(int64_t max_rows, int64_t n_in, int64_t n_out, dpdr_dtype operands,
+                                        dpdr_dtype result, dpdr_dtype gradients, dpdr_act act)
+{
+    return reinterpret_cast<dpdr_proj_t>(
+        make(false, max_rows, n_in, n_out, operands, result, gradients, act, "dpdr_linear_plan"));
+}
+
+extern "C" dpdr_proj_t dpdr_gated_plan(int64_t max_rows, int64_t n_in, int64_t n_hidden, dpdr_dtype operands,
+                                       dpdr_dtype result, dpdr_dtype gradients, dpdr_act act)
+{
+    return reinterpret_cast<dpdr_proj_t>(
+        make(true, max_rows, n_in, n_hidden, operands, result, gradients, act, "dpdr_gated_plan"));
+}
+
+extern "C" int dpdr_linear(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w, const void* bias,
+                           const dpdr_matrix* residual, const dpdr_matrix* y, const dpdr_matrix* pre,
+                           dpdr_stream_t stream)
+{
+    Proj* P = plan_of(h);
+    int rc = check_plan(P, false, rows, "dpdr_linear");
+    if (rc) return rc;
+    const int es = P->out_f32 ? 4 : 2;
+    Args a{"dpdr_linear"};
+    a.input("x", x, rows, P->n_in, 2);
+    a.input("w", w, P->n_out, P->n_in, 2);
+    if (bias) a.vector("bias", bias, P->n_out, 2, false);
+    // y may be the residual itself: each element is read by the thread that
+    // then writes it
+    const bool same = residual && y && residual->data == y->data && (rows < 2 || residual->row_stride == y->row_stride) &&
+                      (P->n_out < 2 || residual->col_stride == y->col_stride);
+    if (residual && !same) a.input("residual", residual, rows, P->n_out, es);
+    a.output("y", y, rows, P->n_out, es);
+    if (pre) a.output("pre", pre, rows, P->n_out, 4);
+    if (a.done()) return a.rc;
+    if (rows == 0) return DPDR_OK;
+    Epilogue e = epilogue_of(P);
+    if (residual) set_other(e, *residual, P->out_f32);
+    e.out = static_cast<char*>(y->data);
+    e.out_rs = y->row_stride;
+    e.out_f32 = P->out_f32;
+    if (pre) {
+        e.pre = static_cast<float*>(pre->data);
+        e.pre_rs = pre->row_stride;
+    }
+    return forward(P, rows, *x, w, nullptr, bias, e, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int dpdr_gated(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w_gate,
+                          const dpdr_matrix* w_up, const dpdr_matrix* out, const dpdr_matrix* pre, dpdr_stream_t stream)
+{
+    Proj* P = plan_of(h);
+    int rc = check_plan(P, true, rows, "dpdr_gated");
+    if (rc) return rc;
+    Args a{"dpdr_gated"};
+    a.input("x", x, rows, P->n_in, 2);
+    a.input("w_gate", w_gate, P->n_out, P->n_in, 2);
+    a.input("w_up", w_up, P->n_out, P->n_in, 2);
+    a.output("h", out, rows, P->n_out, P->out_f32 ? 4 : 2);
+    if (pre) a.output("pre", pre, rows, 2 * P->n_out, 4);
+    if (a.done()) return a.rc;
+    if (rows == 0) return DPDR_OK;
+    Epilogue e = epilogue_of(P);
+    e.out = static_cast<char*>(out->data);
+    e.out_rs = out->row_stride;
+    e.out_f32 = P->out_f32;
+    if (pre) {
+        e.pre = static_cast<float*>(pre->data);
+        e.pre_rs = pre->row_stride;
+        e.pre_up = P->n_out;
+    }
+    return forward(P, rows, *x, w_gate, w_up, nullptr, e, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int dpdr_linear_backward(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w,
+                                    const void* bias, const dpdr_matrix* dy, const dpdr_matrix* pre,
+                                    const dpdr_matrix* dx, const dpdr_matrix* dw, void* dbias, dpdr_stream_t stream)
+{
+    Proj* P = plan_of(h);
+    int rc = check_plan(P, false, rows, "dpdr_linear_backward");
+    if (rc) return rc;
+    const int qs = P->grad_f32 ? 4 : 2;
+    Args a{"dpdr_linear_backward"};
+    a.input("x", x, rows, P->n_in, 2);
+    a.input("w", w, P->n_out, P->n_in, 2);
+    if (bias) a.vector("bias", bias, P->n_out, 2, false);
+    a.input("dy", dy, rows, P->n_out, P->out_f32 ? 4 : 2);
+    if (pre) a.input("pre", pre, rows, P->n_out, 4);
+    if (pre && P->n_out > 1 && pre->col_stride != 1) a.refuse("pre", "needs col_stride 1");
+    if (dx) a.output("dx", dx, rows, P->n_in, qs);
+    if (dw) a.output("dw", dw, P->n_out, P->n_in, qs);
+    if (dbias) a.vector("dbias", dbias, P->n_out, qs, true);
+    if (a.done()) return a.rc;
+    return backward(P, rows, Backward{x, w, nullptr, dy, pre, dx, dw, nullptr, bias, dbias},
+                    reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int dpdr_gated_backward(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w_gate,
+                                   const dpdr_matrix* w_up, const dpdr_matrix* dh, const dpdr_matrix* pre,
+                                   const dpdr_matrix* dx, const dpdr_matrix* dw_gate, const dpdr_matrix* dw_up,
+                                   dpdr_stream_t stream)
+{
+    Proj* P = plan_of(h);
+    int rc = check_plan(P, true, rows, "dpdr_gated_backward");
+    if (rc) return rc;
+    const int qs = P->grad_f32 ? 4 : 2;
+    Args a{"dpdr_gated_backward"};
+    a.input("x", x, rows, P->n_in, 2);
+    a.input("w_gate", w_gate, P->n_out, P->n_in, 2);
+    a.input("w_up", w_up, P->n_out, P->n_in, 2);
+    a.input("dh", dh, rows, P->n_out, P->out_f32 ? 4 : 2);
+    if (pre) a.input("pre", pre, rows, 2 * P->n_out, 4);
+    if (pre && pre->col_stride != 1) a.refuse("pre", "needs col_stride 1");
+    if (dx) a.output("dx", dx, rows, P->n_in, qs);
+    if (!dw_gate != !dw_up) a.refuse("dw_gate and dw_up", "go together");
+    if (dw_gate) a.output("dw_gate", dw_gate, P->n_out, P->n_in, qs);
+    if (dw_up) a.output("dw_up", dw_up, P->n_out, P->n_in, qs);
+    if (a.done()) return a.rc;
+    return backward(P, rows, Backward{x, w_gate, w_up, dh, pre, dx, dw_gate, dw_up, nullptr, nullptr},
+                    reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int dpdr_proj_sync(dpdr_proj_t h, dpdr_stream_t stream)
+{
+    Proj* P = plan_of(h);
+    if (!P) return refuse("dpdr_proj_sync", "NULL plan");
+    cudaError_t e = cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail_c(e, "stream synchronize");
+    uint32_t err = 0;
+    e = cudaMemcpy(&err, P->err, sizeof err, cudaMemcpyDeviceToHost);
+    if (e != cudaSuccess) return cuda_fail_c(e, "error word read");
+    if (err == 0) return DPDR_OK;
+    e = cudaMemset(P->err, 0, sizeof err);
+    if (e != cudaSuccess) return cuda_fail_c(e, "error word clear");
+    return fail_c(DPDR_ERR_TIMEOUT, "projection: a bounded wait expired");
+}
+
+extern "C" void dpdr_proj_destroy(dpdr_proj_t h)
+{
+    Proj* P = plan_of(h);
+    if (!P) return;
+    cudaFree(P->scratch);
+    cudaFree(P->err);
+    delete P;
+}

@@ -1,0 +1,83 @@
+// proj.h -- what the host side of the projections (proj.cpp) hands to their
+// kernels: operands by address and strides, and what becomes of a finished
+// sum.  Not part of the public ABI.
+#pragma once
+
+#include <cstdint>
+
+#include "dpdr_internal.h"
+
+namespace dpdr {
+namespace proj {
+
+// An operand, indexed [i][k], k the index that is summed over.
+struct Operand {
+    const char* p;
+    int64_t is, ks;   // strides in elements
+};
+
+// What a product is: D = A B^T and its bookkeeping.
+//   kSingle  sum_k a0[m][k] b0[n][k]
+//   kPair    the same a0 with b0 and b1: two sums of one output (gated forward)
+//   kChain   sum_k a0 b0 + sum_k a1 b1 (the gated operator's dx)
+//   kTwin    two products of one shape, a0 b0 -> out and a1 b0 -> out2 (its
+//            weight gradients)
+enum Kind { kSingle, kPair, kChain, kTwin };
+
+// What becomes of z = sum (+ bias), or of the pair g, u:
+//   kValue   act(z) + other, or act(g) * u
+//   kSlope   other * act'(z), or other * u * act'(g) -> out and
+//            other * act(g) -> out2
+enum Finish { kValue, kSlope };
+
+struct Epilogue {
+    int finish = kValue;
+    int act = DPDR_ACT_NONE;
+    int half = 0;                  // operand type: 0 bfloat16, 1 float16
+    const void* bias = nullptr;    // operand type
+    const char* other = nullptr;   // residual, dy or dh
+    int64_t other_rs = 0, other_cs = 0;
+    int other_f32 = 0;
+    char* out = nullptr;
+    char* out2 = nullptr;
+    int64_t out_rs = 0, out2_rs = 0;
+    int out_f32 = 0;
+    float* pre = nullptr;          // z, or g and, pre_up columns on, u
+    int64_t pre_rs = 0, pre_up = 0;
+};
+
+struct Product {
+    Kind kind = kSingle;
+    int64_t M = 0, N = 0, K = 0;
+    Operand a[2] = {}, b[2] = {};
+    Epilogue e;
+};
+
+// the plan behind dpdr_proj_t
+struct Proj {
+    bool gated = false;
+    int64_t max_rows = 0, n_in = 0, n_out = 0;
+    int half = 0, out_f32 = 0, grad_f32 = 0, act = 0;
+    int device = 0, num_sms = 0;
+    char* scratch = nullptr;
+    size_t scratch_bytes = 0;
+    uint32_t* err = nullptr;       // device error word
+};
+
+int product_launch(Proj* P, const Product& p, cudaStream_t s);
+
+// dz (or dg and du) from the kept projections: e.pre in, e.out (and out2) out
+int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, cudaStream_t s);
+
+// out[c] = sum over r of z[r][c]: z as 16-bit (half: its kind) or float32
+int column_sums_launch(const char* z, int64_t rs, int64_t cs, int z_f32, int half, int64_t rows,
+                       int64_t cols, void* out, int out_f32, float* scratch, cudaStream_t s);
+// rows of the scratch that column_sums_launch needs, cols floats each
+int column_sum_parts(int64_t rows);
+
+// a copy with unit column stride and rows ld apart, rounded to 16 bits
+int pack_launch(const char* src, int64_t rs, int64_t cs, int src_f32, int half, int64_t rows,
+                int64_t cols, char* dst, int64_t ld, cudaStream_t s);
+
+}  // namespace proj
+}  // namespace dpdr
