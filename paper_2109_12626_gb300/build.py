@@ -25,7 +25,7 @@ SOURCES = ["plan.cpp", "api.cpp", "fused.cu", "fused_stream.cu", "fused_tile.cu"
            "fused_split.cu", "fused_bulk.cu", "schedule.cu",
            "schedule_ll.cu", "cells.cpp", "schedule_words.cu",
            "schedule_walk.cu", "schedule_walk_rb.cu", "fused_tree.cu",
-           "proj.cpp", "proj_simple.cu"]
+           "proj.cpp", "proj_elem.cu", "proj_tile.cu"]
 
 
 def nvcc() -> str:

@@ -191,13 +191,95 @@ void set_other(Epilogue& e, const dpdr_matrix& m, int f32)
     e.other_f32 = f32;
 }
 
+// A driver call by name: the library links no libcuda.
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+// TMA's strides are below 2^40 bytes
+constexpr int64_t kFarthest = int64_t(1) << 39;
 size_t upto256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
+int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int half, int rows, int step)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return fail_c(DPDR_ERR_CUDA, "projection: the driver has no cuTensorMapEncodeTiled");
+    const bool inner_k = o.ks == 1;
+    const cuuint64_t dims[2] = {cuuint64_t(inner_k ? k : n), cuuint64_t(inner_k ? n : k)};
+    const cuuint64_t pitch[1] = {cuuint64_t(inner_k ? o.is : o.ks) * 2};
+    const cuuint32_t box[2] = {cuuint32_t(inner_k ? step : 64), cuuint32_t(inner_k ? rows : step)};
+    const cuuint32_t one[2] = {1, 1};
+    const CUresult r = encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                              const_cast<char*>(o.p), dims, pitch, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DPDR_OK : fail_c(DPDR_ERR_CUDA, "projection: tensor map refused");
+}
+
+// A packed copy in the plan's slot, made m's place
+static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int f32, int slot, cudaStream_t s)
+{
+    const int64_t ld = padded(cols);
+    const size_t bytes = size_t(most_rows) * size_t(ld) * 2;
+    if (bytes > P->packed_bytes[slot]) {
+        cudaFree(P->packed[slot]);   // waits for its last use
+        P->packed[slot] = nullptr;
+        P->packed_bytes[slot] = 0;
+        const cudaError_t e = cudaMalloc(&P->packed[slot], bytes);
+        if (e != cudaSuccess) return cuda_fail_c(e, "projection operand copy");
+        P->packed_bytes[slot] = bytes;
+    }
+    const int rc = pack_launch(static_cast<const char*>(m.data), m.row_stride, m.col_stride, f32, P->half, rows, cols,
+                               P->packed[slot], ld, s);
+    m = dpdr_matrix{P->packed[slot], ld, 1};
+    return rc;
+}
+
+// The matrix as TMA can load it: as it lies where one stride is 1, the other a
+// multiple of 8 that is no shorter than a row (column), and the address a
+// multiple of 16 bytes; else a packed copy in the plan's slot.
+static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int f32, int slot,
+                    cudaStream_t s)
+{
+    if (rows == 0 || cols == 0) return DPDR_OK;
+    const bool placed = !f32 && reinterpret_cast<uintptr_t>(m.data) % 16 == 0;
+    dpdr_matrix as = m;
+    if (rows == 1) as.row_stride = padded(cols);   // never stepped over
+    if (placed && (as.col_stride == 1 || cols == 1) && as.row_stride % 8 == 0 && as.row_stride >= cols &&
+        as.row_stride < kFarthest) {
+        as.col_stride = 1;
+        m = as;
+        return DPDR_OK;
+    }
+    as = m;
+    if (cols == 1) as.col_stride = padded(rows);
+    if (placed && (as.row_stride == 1 || rows == 1) && as.col_stride % 8 == 0 && as.col_stride >= rows &&
+        as.col_stride < kFarthest) {
+        as.row_stride = 1;
+        m = as;
+        return DPDR_OK;
+    }
+    return pack(P, m, rows, cols, most_rows, f32, slot, s);
+}
+
 // The forward product, or with slope the same product finished as dz (dg, du).
-static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix* w0, const dpdr_matrix* w1,
+static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w0, const dpdr_matrix& w1,
                    const void* bias, const Epilogue& e, cudaStream_t s)
 {
     Product p;
@@ -206,11 +288,42 @@ static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matri
     p.N = P->n_out;
     p.K = P->n_in;
     p.a[0] = rows_of(x);
-    p.b[0] = rows_of(*w0);
-    if (w1) p.b[1] = rows_of(*w1);
+    p.b[0] = rows_of(w0);
+    p.b[1] = rows_of(w1);
     p.e = e;
     p.e.bias = bias;
-    return product_launch(P, p, s);
+    return tile_launch(P, p, s);
+}
+
+// The operands as loadable matrices: x and each weight, those that a call
+// reads.  Both weights of a pair have to lie the same way (one tile layout);
+// otherwise the second is copied too.
+struct Operands {
+    dpdr_matrix x{}, w[2] = {};
+};
+
+static int operands(Proj* P, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w0, const dpdr_matrix* w1,
+                    Operands& o, cudaStream_t s)
+{
+    int rc = DPDR_OK;
+    if (x) {
+        o.x = *x;
+        rc = loadable(P, o.x, rows, P->n_in, P->max_rows, 0, 0, s);
+    }
+    const dpdr_matrix* w[2] = {w0, w1};
+    for (int i = 0; i < 2 && !rc; i++) {
+        if (!w[i]) continue;
+        o.w[i] = *w[i];
+        rc = loadable(P, o.w[i], P->n_out, P->n_in, P->n_out, 0, 1 + i, s);
+    }
+    if (!rc && w0 && w1 && o.w[0].col_stride != o.w[1].col_stride &&
+        (o.w[0].col_stride == 1 || o.w[1].col_stride == 1)) {
+        // one lies by rows, the other by columns: the latter is copied
+        const int i = o.w[0].col_stride == 1 ? 1 : 0;
+        o.w[i].data = w[i]->data;
+        rc = pack(P, o.w[i], P->n_out, P->n_in, P->n_out, 0, 1 + i, s);
+    }
+    return rc;
 }
 
 struct Backward {
@@ -224,6 +337,15 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     const int n = P->gated ? 2 : 1;
     const int64_t N = P->n_out, K = P->n_in;
     if (!c.dx && !c.dw0 && !c.dbias) return DPDR_OK;
+    if (rows == 0) {
+        const size_t qs = P->grad_f32 ? 4 : 2;
+        cudaError_t e = cudaSuccess;
+        for (const dpdr_matrix* d : {c.dw0, c.dw1})
+            if (d && e == cudaSuccess)
+                e = cudaMemset2DAsync(d->data, size_t(N > 1 ? d->row_stride : K) * qs, 0, size_t(K) * qs, size_t(N), s);
+        if (c.dbias && e == cudaSuccess) e = cudaMemsetAsync(c.dbias, 0, size_t(N) * qs, s);
+        return e == cudaSuccess ? DPDR_OK : cuda_fail_c(e, "zero gradients");
+    }
     // dz as operands: dy itself where it already is (no activation, 16 bits)
     const bool as_is = !P->gated && P->act == DPDR_ACT_NONE && !P->out_f32;
     const int64_t ld = padded(N);
@@ -231,26 +353,33 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     const size_t sum_bytes = c.dbias ? upto256(size_t(column_sum_parts(P->max_rows)) * size_t(N) * 4) : 0;
     int rc = reserve(P, n * dz_bytes + sum_bytes);
     if (rc) return rc;
+    const bool again = !as_is && !c.pre && (P->gated || P->act != DPDR_ACT_NONE);
+    Operands o;
+    const bool need_w = again || c.dx;
+    rc = operands(P, rows, again || c.dw0 ? c.x : nullptr, need_w ? c.w0 : nullptr, need_w ? c.w1 : nullptr, o, s);
+    if (rc) return rc;
     dpdr_matrix dz[2] = {{P->scratch, ld, 1}, {P->scratch + dz_bytes, ld, 1}};
     float* sums = reinterpret_cast<float*>(P->scratch + n * dz_bytes);
     Epilogue e = epilogue_of(P);
     if (as_is) {
         dz[0] = *c.dy;
+        if (c.dx || c.dw0) rc = loadable(P, dz[0], rows, N, P->max_rows, 0, 3, s);
+        if (rc) return rc;
     } else {
         e.finish = kSlope;
         set_other(e, *c.dy, P->out_f32);
         e.out = static_cast<char*>(dz[0].data);
         e.out2 = static_cast<char*>(dz[1].data);
         e.out_rs = e.out2_rs = ld;
-        if (c.pre) {
+        if (again) {
+            rc = forward(P, rows, o.x, o.w[0], o.w[1], c.bias, e, s);
+        } else if (c.pre) {
             e.pre = static_cast<float*>(c.pre->data);
             e.pre_rs = c.pre->row_stride;
             e.pre_up = N;
             rc = slope_launch(e, P->gated, rows, N, s);
-        } else if (!P->gated && P->act == DPDR_ACT_NONE) {
-            rc = slope_launch(e, false, rows, N, s);   // dy rounded to the operand type
         } else {
-            rc = forward(P, rows, *c.x, c.w0, c.w1, c.bias, e, s);
+            rc = slope_launch(e, false, rows, N, s);   // dy rounded to the operand type
         }
         if (rc) return rc;
     }
@@ -262,13 +391,13 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         p.K = N;
         for (int i = 0; i < n; i++) {
             p.a[i] = rows_of(dz[i]);
-            p.b[i] = cols_of(i ? *c.w1 : *c.w0);
+            p.b[i] = cols_of(o.w[i]);
         }
         p.e.half = P->half;
         p.e.out = static_cast<char*>(c.dx->data);
         p.e.out_rs = c.dx->row_stride;
         p.e.out_f32 = P->grad_f32;
-        rc = product_launch(P, p, s);
+        rc = tile_launch(P, p, s);
         if (rc) return rc;
     }
     if (c.dw0) {
@@ -278,7 +407,7 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         p.N = K;
         p.K = rows;
         for (int i = 0; i < n; i++) p.a[i] = cols_of(dz[i]);
-        p.b[0] = cols_of(*c.x);
+        p.b[0] = cols_of(o.x);
         p.e.half = P->half;
         p.e.out = static_cast<char*>(c.dw0->data);
         p.e.out_rs = c.dw0->row_stride;
@@ -287,7 +416,7 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
             p.e.out2 = static_cast<char*>(c.dw1->data);
             p.e.out2_rs = c.dw1->row_stride;
         }
-        rc = product_launch(P, p, s);
+        rc = tile_launch(P, p, s);
         if (rc) return rc;
     }
     if (c.dbias)
@@ -348,7 +477,10 @@ extern "C" int dpdr_linear(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, co
         e.pre = static_cast<float*>(pre->data);
         e.pre_rs = pre->row_stride;
     }
-    return forward(P, rows, *x, w, nullptr, bias, e, reinterpret_cast<cudaStream_t>(stream));
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    Operands o;
+    rc = operands(P, rows, x, w, nullptr, o, s);
+    return rc ? rc : forward(P, rows, o.x, o.w[0], o.w[1], bias, e, s);
 }
 
 extern "C" int dpdr_gated(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w_gate,
@@ -374,7 +506,10 @@ extern "C" int dpdr_gated(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, con
         e.pre_rs = pre->row_stride;
         e.pre_up = P->n_out;
     }
-    return forward(P, rows, *x, w_gate, w_up, nullptr, e, reinterpret_cast<cudaStream_t>(stream));
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    Operands o;
+    rc = operands(P, rows, x, w_gate, w_up, o, s);
+    return rc ? rc : forward(P, rows, o.x, o.w[0], o.w[1], nullptr, e, s);
 }
 
 extern "C" int dpdr_linear_backward(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w,
@@ -445,6 +580,7 @@ extern "C" void dpdr_proj_destroy(dpdr_proj_t h)
     Proj* P = plan_of(h);
     if (!P) return;
     cudaFree(P->scratch);
+    for (char* p : P->packed) cudaFree(p);
     cudaFree(P->err);
     delete P;
 }

@@ -5,6 +5,8 @@
 
 #include <cstdint>
 
+#include <cuda.h>
+
 #include "dpdr_internal.h"
 
 namespace dpdr {
@@ -53,6 +55,8 @@ struct Product {
     Epilogue e;
 };
 
+constexpr int kPacked = 4;   // x, the weights, dy
+
 // the plan behind dpdr_proj_t
 struct Proj {
     bool gated = false;
@@ -61,10 +65,20 @@ struct Proj {
     int device = 0, num_sms = 0;
     char* scratch = nullptr;
     size_t scratch_bytes = 0;
+    // copies of operands that the tensor cores' loads cannot take as they lie
+    char* packed[kPacked] = {};
+    size_t packed_bytes[kPacked] = {};
     uint32_t* err = nullptr;       // device error word
+    bool tile_set[2] = {};         // kernel attributes set
 };
 
-int product_launch(Proj* P, const Product& p, cudaStream_t s);
+// Tensor-core product of operands that TMA can load: one stride 1, the other
+// a multiple of 8, addresses multiples of 16 bytes (proj_tile.cu).  K >= 1.
+int tile_launch(Proj* P, const Product& p, cudaStream_t s);
+
+// Tensor map of operand o, n x k elements, for boxes of `rows` x `step` (n by
+// summed index), or of 64 x `step` where the summed index is the outer one
+int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int half, int rows, int step);
 
 // dz (or dg and du) from the kept projections: e.pre in, e.out (and out2) out
 int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, cudaStream_t s);
