@@ -25,7 +25,8 @@ SOURCES = ["plan.cpp", "api.cpp", "fused.cu", "fused_stream.cu", "fused_tile.cu"
            "fused_split.cu", "fused_bulk.cu", "schedule.cu",
            "schedule_ll.cu", "cells.cpp", "schedule_words.cu",
            "schedule_walk.cu", "schedule_walk_rb.cu", "fused_tree.cu",
-           "proj.cpp", "proj_elem.cu", "proj_tile.cu"]
+           "proj.cpp", "proj_elem.cu", "proj_tile.cu",
+           "proj_tile_pair.cu"]
 
 
 def nvcc() -> str:

@@ -42,9 +42,10 @@ constexpr float kCubic = 0.044715f;
 
 // (1 + tanh(a)) / 2 is the logistic function of 2 a, so the tanh form of gelu
 // is z logistic(2 sqrt(2/pi) (z + 0.044715 z^3)).
-__device__ __forceinline__ float act_value(int act, float z)
+template <int ACT>
+__device__ __forceinline__ float act_value(float z)
 {
-    switch (act) {
+    switch (ACT) {
     case DPDR_ACT_RELU: return z < 0.0f ? 0.0f : z;   // NaN stays NaN
     case DPDR_ACT_GELU: return 0.5f * z * erfcf(-z * kRootHalf);
     case DPDR_ACT_GELU_TANH: return z * logistic(kRoot8Pi * (z + kCubic * z * z * z));
@@ -55,9 +56,10 @@ __device__ __forceinline__ float act_value(int act, float z)
 }
 
 // act(z) and act'(z)
-__device__ __forceinline__ void act_both(int act, float z, float& v, float& d)
+template <int ACT>
+__device__ __forceinline__ void act_both(float z, float& v, float& d)
 {
-    switch (act) {
+    switch (ACT) {
     case DPDR_ACT_RELU:
         v = z < 0.0f ? 0.0f : z;
         d = z > 0.0f ? 1.0f : 0.0f;
@@ -90,20 +92,33 @@ __device__ __forceinline__ void act_both(int act, float z, float& v, float& d)
     }
 }
 
-// One output: z (the bias in it), or the pair g, u -> what e says.
-__device__ __forceinline__ void finish1(const Epilogue& e, bool pair, float g, float u, float other,
-                                        float& out, float& out2)
+// One output: z (the bias in it), or the pair g, u -> what Finish says.
+template <bool PAIR, int FINISH, int ACT>
+__device__ __forceinline__ void finish1(float g, float u, float other, float& out, float& out2)
 {
-    if (e.finish == kValue) {
-        const float v = act_value(e.act, g);
-        out = pair ? v * u : v + other;
+    if (FINISH == kValue) {
+        const float v = act_value<ACT>(g);
+        out = PAIR ? v * u : v + other;
     } else {
         float v, d;
-        act_both(e.act, g, v, d);
-        out = pair ? other * u * d : other * d;
+        act_both<ACT>(g, v, d);
+        out = PAIR ? other * u * d : other * d;
         out2 = other * v;
     }
 }
+
+// f<ACT>() for the activation that a call names.  Each is a kernel of its
+// own: with the choice made per element, one kernel's row loop held the code
+// of all of them, and fetching it took 38 us a 256 x 256 tile.
+#define DPDR_FOR_ACT(act, CALL)                              \
+    switch (act) {                                           \
+    case DPDR_ACT_RELU: CALL(DPDR_ACT_RELU); break;          \
+    case DPDR_ACT_GELU: CALL(DPDR_ACT_GELU); break;          \
+    case DPDR_ACT_GELU_TANH: CALL(DPDR_ACT_GELU_TANH); break;\
+    case DPDR_ACT_SILU: CALL(DPDR_ACT_SILU); break;          \
+    case DPDR_ACT_SIGMOID: CALL(DPDR_ACT_SIGMOID); break;    \
+    default: CALL(DPDR_ACT_NONE);                            \
+    }
 
 }  // namespace proj
 }  // namespace dpdr

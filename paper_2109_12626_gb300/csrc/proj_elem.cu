@@ -7,18 +7,19 @@ namespace proj {
 
 namespace {
 
-__global__ void __launch_bounds__(256) slope_kernel(const Epilogue e, int pair, int64_t rows, int64_t cols)
+template <bool PAIR, int ACT>
+__global__ void __launch_bounds__(256) slope_kernel(const Epilogue e, int64_t rows, int64_t cols)
 {
     const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (n >= cols) return;
     for (int64_t m = blockIdx.y; m < rows; m += gridDim.y) {
         const float g = e.pre ? e.pre[m * e.pre_rs + n] : 0.0f;
-        const float u = pair ? e.pre[m * e.pre_rs + e.pre_up + n] : 0.0f;
+        const float u = PAIR ? e.pre[m * e.pre_rs + e.pre_up + n] : 0.0f;
         const float o = load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half);
         float v = 0.0f, w = 0.0f;
-        finish1(e, pair, g, u, o, v, w);
+        finish1<PAIR, kSlope, ACT>(g, u, o, v, w);
         store1(e.out, m * e.out_rs + n, v, e.out_f32, e.half);
-        if (pair) store1(e.out2, m * e.out2_rs + n, w, e.out_f32, e.half);
+        if (PAIR) store1(e.out2, m * e.out2_rs + n, w, e.out_f32, e.half);
     }
 }
 
@@ -69,7 +70,12 @@ unsigned row_blocks(int64_t rows) { return unsigned(rows < 1024 ? rows : 1024); 
 int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, cudaStream_t s)
 {
     if (rows == 0 || cols == 0) return DPDR_OK;
-    slope_kernel<<<dim3(blocks_of(cols), row_blocks(rows)), 256, 0, s>>>(e, pair, rows, cols);
+    const dim3 grid(blocks_of(cols), row_blocks(rows));
+#define DPDR_CALL(A)                                                         \
+    pair ? slope_kernel<true, A><<<grid, 256, 0, s>>>(e, rows, cols)         \
+         : slope_kernel<false, A><<<grid, 256, 0, s>>>(e, rows, cols)
+    DPDR_FOR_ACT(e.act, DPDR_CALL)
+#undef DPDR_CALL
     return launched("projection gradient");
 }
 
