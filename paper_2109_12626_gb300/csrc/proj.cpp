@@ -278,6 +278,20 @@ static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t
     return pack(P, m, rows, cols, most_rows, f32, slot, s);
 }
 
+// Few rows take row_kernel, which reads the weights once for up to 128 rows
+// and splits the sum over k; so do products whose tiles of 128 x 128 (of a
+// pair 64 x 128) are no more than the SMs, which the 256 x 256 tiles of
+// tile_kernel would leave idle.  4096 x 4096 weights, us with row_kernel and
+// tile_kernel: 64 rows 13.1 and 30.6, 256 rows 19.3 and 31.2, 512 rows 28.9
+// and 31.7, 1024 rows (256 tiles) 43.5 and 32.8; the gated operator, 8192 x
+// 4096: 128 rows 33.9 and 40.0, 256 rows (256 tiles) 43.1 and 40.7.
+static int product_launch(Proj* P, const Product& p, cudaStream_t s)
+{
+    const int64_t width = p.kind == kPair ? 64 : 128;
+    const bool few = p.M <= 128 || ((p.M + 127) / 128) * ((p.N + width - 1) / width) <= P->num_sms;
+    return p.kind != kTwin && few ? row_launch(P, p, s) : tile_launch(P, p, s);
+}
+
 // The forward product, or with slope the same product finished as dz (dg, du).
 static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w0, const dpdr_matrix& w1,
                    const void* bias, const Epilogue& e, cudaStream_t s)
@@ -292,7 +306,7 @@ static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matri
     p.b[1] = rows_of(w1);
     p.e = e;
     p.e.bias = bias;
-    return tile_launch(P, p, s);
+    return product_launch(P, p, s);
 }
 
 // The operands as loadable matrices: x and each weight, those that a call
@@ -397,7 +411,7 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         p.e.out = static_cast<char*>(c.dx->data);
         p.e.out_rs = c.dx->row_stride;
         p.e.out_f32 = P->grad_f32;
-        rc = tile_launch(P, p, s);
+        rc = product_launch(P, p, s);
         if (rc) return rc;
     }
     if (c.dw0) {
@@ -416,7 +430,7 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
             p.e.out2 = static_cast<char*>(c.dw1->data);
             p.e.out2_rs = c.dw1->row_stride;
         }
-        rc = tile_launch(P, p, s);
+        rc = product_launch(P, p, s);
         if (rc) return rc;
     }
     if (c.dbias)

@@ -69,12 +69,15 @@ struct Proj {
     char* packed[kPacked] = {};
     size_t packed_bytes[kPacked] = {};
     uint32_t* err = nullptr;       // device error word
-    bool tile_set[2][2][2] = {};   // kernel attributes set
+    bool tile_set[2][2][2] = {}, row_set[2][2][2] = {};   // kernel attributes set
 };
 
 // Tensor-core product of operands that TMA can load: one stride 1, the other
 // a multiple of 8, addresses multiples of 16 bytes (proj_tile.cu).  K >= 1.
 int tile_launch(Proj* P, const Product& p, cudaStream_t s);
+
+// The same for few rows (proj_rows.cu); not for kTwin.
+int row_launch(Proj* P, const Product& p, cudaStream_t s);
 
 // Tensor map of operand o, n x k elements, for boxes of `rows` x `step` (n by
 // summed index), or of 64 x `step` where the summed index is the outer one

@@ -1,0 +1,80 @@
+// proj_rows.cu -- which kernel of proj_rows.cuh a product takes, how it is
+// split, its tensor maps and launch.
+#include <algorithm>
+
+#include "proj_rows.cuh"
+
+namespace dpdr {
+namespace proj {
+
+RowKernel row_kernel_single(int finish, int act)
+{
+    RowKernel k = nullptr;
+#define DPDR_CALL(A) k = finish == kSlope ? row_kernel<false, kSlope, A> : row_kernel<false, kValue, A>
+    DPDR_FOR_ACT(act, DPDR_CALL)
+#undef DPDR_CALL
+    return k;
+}
+
+RowKernel row_kernel_pair(int finish, int act);   // proj_rows_pair.cu
+
+int row_launch(Proj* P, const Product& p, cudaStream_t s)
+{
+    const bool pair = p.kind == kPair, two_x = p.kind == kChain, two_w = pair || two_x;
+    RowArgs t;
+    t.w_mn = p.b[0].ks != 1;
+    t.x_mn = p.a[0].ks != 1;
+    t.segments = two_x ? 2 : 1;
+    t.steps = int((p.K + kRowStep - 1) / kRowStep);
+    t.width = pair ? 64 : kRowFeatures;
+    t.columns = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    t.x_bytes = (t.x_mn ? std::max(64, t.columns) : t.columns) * kRowStep * 2;
+    t.M = p.M;
+    t.N = p.N;
+    t.e = p.e;
+    t.err = P->err;
+    const int64_t across = (p.N + t.width - 1) / t.width, down = (p.M + t.columns - 1) / t.columns;
+    const int64_t tiles = across * down;
+    const int steps = t.steps * t.segments;
+    // As many CTAs of a cluster as fit beside each other, two an SM, while each
+    // still has four stages to load: 4096 x 4096 weights for one row, 1, 2, 4
+    // and 8 CTAs: 22.2, 14.3, 10.8 and 11.0 us; gated 8192 x 4096: 26.3, 25.8,
+    // 28.8 and 35.0 (more than two an SM).  One CTA an SM with twice the stages
+    // is no faster where all fit (4 CTAs: 11.1) and slower where not.
+    constexpr int kRoom = 110 * 1024;
+    int split = 1;
+    while (split < 8 && tiles * (split + 1) <= 2 * P->num_sms && steps >= 4 * (split + 1)) split++;
+    t.split = split;
+    const int stage = kRowFeatures * kRowStep * 2 + t.x_bytes, mine = (steps + split - 1) / split;
+    t.stages = std::max(2, std::min({mine, kRoom / stage, kRowMaxStages}));
+    const int smem = 1024 + std::max(t.stages * stage, kRowFeatures * t.columns * 4);
+    int rc = tensor_map(&t.w[0], p.b[0], p.N, p.K, p.e.half, pair ? 64 : 128, kRowStep);
+    if (!rc && two_w) rc = tensor_map(&t.w[1], p.b[1], p.N, p.K, p.e.half, pair ? 64 : 128, kRowStep);
+    if (!rc) rc = tensor_map(&t.x[0], p.a[0], p.M, p.K, p.e.half, t.columns, kRowStep);
+    if (!rc && two_x) rc = tensor_map(&t.x[1], p.a[1], p.M, p.K, p.e.half, t.columns, kRowStep);
+    if (rc) return rc;
+    const RowKernel kernel = pair ? row_kernel_pair(p.e.finish, p.e.act) : row_kernel_single(p.e.finish, p.e.act);
+    bool& set = P->row_set[pair][p.e.finish][p.e.act != DPDR_ACT_NONE];
+    cudaError_t e = cudaSuccess;
+    if (!set) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
+        if (e != cudaSuccess) return cuda_fail_c(e, "projection row kernel");
+        set = true;
+    }
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(unsigned(across * split), unsigned(down));
+    c.blockDim = dim3(kRowThreads);
+    c.dynamicSmemBytes = size_t(smem);
+    c.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = unsigned(split);
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    e = cudaLaunchKernelEx(&c, kernel, t);
+    return e == cudaSuccess ? DPDR_OK : cuda_fail_c(e, "projection row kernel");
+}
+
+}  // namespace proj
+}  // namespace dpdr

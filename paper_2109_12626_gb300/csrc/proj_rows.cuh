@@ -1,0 +1,195 @@
+// proj_rows.cuh -- the projections' products for few rows: the weights are
+// read once, by as many CTAs as keep the memory busy.
+//
+// With M rows of a few (tokens being answered) the weights' bytes bound the
+// product.  The tensor core's 128 rows are then 128 features (64 of each
+// weight of a pair) and its N columns the M rows of x, so that one pass over a
+// weight serves all of them; the sum over k is split over the S CTAs of a
+// cluster, which each load their part through a ring of TMA stages (all of it
+// in flight at once where it fits), leave their partial tile in shared memory
+// and then add up the S partials of their share of the columns in the order
+// of the CTAs: one launch, no atomics, the same bits every time.
+#pragma once
+
+#include "proj_common.cuh"
+#include "proj_ptx.cuh"
+
+namespace dpdr {
+namespace proj {
+
+constexpr int kRowStep = 64;               // summed elements a stage
+constexpr int kRowFeatures = 128;
+constexpr int kRowMaxStages = 12;
+constexpr int kRowThreads = 256;
+
+struct RowArgs {
+    CUtensorMap w[2], x[2];
+    int w_mn, x_mn;
+    int steps, segments;      // stages a segment, of all CTAs of a cluster
+    int split;                // CTAs of a cluster
+    int columns;              // rows of x a tile: 16, 32, 64 or 128
+    int x_bytes;              // bytes of x a stage
+    int stages;
+    int width;                // features a tile: 128, of a pair 64
+    int64_t M, N;             // rows of x, features
+    Epilogue e;
+    uint32_t* err;
+};
+
+namespace {
+
+template <bool PAIR, int FINISH, int ACT>
+__global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant__ RowArgs t)
+{
+    extern __shared__ char raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kRowMaxStages + 1];
+    __shared__ uint32_t tmem_at, stop;
+    char* base = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = t.split > 1 ? int(cluster_rank()) : 0;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kRowMaxStages, ready = empty + 8 * kRowMaxStages;
+    const Waits waits{&stop, t.err};
+    const int64_t n0 = int64_t(blockIdx.x / t.split) * t.width, m0 = int64_t(blockIdx.y) * t.columns;
+    const int cols = int(min(int64_t(t.columns), t.M - m0));
+    constexpr int kWBytes = kRowFeatures * kRowStep * 2;
+    const int stage_bytes = kWBytes + t.x_bytes;
+    // this CTA's share of the steps
+    const int steps = t.steps * t.segments;
+    const int k_first = int(int64_t(steps) * rank / t.split), k_last = int(int64_t(steps) * (rank + 1) / t.split);
+
+    if (threadIdx.x == 0) {
+        stop = 0;
+        for (int i = 0; i < t.stages; i++) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, 1);
+        }
+        bar_init(ready, 1);
+        bar_init_fence();
+    }
+    if (warp == 2) tmem_alloc<1>(smem_addr(&tmem_at), max(32, t.columns));
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+
+    if (warp == 0 && lane == 0) {
+        int stage = 0, used = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int k = k_first; k < k_last; k++) {
+            if (!(ok = bar_wait(empty + 8 * stage, phase ^ 1, waits))) break;
+            const int seg = k >= t.steps, k0 = (seg ? k - t.steps : k) * kRowStep;
+            const uint32_t dst = smem_addr(base) + stage * stage_bytes, bar = full + 8 * stage;
+            bar_expect(bar, stage_bytes);
+            if (PAIR) {   // 64 features of either weight
+                const int a = int(n0);
+                if (t.w_mn) {
+                    tma_load(dst, &t.w[0], a, k0, bar);
+                    tma_load(dst + kWBytes / 2, &t.w[1], a, k0, bar);
+                } else {
+                    tma_load(dst, &t.w[0], k0, a, bar);
+                    tma_load(dst + kWBytes / 2, &t.w[1], k0, a, bar);
+                }
+            } else if (t.w_mn) {
+                tma_load(dst, &t.w[seg], int(n0), k0, bar);
+                tma_load(dst + kWBytes / 2, &t.w[seg], int(n0) + 64, k0, bar);
+            } else {
+                tma_load(dst, &t.w[seg], k0, int(n0), bar);
+            }
+            if (t.x_mn) {
+                for (int c = 0; c < t.columns; c += 64)
+                    tma_load(dst + kWBytes + c * kRowStep * 2, &t.x[seg], int(m0) + c, k0, bar);
+            } else {
+                tma_load(dst + kWBytes, &t.x[seg], k0, int(m0), bar);
+            }
+            used++;
+            if (++stage == t.stages) stage = 0, phase ^= 1;
+        }
+        if (!ok)   // loads still under way write to shared memory
+            for (int n = min(used, t.stages); n > 0; n--) {
+                if (--stage < 0) stage = t.stages - 1, phase ^= 1;
+                bar_drain(full + 8 * stage, phase);
+            }
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t desc = mma_desc(kRowFeatures, t.columns, t.e.half, t.w_mn, t.x_mn);
+        const uint32_t w_lead = t.w_mn ? kWBytes / 2 : 0, x_lead = t.x_mn ? 64 * kRowStep * 2 : 0;
+        const uint32_t w_step = t.w_mn ? 2048 : 32, x_step = t.x_mn ? 2048 : 32;
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int k = k_first; k < k_last; k++) {
+            if (!bar_wait(full + 8 * stage, phase, waits)) break;
+            tc_fence_after();
+            const uint32_t at = smem_addr(base) + stage * stage_bytes;
+#pragma unroll
+            for (int j = 0; j < kRowStep / 16; j++)
+                mma_f16<1>(tmem, tile_desc(at + j * w_step, w_lead), tile_desc(at + kWBytes + j * x_step, x_lead), desc,
+                           k > k_first || j > 0);
+            mma_commit(empty + 8 * stage);
+            if (++stage == t.stages) stage = 0, phase ^= 1;
+        }
+        mma_commit(ready);
+    }
+    __syncwarp();
+    // All products done (and with them every load): the stages' memory now
+    // takes the partial tile, column by column.
+    float* part = reinterpret_cast<float*>(base);
+    const bool some = k_last > k_first;
+    bool ok = bar_wait(ready, 0, waits);
+    tc_fence_after();
+    ok = __syncthreads_and(ok && !stop);   // every role is done with the stages
+    if (ok) {
+        const int quarter = warp & 3;
+        for (int c0 = (warp >> 2) * 32; c0 < cols; c0 += 64) {
+            float v[32];
+            tmem_load32(v, tmem + c0 + (uint32_t(quarter) << 21));
+            tmem_load_wait();
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (c0 + i < cols) part[(c0 + i) * kRowFeatures + quarter * 32 + lane] = some ? v[i] : 0.0f;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (t.split > 1) cluster_sync();
+    if (ok) {
+        // ------------------------------------------------ results
+        const Epilogue& e = t.e;
+        constexpr int kAcross = PAIR ? 64 : 128;            // threads along the features
+        const int f = threadIdx.x % kAcross;
+        const int64_t n = n0 + f;
+        if (n < t.N) {
+            const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
+            for (int c = rank + t.split * int(threadIdx.x / kAcross); c < cols; c += t.split * (kRowThreads / kAcross)) {
+                const int64_t m = m0 + c;
+                const float o = e.other ? load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half) : 0.0f;
+                float z = 0.0f, u = 0.0f;
+                const uint32_t at = smem_addr(part + c * kRowFeatures + f);
+                for (int s = 0; s < t.split; s++) {
+                    const uint32_t from = t.split > 1 ? in_cta(at, s) : at;
+                    z += cluster_load(from);
+                    if (PAIR) u += cluster_load(from + 64 * 4);
+                }
+                z += bias;
+                if (e.pre) {
+                    e.pre[m * e.pre_rs + n] = z;
+                    if (PAIR) e.pre[m * e.pre_rs + e.pre_up + n] = u;
+                }
+                float v = 0.0f, w = 0.0f;
+                finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
+                store1(e.out, m * e.out_rs + n, v, e.out_f32, e.half);
+                if (PAIR && FINISH == kSlope) store1(e.out2, m * e.out2_rs + n, w, e.out_f32, e.half);
+            }
+        }
+    }
+    __syncwarp();
+    if (t.split > 1) cluster_sync();   // the others have read this CTA's partials
+    tc_fence_after();
+    if (warp == 2) tmem_free<1>(tmem, max(32, t.columns));
+}
+
+}  // namespace
+
+using RowKernel = void (*)(RowArgs);
+
+}  // namespace proj
+}  // namespace dpdr
