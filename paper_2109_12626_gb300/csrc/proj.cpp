@@ -216,6 +216,17 @@ size_t upto256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
+bool by_fours(const Epilogue& e)
+{
+    auto fits = [](const void* q, int64_t rs, int esize) {
+        return reinterpret_cast<uintptr_t>(q) % uintptr_t(4 * esize) == 0 && rs % 4 == 0;
+    };
+    const int os = e.out_f32 ? 4 : 2;
+    return fits(e.out, e.out_rs, os) && fits(e.out2, e.out2_rs, os) &&
+           (!e.other || (e.other_cs == 1 && fits(e.other, e.other_rs, e.other_f32 ? 4 : 2))) &&
+           (!e.pre || (fits(e.pre, e.pre_rs, 4) && e.pre_up % 4 == 0)) && fits(e.bias, 0, 2);
+}
+
 int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int half, int rows, int step)
 {
     const EncodeTiled encode = encode_tiled();

@@ -79,6 +79,10 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s);
 // The same for few rows (proj_rows.cu); not for kTwin.
 int row_launch(Proj* P, const Product& p, cudaStream_t s);
 
+// Whether the results and what else an epilogue reads allow four elements at
+// a time: addresses and row strides of four elements, unit column strides
+bool by_fours(const Epilogue& e);
+
 // Tensor map of operand o, n x k elements, for boxes of `rows` x `step` (n by
 // summed index), or of 64 x `step` where the summed index is the outer one
 int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int half, int rows, int step);

@@ -1,6 +1,7 @@
 // proj_elem.cu -- the projections' element-wise and reducing kernels: dz from
 // kept projections, column sums, copies of operands.
 #include "proj_common.cuh"
+#include "proj_launch.cuh"
 
 namespace dpdr {
 namespace proj {
@@ -10,6 +11,7 @@ namespace {
 template <bool PAIR, int ACT>
 __global__ void __launch_bounds__(256) slope_kernel(const Epilogue e, int64_t rows, int64_t cols)
 {
+    wait_previous();
     const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (n >= cols) return;
     for (int64_t m = blockIdx.y; m < rows; m += gridDim.y) {
@@ -28,6 +30,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const Epilogue e, int64_t ro
 __global__ void __launch_bounds__(256) column_part_kernel(const char* z, int64_t rs, int64_t cs, int f32, int half,
                                                           int64_t rows, int64_t cols, float* part)
 {
+    wait_previous();
     const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (n >= cols) return;
     const int64_t per = (rows + gridDim.y - 1) / gridDim.y;
@@ -40,6 +43,7 @@ __global__ void __launch_bounds__(256) column_part_kernel(const char* z, int64_t
 __global__ void __launch_bounds__(256) column_join_kernel(const float* part, int parts, int64_t cols, char* out,
                                                           int out_f32, int half)
 {
+    wait_previous();
     const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (n >= cols) return;
     float s = 0.0f;
@@ -50,16 +54,11 @@ __global__ void __launch_bounds__(256) column_join_kernel(const float* part, int
 __global__ void __launch_bounds__(256) pack_kernel(const char* src, int64_t rs, int64_t cs, int f32, int half,
                                                    int64_t rows, int64_t cols, char* dst, int64_t ld)
 {
+    wait_previous();
     const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (n >= cols) return;
     for (int64_t m = blockIdx.y; m < rows; m += gridDim.y)
         store1(dst, m * ld + n, load1(src, m * rs + n * cs, f32, half), 0, half);
-}
-
-int launched(const char* what)
-{
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? DPDR_OK : cuda_fail_c(e, what);
 }
 
 unsigned blocks_of(int64_t n) { return unsigned((n + 255) / 256); }
@@ -71,12 +70,11 @@ int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, cudaS
 {
     if (rows == 0 || cols == 0) return DPDR_OK;
     const dim3 grid(blocks_of(cols), row_blocks(rows));
-#define DPDR_CALL(A)                                                         \
-    pair ? slope_kernel<true, A><<<grid, 256, 0, s>>>(e, rows, cols)         \
-         : slope_kernel<false, A><<<grid, 256, 0, s>>>(e, rows, cols)
+    void (*kernel)(Epilogue, int64_t, int64_t) = nullptr;
+#define DPDR_CALL(A) kernel = pair ? slope_kernel<true, A> : slope_kernel<false, A>
     DPDR_FOR_ACT(e.act, DPDR_CALL)
 #undef DPDR_CALL
-    return launched("projection gradient");
+    return launch(kernel, grid, 256, 0, 1, s, "projection gradient", e, rows, cols);
 }
 
 int column_sum_parts(int64_t rows) { return int(rows < 64 ? 1 : rows < 16384 ? rows / 64 : 256); }
@@ -85,19 +83,19 @@ int column_sums_launch(const char* z, int64_t rs, int64_t cs, int z_f32, int hal
                        void* out, int out_f32, float* scratch, cudaStream_t s)
 {
     const int parts = column_sum_parts(rows);
-    column_part_kernel<<<dim3(blocks_of(cols), parts), 256, 0, s>>>(z, rs, cs, z_f32, half, rows, cols, scratch);
-    column_join_kernel<<<blocks_of(cols), 256, 0, s>>>(scratch, parts, cols, static_cast<char*>(out), out_f32,
-                                                       half);
-    return launched("bias gradient");
+    const int rc = launch(column_part_kernel, dim3(blocks_of(cols), parts), 256, 0, 1, s, "bias gradient", z, rs, cs,
+                          z_f32, half, rows, cols, scratch);
+    if (rc) return rc;
+    return launch(column_join_kernel, dim3(blocks_of(cols)), 256, 0, 1, s, "bias gradient", scratch, parts, cols,
+                  static_cast<char*>(out), out_f32, half);
 }
 
 int pack_launch(const char* src, int64_t rs, int64_t cs, int src_f32, int half, int64_t rows, int64_t cols,
                 char* dst, int64_t ld, cudaStream_t s)
 {
     if (rows == 0 || cols == 0) return DPDR_OK;
-    pack_kernel<<<dim3(blocks_of(cols), row_blocks(rows)), 256, 0, s>>>(src, rs, cs, src_f32, half, rows, cols,
-                                                                        dst, ld);
-    return launched("operand copy");
+    return launch(pack_kernel, dim3(blocks_of(cols), row_blocks(rows)), 256, 0, 1, s, "operand copy", src, rs, cs,
+                  src_f32, half, rows, cols, dst, ld);
 }
 
 }  // namespace proj

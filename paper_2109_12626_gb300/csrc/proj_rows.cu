@@ -32,6 +32,7 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.M = p.M;
     t.N = p.N;
     t.e = p.e;
+    t.vec = by_fours(p.e);
     t.err = P->err;
     const int64_t across = (p.N + t.width - 1) / t.width, down = (p.M + t.columns - 1) / t.columns;
     const int64_t tiles = across * down;
@@ -55,25 +56,13 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     if (rc) return rc;
     const RowKernel kernel = pair ? row_kernel_pair(p.e.finish, p.e.act) : row_kernel_single(p.e.finish, p.e.act);
     bool& set = P->row_set[pair][p.e.finish][p.e.act != DPDR_ACT_NONE];
-    cudaError_t e = cudaSuccess;
     if (!set) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
         if (e != cudaSuccess) return cuda_fail_c(e, "projection row kernel");
         set = true;
     }
-    cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(unsigned(across * split), unsigned(down));
-    c.blockDim = dim3(kRowThreads);
-    c.dynamicSmemBytes = size_t(smem);
-    c.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = unsigned(split);
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    c.attrs = at;
-    c.numAttrs = 1;
-    e = cudaLaunchKernelEx(&c, kernel, t);
-    return e == cudaSuccess ? DPDR_OK : cuda_fail_c(e, "projection row kernel");
+    return launch(kernel, dim3(unsigned(across * split), unsigned(down)), kRowThreads, size_t(smem), split, s,
+                  "projection row kernel", t);
 }
 
 }  // namespace proj

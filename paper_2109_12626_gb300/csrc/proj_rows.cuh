@@ -12,6 +12,7 @@
 #pragma once
 
 #include "proj_common.cuh"
+#include "proj_launch.cuh"
 #include "proj_ptx.cuh"
 
 namespace dpdr {
@@ -21,6 +22,7 @@ constexpr int kRowStep = 64;               // summed elements a stage
 constexpr int kRowFeatures = 128;
 constexpr int kRowMaxStages = 12;
 constexpr int kRowThreads = 256;
+constexpr int kRowSplits = 8;              // CTAs of a cluster, at most
 
 struct RowArgs {
     CUtensorMap w[2], x[2];
@@ -31,12 +33,30 @@ struct RowArgs {
     int x_bytes;              // bytes of x a stage
     int stages;
     int width;                // features a tile: 128, of a pair 64
+    int vec;                  // results and what else is read allow 4 elements at a time
     int64_t M, N;             // rows of x, features
     Epilogue e;
     uint32_t* err;
 };
 
 namespace {
+
+// Four sums side by side from the partials of the cluster's CTAs, in their order
+__device__ __forceinline__ void join(uint32_t at, int split, float (&z)[4])
+{
+    float p[kRowSplits][4];
+#pragma unroll
+    for (int s = 0; s < kRowSplits; s++) {
+        p[s][0] = p[s][1] = p[s][2] = p[s][3] = 0.0f;
+        if (s < split) cluster_load4(split > 1 ? in_cta(at, s) : at, p[s]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        z[i] = p[0][i];
+#pragma unroll
+        for (int s = 1; s < kRowSplits; s++) z[i] += p[s][i];
+    }
+}
 
 template <bool PAIR, int FINISH, int ACT>
 __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant__ RowArgs t)
@@ -71,6 +91,8 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
+    wait_previous();
+    allow_next();
 
     if (warp == 0 && lane == 0) {
         int stage = 0, used = 0;
@@ -153,33 +175,37 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     if (t.split > 1) cluster_sync();
     if (ok) {
         // ------------------------------------------------ results
+        // A thread takes four features of a column; the partials of all CTAs
+        // are asked for before the first is added (one after the other, each a
+        // trip to another SM, took 8 of the 12 us of 333 rows, 2500 to 1000).
         const Epilogue& e = t.e;
-        constexpr int kAcross = PAIR ? 64 : 128;            // threads along the features
-        const int f = threadIdx.x % kAcross;
+        constexpr int kAcross = (PAIR ? 64 : 128) / 4;
+        const int f = 4 * (int(threadIdx.x) % kAcross);
         const int64_t n = n0 + f;
-        if (n < t.N) {
-            const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
+        const bool four = t.vec && n + 3 < t.N;
+        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e.bias) {
+            if (four)
+                load4(static_cast<const char*>(e.bias), n, 0, e.half, bias);
+            else
+                for (int i = 0; i < 4; i++)
+                    if (n + i < t.N) bias[i] = load1(static_cast<const char*>(e.bias), n + i, 0, e.half);
+        }
+        if (n < t.N)
             for (int c = rank + t.split * int(threadIdx.x / kAcross); c < cols; c += t.split * (kRowThreads / kAcross)) {
                 const int64_t m = m0 + c;
-                const float o = e.other ? load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half) : 0.0f;
-                float z = 0.0f, u = 0.0f;
                 const uint32_t at = smem_addr(part + c * kRowFeatures + f);
-                for (int s = 0; s < t.split; s++) {
-                    const uint32_t from = t.split > 1 ? in_cta(at, s) : at;
-                    z += cluster_load(from);
-                    if (PAIR) u += cluster_load(from + 64 * 4);
-                }
-                z += bias;
-                if (e.pre) {
-                    e.pre[m * e.pre_rs + n] = z;
-                    if (PAIR) e.pre[m * e.pre_rs + e.pre_up + n] = u;
-                }
-                float v = 0.0f, w = 0.0f;
-                finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
-                store1(e.out, m * e.out_rs + n, v, e.out_f32, e.half);
-                if (PAIR && FINISH == kSlope) store1(e.out2, m * e.out2_rs + n, w, e.out_f32, e.half);
+                float z[4], u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (four && e.other) load4(e.other, m * e.other_rs + n, e.other_f32, e.half, o);
+                join(at, t.split, z);
+                if (PAIR) join(at + 64 * 4, t.split, u);
+                if (four)
+                    put4<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n, z, u, bias, o);
+                else
+                    for (int i = 0; i < 4; i++)
+                        if (n + i < t.N)
+                            put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[i], u[i], bias[i]);
             }
-        }
     }
     __syncwarp();
     if (t.split > 1) cluster_sync();   // the others have read this CTA's partials

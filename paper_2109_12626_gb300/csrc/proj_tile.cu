@@ -17,18 +17,6 @@ TileKernel tile_kernel_single(int finish, int act)
 
 TileKernel tile_kernel_pair(int finish, int act);   // proj_tile_pair.cu
 
-bool tile_vec(const Product& p)
-{
-    const Epilogue& e = p.e;
-    auto fits = [](const void* q, int64_t rs, int esize) {
-        return reinterpret_cast<uintptr_t>(q) % uintptr_t(4 * esize) == 0 && rs % 4 == 0;
-    };
-    const int os = e.out_f32 ? 4 : 2;
-    return fits(e.out, e.out_rs, os) && fits(e.out2, e.out2_rs, os) &&
-           (!e.other || (e.other_cs == 1 && fits(e.other, e.other_rs, e.other_f32 ? 4 : 2))) &&
-           (!e.pre || (fits(e.pre, e.pre_rs, 4) && e.pre_up % 4 == 0)) && fits(e.bias, 0, 2);
-}
-
 int tile_launch(Proj* P, const Product& p, cudaStream_t s)
 {
     TileArgs t;
@@ -43,7 +31,7 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     const int64_t tiles = int64_t(t.tiles_m) * t.tiles_n * (p.kind == kTwin ? 2 : 1);
     if (tiles > (int64_t(1) << 30)) return fail_c(DPDR_ERR_INVALID, "projection: more than 2^30 tiles");
     t.tiles = int(tiles);
-    t.vec = tile_vec(p);
+    t.vec = by_fours(p.e);
     t.M = p.M;
     t.N = p.N;
     t.e = p.e;
@@ -64,9 +52,7 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
         set = true;
     }
     const int pairs = int(tiles < P->num_sms / 2 ? tiles : P->num_sms / 2);
-    kernel<<<2 * pairs, kThreads, kSmem, s>>>(t);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? DPDR_OK : cuda_fail_c(e, "projection tile kernel");
+    return launch(kernel, dim3(unsigned(2 * pairs)), kThreads, kSmem, 2, s, "projection tile kernel", t);
 }
 
 }  // namespace proj

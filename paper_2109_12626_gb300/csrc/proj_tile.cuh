@@ -16,6 +16,7 @@
 #pragma once
 
 #include "proj_common.cuh"
+#include "proj_launch.cuh"
 #include "proj_ptx.cuh"
 
 namespace dpdr {
@@ -37,7 +38,7 @@ struct TileArgs {
     int kind, steps, segments;     // stages a segment
     int tiles_m, tiles_n, tiles;   // tiles_m of one of kTwin's products
     int width;                     // result columns a tile
-    int vec;                       // the results and what else is read allow 4 elements at a time
+    int vec;                       // results and what else is read allow 4 elements at a time
     int64_t M, N;
     Epilogue e;
     uint32_t* err;
@@ -52,67 +53,6 @@ __device__ __forceinline__ void tile_place(const TileArgs& t, int i, int& tm, in
     const int high = min(8, rows - first), in = i - b * band;
     tm = first + in % high;
     tn = in / high;
-}
-
-__device__ __forceinline__ void load4(const char* p, int64_t i, int f32, int half, float (&v)[4])
-{
-    if (f32) {
-        const float4 x = *reinterpret_cast<const float4*>(p + 4 * i);
-        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-    } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(p + 2 * i);
-        v[0] = widen(uint16_t(x.x), half), v[1] = widen(uint16_t(x.x >> 16), half);
-        v[2] = widen(uint16_t(x.y), half), v[3] = widen(uint16_t(x.y >> 16), half);
-    }
-}
-
-__device__ __forceinline__ void store4(char* p, int64_t i, int f32, int half, const float (&v)[4])
-{
-    if (f32)
-        *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[0], v[1], v[2], v[3]);
-    else
-        *reinterpret_cast<uint2*>(p + 2 * i) =
-            make_uint2(uint32_t(narrow(v[0], half)) | uint32_t(narrow(v[1], half)) << 16,
-                       uint32_t(narrow(v[2], half)) | uint32_t(narrow(v[3], half)) << 16);
-}
-
-// One result element from its sum (or pair of sums)
-template <bool PAIR, int FINISH, int ACT>
-__device__ __forceinline__ void put1(const Epilogue& e, char* out, int64_t out_rs, int64_t m, int64_t n, float z,
-                                     float u, float bias)
-{
-    z += bias;
-    if (e.pre) {
-        e.pre[m * e.pre_rs + n] = z;
-        if (PAIR) e.pre[m * e.pre_rs + e.pre_up + n] = u;
-    }
-    const float o = e.other ? load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half) : 0.0f;
-    float v = 0.0f, w = 0.0f;
-    finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
-    store1(out, m * out_rs + n, v, e.out_f32, e.half);
-    if (PAIR && FINISH == kSlope) store1(e.out2, m * e.out2_rs + n, w, e.out_f32, e.half);
-}
-
-// Four of them side by side
-template <bool PAIR, int FINISH, int ACT>
-__device__ __forceinline__ void put4(const Epilogue& e, char* out, int64_t out_rs, int64_t m, int64_t n, float (&z)[4],
-                                     const float (&u)[4], const float (&bias)[4], const float (&o)[4])
-{
-#pragma unroll
-    for (int i = 0; i < 4; i++) z[i] += bias[i];
-    if (e.pre) {
-        *reinterpret_cast<float4*>(e.pre + m * e.pre_rs + n) = make_float4(z[0], z[1], z[2], z[3]);
-        if (PAIR)
-            *reinterpret_cast<float4*>(e.pre + m * e.pre_rs + e.pre_up + n) = make_float4(u[0], u[1], u[2], u[3]);
-    }
-    float v[4], w[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        w[i] = 0.0f;
-        finish1<PAIR, FINISH, ACT>(z[i], u[i], o[i], v[i], w[i]);
-    }
-    store4(out, m * out_rs + n, e.out_f32, e.half, v);
-    if (PAIR && FINISH == kSlope) store4(e.out2, m * e.out2_rs + n, e.out_f32, e.half, w);
 }
 
 // Finishes a warp's 32 rows of a tile.  The tensor memory hands each thread a
@@ -194,7 +134,7 @@ __device__ __forceinline__ void finish_rows(const TileArgs& t, uint32_t tmem, fl
 }
 
 template <bool PAIR, int FINISH, int ACT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t)
+__global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t)
 {
     extern __shared__ char raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
@@ -227,6 +167,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tile_ke
     tc_fence_after();
     const uint32_t tmem = tmem_at;
     const int steps = t.steps * t.segments;
+    wait_previous();
 
     if (warp == 0 && lane == 0) {
         // ------------------------------------------------ loads
