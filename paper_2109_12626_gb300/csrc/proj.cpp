@@ -303,9 +303,15 @@ static int product_launch(Proj* P, const Product& p, cudaStream_t s)
     return p.kind != kTwin && few ? row_launch(P, p, s) : tile_launch(P, p, s);
 }
 
+// Whether a forward call goes to token_kernel as its operands lie
+static bool for_token(int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w0, const dpdr_matrix* w1)
+{
+    return rows == 1 && x.col_stride == 1 && w0.col_stride == 1 && (!w1 || w1->col_stride == 1);
+}
+
 // The forward product, or with slope the same product finished as dz (dg, du).
 static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w0, const dpdr_matrix& w1,
-                   const void* bias, const Epilogue& e, cudaStream_t s)
+                   const void* bias, const Epilogue& e, cudaStream_t s, bool token = false)
 {
     Product p;
     p.kind = P->gated ? kPair : kSingle;
@@ -317,7 +323,7 @@ static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matri
     p.b[1] = rows_of(w1);
     p.e = e;
     p.e.bias = bias;
-    return product_launch(P, p, s);
+    return token ? token_launch(P, p, s) : product_launch(P, p, s);
 }
 
 // The operands as loadable matrices: x and each weight, those that a call
@@ -503,6 +509,7 @@ extern "C" int dpdr_linear(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, co
         e.pre_rs = pre->row_stride;
     }
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (for_token(rows, *x, *w, nullptr)) return forward(P, rows, *x, *w, dpdr_matrix{}, bias, e, s, true);
     Operands o;
     rc = operands(P, rows, x, w, nullptr, o, s);
     return rc ? rc : forward(P, rows, o.x, o.w[0], o.w[1], bias, e, s);
@@ -532,6 +539,7 @@ extern "C" int dpdr_gated(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, con
         e.pre_up = P->n_out;
     }
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (for_token(rows, *x, *w_gate, w_up)) return forward(P, rows, *x, *w_gate, *w_up, nullptr, e, s, true);
     Operands o;
     rc = operands(P, rows, x, w_gate, w_up, o, s);
     return rc ? rc : forward(P, rows, o.x, o.w[0], o.w[1], nullptr, e, s);

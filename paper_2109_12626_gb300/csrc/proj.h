@@ -69,7 +69,7 @@ struct Proj {
     char* packed[kPacked] = {};
     size_t packed_bytes[kPacked] = {};
     uint32_t* err = nullptr;       // device error word
-    bool tile_set[2][2][2] = {}, row_set[2][2][2] = {};   // kernel attributes set
+    bool tile_set[2][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
 };
 
 // Tensor-core product of operands that TMA can load: one stride 1, the other
@@ -78,6 +78,10 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s);
 
 // The same for few rows (proj_rows.cu); not for kTwin.
 int row_launch(Proj* P, const Product& p, cudaStream_t s);
+
+// The same for one row, forward only (proj_token.cu): the summed index of all
+// operands contiguous, any alignment and row stride.
+int token_launch(Proj* P, const Product& p, cudaStream_t s);
 
 // Whether the results and what else an epilogue reads allow four elements at
 // a time: addresses and row strides of four elements, unit column strides

@@ -7,16 +7,12 @@
 namespace dpdr {
 namespace proj {
 
-RowKernel row_kernel_single(int finish, int act)
+RowKernel row_kernel_single(int finish, int act, int split)
 {
-    RowKernel k = nullptr;
-#define DPDR_CALL(A) k = finish == kSlope ? row_kernel<false, kSlope, A> : row_kernel<false, kValue, A>
-    DPDR_FOR_ACT(act, DPDR_CALL)
-#undef DPDR_CALL
-    return k;
+    return finish == kSlope ? row_kernel_of<false, kSlope>(act, split) : row_kernel_of<false, kValue>(act, split);
 }
 
-RowKernel row_kernel_pair(int finish, int act);   // proj_rows_pair.cu
+RowKernel row_kernel_pair(int finish, int act, int split);   // proj_rows_pair.cu
 
 int row_launch(Proj* P, const Product& p, cudaStream_t s)
 {
@@ -27,24 +23,31 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.segments = two_x ? 2 : 1;
     t.steps = int((p.K + kRowStep - 1) / kRowStep);
     t.width = pair ? 64 : kRowFeatures;
-    t.columns = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    // Tiles of 64 rows where 128 would leave SMs without one: 128 rows of 4096 x
+    // 4096 12.5 against 14.9 us, 1024 rows of 1024 x 1024 8.3 against 9.4; with
+    // more tiles than SMs, 512 rows of 4096 x 4096, 25.3 against 21.1.
+    const int64_t across = (p.N + t.width - 1) / t.width;
+    t.columns = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 || (p.M + 63) / 64 * across <= P->num_sms ? 64 : 128;
     t.x_bytes = (t.x_mn ? std::max(64, t.columns) : t.columns) * kRowStep * 2;
     t.M = p.M;
     t.N = p.N;
     t.e = p.e;
     t.vec = by_fours(p.e);
     t.err = P->err;
-    const int64_t across = (p.N + t.width - 1) / t.width, down = (p.M + t.columns - 1) / t.columns;
+    const int64_t down = (p.M + t.columns - 1) / t.columns;
     const int64_t tiles = across * down;
     const int steps = t.steps * t.segments;
     // As many CTAs of a cluster as fit beside each other, two an SM, while each
     // still has four stages to load: 4096 x 4096 weights for one row, 1, 2, 4
-    // and 8 CTAs: 22.2, 14.3, 10.8 and 11.0 us; gated 8192 x 4096: 26.3, 25.8,
-    // 28.8 and 35.0 (more than two an SM).  One CTA an SM with twice the stages
-    // is no faster where all fit (4 CTAs: 11.1) and slower where not.
+    // and 8 CTAs: 22.2, 14.3, 10.8 and 11.0 us; a pair of 8192 x 4096: 26.3,
+    // 25.8, 28.8 and 35.0 (more than two an SM).  One CTA an SM with twice the
+    // stages is no faster where all fit (4 CTAs: 11.1) and slower where not.
+    // From 64 columns on at most four: the partials that the SMs send each
+    // other grow with both (333 rows, 2500 to 1000: 9.8 against 12.4 with eight).
     constexpr int kRoom = 110 * 1024;
+    const int most = t.columns >= 64 ? 4 : kRowSplits;
     int split = 1;
-    while (split < 8 && tiles * (split + 1) <= 2 * P->num_sms && steps >= 4 * (split + 1)) split++;
+    while (split < most && tiles * (split + 1) <= 2 * P->num_sms && steps >= 4 * (split + 1)) split++;
     t.split = split;
     const int stage = kRowFeatures * kRowStep * 2 + t.x_bytes, mine = (steps + split - 1) / split;
     t.stages = std::max(2, std::min({mine, kRoom / stage, kRowMaxStages}));
@@ -54,8 +57,8 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     if (!rc) rc = tensor_map(&t.x[0], p.a[0], p.M, p.K, p.e.half, t.columns, kRowStep);
     if (!rc && two_x) rc = tensor_map(&t.x[1], p.a[1], p.M, p.K, p.e.half, t.columns, kRowStep);
     if (rc) return rc;
-    const RowKernel kernel = pair ? row_kernel_pair(p.e.finish, p.e.act) : row_kernel_single(p.e.finish, p.e.act);
-    bool& set = P->row_set[pair][p.e.finish][p.e.act != DPDR_ACT_NONE];
+    const RowKernel kernel = pair ? row_kernel_pair(p.e.finish, p.e.act, split) : row_kernel_single(p.e.finish, p.e.act, split);
+    bool& set = P->row_set[pair][p.e.finish][p.e.act != DPDR_ACT_NONE][row_split_class(split)];
     if (!set) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
         if (e != cudaSuccess) return cuda_fail_c(e, "projection row kernel");

@@ -42,11 +42,12 @@ struct RowArgs {
 namespace {
 
 // Four sums side by side from the partials of the cluster's CTAs, in their order
+template <int SPLIT>
 __device__ __forceinline__ void join(uint32_t at, int split, float (&z)[4])
 {
-    float p[kRowSplits][4];
+    float p[SPLIT][4];
 #pragma unroll
-    for (int s = 0; s < kRowSplits; s++) {
+    for (int s = 0; s < SPLIT; s++) {
         p[s][0] = p[s][1] = p[s][2] = p[s][3] = 0.0f;
         if (s < split) cluster_load4(split > 1 ? in_cta(at, s) : at, p[s]);
     }
@@ -54,11 +55,11 @@ __device__ __forceinline__ void join(uint32_t at, int split, float (&z)[4])
     for (int i = 0; i < 4; i++) {
         z[i] = p[0][i];
 #pragma unroll
-        for (int s = 1; s < kRowSplits; s++) z[i] += p[s][i];
+        for (int s = 1; s < SPLIT; s++) z[i] += p[s][i];
     }
 }
 
-template <bool PAIR, int FINISH, int ACT>
+template <bool PAIR, int FINISH, int ACT, int SPLIT>
 __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant__ RowArgs t)
 {
     extern __shared__ char raw[];
@@ -172,14 +173,18 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    if (t.split > 1) cluster_sync();
+    tc_fence_after();
+    if (t.split > 1) cluster_arrive();
+    if (warp == 2) tmem_free<1>(tmem, max(32, t.columns));
+    if (t.split > 1) cluster_wait();
     if (ok) {
         // ------------------------------------------------ results
         // A thread takes four features of a column; the partials of all CTAs
         // are asked for before the first is added (one after the other, each a
         // trip to another SM, took 8 of the 12 us of 333 rows, 2500 to 1000).
         const Epilogue& e = t.e;
-        constexpr int kAcross = (PAIR ? 64 : 128) / 4;
+        constexpr int kAcross = (PAIR ? 64 : 128) / 4, kApart = kRowThreads / kAcross;
+        constexpr int kBatch = SPLIT > 2 ? 1 : 2;   // columns whose partials are asked for together
         const int f = 4 * (int(threadIdx.x) % kAcross);
         const int64_t n = n0 + f;
         const bool four = t.vec && n + 3 < t.N;
@@ -192,30 +197,53 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                     if (n + i < t.N) bias[i] = load1(static_cast<const char*>(e.bias), n + i, 0, e.half);
         }
         if (n < t.N)
-            for (int c = rank + t.split * int(threadIdx.x / kAcross); c < cols; c += t.split * (kRowThreads / kAcross)) {
-                const int64_t m = m0 + c;
-                const uint32_t at = smem_addr(part + c * kRowFeatures + f);
-                float z[4], u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (four && e.other) load4(e.other, m * e.other_rs + n, e.other_f32, e.half, o);
-                join(at, t.split, z);
-                if (PAIR) join(at + 64 * 4, t.split, u);
-                if (four)
-                    put4<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n, z, u, bias, o);
-                else
-                    for (int i = 0; i < 4; i++)
-                        if (n + i < t.N)
-                            put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[i], u[i], bias[i]);
+            for (int c = rank + t.split * int(threadIdx.x / kAcross); c < cols; c += kBatch * kApart * t.split) {
+                float z[kBatch][4], u[kBatch][4], o[kBatch][4];
+#pragma unroll
+                for (int b = 0; b < kBatch; b++) {
+                    const int at = min(c + b * kApart * t.split, cols - 1);
+                    const uint32_t from = smem_addr(part + at * kRowFeatures + f);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) u[b][i] = o[b][i] = 0.0f;
+                    if (four && e.other) load4(e.other, (m0 + at) * e.other_rs + n, e.other_f32, e.half, o[b]);
+                    join<SPLIT>(from, t.split, z[b]);
+                    if (PAIR) join<SPLIT>(from + 64 * 4, t.split, u[b]);
+                }
+#pragma unroll
+                for (int b = 0; b < kBatch; b++) {
+                    const int64_t m = m0 + c + b * kApart * t.split;
+                    if (m >= m0 + cols) break;
+                    if (four)
+                        put4<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n, z[b], u[b], bias, o[b]);
+                    else
+                        for (int i = 0; i < 4; i++)
+                            if (n + i < t.N)
+                                put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[b][i], u[b][i], bias[i]);
+                }
             }
     }
     __syncwarp();
     if (t.split > 1) cluster_sync();   // the others have read this CTA's partials
-    tc_fence_after();
-    if (warp == 2) tmem_free<1>(tmem, max(32, t.columns));
 }
 
 }  // namespace
 
 using RowKernel = void (*)(RowArgs);
+
+// kernels for up to 2, 4 and 8 CTAs of a cluster: as many partials as are
+// asked for at a time
+inline int row_split_class(int split) { return split <= 2 ? 0 : split <= 4 ? 1 : 2; }
+
+template <bool PAIR, int FINISH>
+RowKernel row_kernel_of(int act, int split)
+{
+    const int c = row_split_class(split);
+    RowKernel k = nullptr;
+#define DPDR_CALL(A) k = c == 0 ? row_kernel<PAIR, FINISH, A, 2> : c == 1 ? row_kernel<PAIR, FINISH, A, 4> : row_kernel<PAIR, FINISH, A, 8>
+    DPDR_FOR_ACT(act, DPDR_CALL)
+#undef DPDR_CALL
+    return k;
+}
 
 }  // namespace proj
 }  // namespace dpdr

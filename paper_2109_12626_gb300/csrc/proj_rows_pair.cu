@@ -4,13 +4,9 @@
 namespace dpdr {
 namespace proj {
 
-RowKernel row_kernel_pair(int finish, int act)
+RowKernel row_kernel_pair(int finish, int act, int split)
 {
-    RowKernel k = nullptr;
-#define DPDR_CALL(A) k = finish == kSlope ? row_kernel<true, kSlope, A> : row_kernel<true, kValue, A>
-    DPDR_FOR_ACT(act, DPDR_CALL)
-#undef DPDR_CALL
-    return k;
+    return finish == kSlope ? row_kernel_of<true, kSlope>(act, split) : row_kernel_of<true, kValue>(act, split);
 }
 
 }  // namespace proj

@@ -77,7 +77,7 @@ class _Projection:
             return 0
         if t.dtype is not dtype:
             raise TypeError("%s is %s, the plan wants %s" % (name, t.dtype, dtype))
-        if tuple(t.shape) != (rows, cols):
+        if t.shape != (rows, cols):
             raise ValueError("%s is %s, the plan wants %s" % (name, tuple(t.shape), (rows, cols)))
         if t.get_device() != self._device:
             raise ValueError("%s is not on the plan's device" % name)
@@ -91,7 +91,7 @@ class _Projection:
             return 0
         if t.dtype is not dtype:
             raise TypeError("%s is %s, the plan wants %s" % (name, t.dtype, dtype))
-        if tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1):
+        if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
             raise ValueError("%s: the plan wants %d contiguous elements" % (name, n))
         if t.get_device() != self._device:
             raise ValueError("%s is not on the plan's device" % name)
