@@ -20,6 +20,17 @@ __device__ __forceinline__ uint16_t narrow(float v, int half)
     return half ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
 }
 
+// two values rounded, the first in the lower half
+__device__ __forceinline__ uint32_t narrow2(float a, float b, int half)
+{
+    if (half) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 __device__ __forceinline__ float load1(const char* p, int64_t i, int f32, int half)
 {
     return f32 ? reinterpret_cast<const float*>(p)[i] : widen(reinterpret_cast<const uint16_t*>(p)[i], half);
@@ -109,16 +120,30 @@ __device__ __forceinline__ void finish1(float g, float u, float other, float& ou
 
 // ------------------------------------------------ results by fours
 
-__device__ __forceinline__ void load4(const char* p, int64_t i, int f32, int half, float (&v)[4])
+__device__ __forceinline__ void widen4(const uint4& x, int f32, int half, float (&v)[4])
 {
     if (f32) {
-        const float4 x = *reinterpret_cast<const float4*>(p + 4 * i);
-        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-    } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(p + 2 * i);
-        v[0] = widen(uint16_t(x.x), half), v[1] = widen(uint16_t(x.x >> 16), half);
-        v[2] = widen(uint16_t(x.y), half), v[3] = widen(uint16_t(x.y >> 16), half);
+        v[0] = __uint_as_float(x.x), v[1] = __uint_as_float(x.y), v[2] = __uint_as_float(x.z), v[3] = __uint_as_float(x.w);
+    } else if (half) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&x.x)),
+                     b = __half22float2(*reinterpret_cast<const __half2*>(&x.y));
+        v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+    } else {   // a bfloat16 is the upper half of a float
+        v[0] = __uint_as_float(x.x << 16), v[1] = __uint_as_float(x.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(x.y << 16), v[3] = __uint_as_float(x.y & 0xFFFF0000u);
     }
+}
+
+__device__ __forceinline__ void load4(const char* p, int64_t i, int f32, int half, float (&v)[4])
+{
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (f32) {
+        x = *reinterpret_cast<const uint4*>(p + 4 * i);
+    } else {
+        const uint2 y = *reinterpret_cast<const uint2*>(p + 2 * i);
+        x.x = y.x, x.y = y.y;
+    }
+    widen4(x, f32, half, v);
 }
 
 __device__ __forceinline__ void store4(char* p, int64_t i, int f32, int half, const float (&v)[4])
@@ -126,9 +151,7 @@ __device__ __forceinline__ void store4(char* p, int64_t i, int f32, int half, co
     if (f32)
         *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[0], v[1], v[2], v[3]);
     else
-        *reinterpret_cast<uint2*>(p + 2 * i) =
-            make_uint2(uint32_t(narrow(v[0], half)) | uint32_t(narrow(v[1], half)) << 16,
-                       uint32_t(narrow(v[2], half)) | uint32_t(narrow(v[3], half)) << 16);
+        *reinterpret_cast<uint2*>(p + 2 * i) = make_uint2(narrow2(v[0], v[1], half), narrow2(v[2], v[3], half));
 }
 
 // One result element from its sum (or pair of sums)

@@ -59,10 +59,13 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// an arrival at a barrier of any CTA of the cluster (address from in_cta)
+// An arrival at a barrier of any CTA of the cluster (address from in_cta).  It
+// orders no memory: it tells that tensor memory has been read, which the
+// fences of tcgen05 order, and as a release it waited for the results' stores
+// to reach L2, 2 us a tile.
 __device__ __forceinline__ void bar_arrive_at(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
@@ -218,7 +221,19 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// 32 columns of this warp's 32 lanes: v[i] is (lane, column + i)
+// 16 columns of this warp's 32 lanes: v[i] is (lane, column + i)
+__device__ __forceinline__ void tmem_load16(float* v, uint32_t at)
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+}
+
+// and 32 columns
 __device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t at)
 {
     uint32_t* r = reinterpret_cast<uint32_t*>(v);
@@ -233,7 +248,19 @@ __device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t at)
         : "r"(at));
 }
 
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The loads so far are complete; v passes through, so that nothing is done
+// with it before.
+__device__ __forceinline__ void tmem_load_wait(float (&v)[32])
+{
+    asm volatile(
+        "tcgen05.wait::ld.sync.aligned;"
+        : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+          "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]),
+          "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]),
+          "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+        :
+        : "memory");
+}
 
 }  // namespace proj
 }  // namespace dpdr

@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
         for (int c0 = (warp >> 2) * 32; c0 < cols; c0 += 64) {
             float v[32];
             tmem_load32(v, tmem + c0 + (uint32_t(quarter) << 21));
-            tmem_load_wait();
+            tmem_load_wait(v);
 #pragma unroll
             for (int i = 0; i < 32; i++)
                 if (c0 + i < cols) part[(c0 + i) * kRowFeatures + quarter * 32 + lane] = some ? v[i] : 0.0f;

@@ -25,12 +25,17 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     t.kind = p.kind;
     t.segments = p.kind == kChain ? 2 : 1;
     t.steps = int((p.K + kStep - 1) / kStep);
-    t.width = p.kind == kPair ? 128 : 256;
+    const int width = p.kind == kPair ? 128 : 256;
     t.tiles_m = int((p.M + 255) / 256);
-    t.tiles_n = int((p.N + t.width - 1) / t.width);
+    t.tiles_n = int((p.N + width - 1) / width);
     const int64_t tiles = int64_t(t.tiles_m) * t.tiles_n * (p.kind == kTwin ? 2 : 1);
     if (tiles > (int64_t(1) << 30)) return fail_c(DPDR_ERR_INVALID, "projection: more than 2^30 tiles");
     t.tiles = int(tiles);
+    // A last round of tiles that fills at most half of the pairs is taken in
+    // halves, which keeps all of them at work for about half as long.
+    const int pairs_all = P->num_sms / 2, left = t.tiles % pairs_all;
+    t.whole = 2 * left <= pairs_all ? t.tiles - left : t.tiles;
+    t.items = t.whole + 2 * (t.tiles - t.whole);
     t.vec = by_fours(p.e);
     t.M = p.M;
     t.N = p.N;
@@ -41,6 +46,10 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     if (!rc && two_a) rc = tensor_map(&t.a[1], p.a[1], p.M, p.K, p.e.half, 128, kStep);
     if (!rc) rc = tensor_map(&t.b[0], p.b[0], p.N, p.K, p.e.half, 128, kStep);
     if (!rc && two_b) rc = tensor_map(&t.b[1], p.b[1], p.N, p.K, p.e.half, 128, kStep);
+    if (t.whole < t.tiles) {
+        if (!rc) rc = tensor_map(&t.b_half[0], p.b[0], p.N, p.K, p.e.half, 64, kStep);
+        if (!rc && two_b) rc = tensor_map(&t.b_half[1], p.b[1], p.N, p.K, p.e.half, 64, kStep);
+    }
     if (rc) return rc;
     const TileKernel kernel = p.kind == kPair ? tile_kernel_pair(p.e.finish, p.e.act)
                                               : tile_kernel_single(p.e.finish, p.e.act);
@@ -51,7 +60,7 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
         if (e != cudaSuccess) return cuda_fail_c(e, "projection tile kernel");
         set = true;
     }
-    const int pairs = int(tiles < P->num_sms / 2 ? tiles : P->num_sms / 2);
+    const int pairs = t.items < pairs_all ? t.items : pairs_all;
     return launch(kernel, dim3(unsigned(2 * pairs)), kThreads, kSmem, 2, s, "projection tile kernel", t);
 }
 

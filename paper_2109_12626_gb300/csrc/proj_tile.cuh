@@ -28,110 +28,212 @@ constexpr int kStages = 6;
 constexpr int kStep = 64;                     // summed elements a stage
 constexpr int kHalf = 128 * kStep * 2;        // bytes of one operand of a stage and CTA
 constexpr int kStage = 2 * kHalf;
-constexpr int kStaging = 4 * 32 * 64 * 4;     // 32 x 64 floats a finishing warp
+constexpr int kFinishers = 8;                 // warps
+constexpr int kStaging = kFinishers * 32 * 32 * 4;   // 32 x 32 floats each
 constexpr int kSmem = 1024 + kStages * kStage + kStaging;
-constexpr int kThreads = 256;                 // warps: load, product, tensor memory, -, 4 finishing
+constexpr int kThreads = 128 + 32 * kFinishers;   // warps: load, product, tensor memory, -, finishing
 
 struct TileArgs {
-    CUtensorMap a[2], b[2];
+    CUtensorMap a[2], b[2], b_half[2];   // B's rows by 128 and by 64
     int a_mn, b_mn;                // the other index is the contiguous one
     int kind, steps, segments;     // stages a segment
     int tiles_m, tiles_n, tiles;   // tiles_m of one of kTwin's products
-    int width;                     // result columns a tile
+    // the first `whole` tiles are taken as they are, the rest in two halves of
+    // their columns: `items` in all
+    int whole, items;
     int vec;                       // results and what else is read allow 4 elements at a time
     int64_t M, N;
     Epilogue e;
     uint32_t* err;
 };
 
-// Tiles in bands of 8 rows of tiles, down each band's columns, so that the
+// What item i is: its rows and columns of the result, which of kTwin's
+// products, and how many columns of sums (of a pair, two for each result).
+// Tiles lie in bands of 8 rows of tiles, down each band's columns, so that the
 // tiles in work at a time share their operands in L2.
-__device__ __forceinline__ void tile_place(const TileArgs& t, int i, int& tm, int& tn)
+struct Item {
+    int m, n, sums, twin;
+};
+
+template <bool PAIR>
+__device__ __forceinline__ Item item_of(const TileArgs& t, int i)
 {
+    Item it;
+    int part = 0;
+    it.sums = 256;
+    if (i >= t.whole) {
+        part = (i - t.whole) & 1;
+        i = t.whole + ((i - t.whole) >> 1);
+        it.sums = 128;
+    }
     const int rows = t.tiles / t.tiles_n;
     const int band = 8 * t.tiles_n, b = i / band, first = 8 * b;
     const int high = min(8, rows - first), in = i - b * band;
-    tm = first + in % high;
-    tn = in / high;
+    const int tm = first + in % high, tn = in / high;
+    it.twin = tm >= t.tiles_m;
+    it.m = (tm - it.twin * t.tiles_m) * 256;
+    it.n = PAIR ? tn * 128 + part * 64 : tn * 256 + part * 128;
+    return it;
 }
 
-// Finishes a warp's 32 rows of a tile.  The tensor memory hands each thread a
-// row, the results want rows across threads: 64 columns at a time (of a pair 32
-// and 32) go through shared memory, 16-byte chunk q of row r at q ^ (r & 7), so
-// that neither way meets a bank twice.
+// Finishing a warp's 32 rows of an item: 32 columns of sums at a time (of a
+// pair 16 and 16), every second such round, the other warp of its rows taking
+// the rest.  The tensor memory hands each thread a row, the results want rows
+// across threads: the round goes through shared memory, 16-byte chunk q of row
+// r at q ^ (r & 7), so that neither way meets a bank twice.  What else a result
+// needs (residual, dy) is asked for before the round's sums are fetched, for
+// the first round while the item's products still run: one row at a time, each
+// a trip to memory, took 45 us a tile.
 template <bool PAIR, int FINISH, int ACT>
-__device__ __forceinline__ void finish_rows(const TileArgs& t, uint32_t tmem, float* stage, int lane, int64_t m0,
-                                            int64_t n0, char* out, int64_t out_rs)
-{
-    const Epilogue& e = t.e;
-    constexpr int kCols = PAIR ? 32 : 64;    // result columns a round
-    constexpr int kPer = kCols / 4;          // threads a row
-    const int rows = int(min(int64_t(32), t.M - m0));
-    const int cols = int(min(int64_t(t.width), t.N - n0));
-    for (int c0 = 0; c0 < cols; c0 += kCols) {
-        float v[32];
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            tmem_load32(v, tmem + (PAIR ? h * 128 + c0 : c0 + h * 32));
-            tmem_load_wait();
-#pragma unroll
-            for (int q = 0; q < 8; q++)
-                *reinterpret_cast<float4*>(stage + lane * 64 + 4 * ((h * 8 + q) ^ (lane & 7))) =
-                    make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-        }
-        __syncwarp();
-        if (t.vec) {
-            const int q = lane % kPer, c = c0 + 4 * q;
-            const int64_t n = n0 + c;
-            if (c + 3 < cols) {
-                float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, e.half, bias);
-                // eight rows' other values are asked for before the first
-                // row's results are stored
-                constexpr int kRows = 32 / kPer, kBatch = 8;
-                for (int r0 = lane / kPer; r0 < rows; r0 += kRows * kBatch) {
-                    float o[kBatch][4];
-#pragma unroll
-                    for (int b = 0; b < kBatch; b++) {
-                        o[b][0] = o[b][1] = o[b][2] = o[b][3] = 0.0f;
-                        if (e.other && r0 + b * kRows < rows)
-                            load4(e.other, (m0 + r0 + b * kRows) * e.other_rs + n, e.other_f32, e.half, o[b]);
-                    }
-#pragma unroll
-                    for (int b = 0; b < kBatch; b++) {
-                        const int r = r0 + b * kRows;
-                        if (r >= rows) break;
-                        const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 64 + 4 * (q ^ (r & 7)));
-                        float z[4] = {z4.x, z4.y, z4.z, z4.w}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        if (PAIR) {
-                            const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 64 + 4 * ((8 + q) ^ (r & 7)));
-                            u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
-                        }
-                        put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o[b]);
-                    }
-                }
-            } else {
-                for (int r = lane / kPer; r < rows; r += 32 / kPer)
-                    for (int i = 0; i < 4 && c + i < cols; i++)
-                        put1<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n + i, stage[r * 64 + 4 * (q ^ (r & 7)) + i],
-                                   PAIR ? stage[r * 64 + 4 * ((8 + q) ^ (r & 7)) + i] : 0.0f,
-                                   e.bias ? load1(static_cast<const char*>(e.bias), n + i, 0, e.half) : 0.0f);
-            }
-        } else {
-            for (int h = 0; h < kCols / 32; h++) {
-                const int c = h * 32 + lane, q = c >> 2, i = c & 3;
-                if (c0 + c >= cols) break;
-                const int64_t n = n0 + c0 + c;
-                const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
-#pragma unroll 4
-                for (int r = 0; r < rows; r++)
-                    put1<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, stage[r * 64 + 4 * (q ^ (r & 7)) + i],
-                               PAIR ? stage[r * 64 + 4 * ((8 + q) ^ (r & 7)) + i] : 0.0f, bias);
-            }
-        }
-        __syncwarp();
+struct Finisher {
+    static constexpr int kCols = PAIR ? 16 : 32;     // result columns a round
+    static constexpr int kPer = kCols / 4;           // threads a row
+    static constexpr int kRows = 32 / kPer;          // rows a step
+    static constexpr int kSteps = 32 / kRows;
+
+    const TileArgs& t;
+    float* stage;
+    int q, row;              // this thread's columns (4 q) and first row of a round
+    int turn;                // which of the two warps of these rows
+    uint4 other[kSteps];
+    // of the item
+    int64_t m0, n0;
+    int rows, cols;
+
+    __device__ __forceinline__ Finisher(const TileArgs& args, float* st, int lane, int tu) : t(args), stage(st), turn(tu)
+    {
+        q = lane % kPer;
+        // of a pair, eight threads on two rows four apart: no bank twice
+        row = PAIR ? ((lane >> 2) & 1) * 4 + (lane >> 3) : lane / kPer;
     }
-}
+
+    // asks for what else the four results of each step need
+    __device__ __forceinline__ void fetch(int c0)
+    {
+        const Epilogue& e = t.e;
+        const int c = c0 + 4 * q;
+        if (!e.other || !t.vec || c + 3 >= cols) return;
+        const int size = e.other_f32 ? 4 : 2;
+        const char* p = e.other + ((m0 + row) * e.other_rs + n0 + c) * size;
+        const int64_t down = e.other_rs * kRows * size;
+#pragma unroll
+        for (int b = 0; b < kSteps; b++, p += down)
+            if (row + b * kRows < rows) {
+                if (e.other_f32) {
+                    other[b] = *reinterpret_cast<const uint4*>(p);
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(p);
+                    other[b].x = x.x, other[b].y = x.y;
+                }
+            }
+    }
+
+    __device__ __forceinline__ void start(int64_t m, int64_t n, int sums)
+    {
+        m0 = m, n0 = n;
+        rows = int(max(int64_t(0), min(int64_t(32), t.M - m)));
+        cols = int(min(int64_t(PAIR ? sums / 2 : sums), t.N - n));
+        fetch(turn * kCols);
+    }
+
+    // the round's results, four columns a thread and step
+    template <int HALF, int F32>
+    __device__ __forceinline__ void by_four(int c0, char* out, int64_t out_rs)
+    {
+        const Epilogue& e = t.e;
+        const int64_t n = n0 + c0 + 4 * q;
+        constexpr int kSize = F32 ? 4 : 2;
+        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, HALF, bias);
+        const int64_t m = m0 + row;
+        char* p = out + (m * out_rs + n) * kSize;
+        char* p2 = e.out2 + (m * e.out2_rs + n) * kSize;
+        float* pre = e.pre + (m * e.pre_rs + n);
+        const int64_t down = out_rs * kRows * kSize, down2 = e.out2_rs * kRows * kSize, down_pre = e.pre_rs * kRows;
+#pragma unroll
+        for (int b = 0; b < kSteps; b++) {
+            const int r = row + b * kRows;
+            if (r < rows) {
+                float z[4], u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4], w[4];
+                const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * (q ^ (r & 7)));
+                z[0] = z4.x + bias[0], z[1] = z4.y + bias[1], z[2] = z4.z + bias[2], z[3] = z4.w + bias[3];
+                if (PAIR) {
+                    const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * ((4 + q) ^ (r & 7)));
+                    u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
+                }
+                if (e.pre) {
+                    *reinterpret_cast<float4*>(pre) = make_float4(z[0], z[1], z[2], z[3]);
+                    if (PAIR) *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[0], u[1], u[2], u[3]);
+                }
+                if (e.other) widen4(other[b], e.other_f32, HALF, o);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    w[i] = 0.0f;
+                    finish1<PAIR, FINISH, ACT>(z[i], u[i], o[i], v[i], w[i]);
+                }
+                store4(p, 0, F32, HALF, v);
+                if (PAIR && FINISH == kSlope) store4(p2, 0, F32, HALF, w);
+            }
+            p += down, p2 += down2, pre += down_pre;
+        }
+    }
+
+    // one element a thread and step, for results that do not lie on fours
+    __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs)
+    {
+        const Epilogue& e = t.e;
+        const int c = lane % kCols;
+        if (c0 + c >= cols) return;
+        const int64_t n = n0 + c0 + c;
+        const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
+#pragma unroll 4
+        for (int r = lane / kCols; r < rows; r += 32 / kCols)
+            put1<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, stage[r * 32 + 4 * ((c >> 2) ^ (r & 7)) + (c & 3)],
+                                    PAIR ? stage[r * 32 + 4 * ((4 + (c >> 2)) ^ (r & 7)) + (c & 3)] : 0.0f, bias);
+    }
+
+    // `taken`: the barrier that tells the products' thread that this warp has
+    // fetched its sums
+    __device__ __forceinline__ void finish(uint32_t tmem, int sums, int lane, char* out, int64_t out_rs, uint32_t taken)
+    {
+        const Epilogue& e = t.e;
+        int c0 = turn * kCols;
+        if (c0 >= cols && lane == 0) bar_arrive_at(taken);
+        for (; c0 < cols; c0 += 2 * kCols) {
+            float v[32];
+            if (PAIR) {
+                tmem_load16(v, tmem + c0);
+                tmem_load16(v + 16, tmem + sums / 2 + c0);
+            } else {
+                tmem_load32(v, tmem + c0);
+            }
+            tmem_load_wait(v);
+            if (c0 + 2 * kCols >= cols) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_at(taken);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                *reinterpret_cast<float4*>(stage + lane * 32 + 4 * (i ^ (lane & 7))) =
+                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            __syncwarp();
+            if (t.vec && c0 + kCols <= cols) {
+                if (e.out_f32) {
+                    if (e.half) by_four<1, 1>(c0, out, out_rs);
+                    else by_four<0, 1>(c0, out, out_rs);
+                } else {
+                    if (e.half) by_four<1, 0>(c0, out, out_rs);
+                    else by_four<0, 0>(c0, out, out_rs);
+                }
+                fetch(c0 + 2 * kCols);
+            } else {
+                by_one(c0, lane, out, out_rs);
+            }
+            __syncwarp();
+        }
+    }
+};
 
 template <bool PAIR, int FINISH, int ACT>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t)
@@ -155,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         }
         for (int i = 0; i < 2; i++) {
             bar_init(ready + 8 * i, 1);
-            bar_init(taken + 8 * i, 8);   // four warps of each CTA
+            bar_init(taken + 8 * i, 2 * kFinishers);   // of both CTAs
         }
         bar_init(last, 1);
         bar_init_fence();
@@ -174,19 +276,17 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         int stage = 0, used = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int i = first; i < t.tiles && ok; i += pairs) {
-            int tm, tn;
-            tile_place(t, i, tm, tn);
-            const int twin = tm >= t.tiles_m;
-            const int m0 = (tm - twin * t.tiles_m) * 256 + int(rank) * 128;
-            const int n0 = PAIR ? tn * 128 : tn * 256 + int(rank) * 128;
+        for (int i = first; i < t.items && ok; i += pairs) {
+            const Item it = item_of<PAIR>(t, i);
+            const int m0 = it.m + int(rank) * 128, n0 = it.n + (PAIR ? 0 : int(rank) * (it.sums / 2));
+            const CUtensorMap* b_maps = it.sums == 256 ? t.b : t.b_half;
             for (int k = 0; k < steps; k++) {
                 if (!(ok = bar_wait(empty + 8 * stage, phase ^ 1, waits))) break;
                 const int seg = k >= t.steps, k0 = (seg ? k - t.steps : k) * kStep;
-                const CUtensorMap* ma = &t.a[twin | seg];
-                const CUtensorMap* mb = &t.b[PAIR ? int(rank) : seg];
+                const CUtensorMap* ma = &t.a[it.twin | seg];
+                const CUtensorMap* mb = &b_maps[PAIR ? int(rank) : seg];
                 const uint32_t dst = smem_addr(base) + stage * kStage, bar = in_cta(full + 8 * stage, 0);
-                if (rank == 0) bar_expect(full + 8 * stage, 2 * kStage);
+                if (rank == 0) bar_expect(full + 8 * stage, 2 * kHalf + it.sums * kStep * 2);
                 if (t.a_mn) {
                     tma_load_pair(dst, ma, m0, k0, bar);
                     tma_load_pair(dst + kHalf / 2, ma, m0 + 64, k0, bar);
@@ -195,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 }
                 if (t.b_mn) {
                     tma_load_pair(dst + kHalf, mb, n0, k0, bar);
-                    tma_load_pair(dst + kHalf + kHalf / 2, mb, n0 + 64, k0, bar);
+                    if (it.sums == 256) tma_load_pair(dst + kHalf + kHalf / 2, mb, n0 + 64, k0, bar);
                 } else {
                     tma_load_pair(dst + kHalf, mb, k0, n0, bar);
                 }
@@ -212,13 +312,13 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             }
     } else if (warp == 1 && lane == 0 && rank == 0) {
         // ------------------------------------------------ products
-        const uint32_t desc = mma_desc(256, 256, t.e.half, t.a_mn, t.b_mn);
         const uint32_t a_lead = t.a_mn ? kHalf / 2 : 0, b_lead = t.b_mn ? kHalf / 2 : 0;
         const uint32_t a_step = t.a_mn ? 2048 : 32, b_step = t.b_mn ? 2048 : 32;   // bytes for 16 summed elements
         int stage = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
         bool ok = true;
-        for (int i = first; i < t.tiles && ok; i += pairs) {
+        for (int i = first; i < t.items && ok; i += pairs) {
+            const uint32_t desc = mma_desc(256, i < t.whole ? 256 : 128, t.e.half, t.a_mn, t.b_mn);
             if (!(ok = bar_wait(taken + 8 * acc, acc_phase ^ 1, waits))) break;
             tc_fence_after();
             for (int k = 0; k < steps; k++) {
@@ -242,21 +342,17 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         }
     } else if (warp >= 4) {
         // ------------------------------------------------ results
-        float* stage = reinterpret_cast<float*>(base + kStages * kStage) + (warp - 4) * 32 * 64;
+        const int mine = warp - 4, quarter = mine & 3;
+        Finisher<PAIR, FINISH, ACT> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane, mine >> 2);
         int acc = 0;
         uint32_t acc_phase = 0;
-        for (int i = first; i < t.tiles; i += pairs) {
-            int tm, tn;
-            tile_place(t, i, tm, tn);
-            const int twin = tm >= t.tiles_m;
-            const int64_t m0 = int64_t(tm - twin * t.tiles_m) * 256 + int64_t(rank) * 128 + (warp - 4) * 32;
+        for (int i = first; i < t.items; i += pairs) {
+            const Item it = item_of<PAIR>(t, i);
+            f.start(int64_t(it.m) + int(rank) * 128 + quarter * 32, it.n, it.sums);
             if (!bar_wait(ready + 8 * acc, acc_phase, waits)) break;
             tc_fence_after();
-            finish_rows<PAIR, FINISH, ACT>(t, tmem + acc * 256 + (uint32_t(warp - 4) << 21), stage, lane, m0, int64_t(tn) * t.width,
-                              twin ? t.e.out2 : t.e.out, twin ? t.e.out2_rs : t.e.out_rs);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive_at(in_cta(taken + 8 * acc, 0));
+            f.finish(tmem + acc * 256 + (uint32_t(quarter) << 21), it.sums, lane, it.twin ? t.e.out2 : t.e.out,
+                     it.twin ? t.e.out2_rs : t.e.out_rs, in_cta(taken + 8 * acc, 0));
             if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
     }
