@@ -243,11 +243,13 @@ int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int hal
     return r == CUDA_SUCCESS ? DPDR_OK : fail_c(DPDR_ERR_CUDA, "projection: tensor map refused");
 }
 
-// A packed copy in the plan's slot, made m's place
-static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int f32, int slot, cudaStream_t s)
+// A packed copy in the plan's slot, made m's place: by rows, or by columns
+// where `turned` (whichever index is contiguous stays so).
+static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int slot, bool turned,
+                cudaStream_t s)
 {
-    const int64_t ld = padded(cols);
-    const size_t bytes = size_t(most_rows) * size_t(ld) * 2;
+    const int64_t ld = padded(turned ? rows : cols);
+    const size_t bytes = size_t(turned ? cols : most_rows) * size_t(padded(turned ? most_rows : cols)) * 2;
     if (bytes > P->packed_bytes[slot]) {
         cudaFree(P->packed[slot]);   // waits for its last use
         P->packed[slot] = nullptr;
@@ -256,20 +258,22 @@ static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t mos
         if (e != cudaSuccess) return cuda_fail_c(e, "projection operand copy");
         P->packed_bytes[slot] = bytes;
     }
-    const int rc = pack_launch(static_cast<const char*>(m.data), m.row_stride, m.col_stride, f32, P->half, rows, cols,
-                               P->packed[slot], ld, s);
-    m = dpdr_matrix{P->packed[slot], ld, 1};
+    const char* from = static_cast<const char*>(m.data);
+    char* to = P->packed[slot];
+    const int rc = turned ? pack_launch(from, m.col_stride, m.row_stride, cols, rows, to, ld, s)
+                          : pack_launch(from, m.row_stride, m.col_stride, rows, cols, to, ld, s);
+    m = turned ? dpdr_matrix{to, 1, ld} : dpdr_matrix{to, ld, 1};
     return rc;
 }
 
 // The matrix as TMA can load it: as it lies where one stride is 1, the other a
 // multiple of 8 that is no shorter than a row (column), and the address a
 // multiple of 16 bytes; else a packed copy in the plan's slot.
-static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int f32, int slot,
+static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int slot,
                     cudaStream_t s)
 {
     if (rows == 0 || cols == 0) return DPDR_OK;
-    const bool placed = !f32 && reinterpret_cast<uintptr_t>(m.data) % 16 == 0;
+    const bool placed = reinterpret_cast<uintptr_t>(m.data) % 16 == 0;
     dpdr_matrix as = m;
     if (rows == 1) as.row_stride = padded(cols);   // never stepped over
     if (placed && (as.col_stride == 1 || cols == 1) && as.row_stride % 8 == 0 && as.row_stride >= cols &&
@@ -286,7 +290,7 @@ static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t
         m = as;
         return DPDR_OK;
     }
-    return pack(P, m, rows, cols, most_rows, f32, slot, s);
+    return pack(P, m, rows, cols, most_rows, slot, m.row_stride == 1 && m.col_stride != 1, s);
 }
 
 // Few rows take row_kernel, which reads the weights once for up to 128 rows
@@ -339,20 +343,19 @@ static int operands(Proj* P, int64_t rows, const dpdr_matrix* x, const dpdr_matr
     int rc = DPDR_OK;
     if (x) {
         o.x = *x;
-        rc = loadable(P, o.x, rows, P->n_in, P->max_rows, 0, 0, s);
+        rc = loadable(P, o.x, rows, P->n_in, P->max_rows, 0, s);
     }
     const dpdr_matrix* w[2] = {w0, w1};
     for (int i = 0; i < 2 && !rc; i++) {
         if (!w[i]) continue;
         o.w[i] = *w[i];
-        rc = loadable(P, o.w[i], P->n_out, P->n_in, P->n_out, 0, 1 + i, s);
+        rc = loadable(P, o.w[i], P->n_out, P->n_in, P->n_out, 1 + i, s);
     }
-    if (!rc && w0 && w1 && o.w[0].col_stride != o.w[1].col_stride &&
-        (o.w[0].col_stride == 1 || o.w[1].col_stride == 1)) {
-        // one lies by rows, the other by columns: the latter is copied
+    if (!rc && w0 && w1 && (o.w[0].col_stride == 1) != (o.w[1].col_stride == 1)) {
+        // one lies by rows, the other by columns: the latter is copied again
         const int i = o.w[0].col_stride == 1 ? 1 : 0;
-        o.w[i].data = w[i]->data;
-        rc = pack(P, o.w[i], P->n_out, P->n_in, P->n_out, 0, 1 + i, s);
+        o.w[i] = *w[i];
+        rc = pack(P, o.w[i], P->n_out, P->n_in, P->n_out, 1 + i, false, s);
     }
     return rc;
 }
@@ -392,9 +395,10 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     dpdr_matrix dz[2] = {{P->scratch, ld, 1}, {P->scratch + dz_bytes, ld, 1}};
     float* sums = reinterpret_cast<float*>(P->scratch + n * dz_bytes);
     Epilogue e = epilogue_of(P);
+    bool summed = false;
     if (as_is) {
         dz[0] = *c.dy;
-        if (c.dx || c.dw0) rc = loadable(P, dz[0], rows, N, P->max_rows, 0, 3, s);
+        if (c.dx || c.dw0) rc = loadable(P, dz[0], rows, N, P->max_rows, 3, s);
         if (rc) return rc;
     } else {
         e.finish = kSlope;
@@ -404,13 +408,15 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         e.out_rs = e.out2_rs = ld;
         if (again) {
             rc = forward(P, rows, o.x, o.w[0], o.w[1], c.bias, e, s);
-        } else if (c.pre) {
-            e.pre = static_cast<float*>(c.pre->data);
-            e.pre_rs = c.pre->row_stride;
-            e.pre_up = N;
-            rc = slope_launch(e, P->gated, rows, N, s);
         } else {
-            rc = slope_launch(e, false, rows, N, s);   // dy rounded to the operand type
+            if (c.pre) {   // without: no activation, dy is rounded to the operand type
+                e.pre = static_cast<float*>(c.pre->data);
+                e.pre_rs = c.pre->row_stride;
+                e.pre_up = N;
+            }
+            if (!c.dx && !c.dw0) e.out = e.out2 = nullptr;
+            rc = slope_launch(e, P->gated, rows, N, c.dbias ? sums : nullptr, s);
+            summed = true;
         }
         if (rc) return rc;
     }
@@ -450,9 +456,15 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         rc = product_launch(P, p, s);
         if (rc) return rc;
     }
-    if (c.dbias)
-        rc = column_sums_launch(static_cast<const char*>(dz[0].data), dz[0].row_stride, dz[0].col_stride, 0, P->half,
-                                rows, N, c.dbias, P->grad_f32, sums, s);
+    if (c.dbias) {
+        if (!summed) {   // of dz as it was stored, or of dy
+            Epilogue d = epilogue_of(P);
+            d.act = DPDR_ACT_NONE;
+            set_other(d, dz[0], 0);
+            rc = slope_launch(d, false, rows, N, sums, s);
+        }
+        if (!rc) rc = join_launch(sums, rows, N, c.dbias, P->grad_f32, P->half, s);
+    }
     return rc;
 }
 

@@ -91,18 +91,17 @@ bool by_fours(const Epilogue& e);
 // summed index), or of 64 x `step` where the summed index is the outer one
 int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int half, int rows, int step);
 
-// dz (or dg and du) from the kept projections: e.pre in, e.out (and out2) out
-int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, cudaStream_t s);
-
-// out[c] = sum over r of z[r][c]: z as 16-bit (half: its kind) or float32
-int column_sums_launch(const char* z, int64_t rs, int64_t cs, int z_f32, int half, int64_t rows,
-                       int64_t cols, void* out, int out_f32, float* scratch, cudaStream_t s);
-// rows of the scratch that column_sums_launch needs, cols floats each
+// dz (or dg and du) of at least one row from the kept projections: e.pre and
+// e.other in, e.out (and out2), where given, out.  With `sums` also dz's column
+// sums over column_sum_parts(rows) runs of rows, cols floats each, which
+// join_launch adds up.  No e.pre: z is 0 (of use without an activation).
+int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, float* sums, cudaStream_t s);
 int column_sum_parts(int64_t rows);
+int join_launch(const float* sums, int64_t rows, int64_t cols, void* out, int out_f32, int half, cudaStream_t s);
 
-// a copy with unit column stride and rows ld apart, rounded to 16 bits
-int pack_launch(const char* src, int64_t rs, int64_t cs, int src_f32, int half, int64_t rows,
-                int64_t cols, char* dst, int64_t ld, cudaStream_t s);
+// a copy of 16-bit elements with unit column stride and rows ld apart
+int pack_launch(const char* src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, char* dst, int64_t ld,
+                cudaStream_t s);
 
 }  // namespace proj
 }  // namespace dpdr

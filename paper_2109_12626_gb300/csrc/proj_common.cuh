@@ -42,9 +42,12 @@ __device__ __forceinline__ void store1(char* p, int64_t i, float v, int f32, int
     else reinterpret_cast<uint16_t*>(p)[i] = narrow(v, half);
 }
 
-// The logistic function.  Both divisions are by at least 1, so exp(-z) may
-// overflow to infinity (z below -88) and the quotient is then 0.
-__device__ __forceinline__ float logistic(float z) { return 1.0f / (1.0f + expf(-z)); }
+// The logistic function, by CUDA's fast exponential and division, whose errors
+// (a few units of 2^-23, and 2^-24 of the exponent's size) are far below a
+// 16-bit result's rounding and of the order of a float32 sum's; the exact ones
+// made the element-wise kernels wait for arithmetic.  The divisor is at least
+// 1; where exp(-z) overflows (z below -88) the quotient is 0.
+__device__ __forceinline__ float logistic(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 constexpr float kRootHalf = 0.70710678118654752f;   // sqrt(1/2)
 constexpr float kRoot8Pi = 1.59576912160573072f;    // 2 sqrt(2/pi)
@@ -78,7 +81,7 @@ __device__ __forceinline__ void act_both(float z, float& v, float& d)
     case DPDR_ACT_GELU: {
         const float phi = 0.5f * erfcf(-z * kRootHalf);
         v = z * phi;
-        d = phi + z * kRoot2PiInv * expf(-0.5f * z * z);
+        d = phi + z * kRoot2PiInv * __expf(-0.5f * z * z);
         return;
     }
     case DPDR_ACT_GELU_TANH: {

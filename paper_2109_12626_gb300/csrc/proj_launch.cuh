@@ -21,7 +21,7 @@ __device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.w
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 template <typename... Params, typename... Args>
-int launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s,
+int launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t s,
            const char* what, const Args&... args)
 {
     cudaLaunchAttribute at[2];
@@ -32,7 +32,7 @@ int launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int c
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c = {};
     c.gridDim = grid;
-    c.blockDim = dim3(unsigned(threads));
+    c.blockDim = block;
     c.dynamicSmemBytes = smem;
     c.stream = s;
     c.attrs = at;

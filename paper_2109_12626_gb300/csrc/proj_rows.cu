@@ -64,7 +64,7 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
         if (e != cudaSuccess) return cuda_fail_c(e, "projection row kernel");
         set = true;
     }
-    return launch(kernel, dim3(unsigned(across * split), unsigned(down)), kRowThreads, size_t(smem), split, s,
+    return launch(kernel, dim3(unsigned(across * split), unsigned(down)), dim3(kRowThreads), size_t(smem), split, s,
                   "projection row kernel", t);
 }
 

@@ -61,7 +61,7 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
         set = true;
     }
     const int pairs = t.items < pairs_all ? t.items : pairs_all;
-    return launch(kernel, dim3(unsigned(2 * pairs)), kThreads, kSmem, 2, s, "projection tile kernel", t);
+    return launch(kernel, dim3(unsigned(2 * pairs)), dim3(kThreads), kSmem, 2, s, "projection tile kernel", t);
 }
 
 }  // namespace proj

@@ -81,9 +81,9 @@ __device__ __forceinline__ Item item_of(const TileArgs& t, int i)
 // the rest.  The tensor memory hands each thread a row, the results want rows
 // across threads: the round goes through shared memory, 16-byte chunk q of row
 // r at q ^ (r & 7), so that neither way meets a bank twice.  What else a result
-// needs (residual, dy) is asked for before the round's sums are fetched, for
-// the first round while the item's products still run: one row at a time, each
-// a trip to memory, took 45 us a tile.
+// needs (residual, dy) is asked into L2 while the item's products still run,
+// and into registers a round ahead: one row at a time, each a trip to memory,
+// took 45 us a tile.
 template <bool PAIR, int FINISH, int ACT>
 struct Finisher {
     static constexpr int kCols = PAIR ? 16 : 32;     // result columns a round
@@ -107,33 +107,44 @@ struct Finisher {
         row = PAIR ? ((lane >> 2) & 1) * 4 + (lane >> 3) : lane / kPer;
     }
 
-    // asks for what else the four results of each step need
-    __device__ __forceinline__ void fetch(int c0)
+    // Asks for what else the four results of step b of a round need.  Where it
+    // lies: columns c0 on of this thread's first row.
+    __device__ __forceinline__ const char* other_at(int c0) const
     {
         const Epilogue& e = t.e;
-        const int c = c0 + 4 * q;
-        if (!e.other || !t.vec || c + 3 >= cols) return;
-        const int size = e.other_f32 ? 4 : 2;
-        const char* p = e.other + ((m0 + row) * e.other_rs + n0 + c) * size;
-        const int64_t down = e.other_rs * kRows * size;
-#pragma unroll
-        for (int b = 0; b < kSteps; b++, p += down)
-            if (row + b * kRows < rows) {
-                if (e.other_f32) {
-                    other[b] = *reinterpret_cast<const uint4*>(p);
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(p);
-                    other[b].x = x.x, other[b].y = x.y;
-                }
-            }
+        return e.other + ((m0 + row) * e.other_rs + n0 + c0 + 4 * q) * (e.other_f32 ? 4 : 2);
     }
+    __device__ __forceinline__ void fetch(int b, const char* at)
+    {
+        const Epilogue& e = t.e;
+        if (row + b * kRows >= rows) return;
+        if (e.other_f32) {
+            other[b] = *reinterpret_cast<const uint4*>(at + b * kRows * e.other_rs * 4);
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(at + b * kRows * e.other_rs * 2);
+            other[b].x = x.x, other[b].y = x.y;
+        }
+    }
+    // whether a round of fours starts at c0
+    __device__ __forceinline__ bool fours(int c0) const { return t.vec && c0 + kCols <= cols; }
 
-    __device__ __forceinline__ void start(int64_t m, int64_t n, int sums)
+    __device__ __forceinline__ void start(int64_t m, int64_t n, int sums, int lane)
     {
         m0 = m, n0 = n;
         rows = int(max(int64_t(0), min(int64_t(32), t.M - m)));
         cols = int(min(int64_t(PAIR ? sums / 2 : sums), t.N - n));
-        fetch(turn * kCols);
+        const Epilogue& e = t.e;
+        if (!e.other || !t.vec || cols <= 0) return;
+        const int size = e.other_f32 ? 4 : 2;
+        if (lane < rows) {   // a row a lane, every second line of it
+            const char* p = e.other + ((m0 + lane) * e.other_rs + n0) * size;
+            for (int at = 128 * turn; at < cols * size; at += 256) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + at));
+        }
+        if (fours(turn * kCols)) {
+            const char* at = other_at(turn * kCols);
+#pragma unroll
+            for (int b = 0; b < kSteps; b++) fetch(b, at);
+        }
     }
 
     // the round's results, four columns a thread and step
@@ -149,6 +160,8 @@ struct Finisher {
         char* p = out + (m * out_rs + n) * kSize;
         char* p2 = e.out2 + (m * e.out2_rs + n) * kSize;
         float* pre = e.pre + (m * e.pre_rs + n);
+        const bool more = e.other && fours(c0 + 2 * kCols);
+        const char* next = more ? other_at(c0 + 2 * kCols) : nullptr;
         const int64_t down = out_rs * kRows * kSize, down2 = e.out2_rs * kRows * kSize, down_pre = e.pre_rs * kRows;
 #pragma unroll
         for (int b = 0; b < kSteps; b++) {
@@ -166,6 +179,7 @@ struct Finisher {
                     if (PAIR) *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[0], u[1], u[2], u[3]);
                 }
                 if (e.other) widen4(other[b], e.other_f32, HALF, o);
+                if (more) fetch(b, next);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     w[i] = 0.0f;
@@ -218,7 +232,7 @@ struct Finisher {
                 *reinterpret_cast<float4*>(stage + lane * 32 + 4 * (i ^ (lane & 7))) =
                     make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             __syncwarp();
-            if (t.vec && c0 + kCols <= cols) {
+            if (fours(c0)) {
                 if (e.out_f32) {
                     if (e.half) by_four<1, 1>(c0, out, out_rs);
                     else by_four<0, 1>(c0, out, out_rs);
@@ -226,7 +240,6 @@ struct Finisher {
                     if (e.half) by_four<1, 0>(c0, out, out_rs);
                     else by_four<0, 0>(c0, out, out_rs);
                 }
-                fetch(c0 + 2 * kCols);
             } else {
                 by_one(c0, lane, out, out_rs);
             }
@@ -348,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         uint32_t acc_phase = 0;
         for (int i = first; i < t.items; i += pairs) {
             const Item it = item_of<PAIR>(t, i);
-            f.start(int64_t(it.m) + int(rank) * 128 + quarter * 32, it.n, it.sums);
+            f.start(int64_t(it.m) + int(rank) * 128 + quarter * 32, it.n, it.sums, lane);
             if (!bar_wait(ready + 8 * acc, acc_phase, waits)) break;
             tc_fence_after();
             f.finish(tmem + acc * 256 + (uint32_t(quarter) << 21), it.sums, lane, it.twin ? t.e.out2 : t.e.out,
