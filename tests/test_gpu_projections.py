@@ -295,6 +295,34 @@ def test_gradients_against_differences(act):
             [t.double() for t in (x, w, w2)], d)
 
 
+@pytest.mark.parametrize("rows,k,n", [(2100, 2100, 2100), (1300, 1600, 3900), (2600, 2104, 1000), (2600, 1000, 2104)])
+def test_products_whose_last_tiles_are_few(rows, k, n):
+    """Sizes whose 256 x 256 tiles leave a last round of few, which is cut
+    finer; twice on one plan, with the same bits."""
+    g = gen(rows, k, n, 23)
+    x, w, w2 = U.matrix(g, rows, k, "bfloat16"), *(U.matrix(g, n, k, "bfloat16", scale=k ** -0.5) for _ in range(2))
+    dy = U.matrix(g, rows, n, "bfloat16")
+    b = U.matrix(g, 1, n, "bfloat16").reshape(-1)
+    with dpdr.Linear(rows, k, n, act="silu") as lin, dpdr.Gated(rows, k, n) as gat:
+        first = None
+        for _ in range(2):
+            y, h, dx, dw, db = (torch.empty_like(t) for t in (dy, dy, x, w, b))
+            gx, gg, gu = (torch.empty_like(t) for t in (x, w, w2))
+            lin.forward(x, w, y, bias=b, residual=dy)
+            lin.backward(x, w, dy, dx, dw, db, bias=b)
+            gat.forward(x, w, w2, h)
+            gat.backward(x, w, w2, dy, gx, gg, gu)
+            lin.sync()
+            gat.sync()
+            got = [y, dx, dw, db, h, gx, gg, gu]
+            assert first is None or all(torch.equal(p, q) for p, q in zip(first, got))
+            first = got
+    U.check_linear(y, x, w, b, dy, "silu", "bfloat16")
+    U.check_linear_gradients(x, w, b, dy, "silu", "bfloat16", "bfloat16", dx, dw, db)
+    U.check_gated(h, x, w, w2, "silu", "bfloat16")
+    U.check_gated_gradients(x, w, w2, dy, "silu", "bfloat16", "bfloat16", gx, [gg, gu])
+
+
 # ------------------------------------------------------- edges of the range
 
 def test_no_rows():
