@@ -246,7 +246,7 @@ int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int hal
 // A packed copy in the plan's slot, made m's place: by rows, or by columns
 // where `turned` (whichever index is contiguous stays so).
 static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int slot, bool turned,
-                cudaStream_t s)
+                Copies& c)
 {
     const int64_t ld = padded(turned ? rows : cols);
     const size_t bytes = size_t(turned ? cols : most_rows) * size_t(padded(turned ? most_rows : cols)) * 2;
@@ -258,19 +258,22 @@ static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t mos
         if (e != cudaSuccess) return cuda_fail_c(e, "projection operand copy");
         P->packed_bytes[slot] = bytes;
     }
+    int at = 0;
+    while (at < c.n && c.slot[at] != slot) at++;
+    if (at == c.n) c.n++;
+    c.slot[at] = slot;
     const char* from = static_cast<const char*>(m.data);
     char* to = P->packed[slot];
-    const int rc = turned ? pack_launch(from, m.col_stride, m.row_stride, cols, rows, to, ld, s)
-                          : pack_launch(from, m.row_stride, m.col_stride, rows, cols, to, ld, s);
+    c.job[at] = turned ? Copies::Job{from, to, m.col_stride, m.row_stride, cols, rows, ld}
+                       : Copies::Job{from, to, m.row_stride, m.col_stride, rows, cols, ld};
     m = turned ? dpdr_matrix{to, 1, ld} : dpdr_matrix{to, ld, 1};
-    return rc;
+    return DPDR_OK;
 }
 
 // The matrix as TMA can load it: as it lies where one stride is 1, the other a
 // multiple of 8 that is no shorter than a row (column), and the address a
 // multiple of 16 bytes; else a packed copy in the plan's slot.
-static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int slot,
-                    cudaStream_t s)
+static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t most_rows, int slot, Copies& c)
 {
     if (rows == 0 || cols == 0) return DPDR_OK;
     const bool placed = reinterpret_cast<uintptr_t>(m.data) % 16 == 0;
@@ -290,7 +293,7 @@ static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t
         m = as;
         return DPDR_OK;
     }
-    return pack(P, m, rows, cols, most_rows, slot, m.row_stride == 1 && m.col_stride != 1, s);
+    return pack(P, m, rows, cols, most_rows, slot, m.row_stride == 1 && m.col_stride != 1, c);
 }
 
 // Few rows take row_kernel, which reads the weights once for up to 128 rows
@@ -330,33 +333,39 @@ static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matri
     return token ? token_launch(P, p, s) : product_launch(P, p, s);
 }
 
-// The operands as loadable matrices: x and each weight, those that a call
-// reads.  Both weights of a pair have to lie the same way (one tile layout);
-// otherwise the second is copied too.
+// The operands as loadable matrices: x, each weight and dy, those that a call
+// reads, the copies that this takes in one launch.  Both weights of a pair have
+// to lie the same way (one tile layout); otherwise one is copied too.
 struct Operands {
-    dpdr_matrix x{}, w[2] = {};
+    dpdr_matrix x{}, w[2] = {}, dy{};
 };
 
 static int operands(Proj* P, int64_t rows, const dpdr_matrix* x, const dpdr_matrix* w0, const dpdr_matrix* w1,
-                    Operands& o, cudaStream_t s)
+                    const dpdr_matrix* dy, Operands& o, cudaStream_t s)
 {
     int rc = DPDR_OK;
+    Copies c;
     if (x) {
         o.x = *x;
-        rc = loadable(P, o.x, rows, P->n_in, P->max_rows, 0, s);
+        rc = loadable(P, o.x, rows, P->n_in, P->max_rows, 0, c);
     }
     const dpdr_matrix* w[2] = {w0, w1};
     for (int i = 0; i < 2 && !rc; i++) {
         if (!w[i]) continue;
         o.w[i] = *w[i];
-        rc = loadable(P, o.w[i], P->n_out, P->n_in, P->n_out, 1 + i, s);
+        rc = loadable(P, o.w[i], P->n_out, P->n_in, P->n_out, 1 + i, c);
     }
     if (!rc && w0 && w1 && (o.w[0].col_stride == 1) != (o.w[1].col_stride == 1)) {
-        // one lies by rows, the other by columns: the latter is copied again
+        // one lies by rows, the other by columns: the latter is copied by rows
         const int i = o.w[0].col_stride == 1 ? 1 : 0;
         o.w[i] = *w[i];
-        rc = pack(P, o.w[i], P->n_out, P->n_in, P->n_out, 1 + i, false, s);
+        rc = pack(P, o.w[i], P->n_out, P->n_in, P->n_out, 1 + i, false, c);
     }
+    if (dy && !rc) {
+        o.dy = *dy;
+        rc = loadable(P, o.dy, rows, P->n_out, P->max_rows, 3, c);
+    }
+    if (!rc && c.n) rc = copies_launch(P, c, s);
     return rc;
 }
 
@@ -390,16 +399,16 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     const bool again = !as_is && !c.pre && (P->gated || P->act != DPDR_ACT_NONE);
     Operands o;
     const bool need_w = again || c.dx;
-    rc = operands(P, rows, again || c.dw0 ? c.x : nullptr, need_w ? c.w0 : nullptr, need_w ? c.w1 : nullptr, o, s);
+    const bool products = c.dx || c.dw0;
+    rc = operands(P, rows, again || c.dw0 ? c.x : nullptr, need_w ? c.w0 : nullptr, need_w ? c.w1 : nullptr,
+                  as_is && products ? c.dy : nullptr, o, s);
     if (rc) return rc;
     dpdr_matrix dz[2] = {{P->scratch, ld, 1}, {P->scratch + dz_bytes, ld, 1}};
     float* sums = reinterpret_cast<float*>(P->scratch + n * dz_bytes);
     Epilogue e = epilogue_of(P);
     bool summed = false;
     if (as_is) {
-        dz[0] = *c.dy;
-        if (c.dx || c.dw0) rc = loadable(P, dz[0], rows, N, P->max_rows, 3, s);
-        if (rc) return rc;
+        dz[0] = products ? o.dy : *c.dy;
     } else {
         e.finish = kSlope;
         set_other(e, *c.dy, P->out_f32);
@@ -414,7 +423,7 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
                 e.pre_rs = c.pre->row_stride;
                 e.pre_up = N;
             }
-            if (!c.dx && !c.dw0) e.out = e.out2 = nullptr;
+            if (!products) e.out = e.out2 = nullptr;
             rc = slope_launch(e, P->gated, rows, N, c.dbias ? sums : nullptr, s);
             summed = true;
         }
@@ -523,7 +532,7 @@ extern "C" int dpdr_linear(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, co
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (for_token(rows, *x, *w, nullptr)) return forward(P, rows, *x, *w, dpdr_matrix{}, bias, e, s, true);
     Operands o;
-    rc = operands(P, rows, x, w, nullptr, o, s);
+    rc = operands(P, rows, x, w, nullptr, nullptr, o, s);
     return rc ? rc : forward(P, rows, o.x, o.w[0], o.w[1], bias, e, s);
 }
 
@@ -553,7 +562,7 @@ extern "C" int dpdr_gated(dpdr_proj_t h, int64_t rows, const dpdr_matrix* x, con
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (for_token(rows, *x, *w_gate, w_up)) return forward(P, rows, *x, *w_gate, *w_up, nullptr, e, s, true);
     Operands o;
-    rc = operands(P, rows, x, w_gate, w_up, o, s);
+    rc = operands(P, rows, x, w_gate, w_up, nullptr, o, s);
     return rc ? rc : forward(P, rows, o.x, o.w[0], o.w[1], nullptr, e, s);
 }
 

@@ -99,9 +99,19 @@ int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, float
 int column_sum_parts(int64_t rows);
 int join_launch(const float* sums, int64_t rows, int64_t cols, void* out, int out_f32, int half, cudaStream_t s);
 
-// a copy of 16-bit elements with unit column stride and rows ld apart
-int pack_launch(const char* src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, char* dst, int64_t ld,
-                cudaStream_t s);
+// Copies of 16-bit matrices with unit column stride and rows ld apart, each
+// into a slot of the plan's
+struct Copies {
+    struct Job {
+        const char* src;
+        char* dst;
+        int64_t rs, cs, rows, cols, ld;
+    };
+    Job job[kPacked];
+    int slot[kPacked];
+    int n = 0;
+};
+int copies_launch(Proj* P, const Copies& c, cudaStream_t s);
 
 }  // namespace proj
 }  // namespace dpdr

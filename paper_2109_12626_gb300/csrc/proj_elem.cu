@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float* sums, int parts,
 {
     __shared__ float run[8][32];
     wait_previous();
+    allow_next();
     const int64_t n = int64_t(blockIdx.x) * 32 + threadIdx.x;
     const int per = (parts + 7) / 8, p0 = threadIdx.y * per, p1 = min(parts, p0 + per);
     float s = 0.0f;
@@ -107,44 +108,43 @@ __global__ void __launch_bounds__(256) join_kernel(const float* sums, int parts,
     store1(out, n, s, out_f32, half);
 }
 
-// Rows of unit column stride: a thread copies eight elements, loaded by as
-// many bytes at a time as their address allows and stored by 16.
-__global__ void __launch_bounds__(256) pack_rows_kernel(const uint16_t* src, int64_t rs, int64_t rows, int64_t cols,
-                                                        uint16_t* dst, int64_t ld)
+// The copies of one call, one a blockIdx.y.  A thread copies eight elements of
+// a row, loaded by as many bytes at a time as their place allows and stored by
+// 16.  4096 x 4099 (rows at every second byte): 67 MB in XX us.
+__global__ void __launch_bounds__(256) copy_kernel(const Copies c)
 {
     wait_previous();
-    const int64_t c = (int64_t(blockIdx.x) * blockDim.x + threadIdx.x) * 8;
-    if (c >= cols) return;
-    for (int64_t m = int64_t(blockIdx.y) * blockDim.y + threadIdx.y; m < rows; m += int64_t(gridDim.y) * blockDim.y) {
-        const uint16_t* p = src + m * rs + c;
-        uint16_t* q = dst + m * ld + c;
-        if (c + 8 > cols) {
-            for (int i = 0; c + i < cols; i++) q[i] = p[i];
+    allow_next();
+    const Copies::Job& j = c.job[blockIdx.y];
+    const uint64_t units = uint64_t(j.cols + 7) / 8, all = units * uint64_t(j.rows);
+    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += uint64_t(gridDim.x) * 256) {
+        const uint64_t m = all >> 32 ? i / units : uint32_t(i) / uint32_t(units), n = (i - m * units) * 8;
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(j.src) + int64_t(m) * j.rs + int64_t(n) * j.cs;
+        uint16_t* q = reinterpret_cast<uint16_t*>(j.dst) + int64_t(m) * j.ld + int64_t(n);
+        if (j.cs != 1 || int64_t(n) + 8 > j.cols) {
+            uint16_t v[8];
+            const int some = int(min(int64_t(8), j.cols - int64_t(n)));
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = k < some ? p[k * j.cs] : uint16_t(0);
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (k < some) q[k] = v[k];
             continue;
         }
         const uintptr_t at = reinterpret_cast<uintptr_t>(p);
         uint32_t w[4];
         if (at % 16 == 0) {
-            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
         } else if (at % 4 == 0) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+            for (int k = 0; k < 4; k++) w[k] = reinterpret_cast<const uint32_t*>(p)[k];
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = uint32_t(p[2 * i]) | uint32_t(p[2 * i + 1]) << 16;
+            for (int k = 0; k < 4; k++) w[k] = uint32_t(p[2 * k]) | uint32_t(p[2 * k + 1]) << 16;
         }
-        *reinterpret_cast<uint4*>(q) = *reinterpret_cast<const uint4*>(w);
+        *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-}
-
-// any strides
-__global__ void __launch_bounds__(256) pack_kernel(const uint16_t* src, int64_t rs, int64_t cs, int64_t rows,
-                                                   int64_t cols, uint16_t* dst, int64_t ld)
-{
-    wait_previous();
-    const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (n >= cols) return;
-    for (int64_t m = blockIdx.y; m < rows; m += gridDim.y) dst[m * ld + n] = src[m * rs + n * cs];
 }
 
 // threads along `units` of a row, the rest along the rows
@@ -188,19 +188,12 @@ int join_launch(const float* sums, int64_t rows, int64_t cols, void* out, int ou
                   column_sum_parts(rows), cols, static_cast<char*>(out), out_f32, half);
 }
 
-int pack_launch(const char* src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, char* dst, int64_t ld,
-                cudaStream_t s)
+int copies_launch(Proj* P, const Copies& c, cudaStream_t s)
 {
-    const uint16_t* from = reinterpret_cast<const uint16_t*>(src);
-    uint16_t* to = reinterpret_cast<uint16_t*>(dst);
-    if (cs == 1) {
-        const dim3 block = block_for((cols + 7) / 8);
-        const dim3 grid(unsigned(((cols + 7) / 8 + block.x - 1) / block.x),
-                        unsigned(std::min<int64_t>((rows + block.y - 1) / block.y, 16384)));
-        return launch(pack_rows_kernel, grid, block, 0, 1, s, "operand copy", from, rs, rows, cols, to, ld);
-    }
-    return launch(pack_kernel, dim3(unsigned((cols + 255) / 256), unsigned(std::min<int64_t>(rows, 16384))), dim3(256), 0,
-                  1, s, "operand copy", from, rs, cs, rows, cols, to, ld);
+    int64_t most = 0;
+    for (int i = 0; i < c.n; i++) most = std::max(most, c.job[i].rows * ((c.job[i].cols + 7) / 8));
+    const unsigned blocks = unsigned(std::min<int64_t>((most + 255) / 256, int64_t(P->num_sms) * 32));
+    return launch(copy_kernel, dim3(blocks, unsigned(c.n)), dim3(256), 0, 1, s, "operand copy", c);
 }
 
 }  // namespace proj
