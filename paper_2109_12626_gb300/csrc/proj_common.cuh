@@ -157,17 +157,22 @@ __device__ __forceinline__ void store4(char* p, int64_t i, int f32, int half, co
         *reinterpret_cast<uint2*>(p + 2 * i) = make_uint2(narrow2(v[0], v[1], half), narrow2(v[2], v[3], half));
 }
 
+// what else a result element needs
+__device__ __forceinline__ float other1(const Epilogue& e, int64_t m, int64_t n)
+{
+    return e.other ? load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half) : 0.0f;
+}
+
 // One result element from its sum (or pair of sums)
 template <bool PAIR, int FINISH, int ACT>
 __device__ __forceinline__ void put1(const Epilogue& e, char* out, int64_t out_rs, int64_t m, int64_t n, float z,
-                                     float u, float bias)
+                                     float u, float bias, float o)
 {
     z += bias;
     if (e.pre) {
         e.pre[m * e.pre_rs + n] = z;
         if (PAIR) e.pre[m * e.pre_rs + e.pre_up + n] = u;
     }
-    const float o = e.other ? load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half) : 0.0f;
     float v = 0.0f, w = 0.0f;
     finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
     store1(out, m * out_rs + n, v, e.out_f32, e.half);

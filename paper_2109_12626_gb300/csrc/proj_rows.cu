@@ -23,11 +23,18 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.segments = two_x ? 2 : 1;
     t.steps = int((p.K + kRowStep - 1) / kRowStep);
     t.width = pair ? 64 : kRowFeatures;
-    // Tiles of 64 rows where 128 would leave SMs without one: 128 rows of 4096 x
-    // 4096 12.5 against 14.9 us, 1024 rows of 1024 x 1024 8.3 against 9.4; with
-    // more tiles than SMs, 512 rows of 4096 x 4096, 25.3 against 21.1.
+    // Tiles of 64 rows where 128 would leave SMs without one, unless the sum is
+    // long and four CTAs a tile fill the SMs, when the fewer bytes of larger
+    // tiles count: 128 rows of 4096 x 4096
+    // 12.5 against 14.9 us, 1024 rows of 1024 x 1024 8.3 against 9.4; 128 rows of
+    // 8192 x 8192, 31.8 against 29.4.  With more tiles than SMs, 512 rows of 4096 x
+    // 4096, 25.3 against 21.1.
     const int64_t across = (p.N + t.width - 1) / t.width;
-    t.columns = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 || (p.M + 63) / 64 * across <= P->num_sms ? 64 : 128;
+    const int steps = t.steps * t.segments;
+    t.columns = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    if (t.columns == 128 && (p.M + 63) / 64 * across <= P->num_sms &&
+        (steps <= 64 || (p.M + 127) / 128 * across * 4 < P->num_sms))
+        t.columns = 64;
     t.x_bytes = (t.x_mn ? std::max(64, t.columns) : t.columns) * kRowStep * 2;
     t.M = p.M;
     t.N = p.N;
@@ -36,7 +43,6 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.err = P->err;
     const int64_t down = (p.M + t.columns - 1) / t.columns;
     const int64_t tiles = across * down;
-    const int steps = t.steps * t.segments;
     // As many CTAs of a cluster as fit beside each other, two an SM, while each
     // still has four stages to load: 4096 x 4096 weights for one row, 1, 2, 4
     // and 8 CTAs: 22.2, 14.3, 10.8 and 11.0 us; a pair of 8192 x 4096: 26.3,

@@ -206,6 +206,10 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
 #pragma unroll
                     for (int i = 0; i < 4; i++) u[b][i] = o[b][i] = 0.0f;
                     if (four && e.other) load4(e.other, (m0 + at) * e.other_rs + n, e.other_f32, e.half, o[b]);
+                    if (!four)
+#pragma unroll
+                        for (int i = 0; i < 4; i++)
+                            if (n + i < t.N) o[b][i] = other1(e, m0 + at, n + i);
                     join<SPLIT>(from, t.split, z[b]);
                     if (PAIR) join<SPLIT>(from + 64 * 4, t.split, u[b]);
                 }
@@ -218,7 +222,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                     else
                         for (int i = 0; i < 4; i++)
                             if (n + i < t.N)
-                                put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[b][i], u[b][i], bias[i]);
+                                put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[b][i], u[b][i], bias[i], o[b][i]);
                 }
             }
     }

@@ -200,10 +200,25 @@ struct Finisher {
         if (c0 + c >= cols) return;
         const int64_t n = n0 + c0 + c;
         const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
-#pragma unroll 4
-        for (int r = lane / kCols; r < rows; r += 32 / kCols)
+        constexpr int kStep = 32 / kCols, kAsk = 8;   // rows apart, rows asked for together
+        auto put = [&](int r, float o) {
             put1<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, stage[r * 32 + 4 * ((c >> 2) ^ (r & 7)) + (c & 3)],
-                                    PAIR ? stage[r * 32 + 4 * ((4 + (c >> 2)) ^ (r & 7)) + (c & 3)] : 0.0f, bias);
+                                    PAIR ? stage[r * 32 + 4 * ((4 + (c >> 2)) ^ (r & 7)) + (c & 3)] : 0.0f, bias, o);
+        };
+        if (!e.other) {
+#pragma unroll 4
+            for (int r = lane / kCols; r < rows; r += kStep) put(r, 0.0f);
+            return;
+        }
+        for (int r0 = lane / kCols; r0 < rows; r0 += kStep * kAsk) {
+            float o[kAsk];
+#pragma unroll
+            for (int b = 0; b < kAsk; b++)
+                o[b] = r0 + b * kStep < rows ? other1(e, m0 + r0 + b * kStep, n) : 0.0f;
+#pragma unroll
+            for (int b = 0; b < kAsk; b++)
+                if (r0 + b * kStep < rows) put(r0 + b * kStep, o[b]);
+        }
     }
 
     // `taken`: the barrier that tells the products' thread that this warp has

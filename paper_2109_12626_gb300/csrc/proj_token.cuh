@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(32 * kTokenWarps) token_kernel(const TokenArgs
     if (lane >= (PAIR ? 1 : 2) || n >= t.N) return;
     const Epilogue& e = t.e;
     const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
-    put1<PAIR, kValue, ACT>(e, e.out, e.out_rs, 0, n, PAIR || lane == 0 ? acc[0] : acc[1], acc[1], bias);
+    put1<PAIR, kValue, ACT>(e, e.out, e.out_rs, 0, n, PAIR || lane == 0 ? acc[0] : acc[1], acc[1], bias, other1(e, 0, n));
 }
 
 }  // namespace
