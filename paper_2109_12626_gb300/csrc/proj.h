@@ -69,7 +69,7 @@ struct Proj {
     char* packed[kPacked] = {};
     size_t packed_bytes[kPacked] = {};
     uint32_t* err = nullptr;       // device error word
-    bool tile_set[2][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
+    bool tile_set[2][2][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
 };
 
 // Tensor-core product of operands that TMA can load: one stride 1, the other

@@ -8,7 +8,9 @@
 // cluster, which each load their part through a ring of TMA stages (all of it
 // in flight at once where it fits), leave their partial tile in shared memory
 // and then add up the S partials of their share of the columns in the order
-// of the CTAs: one launch, no atomics, the same bits every time.
+// of the CTAs: one launch, no atomics, the same bits every time.  A long part is
+// summed in several runs, each in columns of tensor memory of its own, which
+// are then added up in float32: the tensor cores cut sums off (proj_tile.cuh).
 #pragma once
 
 #include "proj_common.cuh"
@@ -32,6 +34,7 @@ struct RowArgs {
     int columns;              // rows of x a tile: 16, 32, 64 or 128
     int x_bytes;              // bytes of x a stage
     int stages;
+    int runs, apart;          // accumulators, and columns of tensor memory between them
     int width;                // features a tile: 128, of a pair 64
     int vec;                  // results and what else is read allow 4 elements at a time
     int64_t M, N;             // rows of x, features
@@ -87,7 +90,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
         bar_init(ready, 1);
         bar_init_fence();
     }
-    if (warp == 2) tmem_alloc<1>(smem_addr(&tmem_at), max(32, t.columns));
+    if (warp == 2) tmem_alloc<1>(smem_addr(&tmem_at), t.runs * t.apart);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -137,16 +140,18 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
         const uint32_t desc = mma_desc(kRowFeatures, t.columns, t.e.half, t.w_mn, t.x_mn);
         const uint32_t w_lead = t.w_mn ? kWBytes / 2 : 0, x_lead = t.x_mn ? 64 * kRowStep * 2 : 0;
         const uint32_t w_step = t.w_mn ? 2048 : 32, x_step = t.x_mn ? 2048 : 32;
-        int stage = 0;
+        int stage = 0, run = -1, next = k_first;   // `next`: the step that begins another run
         uint32_t phase = 0;
         for (int k = k_first; k < k_last; k++) {
             if (!bar_wait(full + 8 * stage, phase, waits)) break;
             tc_fence_after();
+            const bool begins = k == next;
+            if (begins) next = k_first + (k_last - k_first) * (++run + 1) / t.runs;
             const uint32_t at = smem_addr(base) + stage * stage_bytes;
 #pragma unroll
             for (int j = 0; j < kRowStep / 16; j++)
-                mma_f16<1>(tmem, tile_desc(at + j * w_step, w_lead), tile_desc(at + kWBytes + j * x_step, x_lead), desc,
-                           k > k_first || j > 0);
+                mma_f16<1>(tmem + run * t.apart, tile_desc(at + j * w_step, w_lead),
+                           tile_desc(at + kWBytes + j * x_step, x_lead), desc, !begins || j > 0);
             mma_commit(empty + 8 * stage);
             if (++stage == t.stages) stage = 0, phase ^= 1;
         }
@@ -156,26 +161,31 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     // All products done (and with them every load): the stages' memory now
     // takes the partial tile, column by column.
     float* part = reinterpret_cast<float*>(base);
-    const bool some = k_last > k_first;
     bool ok = bar_wait(ready, 0, waits);
     tc_fence_after();
     ok = __syncthreads_and(ok && !stop);   // every role is done with the stages
     if (ok) {
         const int quarter = warp & 3;
         for (int c0 = (warp >> 2) * 32; c0 < cols; c0 += 64) {
-            float v[32];
+            float v[32], w[32];
             tmem_load32(v, tmem + c0 + (uint32_t(quarter) << 21));
             tmem_load_wait(v);
+            for (int r = 1; r < t.runs; r++) {
+                tmem_load32(w, tmem + r * t.apart + c0 + (uint32_t(quarter) << 21));
+                tmem_load_wait(w);
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] += w[i];
+            }
 #pragma unroll
             for (int i = 0; i < 32; i++)
-                if (c0 + i < cols) part[(c0 + i) * kRowFeatures + quarter * 32 + lane] = some ? v[i] : 0.0f;
+                if (c0 + i < cols) part[(c0 + i) * kRowFeatures + quarter * 32 + lane] = v[i];
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (t.split > 1) cluster_arrive();
-    if (warp == 2) tmem_free<1>(tmem, max(32, t.columns));
+    if (warp == 2) tmem_free<1>(tmem, t.runs * t.apart);
     if (t.split > 1) cluster_wait();
     if (ok) {
         // ------------------------------------------------ results

@@ -6,16 +6,18 @@
 namespace dpdr {
 namespace proj {
 
-TileKernel tile_kernel_single(int finish, int act)
+TileKernel tile_kernel_single(int finish, int act, int f32)
 {
     TileKernel k = nullptr;
-#define DPDR_CALL(A) k = finish == kSlope ? tile_kernel<false, kSlope, A> : tile_kernel<false, kValue, A>
+#define DPDR_CALL(A)                                                              \
+    k = f32 ? tile_kernel<false, kValue, A, true>                                 \
+            : finish == kSlope ? tile_kernel<false, kSlope, A, false> : tile_kernel<false, kValue, A, false>
     DPDR_FOR_ACT(act, DPDR_CALL)
 #undef DPDR_CALL
     return k;
 }
 
-TileKernel tile_kernel_pair(int finish, int act);   // proj_tile_pair.cu
+TileKernel tile_kernel_pair(int finish, int act, int f32);   // proj_tile_pair.cu
 
 int tile_launch(Proj* P, const Product& p, cudaStream_t s)
 {
@@ -51,10 +53,10 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
         if (!rc && two_b) rc = tensor_map(&t.b_half[1], p.b[1], p.N, p.K, p.e.half, 64, kStep);
     }
     if (rc) return rc;
-    const TileKernel kernel = p.kind == kPair ? tile_kernel_pair(p.e.finish, p.e.act)
-                                              : tile_kernel_single(p.e.finish, p.e.act);
+    const TileKernel kernel = p.kind == kPair ? tile_kernel_pair(p.e.finish, p.e.act, p.e.out_f32)
+                                              : tile_kernel_single(p.e.finish, p.e.act, p.e.out_f32);
     // a plan's activation is fixed, but its gradients' products have none
-    bool& set = P->tile_set[p.kind == kPair][p.e.finish][p.e.act != DPDR_ACT_NONE];
+    bool& set = P->tile_set[p.kind == kPair][p.e.finish][p.e.act != DPDR_ACT_NONE][p.e.out_f32];
     if (!set) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return cuda_fail_c(e, "projection tile kernel");

@@ -13,6 +13,12 @@
 // as the forward product, nothing transposed.  For the gated operator B is the
 // two weights' 128 rows of the same features, one weight a CTA: the pair g, u
 // of an output ends in columns n and n + 128 of one thread's row.
+//
+// The tensor cores add to a sum by cutting off, not by rounding: a sum of K
+// products comes out smaller by about 1e-9 K of its size (measured: 1.25e-6 at K
+// = 1024, 9.7e-6 at 8192).  No 16-bit result shows that.  For float32 results
+// (F32) a sum is taken in runs of at most 640 products, and the finishing warps add up
+// the runs in registers, rounded, while the next run's products are at work.
 #pragma once
 
 #include "proj_common.cuh"
@@ -28,10 +34,11 @@ constexpr int kStages = 6;
 constexpr int kStep = 64;                     // summed elements a stage
 constexpr int kHalf = 128 * kStep * 2;        // bytes of one operand of a stage and CTA
 constexpr int kStage = 2 * kHalf;
+constexpr int kRun = 10;                      // stages of a run, at most
 constexpr int kFinishers = 8;                 // warps
 constexpr int kStaging = kFinishers * 32 * 32 * 4;   // 32 x 32 floats each
 constexpr int kSmem = 1024 + kStages * kStage + kStaging;
-constexpr int kThreads = 128 + 32 * kFinishers;   // warps: load, product, tensor memory, -, finishing
+constexpr int kThreads = 64 + 32 * kFinishers;   // warps: load, product, finishing (200 registers a thread)
 
 struct TileArgs {
     CUtensorMap a[2], b[2], b_half[2];   // B's rows by 128 and by 64
@@ -84,7 +91,7 @@ __device__ __forceinline__ Item item_of(const TileArgs& t, int i)
 // needs (residual, dy) is asked into L2 while the item's products still run,
 // and into registers a round ahead: one row at a time, each a trip to memory,
 // took 45 us a tile.
-template <bool PAIR, int FINISH, int ACT>
+template <bool PAIR, int FINISH, int ACT, bool F32>
 struct Finisher {
     static constexpr int kCols = PAIR ? 16 : 32;     // result columns a round
     static constexpr int kPer = kCols / 4;           // threads a row
@@ -140,7 +147,7 @@ struct Finisher {
             const char* p = e.other + ((m0 + lane) * e.other_rs + n0) * size;
             for (int at = 128 * turn; at < cols * size; at += 256) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + at));
         }
-        if (fours(turn * kCols)) {
+        if (!F32 && fours(turn * kCols)) {
             const char* at = other_at(turn * kCols);
 #pragma unroll
             for (int b = 0; b < kSteps; b++) fetch(b, at);
@@ -148,7 +155,7 @@ struct Finisher {
     }
 
     // the round's results, four columns a thread and step
-    template <int HALF, int F32>
+    template <int HALF>
     __device__ __forceinline__ void by_four(int c0, char* out, int64_t out_rs)
     {
         const Epilogue& e = t.e;
@@ -192,6 +199,30 @@ struct Finisher {
         }
     }
 
+    // The same for float32 results, in as few registers as it can be: the other
+    // rounds' sums hold most of them.
+    __device__ __forceinline__ void by_four_f32(int c0, char* out, int64_t out_rs)
+    {
+        const Epilogue& e = t.e;
+        const int64_t n = n0 + c0 + 4 * q;
+        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, e.half, bias);
+#pragma unroll 2
+        for (int b = 0; b < kSteps; b++) {
+            const int r = row + b * kRows;
+            if (r >= rows) break;
+            float o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (e.other) load4(e.other, (m0 + r) * e.other_rs + n, 1, 0, o);
+            const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * (q ^ (r & 7)));
+            float z[4] = {z4.x, z4.y, z4.z, z4.w};
+            if (PAIR) {
+                const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * ((4 + q) ^ (r & 7)));
+                u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
+            }
+            put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o);
+        }
+    }
+
     // one element a thread and step, for results that do not lie on fours
     __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs)
     {
@@ -221,49 +252,73 @@ struct Finisher {
         }
     }
 
+    // a round's sums (two halves of its columns), to its results
+    __device__ __forceinline__ void put(const float (&v)[16], const float (&w)[16], int c0, int lane, char* out,
+                                        int64_t out_rs)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            *reinterpret_cast<float4*>(stage + lane * 32 + 4 * (i ^ (lane & 7))) =
+                make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            *reinterpret_cast<float4*>(stage + lane * 32 + 4 * ((4 + i) ^ (lane & 7))) =
+                make_float4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
+        __syncwarp();
+        if (!fours(c0)) by_one(c0, lane, out, out_rs);
+        else if (F32) by_four_f32(c0, out, out_rs);
+        else if (t.e.half) by_four<1>(c0, out, out_rs);
+        else by_four<0>(c0, out, out_rs);
+        __syncwarp();
+    }
+
     // `taken`: the barrier that tells the products' thread that this warp has
     // fetched its sums
+    __device__ __forceinline__ void fetched(int lane, uint32_t taken)
+    {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_at(taken);
+    }
+
     __device__ __forceinline__ void finish(uint32_t tmem, int sums, int lane, char* out, int64_t out_rs, uint32_t taken)
     {
-        const Epilogue& e = t.e;
         int c0 = turn * kCols;
-        if (c0 >= cols && lane == 0) bar_arrive_at(taken);
+        if (c0 >= cols) fetched(lane, taken);
         for (; c0 < cols; c0 += 2 * kCols) {
-            float v[32];
-            if (PAIR) {
-                tmem_load16(v, tmem + c0);
-                tmem_load16(v + 16, tmem + sums / 2 + c0);
-            } else {
-                tmem_load32(v, tmem + c0);
-            }
-            tmem_load_wait(v);
-            if (c0 + 2 * kCols >= cols) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive_at(taken);
-            }
+            float v[16], w[16];
+            tmem_load16(v, tmem + c0);
+            tmem_load16(w, tmem + c0 + (PAIR ? sums / 2 : 16));
+            tmem_load_wait(v, w);
+            if (c0 + 2 * kCols >= cols) fetched(lane, taken);
+            put(v, w, c0, lane, out, out_rs);
+        }
+    }
+
+    // F32: adds a run to this warp's sums so far, 16 columns each: half a round (of
+    // a pair, one weight's), whether the result has them or not
+    static __device__ __forceinline__ void add_run(float (&sum)[8][16], uint32_t tmem, int sums)
+    {
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                *reinterpret_cast<float4*>(stage + lane * 32 + 4 * (i ^ (lane & 7))) =
-                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            __syncwarp();
-            if (fours(c0)) {
-                if (e.out_f32) {
-                    if (e.half) by_four<1, 1>(c0, out, out_rs);
-                    else by_four<0, 1>(c0, out, out_rs);
-                } else {
-                    if (e.half) by_four<1, 0>(c0, out, out_rs);
-                    else by_four<0, 0>(c0, out, out_rs);
-                }
-            } else {
-                by_one(c0, lane, out, out_rs);
-            }
-            __syncwarp();
+        for (int r = 0; r < 8; r++) {
+            float v[16];
+            tmem_load16(v, tmem + (r >> 1) * 2 * kCols + (r & 1) * (PAIR ? sums / 2 : 16));
+            tmem_load_wait(v);
+#pragma unroll
+            for (int i = 0; i < 16; i++) sum[r][i] += v[i];
+        }
+    }
+
+    __device__ __forceinline__ void put_runs(const float (&sum)[8][16], int lane, char* out, int64_t out_rs)
+    {
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int c0 = turn * kCols + r * 2 * kCols;
+            if (c0 < cols) put(sum[2 * r], sum[2 * r + 1], c0, lane, out, out_rs);
         }
     }
 };
 
-template <bool PAIR, int FINISH, int ACT>
+template <bool PAIR, int FINISH, int ACT, bool F32>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t)
 {
     extern __shared__ char raw[];
@@ -290,13 +345,13 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         bar_init(last, 1);
         bar_init_fence();
     }
-    if (warp == 2) tmem_alloc<2>(smem_addr(&tmem_at), 512);
+    if (warp == 1) tmem_alloc<2>(smem_addr(&tmem_at), 512);
     tc_fence_before();
     __syncthreads();
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    const int steps = t.steps * t.segments;
+    const int steps = t.steps * t.segments, runs = F32 ? (steps + kRun - 1) / kRun : 1;
     wait_previous();
 
     if (warp == 0 && lane == 0) {
@@ -347,48 +402,67 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         bool ok = true;
         for (int i = first; i < t.items && ok; i += pairs) {
             const uint32_t desc = mma_desc(256, i < t.whole ? 256 : 128, t.e.half, t.a_mn, t.b_mn);
-            if (!(ok = bar_wait(taken + 8 * acc, acc_phase ^ 1, waits))) break;
-            tc_fence_after();
-            for (int k = 0; k < steps; k++) {
-                if (!(ok = bar_wait(full + 8 * stage, phase, waits))) break;
+            for (int run = 0, k = 0; run < runs && ok; run++) {
+                const int k_first = k, k_last = F32 ? steps * (run + 1) / runs : steps;
+                if (!(ok = bar_wait(taken + 8 * acc, acc_phase ^ 1, waits))) break;
                 tc_fence_after();
-                const uint32_t at = smem_addr(base) + stage * kStage;
+                for (; k < k_last; k++) {
+                    if (!(ok = bar_wait(full + 8 * stage, phase, waits))) break;
+                    tc_fence_after();
+                    const uint32_t at = smem_addr(base) + stage * kStage;
 #pragma unroll
-                for (int j = 0; j < kStep / 16; j++)
-                    mma_f16<2>(tmem + acc * 256, tile_desc(at + j * a_step, a_lead),
-                               tile_desc(at + kHalf + j * b_step, b_lead), desc, (k | j) != 0);
-                mma_commit_pair(empty + 8 * stage);
-                if (++stage == kStages) stage = 0, phase ^= 1;
+                    for (int j = 0; j < kStep / 16; j++)
+                        mma_f16<2>(tmem + acc * 256, tile_desc(at + j * a_step, a_lead),
+                                   tile_desc(at + kHalf + j * b_step, b_lead), desc, k > k_first || j > 0);
+                    mma_commit_pair(empty + 8 * stage);
+                    if (++stage == kStages) stage = 0, phase ^= 1;
+                }
+                if (!ok) break;
+                mma_commit_pair(ready + 8 * acc);
+                if (++acc == 2) acc = 0, acc_phase ^= 1;
             }
-            if (!ok) break;
-            mma_commit_pair(ready + 8 * acc);
-            if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
         if (!ok) {   // the products under way still read shared memory
             mma_commit_pair(last);
             bar_drain(last, 0);
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 2) {
         // ------------------------------------------------ results
-        const int mine = warp - 4, quarter = mine & 3;
-        Finisher<PAIR, FINISH, ACT> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane, mine >> 2);
+        const int mine = warp - 2, quarter = warp & 3;   // a warp reaches the 32 lanes of its number's quarter
+        Finisher<PAIR, FINISH, ACT, F32> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane, mine >> 2);
         int acc = 0;
         uint32_t acc_phase = 0;
         for (int i = first; i < t.items; i += pairs) {
             const Item it = item_of<PAIR>(t, i);
             f.start(int64_t(it.m) + int(rank) * 128 + quarter * 32, it.n, it.sums, lane);
-            if (!bar_wait(ready + 8 * acc, acc_phase, waits)) break;
-            tc_fence_after();
-            f.finish(tmem + acc * 256 + (uint32_t(quarter) << 21), it.sums, lane, it.twin ? t.e.out2 : t.e.out,
-                     it.twin ? t.e.out2_rs : t.e.out_rs, in_cta(taken + 8 * acc, 0));
-            if (++acc == 2) acc = 0, acc_phase ^= 1;
+            char* out = it.twin ? t.e.out2 : t.e.out;
+            const int64_t out_rs = it.twin ? t.e.out2_rs : t.e.out_rs;
+            const uint32_t lanes = tmem + (uint32_t(quarter) << 21);
+            if (F32) {
+                float sum[8][16] = {};
+                bool ok = true;
+                for (int run = 0; run < runs; run++) {
+                    if (!(ok = bar_wait(ready + 8 * acc, acc_phase, waits))) break;
+                    tc_fence_after();
+                    f.add_run(sum, lanes + acc * 256 + (mine >> 2) * f.kCols, it.sums);
+                    f.fetched(lane, in_cta(taken + 8 * acc, 0));
+                    if (++acc == 2) acc = 0, acc_phase ^= 1;
+                }
+                if (!ok) break;
+                f.put_runs(sum, lane, out, out_rs);
+            } else {
+                if (!bar_wait(ready + 8 * acc, acc_phase, waits)) break;
+                tc_fence_after();
+                f.finish(lanes + acc * 256, it.sums, lane, out, out_rs, in_cta(taken + 8 * acc, 0));
+                if (++acc == 2) acc = 0, acc_phase ^= 1;
+            }
         }
     }
     __syncwarp();
     __syncthreads();
     cluster_sync();
     tc_fence_after();
-    if (warp == 2) tmem_free<2>(tmem, 512);
+    if (warp == 1) tmem_free<2>(tmem, 512);
 }
 
 }  // namespace
