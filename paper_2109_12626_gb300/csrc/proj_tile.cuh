@@ -207,12 +207,10 @@ struct Finisher {
         const int64_t n = n0 + c0 + 4 * q;
         float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, e.half, bias);
-#pragma unroll 2
-        for (int b = 0; b < kSteps; b++) {
+        auto step = [&](int b, const float (&o)[4]) {
             const int r = row + b * kRows;
-            if (r >= rows) break;
-            float o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (e.other) load4(e.other, (m0 + r) * e.other_rs + n, 1, 0, o);
+            if (r >= rows) return;
+            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * (q ^ (r & 7)));
             float z[4] = {z4.x, z4.y, z4.z, z4.w};
             if (PAIR) {
@@ -220,6 +218,24 @@ struct Finisher {
                 u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
             }
             put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o);
+        };
+        if (PAIR || !e.other) {
+            const float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+            for (int b = 0; b < kSteps; b++) step(b, o);
+            return;
+        }
+        for (int b0 = 0; b0 < kSteps; b0 += 4) {
+            float o[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+                const int r = row + (b0 + b) * kRows;
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[b][i] = 0.0f;
+                if (r < rows) load4(e.other, (m0 + r) * e.other_rs + n, 1, 0, o[b]);
+            }
+#pragma unroll
+            for (int b = 0; b < 4; b++) step(b0 + b, o[b]);
         }
     }
 
