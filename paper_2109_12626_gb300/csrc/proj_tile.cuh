@@ -88,9 +88,10 @@ __device__ __forceinline__ Item item_of(const TileArgs& t, int i)
 // the rest.  The tensor memory hands each thread a row, the results want rows
 // across threads: the round goes through shared memory, 16-byte chunk q of row
 // r at q ^ (r & 7), so that neither way meets a bank twice.  What else a result
-// needs (residual, dy) is asked into L2 while the item's products still run,
-// and into registers a round ahead: one row at a time, each a trip to memory,
-// took 45 us a tile.
+// needs (residual, dy) is asked into L2 while the item's products still run, and
+// all of a round's together when the round comes: one row at a time, each a trip
+// to memory, took 45 us a tile; registers filled a round ahead, between a round's
+// stores, half as long again as this.
 template <bool PAIR, int FINISH, int ACT, bool F32>
 struct Finisher {
     static constexpr int kCols = PAIR ? 16 : 32;     // result columns a round
@@ -102,7 +103,6 @@ struct Finisher {
     float* stage;
     int q, row;              // this thread's columns (4 q) and first row of a round
     int turn;                // which of the two warps of these rows
-    uint4 other[kSteps];
     // of the item
     int64_t m0, n0;
     int rows, cols;
@@ -114,24 +114,6 @@ struct Finisher {
         row = PAIR ? ((lane >> 2) & 1) * 4 + (lane >> 3) : lane / kPer;
     }
 
-    // Asks for what else the four results of step b of a round need.  Where it
-    // lies: columns c0 on of this thread's first row.
-    __device__ __forceinline__ const char* other_at(int c0) const
-    {
-        const Epilogue& e = t.e;
-        return e.other + ((m0 + row) * e.other_rs + n0 + c0 + 4 * q) * (e.other_f32 ? 4 : 2);
-    }
-    __device__ __forceinline__ void fetch(int b, const char* at)
-    {
-        const Epilogue& e = t.e;
-        if (row + b * kRows >= rows) return;
-        if (e.other_f32) {
-            other[b] = *reinterpret_cast<const uint4*>(at + b * kRows * e.other_rs * 4);
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(at + b * kRows * e.other_rs * 2);
-            other[b].x = x.x, other[b].y = x.y;
-        }
-    }
     // whether a round of fours starts at c0
     __device__ __forceinline__ bool fours(int c0) const { return t.vec && c0 + kCols <= cols; }
 
@@ -146,11 +128,6 @@ struct Finisher {
         if (lane < rows) {   // a row a lane, every second line of it
             const char* p = e.other + ((m0 + lane) * e.other_rs + n0) * size;
             for (int at = 128 * turn; at < cols * size; at += 256) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + at));
-        }
-        if (!F32 && fours(turn * kCols)) {
-            const char* at = other_at(turn * kCols);
-#pragma unroll
-            for (int b = 0; b < kSteps; b++) fetch(b, at);
         }
     }
 
@@ -167,8 +144,22 @@ struct Finisher {
         char* p = out + (m * out_rs + n) * kSize;
         char* p2 = e.out2 + (m * e.out2_rs + n) * kSize;
         float* pre = e.pre + (m * e.pre_rs + n);
-        const bool more = e.other && fours(c0 + 2 * kCols);
-        const char* next = more ? other_at(c0 + 2 * kCols) : nullptr;
+        uint4 other[kSteps];
+        if (e.other) {
+            const int size = e.other_f32 ? 4 : 2;
+            const char* at = e.other + (m * e.other_rs + n) * size;
+            const int64_t apart = e.other_rs * kRows * size;
+#pragma unroll
+            for (int b = 0; b < kSteps; b++, at += apart)
+                if (row + b * kRows < rows) {
+                    if (e.other_f32) {
+                        other[b] = *reinterpret_cast<const uint4*>(at);
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2*>(at);
+                        other[b].x = x.x, other[b].y = x.y;
+                    }
+                }
+        }
         const int64_t down = out_rs * kRows * kSize, down2 = e.out2_rs * kRows * kSize, down_pre = e.pre_rs * kRows;
 #pragma unroll
         for (int b = 0; b < kSteps; b++) {
@@ -186,7 +177,6 @@ struct Finisher {
                     if (PAIR) *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[0], u[1], u[2], u[3]);
                 }
                 if (e.other) widen4(other[b], e.other_f32, HALF, o);
-                if (more) fetch(b, next);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     w[i] = 0.0f;
