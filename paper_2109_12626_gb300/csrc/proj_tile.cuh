@@ -123,7 +123,7 @@ struct Finisher {
         rows = int(max(int64_t(0), min(int64_t(32), t.M - m)));
         cols = int(min(int64_t(PAIR ? sums / 2 : sums), t.N - n));
         const Epilogue& e = t.e;
-        if (!e.other || !t.vec || cols <= 0) return;
+        if (!e.other || e.other_cs != 1 || cols <= 0) return;
         const int size = e.other_f32 ? 4 : 2;
         if (lane < rows) {   // a row a lane, every second line of it
             const char* p = e.other + ((m0 + lane) * e.other_rs + n0) * size;
@@ -229,32 +229,44 @@ struct Finisher {
         }
     }
 
-    // one element a thread and step, for results that do not lie on fours
+    // One element a thread and step, for results that do not lie on fours, eight
+    // steps' other values asked for together.
+    template <int HALF>
     __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs)
     {
         const Epilogue& e = t.e;
-        const int c = lane % kCols;
+        constexpr int kSize = F32 ? 4 : 2, kStep = 32 / kCols, kAsk = 8;   // kStep: rows a step
+        const int c = lane % kCols, first = lane / kCols;
         if (c0 + c >= cols) return;
-        const int64_t n = n0 + c0 + c;
-        const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, e.half) : 0.0f;
-        constexpr int kStep = 32 / kCols, kAsk = 8;   // rows apart, rows asked for together
-        auto put = [&](int r, float o) {
-            put1<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, stage[r * 32 + 4 * ((c >> 2) ^ (r & 7)) + (c & 3)],
-                                    PAIR ? stage[r * 32 + 4 * ((4 + (c >> 2)) ^ (r & 7)) + (c & 3)] : 0.0f, bias, o);
+        const int64_t n = n0 + c0 + c, m = m0 + first;
+        const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, HALF) : 0.0f;
+        char* at = out + (m * out_rs + n) * kSize;
+        const int64_t down = out_rs * kStep * kSize;
+        auto step = [&](int r, char* p, float o) {
+            const float z = stage[r * 32 + 4 * ((c >> 2) ^ (r & 7)) + (c & 3)] + bias;
+            const float u = PAIR ? stage[r * 32 + 4 * ((4 + (c >> 2)) ^ (r & 7)) + (c & 3)] : 0.0f;
+            if (e.pre) {
+                float* pre = e.pre + ((m0 + r) * e.pre_rs + n);
+                *pre = z;
+                if (PAIR) pre[e.pre_up] = u;
+            }
+            float v = 0.0f, w = 0.0f;
+            finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
+            store1(p, 0, v, F32, HALF);
+            if (PAIR && FINISH == kSlope) store1(e.out2, (m0 + r) * e.out2_rs + n, w, F32, HALF);
         };
         if (!e.other) {
 #pragma unroll 4
-            for (int r = lane / kCols; r < rows; r += kStep) put(r, 0.0f);
+            for (int r = first; r < rows; r += kStep, at += down) step(r, at, 0.0f);
             return;
         }
-        for (int r0 = lane / kCols; r0 < rows; r0 += kStep * kAsk) {
+        for (int r0 = first; r0 < rows; r0 += kStep * kAsk, at += kAsk * down) {
             float o[kAsk];
 #pragma unroll
-            for (int b = 0; b < kAsk; b++)
-                o[b] = r0 + b * kStep < rows ? other1(e, m0 + r0 + b * kStep, n) : 0.0f;
+            for (int b = 0; b < kAsk; b++) o[b] = r0 + b * kStep < rows ? other1(e, m0 + r0 + b * kStep, n) : 0.0f;
 #pragma unroll
             for (int b = 0; b < kAsk; b++)
-                if (r0 + b * kStep < rows) put(r0 + b * kStep, o[b]);
+                if (r0 + b * kStep < rows) step(r0 + b * kStep, at + b * down, o[b]);
         }
     }
 
@@ -270,10 +282,16 @@ struct Finisher {
                 make_float4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         }
         __syncwarp();
-        if (!fours(c0)) by_one(c0, lane, out, out_rs);
-        else if (F32) by_four_f32(c0, out, out_rs);
-        else if (t.e.half) by_four<1>(c0, out, out_rs);
-        else by_four<0>(c0, out, out_rs);
+        if (!fours(c0)) {
+            if (t.e.half) by_one<1>(c0, lane, out, out_rs);
+            else by_one<0>(c0, lane, out, out_rs);
+        } else if (F32) {
+            by_four_f32(c0, out, out_rs);
+        } else if (t.e.half) {
+            by_four<1>(c0, out, out_rs);
+        } else {
+            by_four<0>(c0, out, out_rs);
+        }
         __syncwarp();
     }
 
