@@ -68,7 +68,7 @@ struct Proj {
     // copies of operands that the tensor cores' loads cannot take as they lie
     char* packed[kPacked] = {};
     size_t packed_bytes[kPacked] = {};
-    uint32_t* err = nullptr;       // device error word
+    uint32_t* err = nullptr;       // error word, in host memory that kernels write to
     bool tile_set[2][2][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
 };
 

@@ -110,7 +110,8 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Wa
         }
     }
     *w.stop = 1u;
-    atomicExch(w.err, 1u);
+    *reinterpret_cast<volatile uint32_t*>(w.err) = 1u;
+    __threadfence_system();
     return false;
 }
 

@@ -229,13 +229,13 @@ struct Finisher {
         }
     }
 
-    // One element a thread and step, for results that do not lie on fours, eight
-    // steps' other values asked for together.
+    // One element a thread and step, for results that do not lie on fours, eight (of a
+    // pair 16) steps' other values asked for together.
     template <int HALF>
     __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs)
     {
         const Epilogue& e = t.e;
-        constexpr int kSize = F32 ? 4 : 2, kStep = 32 / kCols, kAsk = 8;   // kStep: rows a step
+        constexpr int kSize = F32 ? 4 : 2, kStep = 32 / kCols, kAsk = PAIR ? 16 : 8;   // kStep: rows a step
         const int c = lane % kCols, first = lane / kCols;
         if (c0 + c >= cols) return;
         const int64_t n = n0 + c0 + c, m = m0 + first;

@@ -520,3 +520,31 @@ def test_refusals():
     for a in ((-1, 4, 4), (4, 0, 4), (4, 4, 0), (1 << 31, 4, 4)):
         with pytest.raises(dpdr.DpdrError):
             dpdr.Gated(*a)
+
+
+# ----------------------------------------------------------- in use together
+
+@pytest.mark.parametrize("ranks,rows,model,hidden", [(4, 200, 264, 544), (1, 1, 64, 128), (7, 33, 136, 700), (2, 600, 512, 2048)])
+def test_feed_forward_split_over_ranks(ranks, rows, model, hidden):
+    """The example: Gated, Linear with float32 partials, and the all-reduce,
+    forward and backward, against the whole block in 64 bits.  Roundings to
+    bfloat16 on the way of a result, 2^-9 of the norm each: h for y and
+    dw_down; dy or dh and then dg and du for the others (2, 3 and the
+    gradient of the activation from a float32 projection)."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import tensor_parallel_ffn as ffn
+    block = ffn.SplitFeedForward(ranks, rows, model, hidden)
+    g = gen(29, ranks)
+    x = U.matrix(g, rows, model, "bfloat16")
+    dy = U.matrix(g, rows, model, "float32")
+    ys = block.forward(x)
+    dxs = block.backward(x, dy)
+    block.sync()
+    for copies in (ys, dxs):   # every rank holds the same bits
+        assert all(torch.equal(copies[0], c) for c in copies)
+    errors = ffn.worst(block, x, dy)
+    for name, steps in (("y", 1), ("dw_down", 2), ("dx", 3), ("dw_gate", 3), ("dw_up", 3)):
+        assert errors[name] <= steps * 2.0 ** -8, (name, errors)
+    block.close()
