@@ -9,7 +9,7 @@ namespace proj {
 
 RowKernel row_kernel_single(int finish, int act, int split)
 {
-    return finish == kSlope ? row_kernel_of<false, kSlope>(act, split) : row_kernel_of<false, kValue>(act, split);
+    return row_kernel_of<false>(finish, act, split);
 }
 
 RowKernel row_kernel_pair(int finish, int act, int split);   // proj_rows_pair.cu
@@ -35,13 +35,15 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     if (t.columns == 128 && (p.M + 63) / 64 * across <= P->num_sms &&
         (steps <= 64 || (p.M + 127) / 128 * across * 4 < P->num_sms))
         t.columns = 64;
-    t.x_bytes = (t.x_mn ? std::max(64, t.columns) : t.columns) * kRowStep * 2;
+    // as many tiles, but of equal height: 130 rows as three of 48
+    const int64_t down = (p.M + t.columns - 1) / t.columns;
+    if (down > 1) t.columns = int((p.M + down - 1) / down + 15) / 16 * 16;
+    t.x_bytes = (t.x_mn ? (t.columns + 63) / 64 * 64 : t.columns) * kRowStep * 2;
     t.M = p.M;
     t.N = p.N;
     t.e = p.e;
     t.vec = by_fours(p.e);
     t.err = P->err;
-    const int64_t down = (p.M + t.columns - 1) / t.columns;
     const int64_t tiles = across * down;
     // As many CTAs of a cluster as fit beside each other, two an SM, while each
     // still has four stages to load: 4096 x 4096 weights for one row, 1, 2, 4
@@ -51,7 +53,7 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     // From 64 columns on at most four: the partials that the SMs send each
     // other grow with both (333 rows, 2500 to 1000: 9.8 against 12.4 with eight).
     constexpr int kRoom = 110 * 1024;
-    const int most = t.columns >= 64 ? 4 : kRowSplits;
+    const int most = t.columns > 32 ? 4 : kRowSplits;
     int split = 1;
     while (split < most && tiles * (split + 1) <= 2 * P->num_sms && steps >= 4 * (split + 1)) split++;
     t.split = split;
@@ -60,7 +62,8 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     // tensor memory for (256 columns each), a power of two and no more than the
     // shortest part's steps.  16-bit results do without: 64 rows of 4096 x 4096 in
     // 9.8 against 12.0 us.
-    t.apart = std::max(32, t.columns);
+    t.apart = 32;
+    while (t.apart < t.columns) t.apart *= 2;
     t.runs = 1;
     while (p.e.out_f32 && 2 * t.runs * t.apart <= 256 && t.runs * 8 < mine && 2 * t.runs <= steps / split) t.runs *= 2;
     t.stages = std::max(2, std::min({mine, kRoom / stage, kRowMaxStages}));

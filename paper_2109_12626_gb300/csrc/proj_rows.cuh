@@ -11,6 +11,14 @@
 // of the CTAs: one launch, no atomics, the same bits every time.  A long part is
 // summed in several runs, each in columns of tensor memory of its own, which
 // are then added up in float32: the tensor cores cut sums off (proj_tile.cuh).
+//
+// Bound by the weights' bytes while there are some megabytes an SM, else by the
+// chain of setting up, one trip to memory, the cluster's barriers and partials
+// (4.4 us at 1024 x 1024): two rows of 8192 x 8192 in 24.8 us (5.4 TB/s, 0.81 of
+// the measured copy), 48 rows of a pair of 2048 x 5120 in 12.9 (3.3 TB/s), 128
+// rows of a pair of 8192 x 4096 in 30.4 (4.4 TB/s).  Loads asked into L2 before
+// the kernel before has ended, or a smaller ring for more CTAs an SM, gained
+// nothing.
 #pragma once
 
 #include "proj_common.cuh"
@@ -31,7 +39,7 @@ struct RowArgs {
     int w_mn, x_mn;
     int steps, segments;      // stages a segment, of all CTAs of a cluster
     int split;                // CTAs of a cluster
-    int columns;              // rows of x a tile: 16, 32, 64 or 128
+    int columns;              // rows of x a tile: a multiple of 16 up to 128
     int x_bytes;              // bytes of x a stage
     int stages;
     int runs, apart;          // accumulators, and columns of tensor memory between them
@@ -248,14 +256,22 @@ using RowKernel = void (*)(RowArgs);
 // asked for at a time
 inline int row_split_class(int split) { return split <= 2 ? 0 : split <= 4 ? 1 : 2; }
 
-template <bool PAIR, int FINISH>
-RowKernel row_kernel_of(int act, int split)
+template <bool PAIR>
+RowKernel row_kernel_of(int finish, int act, int split)
 {
     const int c = row_split_class(split);
     RowKernel k = nullptr;
-#define DPDR_CALL(A) k = c == 0 ? row_kernel<PAIR, FINISH, A, 2> : c == 1 ? row_kernel<PAIR, FINISH, A, 4> : row_kernel<PAIR, FINISH, A, 8>
+    // without an activation a single dz is dy, and no product is finished as one
+#define DPDR_KERNELS(F, A) c == 0 ? row_kernel<PAIR, F, A, 2> : c == 1 ? row_kernel<PAIR, F, A, 4> : row_kernel<PAIR, F, A, 8>
+#define DPDR_CALL(A)                                                                       \
+    if ((PAIR || A != DPDR_ACT_NONE) && finish == kSlope) {                                 \
+        k = DPDR_KERNELS((PAIR || A != DPDR_ACT_NONE ? kSlope : kValue), A);                \
+    } else {                                                                               \
+        k = DPDR_KERNELS(kValue, A);                                                       \
+    }
     DPDR_FOR_ACT(act, DPDR_CALL)
 #undef DPDR_CALL
+#undef DPDR_KERNELS
     return k;
 }
 

@@ -6,7 +6,7 @@ namespace proj {
 
 RowKernel row_kernel_pair(int finish, int act, int split)
 {
-    return finish == kSlope ? row_kernel_of<true, kSlope>(act, split) : row_kernel_of<true, kValue>(act, split);
+    return row_kernel_of<true>(finish, act, split);
 }
 
 }  // namespace proj

@@ -9,9 +9,11 @@ namespace proj {
 TileKernel tile_kernel_single(int finish, int act, int f32)
 {
     TileKernel k = nullptr;
-#define DPDR_CALL(A)                                                              \
-    k = f32 ? tile_kernel<false, kValue, A, true>                                 \
-            : finish == kSlope ? tile_kernel<false, kSlope, A, false> : tile_kernel<false, kValue, A, false>
+    // without an activation dz is dy, and no product is finished as one
+#define DPDR_CALL(A)                                                                                  \
+    k = f32 ? tile_kernel<false, kValue, A, true>                                                     \
+        : A != DPDR_ACT_NONE && finish == kSlope ? tile_kernel<false, A ? kSlope : kValue, A, false>   \
+                                                 : tile_kernel<false, kValue, A, false>
     DPDR_FOR_ACT(act, DPDR_CALL)
 #undef DPDR_CALL
     return k;
@@ -24,7 +26,6 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     TileArgs t;
     t.a_mn = p.a[0].ks != 1;
     t.b_mn = p.b[0].ks != 1;
-    t.kind = p.kind;
     t.segments = p.kind == kChain ? 2 : 1;
     t.steps = int((p.K + kStep - 1) / kStep);
     const int width = p.kind == kPair ? 128 : 256;
@@ -34,7 +35,8 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     if (tiles > (int64_t(1) << 30)) return fail_c(DPDR_ERR_INVALID, "projection: more than 2^30 tiles");
     t.tiles = int(tiles);
     // A last round of tiles that fills at most half of the pairs is taken in
-    // halves, which keeps all of them at work for about half as long.
+    // halves: 4096 x 4096 x 4096 (256 tiles on 76 pairs) with bias and residual 91
+    // against 103 us, 4096 x 1000 x 4096 33.5 against 36.6.
     const int pairs_all = P->num_sms / 2, left = t.tiles % pairs_all;
     t.whole = 2 * left <= pairs_all ? t.tiles - left : t.tiles;
     t.items = t.whole + 2 * (t.tiles - t.whole);

@@ -6,19 +6,31 @@
 // B's 256 (64 summed elements at a time, by TMA, into a ring of stages), one
 // thread of CTA 0 issues the pair's products (256 x 256 x 16 each, cta_group::2),
 // and CTA r holds the sums of its 128 rows in half of its tensor memory, so
-// that the other half takes the next tile's sums while four warps finish this
-// one's.  Each operand may have the summed index contiguous or the other one;
+// that the other half takes the next tile's sums while eight warps finish this
+// one's.  A pair reads 512 rows of operands for 256 x 256 results, half of what
+// two CTAs of 128 x 256 would.  Each operand may have the summed index contiguous or the other one;
 // the tile in shared memory is then laid out the other way and the
 // instruction told so, so that the gradients' products read the same arrays
 // as the forward product, nothing transposed.  For the gated operator B is the
 // two weights' 128 rows of the same features, one weight a CTA: the pair g, u
 // of an output ends in columns n and n + 128 of one thread's row.
 //
+// Bound by the tensor cores: 8192 x 8192 x 4096 in 297 us (1.85 PFLOP/s, 0.97 of
+// the measured burst; with bias and residual, over inputs that do not stay in
+// L2, 332 us, 0.97 of the rate that a long loop sustains), the gated operator
+// 8192 x 4096 x 8192 in 570 us (1.93 PFLOP/s).  With fewer than some ten rounds
+// of tiles the last one's idle pairs show: 4096 x 4096 x 4096, 3.4 rounds, in 84
+// us (1.63 PFLOP/s); short sums are bound by finishing: 4096 x 1000 x 4096 in 33.
+// Tried and not kept: asking a ring's length ahead into L2 (411 against 299 us),
+// the last round's tiles summed by several pairs that join their sums (no
+// faster, and 43 against 33 us for the short sums).
+//
 // The tensor cores add to a sum by cutting off, not by rounding: a sum of K
 // products comes out smaller by about 1e-9 K of its size (measured: 1.25e-6 at K
 // = 1024, 9.7e-6 at 8192).  No 16-bit result shows that.  For float32 results
-// (F32) a sum is taken in runs of at most 640 products, and the finishing warps add up
-// the runs in registers, rounded, while the next run's products are at work.
+// (F32) a sum is taken in runs of at most 640 products, and the finishing warps
+// add up the runs in registers, rounded, while the next run's products are at
+// work: 7.9e-7 at K = 8192, 4096 x 4096 x 4096 in 95 us instead of 84.
 #pragma once
 
 #include "proj_common.cuh"
@@ -43,7 +55,7 @@ constexpr int kThreads = 64 + 32 * kFinishers;   // warps: load, product, finish
 struct TileArgs {
     CUtensorMap a[2], b[2], b_half[2];   // B's rows by 128 and by 64
     int a_mn, b_mn;                // the other index is the contiguous one
-    int kind, steps, segments;     // stages a segment
+    int steps, segments;           // stages a segment
     int tiles_m, tiles_n, tiles;   // tiles_m of one of kTwin's products
     // the first `whole` tiles are taken as they are, the rest in two halves of
     // their columns: `items` in all
@@ -131,18 +143,17 @@ struct Finisher {
         }
     }
 
-    // the round's results, four columns a thread and step
+    // the round's results in 16 bits, four columns a thread and step
     template <int HALF>
     __device__ __forceinline__ void by_four(int c0, char* out, int64_t out_rs)
     {
         const Epilogue& e = t.e;
         const int64_t n = n0 + c0 + 4 * q;
-        constexpr int kSize = F32 ? 4 : 2;
         float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, HALF, bias);
         const int64_t m = m0 + row;
-        char* p = out + (m * out_rs + n) * kSize;
-        char* p2 = e.out2 + (m * e.out2_rs + n) * kSize;
+        char* p = out + (m * out_rs + n) * 2;
+        char* p2 = e.out2 + (m * e.out2_rs + n) * 2;
         float* pre = e.pre + (m * e.pre_rs + n);
         uint4 other[kSteps];
         if (e.other) {
@@ -160,7 +171,7 @@ struct Finisher {
                     }
                 }
         }
-        const int64_t down = out_rs * kRows * kSize, down2 = e.out2_rs * kRows * kSize, down_pre = e.pre_rs * kRows;
+        const int64_t down = out_rs * kRows * 2, down2 = e.out2_rs * kRows * 2, down_pre = e.pre_rs * kRows;
 #pragma unroll
         for (int b = 0; b < kSteps; b++) {
             const int r = row + b * kRows;
@@ -182,8 +193,8 @@ struct Finisher {
                     w[i] = 0.0f;
                     finish1<PAIR, FINISH, ACT>(z[i], u[i], o[i], v[i], w[i]);
                 }
-                store4(p, 0, F32, HALF, v);
-                if (PAIR && FINISH == kSlope) store4(p2, 0, F32, HALF, w);
+                store4(p, 0, 0, HALF, v);
+                if (PAIR && FINISH == kSlope) store4(p2, 0, 0, HALF, w);
             }
             p += down, p2 += down2, pre += down_pre;
         }
