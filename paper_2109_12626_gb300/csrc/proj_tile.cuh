@@ -50,7 +50,7 @@ constexpr int kRun = 10;                      // stages of a run, at most
 constexpr int kFinishers = 8;                 // warps
 constexpr int kStaging = kFinishers * 32 * 32 * 4;   // 32 x 32 floats each
 constexpr int kSmem = 1024 + kStages * kStage + kStaging;
-constexpr int kThreads = 64 + 32 * kFinishers;   // warps: load, product, finishing (200 registers a thread)
+constexpr int kThreads = 96 + 32 * kFinishers;   // warps: load A, load B, product, finishing
 
 struct TileArgs {
     CUtensorMap a[2], b[2], b_half[2];   // B's rows by 128 and by 64
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         bar_init(last, 1);
         bar_init_fence();
     }
-    if (warp == 1) tmem_alloc<2>(smem_addr(&tmem_at), 512);
+    if (warp == 2) tmem_alloc<2>(smem_addr(&tmem_at), 512);
     tc_fence_before();
     __syncthreads();
     cluster_sync();
@@ -389,66 +389,66 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     const int steps = t.steps * t.segments, runs = F32 ? (steps + kRun - 1) / kRun : 1;
     wait_previous();
 
-    if (warp == 0 && lane == 0) {
+    if (warp < 2 && lane == 0) {
         // ------------------------------------------------ loads
+        // A thread for each operand: what one thread spent on a stage's waits and
+        // loads of both was longer than its products.
+        const bool b = warp == 1, mn = b ? t.b_mn : t.a_mn;
+        const uint32_t to = smem_addr(base) + (b ? kHalf : 0), there = in_cta(full, 0);
         int stage = 0, used = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int i = first; i < t.items && ok; i += pairs) {
             const Item it = item_of<PAIR>(t, i);
-            const int m0 = it.m + int(rank) * 128, n0 = it.n + (PAIR ? 0 : int(rank) * (it.sums / 2));
-            const CUtensorMap* b_maps = it.sums == 256 ? t.b : t.b_half;
-            for (int k = 0; k < steps; k++) {
-                if (!(ok = bar_wait(empty + 8 * stage, phase ^ 1, waits))) break;
-                const int seg = k >= t.steps, k0 = (seg ? k - t.steps : k) * kStep;
-                const CUtensorMap* ma = &t.a[it.twin | seg];
-                const CUtensorMap* mb = &b_maps[PAIR ? int(rank) : seg];
-                const uint32_t dst = smem_addr(base) + stage * kStage, bar = in_cta(full + 8 * stage, 0);
-                if (rank == 0) bar_expect(full + 8 * stage, 2 * kHalf + it.sums * kStep * 2);
-                if (t.a_mn) {
-                    tma_load_pair(dst, ma, m0, k0, bar);
-                    tma_load_pair(dst + kHalf / 2, ma, m0 + 64, k0, bar);
-                } else {
-                    tma_load_pair(dst, ma, k0, m0, bar);
+            const bool two = mn && (!b || it.sums == 256);   // boxes of 64
+            const int row = b ? it.n + (PAIR ? 0 : int(rank) * (it.sums / 2)) : it.m + int(rank) * 128;
+            const int bytes = 2 * kHalf + it.sums * kStep * 2;
+            for (int seg = 0, k = 0; seg < t.segments && ok; seg++) {
+                const CUtensorMap* map = !b ? &t.a[it.twin | seg] : &(it.sums == 256 ? t.b : t.b_half)[PAIR ? int(rank) : seg];
+                const int k_last = (seg + 1) * t.steps;
+                for (int at = 0; k < k_last; k++, at += kStep) {
+                    if (!(ok = bar_wait(empty + 8 * stage, phase ^ 1, waits))) break;
+                    if (!b && rank == 0) bar_expect(full + 8 * stage, bytes);
+                    const uint32_t dst = to + stage * kStage, bar = there + 8 * stage;
+                    tma_load_pair(dst, map, mn ? row : at, mn ? at : row, bar);
+                    if (two) tma_load_pair(dst + kHalf / 2, map, row + 64, at, bar);
+                    used++;
+                    if (++stage == kStages) stage = 0, phase ^= 1;
                 }
-                if (t.b_mn) {
-                    tma_load_pair(dst + kHalf, mb, n0, k0, bar);
-                    if (it.sums == 256) tma_load_pair(dst + kHalf + kHalf / 2, mb, n0 + 64, k0, bar);
-                } else {
-                    tma_load_pair(dst + kHalf, mb, k0, n0, bar);
-                }
-                used++;
-                if (++stage == kStages) stage = 0, phase ^= 1;
             }
         }
         // Both CTAs' loads have landed once the products that take them are
         // issued; after a failed wait they are waited for here.
-        if (!ok && rank == 0)
+        if (!ok && !b && rank == 0)
             for (int n = min(used, kStages); n > 0; n--) {
                 if (--stage < 0) stage = kStages - 1, phase ^= 1;
                 bar_drain(full + 8 * stage, phase);
             }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 2 && lane == 0 && rank == 0) {
         // ------------------------------------------------ products
-        const uint32_t a_lead = t.a_mn ? kHalf / 2 : 0, b_lead = t.b_mn ? kHalf / 2 : 0;
-        const uint32_t a_step = t.a_mn ? 2048 : 32, b_step = t.b_mn ? 2048 : 32;   // bytes for 16 summed elements
+        const uint64_t a_desc = tile_desc(smem_addr(base), t.a_mn ? kHalf / 2 : 0),
+                       b_desc = tile_desc(smem_addr(base) + kHalf, t.b_mn ? kHalf / 2 : 0);
+        const uint32_t a_step = (t.a_mn ? 2048 : 32) >> 4, b_step = (t.b_mn ? 2048 : 32) >> 4;   // 16 summed elements
         int stage = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
         bool ok = true;
         for (int i = first; i < t.items && ok; i += pairs) {
             const uint32_t desc = mma_desc(256, i < t.whole ? 256 : 128, t.e.half, t.a_mn, t.b_mn);
             for (int run = 0, k = 0; run < runs && ok; run++) {
-                const int k_first = k, k_last = F32 ? steps * (run + 1) / runs : steps;
+                const int k_last = F32 ? steps * (run + 1) / runs : steps;
+                bool add = false;
                 if (!(ok = bar_wait(taken + 8 * acc, acc_phase ^ 1, waits))) break;
                 tc_fence_after();
                 for (; k < k_last; k++) {
                     if (!(ok = bar_wait(full + 8 * stage, phase, waits))) break;
                     tc_fence_after();
-                    const uint32_t at = smem_addr(base) + stage * kStage;
+                    // addresses stay below 2^18, so the descriptors' fields do not run over
+                    const uint64_t a = a_desc + uint32_t(stage * (kStage >> 4)), b = b_desc + uint32_t(stage * (kStage >> 4));
 #pragma unroll
-                    for (int j = 0; j < kStep / 16; j++)
-                        mma_f16<2>(tmem + acc * 256, tile_desc(at + j * a_step, a_lead),
-                                   tile_desc(at + kHalf + j * b_step, b_lead), desc, k > k_first || j > 0);
+                    for (int j = 0; j < kStep / 16; j++) {
+                        mma_f16<2>(tmem + acc * 256, a + j * a_step, b + j * b_step, desc, add);
+                        add = true;
+                    }
                     mma_commit_pair(empty + 8 * stage);
                     if (++stage == kStages) stage = 0, phase ^= 1;
                 }
@@ -461,9 +461,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             mma_commit_pair(last);
             bar_drain(last, 0);
         }
-    } else if (warp >= 2) {
+    } else if (warp >= 3) {
         // ------------------------------------------------ results
-        const int mine = warp - 2, quarter = warp & 3;   // a warp reaches the 32 lanes of its number's quarter
+        const int mine = warp - 3, quarter = warp & 3;   // a warp reaches the 32 lanes of its number's quarter
         Finisher<PAIR, FINISH, ACT, F32> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane, mine >> 2);
         int acc = 0;
         uint32_t acc_phase = 0;
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     __syncthreads();
     cluster_sync();
     tc_fence_after();
-    if (warp == 1) tmem_free<2>(tmem, 512);
+    if (warp == 2) tmem_free<2>(tmem, 512);
 }
 
 }  // namespace
