@@ -73,7 +73,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
     uint32_t ok;
     asm volatile(
         "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
@@ -114,6 +114,30 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Wa
     __threadfence_system();
     return false;
 }
+
+// The same for a whole warp, with one answer for it.  The warps that issue loads
+// and products stay together, and one lane of them issues: what those
+// instructions take then stays in the registers that a warp shares.  A lone
+// thread moved each operand there anew, which took 126 cycles a product.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, const Waits& w)
+{
+    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, w));
+}
+
+// true in one lane of a warp that is together
+__device__ __forceinline__ bool elected()
+{
+    uint32_t is;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "elect.sync _|p, 0xFFFFFFFF;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(is));
+    return is != 0;
+}
+
+// this thread's warp, as a value that the whole warp shares
+__device__ __forceinline__ int warp_number() { return __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0); }
 
 // for leaving after a failed wait: one more bounded wait, whatever `stop` says
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)

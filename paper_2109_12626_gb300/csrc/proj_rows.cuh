@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     __shared__ __align__(8) uint64_t bars[2 * kRowMaxStages + 1];
     __shared__ uint32_t tmem_at, stop;
     char* base = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_number(), lane = threadIdx.x & 31;
     const int rank = t.split > 1 ? int(cluster_rank()) : 0;
     const uint32_t full = smem_addr(bars), empty = full + 8 * kRowMaxStages, ready = empty + 8 * kRowMaxStages;
     const Waits waits{&stop, t.err};
@@ -106,35 +106,37 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     wait_previous();
     allow_next();
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         int stage = 0, used = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int k = k_first; k < k_last; k++) {
-            if (!(ok = bar_wait(empty + 8 * stage, phase ^ 1, waits))) break;
+            if (!(ok = bar_wait_warp(empty + 8 * stage, phase ^ 1, waits))) break;
             const int seg = k >= t.steps, k0 = (seg ? k - t.steps : k) * kRowStep;
             const uint32_t dst = smem_addr(base) + stage * stage_bytes, bar = full + 8 * stage;
-            bar_expect(bar, stage_bytes);
-            if (PAIR) {   // 64 features of either weight
-                const int a = int(n0);
-                if (t.w_mn) {
-                    tma_load(dst, &t.w[0], a, k0, bar);
-                    tma_load(dst + kWBytes / 2, &t.w[1], a, k0, bar);
+            if (elected()) {
+                bar_expect(bar, stage_bytes);
+                if (PAIR) {   // 64 features of either weight
+                    const int a = int(n0);
+                    if (t.w_mn) {
+                        tma_load(dst, &t.w[0], a, k0, bar);
+                        tma_load(dst + kWBytes / 2, &t.w[1], a, k0, bar);
+                    } else {
+                        tma_load(dst, &t.w[0], k0, a, bar);
+                        tma_load(dst + kWBytes / 2, &t.w[1], k0, a, bar);
+                    }
+                } else if (t.w_mn) {
+                    tma_load(dst, &t.w[seg], int(n0), k0, bar);
+                    tma_load(dst + kWBytes / 2, &t.w[seg], int(n0) + 64, k0, bar);
                 } else {
-                    tma_load(dst, &t.w[0], k0, a, bar);
-                    tma_load(dst + kWBytes / 2, &t.w[1], k0, a, bar);
+                    tma_load(dst, &t.w[seg], k0, int(n0), bar);
                 }
-            } else if (t.w_mn) {
-                tma_load(dst, &t.w[seg], int(n0), k0, bar);
-                tma_load(dst + kWBytes / 2, &t.w[seg], int(n0) + 64, k0, bar);
-            } else {
-                tma_load(dst, &t.w[seg], k0, int(n0), bar);
-            }
-            if (t.x_mn) {
-                for (int c = 0; c < t.columns; c += 64)
-                    tma_load(dst + kWBytes + c * kRowStep * 2, &t.x[seg], int(m0) + c, k0, bar);
-            } else {
-                tma_load(dst + kWBytes, &t.x[seg], k0, int(m0), bar);
+                if (t.x_mn) {
+                    for (int c = 0; c < t.columns; c += 64)
+                        tma_load(dst + kWBytes + c * kRowStep * 2, &t.x[seg], int(m0) + c, k0, bar);
+                } else {
+                    tma_load(dst + kWBytes, &t.x[seg], k0, int(m0), bar);
+                }
             }
             used++;
             if (++stage == t.stages) stage = 0, phase ^= 1;
@@ -144,26 +146,28 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                 if (--stage < 0) stage = t.stages - 1, phase ^= 1;
                 bar_drain(full + 8 * stage, phase);
             }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         const uint32_t desc = mma_desc(kRowFeatures, t.columns, t.e.half, t.w_mn, t.x_mn);
-        const uint32_t w_lead = t.w_mn ? kWBytes / 2 : 0, x_lead = t.x_mn ? 64 * kRowStep * 2 : 0;
-        const uint32_t w_step = t.w_mn ? 2048 : 32, x_step = t.x_mn ? 2048 : 32;
+        const uint64_t w_desc = tile_desc(smem_addr(base), t.w_mn ? kWBytes / 2 : 0),
+                       x_desc = tile_desc(smem_addr(base) + kWBytes, t.x_mn ? 64 * kRowStep * 2 : 0);
+        const uint32_t w_step = (t.w_mn ? 2048 : 32) >> 4, x_step = (t.x_mn ? 2048 : 32) >> 4;   // 16 summed elements
         int stage = 0, run = -1, next = k_first;   // `next`: the step that begins another run
         uint32_t phase = 0;
         for (int k = k_first; k < k_last; k++) {
-            if (!bar_wait(full + 8 * stage, phase, waits)) break;
+            if (!bar_wait_warp(full + 8 * stage, phase, waits)) break;
             tc_fence_after();
             const bool begins = k == next;
             if (begins) next = k_first + (k_last - k_first) * (++run + 1) / t.runs;
-            const uint32_t at = smem_addr(base) + stage * stage_bytes;
+            const uint64_t w = w_desc + uint32_t(stage * (stage_bytes >> 4)), x = x_desc + uint32_t(stage * (stage_bytes >> 4));
+            if (elected()) {
 #pragma unroll
-            for (int j = 0; j < kRowStep / 16; j++)
-                mma_f16<1>(tmem + run * t.apart, tile_desc(at + j * w_step, w_lead),
-                           tile_desc(at + kWBytes + j * x_step, x_lead), desc, !begins || j > 0);
-            mma_commit(empty + 8 * stage);
+                for (int j = 0; j < kRowStep / 16; j++)
+                    mma_f16<1>(tmem + run * t.apart, w + j * w_step, x + j * x_step, desc, !begins || j > 0);
+                mma_commit(empty + 8 * stage);
+            }
             if (++stage == t.stages) stage = 0, phase ^= 1;
         }
-        mma_commit(ready);
+        if (elected()) mma_commit(ready);
     }
     __syncwarp();
     // All products done (and with them every load): the stages' memory now

@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
     __shared__ uint32_t tmem_at, stop;
     char* base = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_number(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages,
                    taken = ready + 16, last = taken + 16;
@@ -389,10 +389,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     const int steps = t.steps * t.segments, runs = F32 ? (steps + kRun - 1) / kRun : 1;
     wait_previous();
 
-    if (warp < 2 && lane == 0) {
-        // ------------------------------------------------ loads
-        // A thread for each operand: what one thread spent on a stage's waits and
-        // loads of both was longer than its products.
+    if (warp < 2) {
+        // ------------------------------------------------ loads, a warp for each operand
         const bool b = warp == 1, mn = b ? t.b_mn : t.a_mn;
         const uint32_t to = smem_addr(base) + (b ? kHalf : 0), there = in_cta(full, 0);
         int stage = 0, used = 0;
@@ -407,11 +405,13 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 const CUtensorMap* map = !b ? &t.a[it.twin | seg] : &(it.sums == 256 ? t.b : t.b_half)[PAIR ? int(rank) : seg];
                 const int k_last = (seg + 1) * t.steps;
                 for (int at = 0; k < k_last; k++, at += kStep) {
-                    if (!(ok = bar_wait(empty + 8 * stage, phase ^ 1, waits))) break;
-                    if (!b && rank == 0) bar_expect(full + 8 * stage, bytes);
-                    const uint32_t dst = to + stage * kStage, bar = there + 8 * stage;
-                    tma_load_pair(dst, map, mn ? row : at, mn ? at : row, bar);
-                    if (two) tma_load_pair(dst + kHalf / 2, map, row + 64, at, bar);
+                    if (!(ok = bar_wait_warp(empty + 8 * stage, phase ^ 1, waits))) break;
+                    if (elected()) {
+                        if (!b && rank == 0) bar_expect(full + 8 * stage, bytes);
+                        const uint32_t dst = to + stage * kStage, bar = there + 8 * stage;
+                        tma_load_pair(dst, map, mn ? row : at, mn ? at : row, bar);
+                        if (two) tma_load_pair(dst + kHalf / 2, map, row + 64, at, bar);
+                    }
                     used++;
                     if (++stage == kStages) stage = 0, phase ^= 1;
                 }
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 if (--stage < 0) stage = kStages - 1, phase ^= 1;
                 bar_drain(full + 8 * stage, phase);
             }
-    } else if (warp == 2 && lane == 0 && rank == 0) {
+    } else if (warp == 2 && rank == 0) {
         // ------------------------------------------------ products
         const uint64_t a_desc = tile_desc(smem_addr(base), t.a_mn ? kHalf / 2 : 0),
                        b_desc = tile_desc(smem_addr(base) + kHalf, t.b_mn ? kHalf / 2 : 0);
@@ -437,28 +437,29 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             for (int run = 0, k = 0; run < runs && ok; run++) {
                 const int k_last = F32 ? steps * (run + 1) / runs : steps;
                 bool add = false;
-                if (!(ok = bar_wait(taken + 8 * acc, acc_phase ^ 1, waits))) break;
+                if (!(ok = bar_wait_warp(taken + 8 * acc, acc_phase ^ 1, waits))) break;
                 tc_fence_after();
                 for (; k < k_last; k++) {
-                    if (!(ok = bar_wait(full + 8 * stage, phase, waits))) break;
+                    if (!(ok = bar_wait_warp(full + 8 * stage, phase, waits))) break;
                     tc_fence_after();
                     // addresses stay below 2^18, so the descriptors' fields do not run over
                     const uint64_t a = a_desc + uint32_t(stage * (kStage >> 4)), b = b_desc + uint32_t(stage * (kStage >> 4));
+                    if (elected()) {
 #pragma unroll
-                    for (int j = 0; j < kStep / 16; j++) {
-                        mma_f16<2>(tmem + acc * 256, a + j * a_step, b + j * b_step, desc, add);
-                        add = true;
+                        for (int j = 0; j < kStep / 16; j++)
+                            mma_f16<2>(tmem + acc * 256, a + j * a_step, b + j * b_step, desc, add || j > 0);
+                        mma_commit_pair(empty + 8 * stage);
                     }
-                    mma_commit_pair(empty + 8 * stage);
+                    add = true;
                     if (++stage == kStages) stage = 0, phase ^= 1;
                 }
                 if (!ok) break;
-                mma_commit_pair(ready + 8 * acc);
+                if (elected()) mma_commit_pair(ready + 8 * acc);
                 if (++acc == 2) acc = 0, acc_phase ^= 1;
             }
         }
         if (!ok) {   // the products under way still read shared memory
-            mma_commit_pair(last);
+            if (elected()) mma_commit_pair(last);
             bar_drain(last, 0);
         }
     } else if (warp >= 3) {
