@@ -108,42 +108,59 @@ __global__ void __launch_bounds__(256) join_kernel(const float* sums, int parts,
     store1(out, n, s, out_f32, half);
 }
 
-// The copies of one call, one a blockIdx.y.  A thread copies eight elements of
-// a row, loaded by as many bytes at a time as their place allows and stored by
-// 16.  4096 x 4099 (rows at every second byte): 67 MB moved in 12 us.
+// Eight elements as they lie, loaded by as many bytes at a time as their place
+// allows
+__device__ __forceinline__ uint4 load8(const uint16_t* p)
+{
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    uint4 w;
+    if (at % 16 == 0) {
+        w = *reinterpret_cast<const uint4*>(p);
+    } else if (at % 8 == 0) {
+        const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + 4);
+        w = make_uint4(a.x, a.y, b.x, b.y);
+    } else if (at % 4 == 0) {
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+        w = make_uint4(q[0], q[1], q[2], q[3]);
+    } else {   // the seven halves between the words' ends, and the two at them
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p + 1);
+        const uint32_t a = p[0], b = q[0], c = q[1], d = q[2], e = p[7];
+        w = make_uint4(a | b << 16, b >> 16 | c << 16, c >> 16 | d << 16, d >> 16 | e << 16);
+    }
+    return w;
+}
+
+// The copies of one call, one a blockIdx.y.  A thread copies eight elements of a
+// row at a time, two such before it stores the first, by 16 bytes.  4096 x 4099
+// (rows at every second byte): 67 MB moved in 15 us (4.4 TB/s).
 __global__ void __launch_bounds__(256) copy_kernel(const Copies c)
 {
     wait_previous();
     allow_next();
     const Copies::Job& j = c.job[blockIdx.y];
-    const uint64_t units = uint64_t(j.cols + 7) / 8, all = units * uint64_t(j.rows);
-    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += uint64_t(gridDim.x) * 256) {
-        const uint64_t m = all >> 32 ? i / units : uint32_t(i) / uint32_t(units), n = (i - m * units) * 8;
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(j.src) + int64_t(m) * j.rs + int64_t(n) * j.cs;
-        uint16_t* q = reinterpret_cast<uint16_t*>(j.dst) + int64_t(m) * j.ld + int64_t(n);
-        if (j.cs != 1 || int64_t(n) + 8 > j.cols) {
-            uint16_t v[8];
-            const int some = int(min(int64_t(8), j.cols - int64_t(n)));
+    const uint64_t units = uint64_t(j.cols + 7) / 8, all = units * uint64_t(j.rows), apart = uint64_t(gridDim.x) * 256;
+    for (uint64_t i0 = uint64_t(blockIdx.x) * 256 + threadIdx.x; i0 < all; i0 += 2 * apart) {
+        uint4 w[2];
+        uint16_t* q[2] = {nullptr, nullptr};
 #pragma unroll
-            for (int k = 0; k < 8; k++) v[k] = k < some ? p[k * j.cs] : uint16_t(0);
-#pragma unroll
-            for (int k = 0; k < 8; k++)
-                if (k < some) q[k] = v[k];
-            continue;
+        for (int h = 0; h < 2; h++) {
+            const uint64_t i = i0 + h * apart;
+            if (i >= all) continue;
+            const uint64_t m = all >> 32 ? i / units : uint32_t(i) / uint32_t(units);
+            const int64_t n = int64_t(i - m * units) * 8;
+            const uint16_t* p = reinterpret_cast<const uint16_t*>(j.src) + int64_t(m) * j.rs + n * j.cs;
+            uint16_t* to = reinterpret_cast<uint16_t*>(j.dst) + int64_t(m) * j.ld + n;
+            if (j.cs == 1 && n + 8 <= j.cols) {
+                w[h] = load8(p);
+                q[h] = to;
+            } else {
+                const int some = int(min(int64_t(8), j.cols - n));
+                for (int k = 0; k < some; k++) to[k] = p[k * j.cs];
+            }
         }
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        uint32_t w[4];
-        if (at % 16 == 0) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p);
-            w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-        } else if (at % 4 == 0) {
 #pragma unroll
-            for (int k = 0; k < 4; k++) w[k] = reinterpret_cast<const uint32_t*>(p)[k];
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; k++) w[k] = uint32_t(p[2 * k]) | uint32_t(p[2 * k + 1]) << 16;
-        }
-        *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int h = 0; h < 2; h++)
+            if (q[h]) *reinterpret_cast<uint4*>(q[h]) = w[h];
     }
 }
 
@@ -192,7 +209,7 @@ int copies_launch(Proj* P, const Copies& c, cudaStream_t s)
 {
     int64_t most = 0;
     for (int i = 0; i < c.n; i++) most = std::max(most, c.job[i].rows * ((c.job[i].cols + 7) / 8));
-    const unsigned blocks = unsigned(std::min<int64_t>((most + 255) / 256, int64_t(P->num_sms) * 32));
+    const unsigned blocks = unsigned(std::min<int64_t>((most + 511) / 512, int64_t(P->num_sms) * 16));
     return launch(copy_kernel, dim3(blocks, unsigned(c.n)), dim3(256), 0, 1, s, "operand copy", c);
 }
 
