@@ -346,15 +346,16 @@ static int loadable(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t
 
 // Few rows take row_kernel, which reads the weights once for up to 128 rows
 // and splits the sum over k; so do products whose tiles of 128 x 128 (of a
-// pair 64 x 128) are no more than the SMs, which the 256 x 256 tiles of
-// tile_kernel would leave idle.  4096 x 4096 weights, us with row_kernel and
-// tile_kernel: 64 rows 13.1 and 30.6, 256 rows 19.3 and 31.2, 512 rows 28.9
-// and 31.7, 1024 rows (256 tiles) 43.5 and 32.8; the gated operator, 8192 x
-// 4096: 128 rows 33.9 and 40.0, 256 rows (256 tiles) 43.1 and 40.7.
+// pair 64 x 128) are no more than two thirds of the SMs, most of which the 256 x
+// 256 tiles of tile_kernel would leave idle.  us with row_kernel and
+// tile_kernel, 4096 x 4096 weights: 64 rows 11.0 and 17.8, 256 rows 15.5 and 18.4,
+// 384 rows (96 tiles) 17.0 and 18.6, 512 rows 20.2 and 18.6, 1024 rows 32.3 and
+// 25.2; 1024 x 1024 weights: 1024 rows (64 tiles) 7.7 and 8.6, 2048 rows 10.3 and
+// 9.0; a pair of 8192 x 4096: 128 rows 28.0 and 30.0, 192 rows 33.7 and 30.1.
 static int product_launch(Proj* P, const Product& p, cudaStream_t s)
 {
     const int64_t width = p.kind == kPair ? 64 : 128;
-    const bool few = p.M <= 128 || ((p.M + 127) / 128) * ((p.N + width - 1) / width) <= P->num_sms;
+    const bool few = p.M <= 128 || 3 * ((p.M + 127) / 128) * ((p.N + width - 1) / width) <= 2 * P->num_sms;
     return p.kind != kTwin && few ? row_launch(P, p, s) : tile_launch(P, p, s);
 }
 
