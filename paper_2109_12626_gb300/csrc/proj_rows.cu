@@ -25,10 +25,9 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.width = pair ? 64 : kRowFeatures;
     // Tiles of 64 rows where 128 would leave SMs without one, unless the sum is
     // long and four CTAs a tile fill the SMs, when the fewer bytes of larger
-    // tiles count: 128 rows of 4096 x 4096
-    // 12.5 against 14.9 us, 1024 rows of 1024 x 1024 8.3 against 9.4; 128 rows of
-    // 8192 x 8192, 31.8 against 29.4.  With more tiles than SMs, 512 rows of 4096 x
-    // 4096, 25.3 against 21.1.
+    // tiles count: 128 rows of 4096 x 4096 12.5 against 14.9 us, 1024 rows of 1024 x
+    // 1024 8.3 against 9.4; 128 rows of 8192 x 8192, 31.8 against 29.4.  With more
+    // tiles than SMs, 512 rows of 4096 x 4096, 25.3 against 21.1.
     const int64_t across = (p.N + t.width - 1) / t.width;
     const int steps = t.steps * t.segments;
     t.columns = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;

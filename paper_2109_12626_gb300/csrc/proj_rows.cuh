@@ -14,9 +14,9 @@
 //
 // Bound by the weights' bytes while there are some megabytes an SM, else by the
 // chain of setting up, one trip to memory, the cluster's barriers and partials
-// (4.4 us at 1024 x 1024): two rows of 8192 x 8192 in 24.8 us (5.4 TB/s, 0.81 of
-// the measured copy), 48 rows of a pair of 2048 x 5120 in 12.9 (3.3 TB/s), 128
-// rows of a pair of 8192 x 4096 in 30.4 (4.4 TB/s).  Loads asked into L2 before
+// (3.7 us at 1024 x 1024): two rows of 8192 x 8192 in 24.4 us (5.5 TB/s, 0.82 of
+// the measured copy), 48 rows of a pair of 2048 x 5120 in 12.4 (3.4 TB/s), 128
+// rows of a pair of 8192 x 4096 in 28.4 (4.8 TB/s).  Loads asked into L2 before
 // the kernel before has ended, or a smaller ring for more CTAs an SM, gained
 // nothing.
 #pragma once

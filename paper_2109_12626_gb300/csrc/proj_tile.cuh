@@ -15,22 +15,20 @@
 // two weights' 128 rows of the same features, one weight a CTA: the pair g, u
 // of an output ends in columns n and n + 128 of one thread's row.
 //
-// Bound by the tensor cores: 8192 x 8192 x 4096 in 297 us (1.85 PFLOP/s, 0.97 of
-// the measured burst; with bias and residual, over inputs that do not stay in
-// L2, 332 us, 0.97 of the rate that a long loop sustains), the gated operator
-// 8192 x 4096 x 8192 in 570 us (1.93 PFLOP/s).  With fewer than some ten rounds
-// of tiles the last one's idle pairs show: 4096 x 4096 x 4096, 3.4 rounds, in 84
-// us (1.63 PFLOP/s); short sums are bound by finishing: 4096 x 1000 x 4096 in 33.
-// Tried and not kept: asking a ring's length ahead into L2 (411 against 299 us),
-// the last round's tiles summed by several pairs that join their sums (no
-// faster, and 43 against 33 us for the short sums).
+// Bound by the tensor cores: 4096 x 4096 x 4096 in 72 us (1.90 PFLOP/s, the
+// measured burst), 8192 x 8192 x 4096 in 280 (1.96), the gated operator 8192 x 4096 x
+// 8192 in 535 (2.06); in a long loop the power limit sets the rate.  Short sums are
+// bound by finishing a tile (3.5 us) and by loads: 4096 x 1000 x 4096 in 32 us.
+// Tried and not kept: asking tiles into L2 ahead of their loads (every pair its
+// own: 411 against 299 us; one pair for all: no faster), the last round's tiles summed by several pairs that join
+// their sums (no faster, and 43 against 33 us for short sums).
 //
 // The tensor cores add to a sum by cutting off, not by rounding: a sum of K
 // products comes out smaller by about 1e-9 K of its size (measured: 1.25e-6 at K
 // = 1024, 9.7e-6 at 8192).  No 16-bit result shows that.  For float32 results
 // (F32) a sum is taken in runs of at most 640 products, and the finishing warps
 // add up the runs in registers, rounded, while the next run's products are at
-// work: 7.9e-7 at K = 8192, 4096 x 4096 x 4096 in 95 us instead of 84.
+// work: 7.9e-7 at K = 8192, 4096 x 4096 x 4096 in 82 us instead of 72.
 #pragma once
 
 #include "proj_common.cuh"
