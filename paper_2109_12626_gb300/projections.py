@@ -23,6 +23,7 @@ class _Projection:
     """What both operators share: the plan handle, and matrix arguments."""
 
     _plan = ""
+    _calls = ()
     _args = 0
 
     def __init__(self, max_rows: int, n_in: int, n_out: int, dtype="bfloat16", out=None,
@@ -39,6 +40,7 @@ class _Projection:
         if not h:
             raise DpdrError(L.dpdr_last_error(), self._plan)
         self._h = h
+        self._forward, self._backward = (getattr(L, f) for f in self._calls)
         self._device = torch.cuda.current_device()
         self.max_rows, self.n_in, self.n_out = int(max_rows), int(n_in), int(n_out)
         self.dtype, self.out, self.grad, self.act = dtype, out, grad, act
@@ -75,12 +77,8 @@ class _Projection:
         """Argument number i as a record; its address, 0 for None."""
         if t is None:
             return 0
-        if t.dtype is not dtype:
-            raise TypeError("%s is %s, the plan wants %s" % (name, t.dtype, dtype))
-        if t.shape != (rows, cols):
-            raise ValueError("%s is %s, the plan wants %s" % (name, tuple(t.shape), (rows, cols)))
-        if t.get_device() != self._device:
-            raise ValueError("%s is not on the plan's device" % name)
+        if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != self._device:
+            self._unfit(name, t, (rows, cols), dtype)
         r = self._rec
         r[3 * i] = t.data_ptr()
         r[3 * i + 1], r[3 * i + 2] = t.stride()
@@ -89,13 +87,18 @@ class _Projection:
     def _vector(self, name, t, n, dtype):
         if t is None:
             return 0
+        if t.dtype is not dtype or t.shape != (n,) or t.get_device() != self._device:
+            self._unfit(name, t, (n,), dtype)
+        if n > 1 and t.stride(0) != 1:
+            raise ValueError("%s: the plan wants contiguous elements" % name)
+        return t.data_ptr()
+
+    def _unfit(self, name, t, shape, dtype):
         if t.dtype is not dtype:
             raise TypeError("%s is %s, the plan wants %s" % (name, t.dtype, dtype))
-        if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
-            raise ValueError("%s: the plan wants %d contiguous elements" % (name, n))
-        if t.get_device() != self._device:
-            raise ValueError("%s is not on the plan's device" % name)
-        return t.data_ptr()
+        if t.shape != shape:
+            raise ValueError("%s is %s, the plan wants %s" % (name, tuple(t.shape), shape))
+        raise ValueError("%s is not on the plan's device" % name)
 
     def _rows(self, x):
         if x.dim() != 2:
@@ -112,6 +115,7 @@ class Linear(_Projection):
     "sigmoid".  Any number of rows up to ``max_rows`` goes through a plan."""
 
     _plan = "dpdr_linear_plan"
+    _calls = ("dpdr_linear", "dpdr_linear_backward")
     _args = 7
 
     def forward(self, x, w, y, bias=None, residual=None, pre=None, stream=None) -> None:
@@ -119,12 +123,12 @@ class Linear(_Projection):
         keeps x w^T + bias for the backward call."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
         m = self._matrix
-        rc = lib().dpdr_linear(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                               m(1, "w", w, n, k, self._operand),
-                               self._vector("bias", bias, n, self._operand),
-                               m(2, "residual", residual, rows, n, self._result),
-                               m(3, "y", y, rows, n, self._result),
-                               m(4, "pre", pre, rows, n, self._float32), _stream(stream))
+        rc = self._forward(self._h, rows, m(0, "x", x, rows, k, self._operand),
+                           m(1, "w", w, n, k, self._operand),
+                           self._vector("bias", bias, n, self._operand),
+                           m(2, "residual", residual, rows, n, self._result),
+                           m(3, "y", y, rows, n, self._result),
+                           m(4, "pre", pre, rows, n, self._float32), _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_linear")
 
@@ -134,15 +138,15 @@ class Linear(_Projection):
         the projection is computed again, for which it needs the bias."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
         m = self._matrix
-        rc = lib().dpdr_linear_backward(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                                        m(1, "w", w, n, k, self._operand),
-                                        self._vector("bias", bias, n, self._operand),
-                                        m(2, "dy", dy, rows, n, self._result),
-                                        m(3, "pre", pre, rows, n, self._float32),
-                                        m(4, "dx", dx, rows, k, self._gradient),
-                                        m(5, "dw", dw, n, k, self._gradient),
-                                        self._vector("dbias", dbias, n, self._gradient),
-                                        _stream(stream))
+        rc = self._backward(self._h, rows, m(0, "x", x, rows, k, self._operand),
+                            m(1, "w", w, n, k, self._operand),
+                            self._vector("bias", bias, n, self._operand),
+                            m(2, "dy", dy, rows, n, self._result),
+                            m(3, "pre", pre, rows, n, self._float32),
+                            m(4, "dx", dx, rows, k, self._gradient),
+                            m(5, "dw", dw, n, k, self._gradient),
+                            self._vector("dbias", dbias, n, self._gradient),
+                            _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_linear_backward")
 
@@ -152,6 +156,7 @@ class Gated(_Projection):
     [n_hidden, n_in].  Types and activations as for Linear."""
 
     _plan = "dpdr_gated_plan"
+    _calls = ("dpdr_gated", "dpdr_gated_backward")
     _args = 8
 
     def __init__(self, max_rows, n_in, n_hidden, dtype="bfloat16", out=None, grad=None, act="silu"):
@@ -163,11 +168,11 @@ class Gated(_Projection):
         projections, the gate's first, for the backward call."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
         m = self._matrix
-        rc = lib().dpdr_gated(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                              m(1, "w_gate", w_gate, n, k, self._operand),
-                              m(2, "w_up", w_up, n, k, self._operand),
-                              m(3, "h", h, rows, n, self._result),
-                              m(4, "pre", pre, rows, 2 * n, self._float32), _stream(stream))
+        rc = self._forward(self._h, rows, m(0, "x", x, rows, k, self._operand),
+                           m(1, "w_gate", w_gate, n, k, self._operand),
+                           m(2, "w_up", w_up, n, k, self._operand),
+                           m(3, "h", h, rows, n, self._result),
+                           m(4, "pre", pre, rows, 2 * n, self._float32), _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_gated")
 
@@ -177,13 +182,13 @@ class Gated(_Projection):
         the projections are computed again."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
         m = self._matrix
-        rc = lib().dpdr_gated_backward(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                                       m(1, "w_gate", w_gate, n, k, self._operand),
-                                       m(2, "w_up", w_up, n, k, self._operand),
-                                       m(3, "dh", dh, rows, n, self._result),
-                                       m(4, "pre", pre, rows, 2 * n, self._float32),
-                                       m(5, "dx", dx, rows, k, self._gradient),
-                                       m(6, "dw_gate", dw_gate, n, k, self._gradient),
-                                       m(7, "dw_up", dw_up, n, k, self._gradient), _stream(stream))
+        rc = self._backward(self._h, rows, m(0, "x", x, rows, k, self._operand),
+                            m(1, "w_gate", w_gate, n, k, self._operand),
+                            m(2, "w_up", w_up, n, k, self._operand),
+                            m(3, "dh", dh, rows, n, self._result),
+                            m(4, "pre", pre, rows, 2 * n, self._float32),
+                            m(5, "dx", dx, rows, k, self._gradient),
+                            m(6, "dw_gate", dw_gate, n, k, self._gradient),
+                            m(7, "dw_up", dw_up, n, k, self._gradient), _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_gated_backward")
