@@ -223,12 +223,14 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                 float z[kBatch][4], u[kBatch][4], o[kBatch][4];
 #pragma unroll
                 for (int b = 0; b < kBatch; b++) {
-                    const int at = min(c + b * kApart * t.split, cols - 1);
-                    const uint32_t from = smem_addr(part + at * kRowFeatures + f);
+                    // a batch's column past the last reads that one's partials
+                    // again, and is dropped
+                    const int at = c + b * kApart * t.split;
+                    const uint32_t from = smem_addr(part + min(at, cols - 1) * kRowFeatures + f);
 #pragma unroll
                     for (int i = 0; i < 4; i++) u[b][i] = o[b][i] = 0.0f;
-                    if (four && e.other) load4(e.other, (m0 + at) * e.other_rs + n, e.other_f32, e.half, o[b]);
-                    if (!four)
+                    if (four && e.other && at < cols) load4(e.other, (m0 + at) * e.other_rs + n, e.other_f32, e.half, o[b]);
+                    if (!four && at < cols)
 #pragma unroll
                         for (int i = 0; i < 4; i++)
                             if (n + i < t.N) o[b][i] = other1(e, m0 + at, n + i);
