@@ -169,27 +169,36 @@ struct Finisher {
                     }
                 }
         }
+        // all of the round's sums before the first result is stored: behind a store
+        // whose place the compiler cannot tell from theirs, each would wait
+        float z[kSteps][4], u[kSteps][4];
+#pragma unroll
+        for (int b = 0; b < kSteps; b++) {
+            const int r = row + b * kRows;
+            const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * (q ^ (r & 7)));
+            z[b][0] = z4.x, z[b][1] = z4.y, z[b][2] = z4.z, z[b][3] = z4.w;
+            if (PAIR) {
+                const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * ((4 + q) ^ (r & 7)));
+                u[b][0] = u4.x, u[b][1] = u4.y, u[b][2] = u4.z, u[b][3] = u4.w;
+            }
+        }
         const int64_t down = out_rs * kRows * 2, down2 = e.out2_rs * kRows * 2, down_pre = e.pre_rs * kRows;
 #pragma unroll
         for (int b = 0; b < kSteps; b++) {
             const int r = row + b * kRows;
             if (r < rows) {
-                float z[4], u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4], w[4];
-                const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * (q ^ (r & 7)));
-                z[0] = z4.x + bias[0], z[1] = z4.y + bias[1], z[2] = z4.z + bias[2], z[3] = z4.w + bias[3];
-                if (PAIR) {
-                    const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * ((4 + q) ^ (r & 7)));
-                    u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
-                }
+                float o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4], w[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) z[b][i] += bias[i];
                 if (e.pre) {
-                    *reinterpret_cast<float4*>(pre) = make_float4(z[0], z[1], z[2], z[3]);
-                    if (PAIR) *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[0], u[1], u[2], u[3]);
+                    *reinterpret_cast<float4*>(pre) = make_float4(z[b][0], z[b][1], z[b][2], z[b][3]);
+                    if (PAIR) *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[b][0], u[b][1], u[b][2], u[b][3]);
                 }
                 if (e.other) widen4(other[b], e.other_f32, HALF, o);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     w[i] = 0.0f;
-                    finish1<PAIR, FINISH, ACT>(z[i], u[i], o[i], v[i], w[i]);
+                    finish1<PAIR, FINISH, ACT>(z[b][i], PAIR ? u[b][i] : 0.0f, o[i], v[i], w[i]);
                 }
                 store4(p, 0, 0, HALF, v);
                 if (PAIR && FINISH == kSlope) store4(p2, 0, 0, HALF, w);
