@@ -227,28 +227,28 @@ struct Finisher {
             }
             put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o);
         };
-        if (PAIR || !e.other) {
-            const float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 2
-            for (int b = 0; b < kSteps; b++) step(b, o);
+        if (!PAIR && e.other) {
+            for (int b0 = 0; b0 < kSteps; b0 += 4) {
+                float o[4][4];
+#pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    const int r = row + (b0 + b) * kRows;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) o[b][i] = 0.0f;
+                    if (r < rows) load4(e.other, (m0 + r) * e.other_rs + n, 1, 0, o[b]);
+                }
+#pragma unroll
+                for (int b = 0; b < 4; b++) step(b0 + b, o[b]);
+            }
             return;
         }
-        for (int b0 = 0; b0 < kSteps; b0 += 4) {
-            float o[4][4];
-#pragma unroll
-            for (int b = 0; b < 4; b++) {
-                const int r = row + (b0 + b) * kRows;
-#pragma unroll
-                for (int i = 0; i < 4; i++) o[b][i] = 0.0f;
-                if (r < rows) load4(e.other, (m0 + r) * e.other_rs + n, 1, 0, o[b]);
-            }
-#pragma unroll
-            for (int b = 0; b < 4; b++) step(b0 + b, o[b]);
-        }
+        const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+        for (int b = 0; b < kSteps; b++) step(b, none);
     }
 
-    // One element a thread and step, for results that do not lie on fours, eight (of a
-    // pair 16) steps' other values asked for together.
+    // One element a thread and step, for results that do not lie on fours; the sums
+    // and other values of eight steps (of a pair 16) before the first is stored.
     template <int HALF>
     __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs)
     {
@@ -260,9 +260,7 @@ struct Finisher {
         const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, HALF) : 0.0f;
         char* at = out + (m * out_rs + n) * kSize;
         const int64_t down = out_rs * kStep * kSize;
-        auto step = [&](int r, char* p, float o) {
-            const float z = stage[r * 32 + 4 * ((c >> 2) ^ (r & 7)) + (c & 3)] + bias;
-            const float u = PAIR ? stage[r * 32 + 4 * ((4 + (c >> 2)) ^ (r & 7)) + (c & 3)] : 0.0f;
+        auto step = [&](int r, char* p, float z, float u, float o) {
             if (e.pre) {
                 float* pre = e.pre + ((m0 + r) * e.pre_rs + n);
                 *pre = z;
@@ -273,18 +271,26 @@ struct Finisher {
             store1(p, 0, v, F32, HALF);
             if (PAIR && FINISH == kSlope) store1(e.out2, (m0 + r) * e.out2_rs + n, w, F32, HALF);
         };
+        auto sum = [&](int r, int side) {
+            return stage[r * 32 + 4 * ((4 * side + (c >> 2)) ^ (r & 7)) + (c & 3)];
+        };
         if (!e.other) {
 #pragma unroll 4
-            for (int r = first; r < rows; r += kStep, at += down) step(r, at, 0.0f);
+            for (int r = first; r < rows; r += kStep, at += down) step(r, at, sum(r, 0) + bias, PAIR ? sum(r, 1) : 0.0f, 0.0f);
             return;
         }
         for (int r0 = first; r0 < rows; r0 += kStep * kAsk, at += kAsk * down) {
-            float o[kAsk];
+            float z[kAsk], u[kAsk], o[kAsk];
 #pragma unroll
-            for (int b = 0; b < kAsk; b++) o[b] = r0 + b * kStep < rows ? other1(e, m0 + r0 + b * kStep, n) : 0.0f;
+            for (int b = 0; b < kAsk; b++) {
+                const int r = r0 + b * kStep;
+                o[b] = r < rows ? other1(e, m0 + r, n) : 0.0f;
+                z[b] = sum(r & 31, 0) + bias;
+                u[b] = PAIR ? sum(r & 31, 1) : 0.0f;
+            }
 #pragma unroll
             for (int b = 0; b < kAsk; b++)
-                if (r0 + b * kStep < rows) step(r0 + b * kStep, at + b * down, o[b]);
+                if (r0 + b * kStep < rows) step(r0 + b * kStep, at + b * down, z[b], u[b], o[b]);
         }
     }
 
