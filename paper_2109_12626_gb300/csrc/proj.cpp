@@ -123,7 +123,8 @@ Span span_of(const dpdr_matrix& m, int64_t rows, int64_t cols, int esize)
     Span s;
     if (rows == 0 || cols == 0) return s;
     s.lo = reinterpret_cast<uintptr_t>(m.data);
-    s.hi = s.lo + (uintptr_t(rows - 1) * uintptr_t(m.row_stride) + uintptr_t(cols - 1) * uintptr_t(m.col_stride) + 1) * esize;
+    const uintptr_t last = uintptr_t(rows - 1) * uintptr_t(m.row_stride) + uintptr_t(cols - 1) * uintptr_t(m.col_stride);
+    s.hi = s.lo + (last + 1) * esize;
     s.pitch = uintptr_t(m.row_stride) * esize;
     s.width = m.col_stride == 1 ? uintptr_t(cols) * esize : s.pitch;
     return s;

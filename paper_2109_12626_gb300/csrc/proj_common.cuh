@@ -126,7 +126,8 @@ __device__ __forceinline__ void finish1(float g, float u, float other, float& ou
 __device__ __forceinline__ void widen4(const uint4& x, int f32, int half, float (&v)[4])
 {
     if (f32) {
-        v[0] = __uint_as_float(x.x), v[1] = __uint_as_float(x.y), v[2] = __uint_as_float(x.z), v[3] = __uint_as_float(x.w);
+        v[0] = __uint_as_float(x.x), v[1] = __uint_as_float(x.y);
+        v[2] = __uint_as_float(x.z), v[3] = __uint_as_float(x.w);
     } else if (half) {
         const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&x.x)),
                      b = __half22float2(*reinterpret_cast<const __half2*>(&x.y));

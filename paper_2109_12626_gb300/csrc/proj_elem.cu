@@ -41,10 +41,9 @@ __global__ void __launch_bounds__(kElemThreads, 4) slope_kernel(const Epilogue e
                 for (int i = 0; i < kW; i++) g[r][i] = u[r][i] = o[r][i] = 0.0f;
                 if (m >= m1) continue;
                 if (VEC) {
-                    if (e.pre) load4(reinterpret_cast<const char*>(e.pre), m * e.pre_rs + n, 1, 0, reinterpret_cast<float(&)[4]>(g[r]));
-                    if (PAIR)
-                        load4(reinterpret_cast<const char*>(e.pre), m * e.pre_rs + e.pre_up + n, 1, 0,
-                              reinterpret_cast<float(&)[4]>(u[r]));
+                    const char* pre = reinterpret_cast<const char*>(e.pre);
+                    if (e.pre) load4(pre, m * e.pre_rs + n, 1, 0, reinterpret_cast<float(&)[4]>(g[r]));
+                    if (PAIR) load4(pre, m * e.pre_rs + e.pre_up + n, 1, 0, reinterpret_cast<float(&)[4]>(u[r]));
                     load4(e.other, m * e.other_rs + n, e.other_f32, e.half, reinterpret_cast<float(&)[4]>(o[r]));
                 } else {
                     if (e.pre) g[r][0] = e.pre[m * e.pre_rs + n];

@@ -72,7 +72,7 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     if (!rc) rc = tensor_map(&t.x[0], p.a[0], p.M, p.K, p.e.half, t.columns, kRowStep);
     if (!rc && two_x) rc = tensor_map(&t.x[1], p.a[1], p.M, p.K, p.e.half, t.columns, kRowStep);
     if (rc) return rc;
-    const RowKernel kernel = pair ? row_kernel_pair(p.e.finish, p.e.act, split) : row_kernel_single(p.e.finish, p.e.act, split);
+    const RowKernel kernel = (pair ? row_kernel_pair : row_kernel_single)(p.e.finish, p.e.act, split);
     bool& set = P->row_set[pair][p.e.finish][p.e.act != DPDR_ACT_NONE][row_split_class(split)];
     if (!set) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);

@@ -158,7 +158,8 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
             tc_fence_after();
             const bool begins = k == next;
             if (begins) next = k_first + (k_last - k_first) * (++run + 1) / t.runs;
-            const uint64_t w = w_desc + uint32_t(stage * (stage_bytes >> 4)), x = x_desc + uint32_t(stage * (stage_bytes >> 4));
+            const uint32_t on = uint32_t(stage * (stage_bytes >> 4));
+            const uint64_t w = w_desc + on, x = x_desc + on;
             if (elected()) {
 #pragma unroll
                 for (int j = 0; j < kRowStep / 16; j++)
@@ -229,7 +230,8 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                     const uint32_t from = smem_addr(part + min(at, cols - 1) * kRowFeatures + f);
 #pragma unroll
                     for (int i = 0; i < 4; i++) u[b][i] = o[b][i] = 0.0f;
-                    if (four && e.other && at < cols) load4(e.other, (m0 + at) * e.other_rs + n, e.other_f32, e.half, o[b]);
+                    if (four && e.other && at < cols)
+                        load4(e.other, (m0 + at) * e.other_rs + n, e.other_f32, e.half, o[b]);
                     if (!four && at < cols)
 #pragma unroll
                         for (int i = 0; i < 4; i++)
@@ -268,7 +270,8 @@ RowKernel row_kernel_of(int finish, int act, int split)
     const int c = row_split_class(split);
     RowKernel k = nullptr;
     // without an activation a single dz is dy, and no product is finished as one
-#define DPDR_KERNELS(F, A) c == 0 ? row_kernel<PAIR, F, A, 2> : c == 1 ? row_kernel<PAIR, F, A, 4> : row_kernel<PAIR, F, A, 8>
+#define DPDR_KERNELS(F, A) \
+    c == 0 ? row_kernel<PAIR, F, A, 2> : c == 1 ? row_kernel<PAIR, F, A, 4> : row_kernel<PAIR, F, A, 8>
 #define DPDR_CALL(A)                                                                       \
     if ((PAIR || A != DPDR_ACT_NONE) && finish == kSlope) {                                 \
         k = DPDR_KERNELS((PAIR || A != DPDR_ACT_NONE ? kSlope : kValue), A);                \

@@ -192,7 +192,8 @@ struct Finisher {
                 for (int i = 0; i < 4; i++) z[b][i] += bias[i];
                 if (e.pre) {
                     *reinterpret_cast<float4*>(pre) = make_float4(z[b][0], z[b][1], z[b][2], z[b][3]);
-                    if (PAIR) *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[b][0], u[b][1], u[b][2], u[b][3]);
+                    if (PAIR)
+                        *reinterpret_cast<float4*>(pre + e.pre_up) = make_float4(u[b][0], u[b][1], u[b][2], u[b][3]);
                 }
                 if (e.other) widen4(other[b], e.other_f32, HALF, o);
 #pragma unroll
@@ -276,7 +277,8 @@ struct Finisher {
         };
         if (!e.other) {
 #pragma unroll 4
-            for (int r = first; r < rows; r += kStep, at += down) step(r, at, sum(r, 0) + bias, PAIR ? sum(r, 1) : 0.0f, 0.0f);
+            for (int r = first; r < rows; r += kStep, at += down)
+                step(r, at, sum(r, 0) + bias, PAIR ? sum(r, 1) : 0.0f, 0.0f);
             return;
         }
         for (int r0 = first; r0 < rows; r0 += kStep * kAsk, at += kAsk * down) {
@@ -415,7 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const int row = b ? it.n + (PAIR ? 0 : int(rank) * (it.sums / 2)) : it.m + int(rank) * 128;
             const int bytes = 2 * kHalf + it.sums * kStep * 2;
             for (int seg = 0, k = 0; seg < t.segments && ok; seg++) {
-                const CUtensorMap* map = !b ? &t.a[it.twin | seg] : &(it.sums == 256 ? t.b : t.b_half)[PAIR ? int(rank) : seg];
+                const CUtensorMap* b_maps = it.sums == 256 ? t.b : t.b_half;
+                const CUtensorMap* map = b ? &b_maps[PAIR ? int(rank) : seg] : &t.a[it.twin | seg];
                 const int k_last = (seg + 1) * t.steps;
                 for (int at = 0; k < k_last; k++, at += kStep) {
                     if (!(ok = bar_wait_warp(empty + 8 * stage, phase ^ 1, waits))) break;
@@ -456,7 +459,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     if (!(ok = bar_wait_warp(full + 8 * stage, phase, waits))) break;
                     tc_fence_after();
                     // addresses stay below 2^18, so the descriptors' fields do not run over
-                    const uint64_t a = a_desc + uint32_t(stage * (kStage >> 4)), b = b_desc + uint32_t(stage * (kStage >> 4));
+                    const uint32_t on = uint32_t(stage * (kStage >> 4));
+                    const uint64_t a = a_desc + on, b = b_desc + on;
                     if (elected()) {
 #pragma unroll
                         for (int j = 0; j < kStep / 16; j++)
@@ -478,7 +482,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     } else if (warp >= 3) {
         // ------------------------------------------------ results
         const int mine = warp - 3, quarter = warp & 3;   // a warp reaches the 32 lanes of its number's quarter
-        Finisher<PAIR, FINISH, ACT, F32> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane, mine >> 2);
+        Finisher<PAIR, FINISH, ACT, F32> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane,
+                                           mine >> 2);
         int acc = 0;
         uint32_t acc_phase = 0;
         for (int i = first; i < t.items; i += pairs) {

@@ -27,7 +27,8 @@ int token_launch(Proj* P, const Product& p, cudaStream_t s)
     while (t.share < 8 && groups * t.share < 8 * P->num_sms && p.K >= 2048 * t.share) t.share *= 2;
     const int64_t per = kTokenWarps / t.share;
     const TokenKernel kernel = pair ? token_kernel_of<true>(p.e.act) : token_kernel_of<false>(p.e.act);
-    return launch(kernel, dim3(unsigned((groups + per - 1) / per)), dim3(32 * kTokenWarps), 0, 1, s, "projection token kernel", t);
+    return launch(kernel, dim3(unsigned((groups + per - 1) / per)), dim3(32 * kTokenWarps), 0, 1, s,
+                  "projection token kernel", t);
 }
 
 }  // namespace proj

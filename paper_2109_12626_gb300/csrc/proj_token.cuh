@@ -7,11 +7,12 @@
 // before it uses the first, so that some 100 KB an SM are under way; x comes
 // from L1.  Nothing is set up or joined between CTAs, which is what
 // row_kernel's tensor memory, barriers and clusters cost: 1024 x 1024 weights
-// in 1.9 against 4.4 us, 512 x 8192 in 3.2 against 8.3, 4096 x 4096 in 6.8
-// against 9.4 (5.0 TB/s), 8192 x 8192 in 22.9 against 24.8 (5.9 TB/s); back to back, weights not in L2.  From two rows on the additions and the
-// reads of x take longer than row_kernel's set-up (four rows, 4096 x 4096: 15.5
-// against 9.5).  Rows that are not 16-byte aligned are read element by element
-// (4096 x 4099 in 18.5 us), still less than a copy of them first.
+// in 1.9 against 3.7 us, 512 x 8192 in 3.2 against 8.3, 4096 x 4096 in 6.8
+// against 8.8 (5.0 TB/s), 8192 x 8192 in 22.9 against 24.4 (5.9 TB/s); back to
+// back, weights not in L2.  From two rows on the additions and the reads of x
+// take longer than row_kernel's set-up (four rows, 4096 x 4096: 15.5 against
+// 9.5).  Rows that are not 16-byte aligned are read element by element (4096 x
+// 4099 in 18.5 us), still less than a copy of them first.
 #pragma once
 
 #include "proj_common.cuh"
@@ -107,7 +108,11 @@ __global__ void __launch_bounds__(32 * kTokenWarps) token_kernel(const TokenArgs
             }
 #pragma unroll
             for (int d = 0; d < kTokenDeep - 1; d++)
-                if (u + d * step < units) a[d] = __ldcs(p0 + u + d * step), b[d] = __ldcs(p1 + u + d * step), v[d] = px[u + d * step];
+                if (u + d * step < units) {
+                    a[d] = __ldcs(p0 + u + d * step);
+                    b[d] = __ldcs(p1 + u + d * step);
+                    v[d] = px[u + d * step];
+                }
 #pragma unroll
             for (int d = 0; d < kTokenDeep - 1; d++)
                 if (u + d * step < units) sum8(a[d], b[d], v[d], half, acc);

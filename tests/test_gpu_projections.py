@@ -480,7 +480,8 @@ def test_refusals():
     mk = lambda *s, t=torch.bfloat16: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
     x, w, y = mk(4, 16), mk(24, 16), mk(4, 24)
     with dpdr.Linear(4, 16, 24) as plan, dpdr.Gated(4, 16, 24) as gated:
-        for bad in (dict(x=mk(5, 16), y=mk(5, 24)), dict(w=mk(24, 15)), dict(y=mk(4, 23)), dict(x=mk(4, 16, t=torch.float16)),
+        for bad in (dict(x=mk(5, 16), y=mk(5, 24)), dict(w=mk(24, 15)), dict(y=mk(4, 23)),
+                    dict(x=mk(4, 16, t=torch.float16)),
                     dict(y=mk(4, 24, t=torch.float32)), dict(bias=mk(23)), dict(bias=mk(48)[::2]),
                     dict(residual=mk(4, 24, t=torch.float32)), dict(pre=mk(4, 24)), dict(x=x.cpu()),
                     dict(y=mk(24, 4).t()), dict(y=mk(1, 24).expand(4, 24)), dict(x=mk(4, 16, 1))):
@@ -524,7 +525,8 @@ def test_refusals():
 
 # ----------------------------------------------------------- in use together
 
-@pytest.mark.parametrize("ranks,rows,model,hidden", [(4, 200, 264, 544), (1, 1, 64, 128), (7, 33, 136, 700), (2, 600, 512, 2048)])
+@pytest.mark.parametrize("ranks,rows,model,hidden", [(4, 200, 264, 544), (1, 1, 64, 128), (7, 33, 136, 700),
+                                                     (2, 600, 512, 2048)])
 def test_feed_forward_split_over_ranks(ranks, rows, model, hidden):
     """The example: Gated, Linear with float32 partials, and the all-reduce,
     forward and backward, against the whole block in 64 bits.  Roundings to
