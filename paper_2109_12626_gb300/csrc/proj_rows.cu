@@ -49,12 +49,22 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     // and 8 CTAs: 22.2, 14.3, 10.8 and 11.0 us; a pair of 8192 x 4096: 26.3,
     // 25.8, 28.8 and 35.0 (more than two an SM).  One CTA an SM with twice the
     // stages is no faster where all fit (4 CTAs: 11.1) and slower where not.
-    // From 64 columns on at most four: the partials that the SMs send each
-    // other grow with both (333 rows, 2500 to 1000: 9.8 against 12.4 with eight).
+    // Clusters leave SMs of their group of SMs unused, and one that finds no
+    // place waits for another's whole time, so room is counted for 19/20 of the
+    // CTAs with three and four a cluster (16 rows of 4096 x 9728, 76 tiles, 3 and 4:
+    // 16.6 and 21.9 us; a pair of 4096 x 2048 and 145 rows, 96 tiles, 2 and 3: 14.7
+    // and 13.0) and for 7/8 with more (64 rows of 8192 x 4864, 38 tiles, 6 and 8:
+    // 18.6 and 25.6).  Beyond 32 columns, where the partials that the CTAs send
+    // each other weigh more, more than four CTAs only with eight stages each: 128
+    // rows of 8192 x 1024 with 4 and 8 13.0 and 10.2 us, 333 of 2504 x 1000 with 4
+    // and 5 10.3 and 9.5; 2 rows of 2048 x 2048 with 4 and 8 5.3 and 5.1.
     constexpr int kRoom = 110 * 1024;
-    const int most = t.columns > 32 ? 4 : kRowSplits;
     int split = 1;
-    while (split < most && tiles * (split + 1) <= 2 * P->num_sms && steps >= 4 * (split + 1)) split++;
+    for (int next = 2; next <= kRowSplits; next++) {
+        const int64_t room = int64_t(2 * P->num_sms) * (next > 4 ? 35 : next > 2 ? 38 : 40) / 40;
+        if (tiles * next > room || steps < (next > 4 && t.columns > 32 ? 8 : 4) * next) break;
+        split = next;
+    }
     t.split = split;
     const int stage = kRowFeatures * kRowStep * 2 + t.x_bytes, mine = (steps + split - 1) / split;
     // For float32 results, runs of 512 products, as many as two CTAs an SM have

@@ -113,6 +113,15 @@ def gated_case(rows, k, n, dtype="bfloat16", act="silu", out=None, lay=("plain",
         U.check_gated(h.check(), x, wg, wu, act, out, p.check() if pre else None)
 
 
+# long sums and few tiles, where the parts of a sum are many; the last has 128 columns
+@pytest.mark.parametrize("out", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows,k,n", [(2, 2500, 300), (40, 3333, 700), (64, 8192, 512), (100, 5000, 2900),
+                                      (150, 4097, 600), (300, 2560, 1000), (520, 6150, 1200)])
+def test_long_sums(rows, k, n, out):
+    linear_case(rows, k, n, out=out, act="silu", pre=True)
+    gated_case(rows, k, (n + 1) // 2, out=out, act="gelu_tanh")
+
+
 @pytest.mark.parametrize("rows,k,n", [(1, 520, 264), (24, 1024, 513), (160, 200, 328), (700, 264, 520)])
 @pytest.mark.parametrize("act", ACTS)
 def test_gated_activations_with_kept_projections(rows, k, n, act):
