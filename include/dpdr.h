@@ -430,7 +430,9 @@ typedef struct {
 
 /* Opaque plan of a projection: its sizes and types, and the device scratch
  * that some calls need (made by the first such call, of the size that
- * max_rows rows need; make that call before any stream capture). */
+ * max_rows rows need in any call; make that call before any stream capture).
+ * Scratch never moves and is freed with the plan, so a captured call can be
+ * replayed after calls of any other kind. */
 typedef struct dpdr_proj_s* dpdr_proj_t;
 
 /* Plans on the current CUDA device.  max_rows >= 0, the other sizes >= 1,

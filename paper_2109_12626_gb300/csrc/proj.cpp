@@ -207,18 +207,14 @@ int check_plan(const Proj* P, bool gated, int64_t rows, const char* who)
     return DPDR_OK;
 }
 
-// Device scratch of at least `bytes`; grown by a plain allocation, before
-// which the old one's last use has finished (cudaFree waits for it).
-int reserve(Proj* P, size_t bytes)
+// Device memory of the plan's, made by the first call that needs it at the
+// size of the largest use that any later call can have for it: a captured call
+// may be replayed after others, so nothing is moved before the plan goes.
+int hold(char*& at, size_t bytes, const char* what)
 {
-    if (bytes <= P->scratch_bytes) return DPDR_OK;
-    cudaFree(P->scratch);
-    P->scratch = nullptr;
-    P->scratch_bytes = 0;
-    const cudaError_t e = cudaMalloc(&P->scratch, bytes);
-    if (e != cudaSuccess) return cuda_fail_c(e, "projection scratch");
-    P->scratch_bytes = bytes;
-    return DPDR_OK;
+    if (at || bytes == 0) return DPDR_OK;
+    const cudaError_t e = cudaMalloc(&at, bytes);
+    return e == cudaSuccess ? DPDR_OK : cuda_fail_c(e, what);
 }
 
 Operand rows_of(const dpdr_matrix& m) { return {static_cast<const char*>(m.data), m.row_stride, m.col_stride}; }
@@ -298,15 +294,10 @@ static int pack(Proj* P, dpdr_matrix& m, int64_t rows, int64_t cols, int64_t mos
                 Copies& c)
 {
     const int64_t ld = padded(turned ? rows : cols);
-    const size_t bytes = size_t(turned ? cols : most_rows) * size_t(padded(turned ? most_rows : cols)) * 2;
-    if (bytes > P->packed_bytes[slot]) {
-        cudaFree(P->packed[slot]);   // waits for its last use
-        P->packed[slot] = nullptr;
-        P->packed_bytes[slot] = 0;
-        const cudaError_t e = cudaMalloc(&P->packed[slot], bytes);
-        if (e != cudaSuccess) return cuda_fail_c(e, "projection operand copy");
-        P->packed_bytes[slot] = bytes;
-    }
+    // either way round
+    const size_t most = std::max(size_t(most_rows) * size_t(padded(cols)), size_t(cols) * size_t(padded(most_rows)));
+    const int rc = hold(P->packed[slot], most * 2, "projection operand copy");
+    if (rc) return rc;
     int at = 0;
     while (at < c.n && c.slot[at] != slot) at++;
     if (at == c.n) c.n++;
@@ -443,8 +434,9 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     const bool as_is = !P->gated && P->act == DPDR_ACT_NONE && !P->out_f32;
     const int64_t ld = padded(N);
     const size_t dz_bytes = as_is ? 0 : upto256(size_t(P->max_rows) * size_t(ld) * 2);
-    const size_t sum_bytes = c.dbias ? upto256(size_t(column_sum_parts(P->max_rows)) * size_t(N) * 4) : 0;
-    int rc = reserve(P, n * dz_bytes + sum_bytes);
+    const size_t sum_bytes = P->gated ? 0 : upto256(size_t(column_sum_parts(P->max_rows)) * size_t(N) * 4);
+    int rc = DPDR_OK;
+    if (!as_is || c.dbias) rc = hold(P->scratch, n * dz_bytes + sum_bytes, "projection scratch");
     if (rc) return rc;
     const bool again = !as_is && !c.pre && (P->gated || P->act != DPDR_ACT_NONE);
     Operands o;

@@ -63,11 +63,9 @@ struct Proj {
     int64_t max_rows = 0, n_in = 0, n_out = 0;
     int half = 0, out_f32 = 0, grad_f32 = 0, act = 0;
     int device = 0, num_sms = 0;
-    char* scratch = nullptr;
-    size_t scratch_bytes = 0;
+    char* scratch = nullptr;       // dz (dg, du) and column sums
     // copies of operands that the tensor cores' loads cannot take as they lie
     char* packed[kPacked] = {};
-    size_t packed_bytes[kPacked] = {};
     uint32_t* err = nullptr;       // error word, in host memory that kernels write to
     bool tile_set[2][2][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
 };

@@ -1,0 +1,107 @@
+"""The projections' host code over a CUDA runtime that only keeps books
+(proj_fake.cpp): allocations, devices and errors of plans and calls."""
+import ctypes
+import os
+import random
+import subprocess
+
+import pytest
+
+from paper_2109_12626_gb300 import _native as N
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+BF16, F16, F32 = N.DPDR_BFLOAT16, N.DPDR_FLOAT16, N.DPDR_FLOAT32
+
+
+@pytest.fixture(scope="module")
+def built(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("fake") / "proj_fake.so")
+    csrc = os.path.join(ROOT, "paper_2109_12626_gb300", "csrc")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-Wall", "-fPIC", "-shared", "-I", os.path.join(CUDA, "include"),
+                        "-I", csrc, os.path.join(csrc, "proj.cpp"), os.path.join(ROOT, "tests", "proj_fake.cpp"),
+                        "-o", so, "-Wl,-z,defs", "-lpthread"], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    L = ctypes.CDLL(so)
+    for name, (res, args) in N.SIGNATURES.items():
+        if name.startswith(("dpdr_linear", "dpdr_gated", "dpdr_proj")):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
+    for name in ("fake_frees", "fake_launches", "fake_syncs"):
+        getattr(L, name).restype = ctypes.c_long
+    L.fake_wrong.restype = L.fake_message.restype = ctypes.c_char_p
+    return L
+
+
+@pytest.fixture
+def fake(built):
+    built.fake_reset()
+    return built
+
+
+class Arrays:
+    """Matrices of a caller: addresses that nothing reads, one region each."""
+
+    def __init__(self):
+        self.at, self.held = 1 << 30, []
+
+    def matrix(self, rows, cols, how="plain", esize=2):
+        rs, cs, off = {"plain": (cols, 1, 0), "turned": (1, rows, 0), "slack": ((cols + 15) // 8 * 8, 1, 0),
+                       "odd": (cols + 3, 1, 1), "apart": (2 * cols, 2, 0), "broadcast": (0, 1, 0)}[how]
+        m = (ctypes.c_int64 * 3)(self.at + off * esize, rs, cs)
+        self.at += ((rows * max(rs, 1) + cols * max(cs, 1) + 16) * 8 + 255) // 256 * 256
+        self.held.append(m)
+        return ctypes.addressof(m)
+
+    def vector(self, n):
+        self.at += (8 * n + 255) // 256 * 256
+        return self.at - (8 * n + 255) // 256 * 256
+
+
+LAYOUTS = ["plain", "turned", "slack", "odd", "apart"]
+
+
+def random_call(L, plan, gated, r, rows, k, n, out, grad):
+    """One forward or backward call of random layouts; its status."""
+    a, es, qs = Arrays(), 4 if out == F32 else 2, 4 if grad == F32 else 2
+    how = lambda: r.choice(LAYOUTS)  # noqa: E731
+    x, w = a.matrix(rows, k, how()), [a.matrix(n, k, how()) for _ in range(2)]
+    maybe = lambda v: v if r.random() < 0.5 else None  # noqa: E731
+    if r.random() < 0.4:
+        y = a.matrix(rows, n, "plain", es)
+        if gated:
+            return L.dpdr_gated(plan, rows, x, w[0], w[1], y, maybe(a.matrix(rows, 2 * n, "plain", 4)), None)
+        return L.dpdr_linear(plan, rows, x, w[0], maybe(a.vector(n)), maybe(a.matrix(rows, n, how(), es)), y,
+                             maybe(a.matrix(rows, n, "plain", 4)), None)
+    dy = a.matrix(rows, n, r.choice(LAYOUTS + ["broadcast"]), es)
+    dx = maybe(a.matrix(rows, k, "plain", qs))
+    dw = [a.matrix(n, k, "plain", qs) for _ in range(2)]
+    if gated:
+        dw = dw if r.random() < 0.5 else [None, None]
+        return L.dpdr_gated_backward(plan, rows, x, w[0], w[1], dy, maybe(a.matrix(rows, 2 * n, "plain", 4)), dx,
+                                     dw[0], dw[1], None)
+    return L.dpdr_linear_backward(plan, rows, x, w[0], maybe(a.vector(n)), dy, maybe(a.matrix(rows, n, "plain", 4)),
+                                  dx, maybe(dw[0]), maybe(a.vector(n)), None)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", [0, 4])
+@pytest.mark.parametrize("out,grad", [(BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("most,k,n", [(1, 13, 9), (60, 100, 37), (333, 24, 130), (5000, 70, 8), (9, 700, 1)])
+def test_scratch_never_moves(fake, gated, act, out, grad, most, k, n):
+    """Whatever calls follow each other on a plan, in any order, nothing that
+    an earlier one used is freed before the plan is (a captured call may be
+    replayed), and every place that a kernel gets holds what it writes."""
+    r = random.Random(most * 7 + act)
+    make = fake.dpdr_gated_plan if gated else fake.dpdr_linear_plan
+    for _ in range(20):
+        plan = make(most, k, n, BF16, out, grad, act)
+        assert plan
+        for _ in range(12):
+            rows = r.choice([0, 1, most, r.randint(0, most)])
+            assert random_call(fake, plan, gated, r, rows, k, n, out, grad) == 0, fake.fake_message()
+            assert fake.fake_frees() == 0
+            assert fake.fake_wrong() == b""
+        fake.dpdr_proj_destroy(plan)
+        assert fake.fake_live() == 0
+        fake.fake_reset()
