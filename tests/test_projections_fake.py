@@ -16,11 +16,12 @@ BF16, F16, F32 = N.DPDR_BFLOAT16, N.DPDR_FLOAT16, N.DPDR_FLOAT32
 
 @pytest.fixture(scope="module")
 def built(tmp_path_factory):
+    # -Bsymbolic: its own CUDA runtime, not one that the process already has
     so = str(tmp_path_factory.mktemp("fake") / "proj_fake.so")
     csrc = os.path.join(ROOT, "paper_2109_12626_gb300", "csrc")
     r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-Wall", "-fPIC", "-shared", "-I", os.path.join(CUDA, "include"),
                         "-I", csrc, os.path.join(csrc, "proj.cpp"), os.path.join(ROOT, "tests", "proj_fake.cpp"),
-                        "-o", so, "-Wl,-z,defs", "-lpthread"], capture_output=True, text=True)
+                        "-o", so, "-Wl,-z,defs", "-Wl,-Bsymbolic", "-lpthread"], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     L = ctypes.CDLL(so)
     for name, (res, args) in N.SIGNATURES.items():
