@@ -204,6 +204,11 @@ int check_plan(const Proj* P, bool gated, int64_t rows, const char* who)
     if (!P) return refuse(who, "NULL plan");
     if (P->gated != gated) return refuse(who, "a plan of the other operator");
     if (rows < 0 || rows > P->max_rows) return refuse(who, "need 0 <= rows <= max_rows");
+    // the plan's scratch, its kernels' attributes and the arrays belong to its device
+    int current = -1;
+    const cudaError_t e = cudaGetDevice(&current);
+    if (e != cudaSuccess) return cuda_fail_c(e, who);
+    if (current != P->device) return refuse(who, "the plan's device is not the current one");
     return DPDR_OK;
 }
 

@@ -106,3 +106,25 @@ def test_scratch_never_moves(fake, gated, act, out, grad, most, k, n):
         fake.dpdr_proj_destroy(plan)
         assert fake.fake_live() == 0
         fake.fake_reset()
+
+
+def test_calls_on_another_device_are_refused(fake):
+    """A plan's scratch and arrays lie on its device: with another one
+    current, a call launches nothing."""
+    a = Arrays()
+    x, w, y, d = a.matrix(4, 16), a.matrix(24, 16), a.matrix(4, 24), a.matrix(4, 16)
+    fake.fake_device(1)
+    lin, gat = fake.dpdr_linear_plan(4, 16, 24, BF16, BF16, BF16, 4), fake.dpdr_gated_plan(4, 16, 24, BF16, BF16, BF16, 4)
+    calls = [lambda: fake.dpdr_linear(lin, 4, x, w, None, None, y, None, None),
+             lambda: fake.dpdr_gated(gat, 4, x, w, w, y, None, None),
+             lambda: fake.dpdr_linear_backward(lin, 4, x, w, None, y, None, d, None, None, None),
+             lambda: fake.dpdr_gated_backward(gat, 4, x, w, w, y, None, d, None, None, None)]
+    for device, rc in ((0, N.DPDR_ERR_INVALID), (2, N.DPDR_ERR_INVALID), (1, N.DPDR_OK)):
+        fake.fake_device(device)
+        before = fake.fake_launches()
+        for call in calls:
+            assert call() == rc
+            assert rc == N.DPDR_OK or b"device" in fake.fake_message()
+        assert (fake.fake_launches() > before) == (rc == N.DPDR_OK)
+    fake.dpdr_proj_destroy(lin)
+    fake.dpdr_proj_destroy(gat)
