@@ -27,47 +27,46 @@ int refuse(const char* who, const char* what, const char* more = "")
 bool is_half_kind(int t) { return t == DPDR_BFLOAT16 || t == DPDR_FLOAT16; }
 
 // Error words of all plans: page-locked host memory that kernels write to and
-// the host reads, allocated once for the process (a device allocation and its
-// clearing made a plan 60 us longer to build).
+// the host reads, allocated for many plans at a time and kept for the process
+// (a device allocation and its clearing made a plan 60 us longer to build).
 class ErrorWords {
 public:
     uint32_t* take(const char* who)
     {
         std::lock_guard<std::mutex> hold(m_);
-        if (!words_) {
+        if (!free_) {
             void* p = nullptr;
-            const cudaError_t e = cudaHostAlloc(&p, kWords * kApart * 4, cudaHostAllocPortable | cudaHostAllocMapped);
+            const cudaError_t e = cudaHostAlloc(&p, kSlots * sizeof(Slot), cudaHostAllocPortable | cudaHostAllocMapped);
             if (e != cudaSuccess) {
                 cuda_fail_c(e, who);
                 return nullptr;
             }
-            words_ = static_cast<uint32_t*>(p);
+            Slot* slots = static_cast<Slot*>(p);
+            for (int i = 0; i < kSlots; i++) slots[i].next = i + 1 < kSlots ? slots + i + 1 : nullptr;
+            free_ = slots;
         }
-        if (free_ < 0 && used_ == kWords) {
-            refuse(who, "too many plans at a time");
-            return nullptr;
-        }
-        int i = free_;
-        if (i >= 0) free_ = next_[i];
-        else i = used_++;
-        words_[i * kApart] = 0;
-        return words_ + i * kApart;
+        Slot* s = free_;
+        free_ = s->next;
+        s->word = 0;
+        return &s->word;
     }
     void give(uint32_t* w)
     {
         if (!w) return;
         std::lock_guard<std::mutex> hold(m_);
-        const int i = int((w - words_) / kApart);
-        next_[i] = free_;
-        free_ = i;
+        Slot* s = reinterpret_cast<Slot*>(w);   // its first member
+        s->next = free_;
+        free_ = s;
     }
 
 private:
-    static constexpr int kWords = 8192, kApart = 8;   // 32 bytes apart
+    struct alignas(32) Slot {
+        uint32_t word;
+        Slot* next;   // of a slot that no plan has
+    };
+    static constexpr int kSlots = 1024;
     std::mutex m_;
-    uint32_t* words_ = nullptr;
-    int used_ = 0, free_ = -1;
-    int next_[kWords];
+    Slot* free_ = nullptr;
 };
 ErrorWords g_errors;
 

@@ -7,6 +7,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <set>
 
 #include "proj.h"
 
@@ -180,4 +181,11 @@ int fake_live(void) { return int(B.live.size()); }
 int fake_last_error(void) { return int(B.last); }
 const char* fake_wrong(void) { return B.wrong; }
 const char* fake_message(void) { return dpdr::message; }
+// how many different error words the plans have
+int fake_error_words(void** plans, int n)
+{
+    std::set<uint32_t*> words;
+    for (int i = 0; i < n; i++) words.insert(static_cast<dpdr::proj::Proj*>(plans[i])->err);
+    return int(words.size());
+}
 }

@@ -128,3 +128,18 @@ def test_calls_on_another_device_are_refused(fake):
         assert (fake.fake_launches() > before) == (rc == N.DPDR_OK)
     fake.dpdr_proj_destroy(lin)
     fake.dpdr_proj_destroy(gat)
+
+
+def test_many_plans_at_a_time(fake):
+    """As many plans as there is memory for, each with an error word of its
+    own; those given back are taken again."""
+    plans = [fake.dpdr_linear_plan(1, 8, 8, BF16, BF16, BF16, 0) for _ in range(20000)]
+    assert all(plans), fake.fake_message()
+    for p in plans[::3]:
+        fake.dpdr_proj_destroy(p)
+    plans[::3] = [fake.dpdr_linear_plan(1, 8, 8, BF16, BF16, BF16, 0) for _ in plans[::3]]
+    assert all(plans)
+    words = fake.fake_error_words((ctypes.c_void_p * len(plans))(*plans), len(plans))
+    assert words == len(plans)
+    for p in plans:
+        fake.dpdr_proj_destroy(p)
