@@ -48,6 +48,11 @@ struct Epilogue {
     int64_t pre_rs = 0, pre_up = 0;
 };
 
+// A long sum is taken in runs of nearly equal length: the step behind run number
+// `run` of `runs` over `steps` steps.  The product passes 32 bits for sums of
+// some ten million.
+constexpr int run_end(int steps, int run, int runs) { return int(int64_t(steps) * (run + 1) / runs); }
+
 struct Product {
     Kind kind = kSingle;
     int64_t M = 0, N = 0, K = 0;

@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         for (int i = first; i < t.items && ok; i += pairs) {
             const uint32_t desc = mma_desc(256, i < t.whole ? 256 : 128, t.e.half, t.a_mn, t.b_mn);
             for (int run = 0, k = 0; run < runs && ok; run++) {
-                const int k_last = F32 ? steps * (run + 1) / runs : steps;
+                const int k_last = F32 ? run_end(steps, run, runs) : steps;
                 bool add = false;
                 if (!(ok = bar_wait_warp(taken + 8 * acc, acc_phase ^ 1, waits))) break;
                 tc_fence_after();

@@ -181,6 +181,19 @@ int fake_live(void) { return int(B.live.size()); }
 int fake_last_error(void) { return int(B.last); }
 const char* fake_wrong(void) { return B.wrong; }
 const char* fake_message(void) { return dpdr::message; }
+// Whether the runs of a sum of `steps` steps, at most `most` a run, are all of
+// 1 to `most` steps, one behind the other, and end with the sum
+int fake_runs_fit(int steps, int most)
+{
+    const int runs = int((int64_t(steps) + most - 1) / most);
+    int k = 0;
+    for (int run = 0; run < runs; run++) {
+        const int end = dpdr::proj::run_end(steps, run, runs);
+        if (end <= k || end - k > most) return 0;
+        k = end;
+    }
+    return k == steps;
+}
 // how many different error words the plans have
 int fake_error_words(void** plans, int n)
 {

@@ -143,3 +143,11 @@ def test_many_plans_at_a_time(fake):
     assert words == len(plans)
     for p in plans:
         fake.dpdr_proj_destroy(p)
+
+
+@pytest.mark.parametrize("most", [10, 512])
+def test_runs_of_a_sum(fake, most):
+    """Sums of up to 2^31 elements (2^25 steps of 64; of two chained ones
+    2^26) split into runs: none empty or too long, every step in one."""
+    for steps in [*range(1, 200), 999, 146540, 146541, 160000, (1 << 25) - 1, 1 << 25, 1 << 26]:
+        assert fake.fake_runs_fit(steps, most), steps
