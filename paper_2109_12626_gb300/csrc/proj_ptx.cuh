@@ -97,8 +97,9 @@ struct Waits {
 constexpr uint64_t kWaitNs = 4000000000ull;
 
 // Waits for the phase of that parity; false if it did not come in time or
-// another wait of the CTA has already given up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Waits& w)
+// another wait of the CTA has already given up.  The answer is each lane's own:
+// kernels ask with bar_wait_warp.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Waits& w, uint64_t limit = kWaitNs)
 {
     if (bar_try(bar, parity)) return true;
     const uint64_t t0 = now_ns();
@@ -106,7 +107,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Wa
         if (bar_try(bar, parity)) return true;
         if ((i & 15u) == 0u) {
             if (*w.stop) return false;
-            if (now_ns() - t0 > kWaitNs) break;
+            if (now_ns() - t0 > limit) break;
         }
     }
     *w.stop = 1u;
@@ -115,13 +116,14 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Wa
     return false;
 }
 
-// The same for a whole warp, with one answer for it.  The warps that issue loads
-// and products stay together, and one lane of them issues: what those
+// The same for a whole warp, with one answer for it: what follows a wait, loads
+// from tensor memory and barriers of the CTA, is for all lanes of a warp or for
+// none.  The warps that issue loads and products stay together, and one lane of them issues: what those
 // instructions take then stays in the registers that a warp shares.  A lone
 // thread moved each operand there anew, which took 126 cycles a product.
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, const Waits& w)
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, const Waits& w, uint64_t limit = kWaitNs)
 {
-    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, w));
+    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, w, limit));
 }
 
 // true in one lane of a warp that is together

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     // All products done (and with them every load): the stages' memory now
     // takes the partial tile, column by column.
     float* part = reinterpret_cast<float*>(base);
-    bool ok = bar_wait(ready, 0, waits);
+    bool ok = bar_wait_warp(ready, 0, waits);
     tc_fence_after();
     ok = __syncthreads_and(ok && !stop);   // every role is done with the stages
     if (ok) {

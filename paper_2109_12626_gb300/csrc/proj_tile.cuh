@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 float sum[8][16] = {};
                 bool ok = true;
                 for (int run = 0; run < runs; run++) {
-                    if (!(ok = bar_wait(ready + 8 * acc, acc_phase, waits))) break;
+                    if (!(ok = bar_wait_warp(ready + 8 * acc, acc_phase, waits))) break;
                     tc_fence_after();
                     f.add_run(sum, lanes + acc * 256 + (mine >> 2) * f.kCols, it.sums);
                     f.fetched(lane, in_cta(taken + 8 * acc, 0));
@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 if (!ok) break;
                 f.put_runs(sum, lane, out, out_rs);
             } else {
-                if (!bar_wait(ready + 8 * acc, acc_phase, waits)) break;
+                if (!bar_wait_warp(ready + 8 * acc, acc_phase, waits)) break;
                 tc_fence_after();
                 f.finish(lanes + acc * 256, it.sums, lane, out, out_rs, in_cta(taken + 8 * acc, 0));
                 if (++acc == 2) acc = 0, acc_phase ^= 1;

@@ -88,3 +88,12 @@ def test_the_definition_against_automatic_differentiation():
     U.check_linear_gradients(x.detach(), wg.detach(), b.detach(), dh, "gelu", "float16", "float32", dx, dw, db)
     with pytest.raises(AssertionError):   # a mistake in a gradient is seen
         U.check_linear_gradients(x.detach(), wg.detach(), b.detach(), dh, "gelu", "float16", "float32", dx, dw.flip(0), db)
+
+
+def test_kernels_wait_by_warps():
+    """What follows a wait in the kernels (loads from tensor memory, barriers
+    of the CTA) is for whole warps, so they never take a lane's own answer."""
+    csrc = os.path.join(ROOT, "paper_2109_12626_gb300", "csrc")
+    for name in ("proj_tile.cuh", "proj_rows.cuh"):
+        text = open(os.path.join(csrc, name)).read()
+        assert "bar_wait_warp(" in text and not re.search(r"\bbar_wait\(", text), name
