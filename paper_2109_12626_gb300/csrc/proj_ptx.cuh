@@ -141,11 +141,14 @@ __device__ __forceinline__ bool elected()
 // this thread's warp, as a value that the whole warp shares
 __device__ __forceinline__ int warp_number() { return __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0); }
 
-// for leaving after a failed wait: one more bounded wait, whatever `stop` says
-__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
+// For a CTA that leaves after a failed wait, once all its warps have ended: its
+// loads that no wait stands for any more still write to its shared memory, and
+// products still read it.  Both take microseconds, whichever barriers they
+// count on; a second is ample.
+__device__ __forceinline__ void settle(uint64_t ns = kWaitNs / 4)
 {
     const uint64_t t0 = now_ns();
-    while (!bar_try(bar, parity) && now_ns() - t0 < kWaitNs / 4) {
+    while (now_ns() - t0 < ns) {
     }
 }
 

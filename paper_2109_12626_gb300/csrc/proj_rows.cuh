@@ -107,11 +107,10 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     allow_next();
 
     if (warp == 0) {
-        int stage = 0, used = 0;
+        int stage = 0;
         uint32_t phase = 0;
-        bool ok = true;
         for (int k = k_first; k < k_last; k++) {
-            if (!(ok = bar_wait_warp(empty + 8 * stage, phase ^ 1, waits))) break;
+            if (!bar_wait_warp(empty + 8 * stage, phase ^ 1, waits)) break;
             const int seg = k >= t.steps, k0 = (seg ? k - t.steps : k) * kRowStep;
             const uint32_t dst = smem_addr(base) + stage * stage_bytes, bar = full + 8 * stage;
             if (elected()) {
@@ -138,14 +137,8 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                     tma_load(dst + kWBytes, &t.x[seg], k0, int(m0), bar);
                 }
             }
-            used++;
             if (++stage == t.stages) stage = 0, phase ^= 1;
         }
-        if (!ok)   // loads still under way write to shared memory
-            for (int n = min(used, t.stages); n > 0; n--) {
-                if (--stage < 0) stage = t.stages - 1, phase ^= 1;
-                bar_drain(full + 8 * stage, phase);
-            }
     } else if (warp == 1) {
         const uint32_t desc = mma_desc(kRowFeatures, t.columns, t.e.half, t.w_mn, t.x_mn);
         const uint64_t w_desc = tile_desc(smem_addr(base), t.w_mn ? kWBytes / 2 : 0),
@@ -177,6 +170,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     bool ok = bar_wait_warp(ready, 0, waits);
     tc_fence_after();
     ok = __syncthreads_and(ok && !stop);   // every role is done with the stages
+    if (!ok) settle();
     if (ok) {
         const int quarter = warp & 3;
         for (int c0 = (warp >> 2) * 32; c0 < cols; c0 += 64) {

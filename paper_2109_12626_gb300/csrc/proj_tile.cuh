@@ -372,13 +372,13 @@ template <bool PAIR, int FINISH, int ACT, bool F32>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t)
 {
     extern __shared__ char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 4];
     __shared__ uint32_t tmem_at, stop;
     char* base = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     const int warp = warp_number(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages,
-                   taken = ready + 16, last = taken + 16;
+                   taken = ready + 16;
     const Waits waits{&stop, t.err};
     const int pairs = gridDim.x >> 1, first = blockIdx.x >> 1;
 
@@ -392,7 +392,6 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             bar_init(ready + 8 * i, 1);
             bar_init(taken + 8 * i, 2 * kFinishers);   // of both CTAs
         }
-        bar_init(last, 1);
         bar_init_fence();
     }
     if (warp == 2) tmem_alloc<2>(smem_addr(&tmem_at), 512);
@@ -408,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         // ------------------------------------------------ loads, a warp for each operand
         const bool b = warp == 1, mn = b ? t.b_mn : t.a_mn;
         const uint32_t to = smem_addr(base) + (b ? kHalf : 0), there = in_cta(full, 0);
-        int stage = 0, used = 0;
+        int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int i = first; i < t.items && ok; i += pairs) {
@@ -428,18 +427,10 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                         tma_load_pair(dst, map, mn ? row : at, mn ? at : row, bar);
                         if (two) tma_load_pair(dst + kHalf / 2, map, row + 64, at, bar);
                     }
-                    used++;
                     if (++stage == kStages) stage = 0, phase ^= 1;
                 }
             }
         }
-        // Both CTAs' loads have landed once the products that take them are
-        // issued; after a failed wait they are waited for here.
-        if (!ok && !b && rank == 0)
-            for (int n = min(used, kStages); n > 0; n--) {
-                if (--stage < 0) stage = kStages - 1, phase ^= 1;
-                bar_drain(full + 8 * stage, phase);
-            }
     } else if (warp == 2 && rank == 0) {
         // ------------------------------------------------ products
         const uint64_t a_desc = tile_desc(smem_addr(base), t.a_mn ? kHalf / 2 : 0),
@@ -475,10 +466,6 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 if (++acc == 2) acc = 0, acc_phase ^= 1;
             }
         }
-        if (!ok) {   // the products under way still read shared memory
-            if (elected()) mma_commit_pair(last);
-            bar_drain(last, 0);
-        }
     } else if (warp >= 3) {
         // ------------------------------------------------ results
         const int mine = warp - 3, quarter = warp & 3;   // a warp reaches the 32 lanes of its number's quarter
@@ -512,8 +499,11 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             }
         }
     }
+    // Where all waits of this CTA ended well, the last sums were ready, and so the
+    // products and both CTAs' loads that they are made of are done.
     __syncwarp();
     __syncthreads();
+    if (stop) settle();
     cluster_sync();
     tc_fence_after();
     if (warp == 2) tmem_free<2>(tmem, 512);

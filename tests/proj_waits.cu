@@ -7,7 +7,8 @@ using namespace dpdr::proj;
 
 namespace {
 
-// answers[thread], then in ns: how long warp 0 waited, warp 2 waited
+// answers[thread]; in ns how long warp 0 waited, warp 2 waited and the CTA
+// settled
 __global__ void __launch_bounds__(96) waits_kernel(uint64_t limit, uint32_t* err, int* answers, uint64_t* took)
 {
     __shared__ __align__(8) uint64_t bars[2];
@@ -32,11 +33,14 @@ __global__ void __launch_bounds__(96) waits_kernel(uint64_t limit, uint32_t* err
     answers[threadIdx.x] = ok;
     if (threadIdx.x == 0) took[0] = t;
     if (threadIdx.x == 64) took[1] = t;
+    __syncthreads();
+    if (stop) settle(2 * limit);
+    if (threadIdx.x == 0) took[2] = now_ns() - t0 - t;
 }
 
 }  // namespace
 
-// err, answers (96) and took (2) are in device memory; a CUDA error code
+// err, answers (96) and took (3) are in device memory; a CUDA error code
 extern "C" int run_waits(uint64_t limit, uint32_t* err, int* answers, uint64_t* took)
 {
     waits_kernel<<<1, 96>>>(limit, err, answers, took);

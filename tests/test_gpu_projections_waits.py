@@ -28,13 +28,14 @@ def test_a_wait_runs_out(waits):
     limit = 20_000_000   # ns
     err = torch.zeros(1, dtype=torch.int32, device="cuda")
     answers = torch.full((96,), -1, dtype=torch.int32, device="cuda")
-    took = torch.zeros(2, dtype=torch.int64, device="cuda")
+    took = torch.zeros(3, dtype=torch.int64, device="cuda")
     torch.cuda.synchronize()
     rc = waits.run_waits(ctypes.c_uint64(limit), *(ctypes.c_void_p(t.data_ptr()) for t in (err, answers, took)))
     assert rc == 0
     assert answers.tolist() == [0] * 32 + [1] * 32 + [0] * 32
     assert err.item() == 1
-    first, ended = took.tolist()
+    first, ended, settled = took.tolist()
     assert limit < first < 10 * limit       # it waited, and no longer than that
     assert ended < 10 * limit               # not its own limit
+    assert 2 * limit <= settled < 20 * limit
     assert torch.ones(1, device="cuda").item() == 1   # the context is as it was

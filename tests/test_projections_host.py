@@ -97,3 +97,16 @@ def test_kernels_wait_by_warps():
     for name in ("proj_tile.cuh", "proj_rows.cuh"):
         text = open(os.path.join(csrc, name)).read()
         assert "bar_wait_warp(" in text and not re.search(r"\bbar_wait\(", text), name
+
+
+def test_a_cta_settles_before_it_leaves():
+    """Loads and products may be under way when a wait has run out, asked for
+    by either loading warp of either CTA of a pair: a CTA with a failed wait
+    settles after the last of its warps has ended and before it frees tensor
+    memory or leaves."""
+    csrc = os.path.join(ROOT, "paper_2109_12626_gb300", "csrc")
+    for name, pattern in (("proj_tile.cuh", r"__syncthreads\(\);\s+if \(stop\) settle\(\);\s+cluster_sync\(\);"),
+                          ("proj_rows.cuh", r"ok = __syncthreads_and\(ok && !stop\);[^\n]*\s+if \(!ok\) settle\(\);")):
+        text = open(os.path.join(csrc, name)).read()
+        at = re.search(pattern, text)
+        assert at and text.index("tmem_free<") > at.end(), name
