@@ -26,8 +26,8 @@ SOURCES = ["plan.cpp", "api.cpp", "fused.cu", "fused_stream.cu", "fused_tile.cu"
            "schedule_ll.cu", "cells.cpp", "schedule_words.cu",
            "schedule_walk.cu", "schedule_walk_rb.cu", "fused_tree.cu",
            "proj.cpp", "proj_elem.cu", "proj_tile.cu",
-           "proj_tile_pair.cu", "proj_rows.cu", "proj_rows_pair.cu",
-           "proj_token.cu"]
+           "proj_tile_pair.cu", "proj_tile_runs.cu", "proj_tile_pair_runs.cu",
+           "proj_rows.cu", "proj_rows_pair.cu", "proj_token.cu"]
 
 
 def nvcc() -> str:

@@ -48,10 +48,34 @@ struct Epilogue {
     int64_t pre_rs = 0, pre_up = 0;
 };
 
-// A long sum is taken in runs of nearly equal length: the step behind run number
-// `run` of `runs` over `steps` steps.  The product passes 32 bits for sums of
-// some ten million.
-constexpr int run_end(int steps, int run, int runs) { return int(int64_t(steps) * (run + 1) / runs); }
+// The tensor cores add to a float32 sum by cutting off, not by rounding, so a
+// long sum comes out too small.  Positive products (of 0.5 to 1.5 each) of
+// bfloat16 lose 4.5e-7 of a sum of 640, 2.5e-5 of 8192 and 6.5e-5 of 16,384, of
+// float16, whose products have more places, 3.4e-6 of 640 and 4.5e-5 of 8192;
+// products of random sign a fraction of that.  Longer sums are taken in runs,
+// which are added up rounded: of at most 10 steps (640 products) for float32
+// results, for 16-bit ones as long as the loss is below a tenth of what the
+// result's rounding may be off by.
+constexpr int kSumStep = 64;   // products a step
+constexpr int most_run_steps(int out_f32, int half) { return out_f32 ? 10 : half ? 128 : 256; }
+
+// The runs of a sum, of nearly equal length: next() gives the step behind each,
+// steps * (run + 1) / runs, without the product, which can pass 32 bits, or a
+// division.
+struct RunEnds {
+    int whole, rest, runs, end, carry;
+    constexpr RunEnds(int steps, int n, int from = 0)
+        : whole(steps / n), rest(steps % n), runs(n), end(from), carry(0)
+    {
+    }
+    constexpr int next()
+    {
+        end += whole;
+        carry += rest;
+        if (carry >= runs) carry -= runs, end++;
+        return end;
+    }
+};
 
 struct Product {
     Kind kind = kSingle;

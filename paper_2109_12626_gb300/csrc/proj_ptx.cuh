@@ -59,6 +59,12 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
+// an arrival at a barrier of this CTA
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // An arrival at a barrier of any CTA of the cluster (address from in_cta).  It
 // orders no memory: it tells that tensor memory has been read, which the
 // fences of tcgen05 order, and as a release it waited for the results' stores
@@ -313,6 +319,18 @@ __device__ __forceinline__ void tmem_load_wait(float (&v)[16], float (&w)[16])
         :
         : "memory");
 }
+
+// v[i] to (lane, column + i), and all such stores done
+__device__ __forceinline__ void tmem_store16(const float (&v)[16], uint32_t at)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"f"(v[0]),
+        "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+        "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 }  // namespace proj
 }  // namespace dpdr

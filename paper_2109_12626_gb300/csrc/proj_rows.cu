@@ -67,14 +67,23 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     }
     t.split = split;
     const int stage = kRowFeatures * kRowStep * 2 + t.x_bytes, mine = (steps + split - 1) / split;
-    // For float32 results, runs of 512 products, as many as two CTAs an SM have
-    // tensor memory for (256 columns each), a power of two and no more than the
-    // shortest part's steps.  16-bit results do without: 64 rows of 4096 x 4096 in
-    // 9.8 against 12.0 us.
+    // Runs with columns of their own, for float32 results of 512 products where two
+    // CTAs an SM have tensor memory for them (256 columns each): a power of two, no
+    // more than the shortest part's steps.  Where those would be longer than a run
+    // may be, as many runs as it takes, in turn.  Most 16-bit results do without
+    // either: 64 rows of 4096 x 4096 in 9.8 against 12.0 us.
     t.apart = 32;
     while (t.apart < t.columns) t.apart *= 2;
     t.runs = 1;
     while (p.e.out_f32 && 2 * t.runs * t.apart <= 256 && t.runs * 8 < mine && 2 * t.runs <= steps / split) t.runs *= 2;
+    t.held = t.runs * t.apart;
+    t.turns = 0;
+    const int most = most_run_steps(p.e.out_f32, p.e.half);
+    if ((mine + t.runs - 1) / t.runs > most) {
+        t.runs = (mine + most - 1) / most;
+        t.turns = 3 * t.apart <= 256 ? 2 : 1;
+        t.held = t.turns == 2 ? 4 * t.apart : 256;
+    }
     t.stages = std::max(2, std::min({mine, kRoom / stage, kRowMaxStages}));
     const int smem = 1024 + std::max(t.stages * stage, kRowFeatures * t.columns * 4);
     int rc = tensor_map(&t.w[0], p.b[0], p.N, p.K, p.e.half, pair ? 64 : 128, kRowStep);

@@ -8,9 +8,12 @@
 // cluster, which each load their part through a ring of TMA stages (all of it
 // in flight at once where it fits), leave their partial tile in shared memory
 // and then add up the S partials of their share of the columns in the order
-// of the CTAs: one launch, no atomics, the same bits every time.  A long part is
-// summed in several runs, each in columns of tensor memory of its own, which
-// are then added up in float32: the tensor cores cut sums off (proj_tile.cuh).
+// of the CTAs: one launch, no atomics, the same bits every time.  A part longer
+// than a run (proj.h) is summed in several, each in columns of tensor memory of
+// its own, which are added up rounded at the end; or, where there are more runs
+// than columns for them, in one or two sets of columns in turn, which four
+// otherwise idle warps add to a total, in tensor memory too, while the next
+// run's products are at work.
 //
 // Bound by the weights' bytes while there are some megabytes an SM, else by the
 // chain of setting up, one trip to memory, the cluster's barriers and partials
@@ -28,7 +31,7 @@
 namespace dpdr {
 namespace proj {
 
-constexpr int kRowStep = 64;               // summed elements a stage
+constexpr int kRowStep = kSumStep;         // summed elements a stage
 constexpr int kRowFeatures = 128;
 constexpr int kRowMaxStages = 12;
 constexpr int kRowThreads = 256;
@@ -42,7 +45,10 @@ struct RowArgs {
     int columns;              // rows of x a tile: a multiple of 16 up to 128
     int x_bytes;              // bytes of x a stage
     int stages;
-    int runs, apart;          // accumulators, and columns of tensor memory between them
+    int runs;                 // of a CTA's part of the sum, each with its own columns,
+    int turns;                // or, if not 0, in this many sets of columns in turn
+    int apart;                // columns of tensor memory from one set to the next
+    int held;                 // and in all, a power of two
     int width;                // features a tile: 128, of a pair 64
     int vec;                  // results and what else is read allow 4 elements at a time
     int64_t M, N;             // rows of x, features
@@ -70,16 +76,45 @@ __device__ __forceinline__ void join(uint32_t at, int split, float (&z)[4])
     }
 }
 
+// Warps 4 to 7, the runs in turn: each added to the total, in tensor memory, 16
+// columns of a thread's row at a time.  Not inline: most calls have no use for it.
+__device__ __noinline__ void add_runs(uint32_t tmem, uint32_t done, uint32_t taken, int runs, int turns, int columns,
+                                      int apart, const Waits waits)
+{
+    const int warp = warp_number();
+    const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);
+    uint32_t turn = 0, use = 0;
+    for (int run = 0; run < runs; run++) {
+        if (!bar_wait_warp(done + 8 * turn, use, waits)) break;
+        tc_fence_after();
+        for (int c = 0; c < columns; c += 16) {
+            float v[16], w[16] = {};
+            tmem_load16(v, lanes + (1 + turn) * apart + c);
+            if (run > 0) tmem_load16(w, lanes + c);
+            tmem_load_wait(v, w);
+#pragma unroll
+            for (int i = 0; i < 16; i++) v[i] += w[i];
+            tmem_store16(v, lanes + c);
+        }
+        tmem_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(taken + 8 * turn);
+        if (++turn == uint32_t(turns)) turn = 0, use ^= 1;
+    }
+}
+
 template <bool PAIR, int FINISH, int ACT, int SPLIT>
 __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant__ RowArgs t)
 {
     extern __shared__ char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kRowMaxStages + 1];
+    __shared__ __align__(8) uint64_t bars[2 * kRowMaxStages + 5];
     __shared__ uint32_t tmem_at, stop;
     char* base = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     const int warp = warp_number(), lane = threadIdx.x & 31;
     const int rank = t.split > 1 ? int(cluster_rank()) : 0;
-    const uint32_t full = smem_addr(bars), empty = full + 8 * kRowMaxStages, ready = empty + 8 * kRowMaxStages;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kRowMaxStages, ready = empty + 8 * kRowMaxStages,
+                   done = ready + 8, taken = done + 16;
     const Waits waits{&stop, t.err};
     const int64_t n0 = int64_t(blockIdx.x / t.split) * t.width, m0 = int64_t(blockIdx.y) * t.columns;
     const int cols = int(min(int64_t(t.columns), t.M - m0));
@@ -96,9 +131,13 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
             bar_init(empty + 8 * i, 1);
         }
         bar_init(ready, 1);
+        for (int i = 0; i < t.turns; i++) {
+            bar_init(done + 8 * i, 1);
+            bar_init(taken + 8 * i, 4);
+        }
         bar_init_fence();
     }
-    if (warp == 2) tmem_alloc<1>(smem_addr(&tmem_at), t.runs * t.apart);
+    if (warp == 2) tmem_alloc<1>(smem_addr(&tmem_at), t.held);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -144,40 +183,57 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
         const uint64_t w_desc = tile_desc(smem_addr(base), t.w_mn ? kWBytes / 2 : 0),
                        x_desc = tile_desc(smem_addr(base) + kWBytes, t.x_mn ? 64 * kRowStep * 2 : 0);
         const uint32_t w_step = (t.w_mn ? 2048 : 32) >> 4, x_step = (t.x_mn ? 2048 : 32) >> 4;   // 16 summed elements
+        RunEnds ends(k_last - k_first, t.runs, k_first);
         int stage = 0, run = -1, next = k_first;   // `next`: the step that begins another run
-        uint32_t phase = 0;
+        uint32_t phase = 0, sums = tmem, turn = 0, use = 0;
         for (int k = k_first; k < k_last; k++) {
+            const bool begins = k == next;
+            if (begins) {
+                next = ends.next();
+                run++;
+                sums = tmem + run * t.apart;
+                if (t.turns) {   // behind the total
+                    if (run > 0 && ++turn == uint32_t(t.turns)) turn = 0, use ^= 1;
+                    sums = tmem + (1 + turn) * t.apart;
+                    if (!bar_wait_warp(taken + 8 * turn, use ^ 1, waits)) break;
+                }
+            }
             if (!bar_wait_warp(full + 8 * stage, phase, waits)) break;
             tc_fence_after();
-            const bool begins = k == next;
-            if (begins) next = k_first + (k_last - k_first) * (++run + 1) / t.runs;
             const uint32_t on = uint32_t(stage * (stage_bytes >> 4));
             const uint64_t w = w_desc + on, x = x_desc + on;
             if (elected()) {
 #pragma unroll
                 for (int j = 0; j < kRowStep / 16; j++)
-                    mma_f16<1>(tmem + run * t.apart, w + j * w_step, x + j * x_step, desc, !begins || j > 0);
+                    mma_f16<1>(sums, w + j * w_step, x + j * x_step, desc, !begins || j > 0);
                 mma_commit(empty + 8 * stage);
+                if (t.turns && k + 1 == next) mma_commit(done + 8 * turn);
             }
             if (++stage == t.stages) stage = 0, phase ^= 1;
         }
         if (elected()) mma_commit(ready);
+    } else if (warp >= 4 && t.turns) {
+        add_runs(tmem, done, taken, t.runs, t.turns, t.columns, t.apart, waits);
     }
     __syncwarp();
     // All products done (and with them every load): the stages' memory now
-    // takes the partial tile, column by column.
+    // takes the partial tile, column by column.  Of runs in turn the warps that
+    // add them know it, and the others wait for those at the barrier: a wait of
+    // theirs would stand for a sum of any length.
     float* part = reinterpret_cast<float*>(base);
-    bool ok = bar_wait_warp(ready, 0, waits);
-    tc_fence_after();
+    bool ok = true;
+    if (!t.turns || warp >= 4) ok = bar_wait_warp(ready, 0, waits);
+    tc_fence_before();
     ok = __syncthreads_and(ok && !stop);   // every role is done with the stages
     if (!ok) settle();
+    tc_fence_after();
     if (ok) {
         const int quarter = warp & 3;
         for (int c0 = (warp >> 2) * 32; c0 < cols; c0 += 64) {
             float v[32], w[32];
             tmem_load32(v, tmem + c0 + (uint32_t(quarter) << 21));
             tmem_load_wait(v);
-            for (int r = 1; r < t.runs; r++) {
+            for (int r = 1; r < t.runs && !t.turns; r++) {
                 tmem_load32(w, tmem + r * t.apart + c0 + (uint32_t(quarter) << 21));
                 tmem_load_wait(w);
 #pragma unroll
@@ -192,7 +248,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     __syncthreads();
     tc_fence_after();
     if (t.split > 1) cluster_arrive();
-    if (warp == 2) tmem_free<1>(tmem, t.runs * t.apart);
+    if (warp == 2) tmem_free<1>(tmem, t.held);
     if (t.split > 1) cluster_wait();
     if (ok) {
         // ------------------------------------------------ results

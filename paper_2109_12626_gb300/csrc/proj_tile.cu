@@ -1,25 +1,16 @@
 // proj_tile.cu -- which kernel of proj_tile.cuh a product takes, its tensor
-// maps and launch; the kernels of one product a tile (proj_tile_pair.cu holds
-// the gated operator's, compiled beside them).
+// maps and launch; the kernels of one product a tile and one run a sum
+// (proj_tile_pair.cu holds the gated operator's, proj_tile_runs.cu and
+// proj_tile_pair_runs.cu those of several runs, compiled beside them).
 #include "proj_tile.cuh"
 
 namespace dpdr {
 namespace proj {
 
-TileKernel tile_kernel_single(int finish, int act, int f32)
-{
-    TileKernel k = nullptr;
-    // without an activation dz is dy, and no product is finished as one
-#define DPDR_CALL(A)                                                                                  \
-    k = f32 ? tile_kernel<false, kValue, A, true>                                                     \
-        : A != DPDR_ACT_NONE && finish == kSlope ? tile_kernel<false, A ? kSlope : kValue, A, false>   \
-                                                 : tile_kernel<false, kValue, A, false>
-    DPDR_FOR_ACT(act, DPDR_CALL)
-#undef DPDR_CALL
-    return k;
-}
-
-TileKernel tile_kernel_pair(int finish, int act, int f32);   // proj_tile_pair.cu
+TileKernel tile_kernel_single(int finish, int act) { return tile_kernel_of<false, false>(finish, act); }
+TileKernel tile_kernel_single_runs(int finish, int act);   // proj_tile_runs.cu
+TileKernel tile_kernel_pair(int finish, int act);          // proj_tile_pair.cu
+TileKernel tile_kernel_pair_runs(int finish, int act);     // proj_tile_pair_runs.cu
 
 int tile_launch(Proj* P, const Product& p, cudaStream_t s)
 {
@@ -28,6 +19,9 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     t.b_mn = p.b[0].ks != 1;
     t.segments = p.kind == kChain ? 2 : 1;
     t.steps = int((p.K + kStep - 1) / kStep);
+    const int most = most_run_steps(p.e.out_f32, p.e.half);
+    t.runs = (t.steps * t.segments + most - 1) / most;
+    const bool runs = p.e.out_f32 || t.runs > 1;
     const int width = p.kind == kPair ? 128 : 256;
     t.tiles_m = int((p.M + 255) / 256);
     t.tiles_n = int((p.N + width - 1) / width);
@@ -55,10 +49,11 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
         if (!rc && two_b) rc = tensor_map(&t.b_half[1], p.b[1], p.N, p.K, p.e.half, 64, kStep);
     }
     if (rc) return rc;
-    const TileKernel kernel = p.kind == kPair ? tile_kernel_pair(p.e.finish, p.e.act, p.e.out_f32)
-                                              : tile_kernel_single(p.e.finish, p.e.act, p.e.out_f32);
+    const TileKernel kernel =
+        p.kind == kPair ? (runs ? tile_kernel_pair_runs : tile_kernel_pair)(p.e.finish, p.e.act)
+                        : (runs ? tile_kernel_single_runs : tile_kernel_single)(p.e.finish, p.e.act);
     // a plan's activation is fixed, but its gradients' products have none
-    bool& set = P->tile_set[p.kind == kPair][p.e.finish][p.e.act != DPDR_ACT_NONE][p.e.out_f32];
+    bool& set = P->tile_set[p.kind == kPair][p.e.finish][p.e.act != DPDR_ACT_NONE][runs];
     if (!set) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return cuda_fail_c(e, "projection tile kernel");

@@ -23,12 +23,10 @@
 // own: 411 against 299 us; one pair for all: no faster), the last round's tiles summed by several pairs that join
 // their sums (no faster, and 43 against 33 us for short sums).
 //
-// The tensor cores add to a sum by cutting off, not by rounding: a sum of K
-// products comes out smaller by about 1e-9 K of its size (measured: 1.25e-6 at K
-// = 1024, 9.7e-6 at 8192).  No 16-bit result shows that.  For float32 results
-// (F32) a sum is taken in runs of at most 640 products, and the finishing warps
-// add up the runs in registers, rounded, while the next run's products are at
-// work: 7.9e-7 at K = 8192, 4096 x 4096 x 4096 in 82 us instead of 72.
+// Sums longer than a run (proj.h) are taken in runs (RUNS), and the finishing
+// warps add up the runs in registers, rounded, while the next run's products are
+// at work: float32 results of 4096 x 4096 x 4096 in 82 us instead of 72.  No wait then stands for more than a run, so that
+// none runs out over a sum of any length.
 #pragma once
 
 #include "proj_common.cuh"
@@ -41,10 +39,9 @@ namespace proj {
 namespace {
 
 constexpr int kStages = 6;
-constexpr int kStep = 64;                     // summed elements a stage
+constexpr int kStep = kSumStep;               // summed elements a stage
 constexpr int kHalf = 128 * kStep * 2;        // bytes of one operand of a stage and CTA
 constexpr int kStage = 2 * kHalf;
-constexpr int kRun = 10;                      // stages of a run, at most
 constexpr int kFinishers = 8;                 // warps
 constexpr int kStaging = kFinishers * 32 * 32 * 4;   // 32 x 32 floats each
 constexpr int kSmem = 1024 + kStages * kStage + kStaging;
@@ -54,6 +51,7 @@ struct TileArgs {
     CUtensorMap a[2], b[2], b_half[2];   // B's rows by 128 and by 64
     int a_mn, b_mn;                // the other index is the contiguous one
     int steps, segments;           // stages a segment
+    int runs;                      // of a sum
     int tiles_m, tiles_n, tiles;   // tiles_m of one of kTwin's products
     // the first `whole` tiles are taken as they are, the rest in two halves of
     // their columns: `items` in all
@@ -102,7 +100,7 @@ __device__ __forceinline__ Item item_of(const TileArgs& t, int i)
 // all of a round's together when the round comes: one row at a time, each a trip
 // to memory, took 45 us a tile; registers filled a round ahead, between a round's
 // stores, half as long again as this.
-template <bool PAIR, int FINISH, int ACT, bool F32>
+template <bool PAIR, int FINISH, int ACT, bool RUNS>
 struct Finisher {
     static constexpr int kCols = PAIR ? 16 : 32;     // result columns a round
     static constexpr int kPer = kCols / 4;           // threads a row
@@ -208,9 +206,9 @@ struct Finisher {
         }
     }
 
-    // The same for float32 results, in as few registers as it can be: the other
-    // rounds' sums hold most of them.
-    __device__ __forceinline__ void by_four_f32(int c0, char* out, int64_t out_rs)
+    // The same for sums in runs, whatever the results' type, in as few registers as
+    // it can be: the other rounds' sums hold most of them.
+    __device__ __forceinline__ void by_four_runs(int c0, char* out, int64_t out_rs)
     {
         const Epilogue& e = t.e;
         const int64_t n = n0 + c0 + 4 * q;
@@ -228,7 +226,7 @@ struct Finisher {
             }
             put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o);
         };
-        if (!PAIR && e.other) {
+        if ((!PAIR || FINISH == kSlope) && e.other) {
             for (int b0 = 0; b0 < kSteps; b0 += 4) {
                 float o[4][4];
 #pragma unroll
@@ -236,7 +234,7 @@ struct Finisher {
                     const int r = row + (b0 + b) * kRows;
 #pragma unroll
                     for (int i = 0; i < 4; i++) o[b][i] = 0.0f;
-                    if (r < rows) load4(e.other, (m0 + r) * e.other_rs + n, 1, 0, o[b]);
+                    if (r < rows) load4(e.other, (m0 + r) * e.other_rs + n, e.other_f32, e.half, o[b]);
                 }
 #pragma unroll
                 for (int b = 0; b < 4; b++) step(b0 + b, o[b]);
@@ -250,17 +248,19 @@ struct Finisher {
 
     // One element a thread and step, for results that do not lie on fours; the sums
     // and other values of eight steps (of a pair 16) before the first is stored.
-    template <int HALF>
-    __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs)
+    __device__ __forceinline__ void by_one(int c0, int lane, char* out, int64_t out_rs, int half)
     {
         const Epilogue& e = t.e;
-        constexpr int kSize = F32 ? 4 : 2, kStep = 32 / kCols, kAsk = PAIR ? 16 : 8;   // kStep: rows a step
+        constexpr int kDown = 32 / kCols;   // rows a step
+        // one for dz of several runs, which only rows of many thousand elements take
+        constexpr int kAsk = RUNS && FINISH == kSlope ? 1 : PAIR ? 16 : 8;
+        const int f32 = RUNS && e.out_f32, size = f32 ? 4 : 2;
         const int c = lane % kCols, first = lane / kCols;
         if (c0 + c >= cols) return;
         const int64_t n = n0 + c0 + c, m = m0 + first;
-        const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, HALF) : 0.0f;
-        char* at = out + (m * out_rs + n) * kSize;
-        const int64_t down = out_rs * kStep * kSize;
+        const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, half) : 0.0f;
+        char* at = out + (m * out_rs + n) * size;
+        const int64_t down = out_rs * kDown * size;
         auto step = [&](int r, char* p, float z, float u, float o) {
             if (e.pre) {
                 float* pre = e.pre + ((m0 + r) * e.pre_rs + n);
@@ -269,30 +269,30 @@ struct Finisher {
             }
             float v = 0.0f, w = 0.0f;
             finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
-            store1(p, 0, v, F32, HALF);
-            if (PAIR && FINISH == kSlope) store1(e.out2, (m0 + r) * e.out2_rs + n, w, F32, HALF);
+            store1(p, 0, v, f32, half);
+            if (PAIR && FINISH == kSlope) store1(e.out2, (m0 + r) * e.out2_rs + n, w, f32, half);
         };
         auto sum = [&](int r, int side) {
             return stage[r * 32 + 4 * ((4 * side + (c >> 2)) ^ (r & 7)) + (c & 3)];
         };
         if (!e.other) {
 #pragma unroll 4
-            for (int r = first; r < rows; r += kStep, at += down)
+            for (int r = first; r < rows; r += kDown, at += down)
                 step(r, at, sum(r, 0) + bias, PAIR ? sum(r, 1) : 0.0f, 0.0f);
             return;
         }
-        for (int r0 = first; r0 < rows; r0 += kStep * kAsk, at += kAsk * down) {
+        for (int r0 = first; r0 < rows; r0 += kDown * kAsk, at += kAsk * down) {
             float z[kAsk], u[kAsk], o[kAsk];
 #pragma unroll
             for (int b = 0; b < kAsk; b++) {
-                const int r = r0 + b * kStep;
+                const int r = r0 + b * kDown;
                 o[b] = r < rows ? other1(e, m0 + r, n) : 0.0f;
                 z[b] = sum(r & 31, 0) + bias;
                 u[b] = PAIR ? sum(r & 31, 1) : 0.0f;
             }
 #pragma unroll
             for (int b = 0; b < kAsk; b++)
-                if (r0 + b * kStep < rows) step(r0 + b * kStep, at + b * down, z[b], u[b], o[b]);
+                if (r0 + b * kDown < rows) step(r0 + b * kDown, at + b * down, z[b], u[b], o[b]);
         }
     }
 
@@ -309,10 +309,11 @@ struct Finisher {
         }
         __syncwarp();
         if (!fours(c0)) {
-            if (t.e.half) by_one<1>(c0, lane, out, out_rs);
-            else by_one<0>(c0, lane, out, out_rs);
-        } else if (F32) {
-            by_four_f32(c0, out, out_rs);
+            if (RUNS) by_one(c0, lane, out, out_rs, t.e.half);
+            else if (t.e.half) by_one(c0, lane, out, out_rs, 1);
+            else by_one(c0, lane, out, out_rs, 0);
+        } else if (RUNS) {
+            by_four_runs(c0, out, out_rs);
         } else if (t.e.half) {
             by_four<1>(c0, out, out_rs);
         } else {
@@ -344,7 +345,7 @@ struct Finisher {
         }
     }
 
-    // F32: adds a run to this warp's sums so far, 16 columns each: half a round (of
+    // RUNS: adds a run to this warp's sums so far, 16 columns each: half a round (of
     // a pair, one weight's), whether the result has them or not
     static __device__ __forceinline__ void add_run(float (&sum)[8][16], uint32_t tmem, int sums)
     {
@@ -368,7 +369,7 @@ struct Finisher {
     }
 };
 
-template <bool PAIR, int FINISH, int ACT, bool F32>
+template <bool PAIR, int FINISH, int ACT, bool RUNS>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t)
 {
     extern __shared__ char raw[];
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    const int steps = t.steps * t.segments, runs = F32 ? (steps + kRun - 1) / kRun : 1;
+    const int steps = t.steps * t.segments, runs = RUNS ? t.runs : 1;
     wait_previous();
 
     if (warp < 2) {
@@ -441,8 +442,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         bool ok = true;
         for (int i = first; i < t.items && ok; i += pairs) {
             const uint32_t desc = mma_desc(256, i < t.whole ? 256 : 128, t.e.half, t.a_mn, t.b_mn);
+            RunEnds ends(steps, runs);
             for (int run = 0, k = 0; run < runs && ok; run++) {
-                const int k_last = F32 ? run_end(steps, run, runs) : steps;
+                const int k_last = RUNS ? ends.next() : steps;
                 bool add = false;
                 if (!(ok = bar_wait_warp(taken + 8 * acc, acc_phase ^ 1, waits))) break;
                 tc_fence_after();
@@ -469,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     } else if (warp >= 3) {
         // ------------------------------------------------ results
         const int mine = warp - 3, quarter = warp & 3;   // a warp reaches the 32 lanes of its number's quarter
-        Finisher<PAIR, FINISH, ACT, F32> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane,
+        Finisher<PAIR, FINISH, ACT, RUNS> f(t, reinterpret_cast<float*>(base + kStages * kStage) + mine * 32 * 32, lane,
                                            mine >> 2);
         int acc = 0;
         uint32_t acc_phase = 0;
@@ -479,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             char* out = it.twin ? t.e.out2 : t.e.out;
             const int64_t out_rs = it.twin ? t.e.out2_rs : t.e.out_rs;
             const uint32_t lanes = tmem + (uint32_t(quarter) << 21);
-            if (F32) {
+            if (RUNS) {
                 float sum[8][16] = {};
                 bool ok = true;
                 for (int run = 0; run < runs; run++) {
@@ -512,6 +514,22 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
 }  // namespace
 
 using TileKernel = void (*)(TileArgs);
+
+template <bool PAIR, bool RUNS>
+TileKernel tile_kernel_of(int finish, int act)
+{
+    TileKernel k = nullptr;
+    // without an activation a single dz is dy, and no product is finished as one
+#define DPDR_CALL(A)                                                                        \
+    if ((PAIR || A != DPDR_ACT_NONE) && finish == kSlope) {                                  \
+        k = tile_kernel<PAIR, (PAIR || A != DPDR_ACT_NONE ? kSlope : kValue), A, RUNS>;      \
+    } else {                                                                                \
+        k = tile_kernel<PAIR, kValue, A, RUNS>;                                              \
+    }
+    DPDR_FOR_ACT(act, DPDR_CALL)
+#undef DPDR_CALL
+    return k;
+}
 
 }  // namespace proj
 }  // namespace dpdr

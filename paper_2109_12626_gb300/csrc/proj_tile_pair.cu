@@ -4,16 +4,7 @@
 namespace dpdr {
 namespace proj {
 
-TileKernel tile_kernel_pair(int finish, int act, int f32)
-{
-    TileKernel k = nullptr;
-#define DPDR_CALL(A)                                                              \
-    k = f32 ? tile_kernel<true, kValue, A, true>                                 \
-            : finish == kSlope ? tile_kernel<true, kSlope, A, false> : tile_kernel<true, kValue, A, false>
-    DPDR_FOR_ACT(act, DPDR_CALL)
-#undef DPDR_CALL
-    return k;
-}
+TileKernel tile_kernel_pair(int finish, int act) { return tile_kernel_of<true, false>(finish, act); }
 
 }  // namespace proj
 }  // namespace dpdr

@@ -15,7 +15,7 @@ namespace {
 
 struct Books {
     int device = 0;
-    long frees = 0, host_allocs = 0, syncs = 0, launches = 0;
+    long frees = 0, host_allocs = 0, syncs = 0, launches = 0, tiles = 0, rows = 0;
     int refuse_mallocs = 0;            // as many allocations fail
     cudaError_t last = cudaSuccess;    // what cudaGetLastError gives
     std::map<uintptr_t, size_t> live;  // device allocations
@@ -139,8 +139,16 @@ int cuda_fail_c(cudaError_t e, const char* what)
     return fail_c(e == cudaErrorMemoryAllocation ? DPDR_ERR_OOM : DPDR_ERR_CUDA, what);
 }
 namespace proj {
-int tile_launch(Proj*, const Product& p, cudaStream_t) { return product(p); }
-int row_launch(Proj*, const Product& p, cudaStream_t) { return product(p); }
+int tile_launch(Proj*, const Product& p, cudaStream_t)
+{
+    B.tiles++;
+    return product(p);
+}
+int row_launch(Proj*, const Product& p, cudaStream_t)
+{
+    B.rows++;
+    return product(p);
+}
 int token_launch(Proj*, const Product& p, cudaStream_t) { return product(p); }
 int column_sum_parts(int64_t rows)
 {
@@ -177,6 +185,8 @@ void fake_refuse_mallocs(int n) { B.refuse_mallocs = n; }
 long fake_frees(void) { return B.frees; }
 long fake_launches(void) { return B.launches; }
 long fake_syncs(void) { return B.syncs; }
+long fake_tiles(void) { return B.tiles; }   // products of tile_launch, row_launch
+long fake_rows(void) { return B.rows; }
 int fake_live(void) { return int(B.live.size()); }
 int fake_last_error(void) { return int(B.last); }
 const char* fake_wrong(void) { return B.wrong; }
@@ -187,9 +197,10 @@ int fake_runs_fit(int steps, int most)
 {
     const int runs = int((int64_t(steps) + most - 1) / most);
     int k = 0;
+    dpdr::proj::RunEnds ends(steps, runs);
     for (int run = 0; run < runs; run++) {
-        const int end = dpdr::proj::run_end(steps, run, runs);
-        if (end <= k || end - k > most) return 0;
+        const int end = ends.next();
+        if (end != int(int64_t(steps) * (run + 1) / runs) || end <= k || end - k > most) return 0;
         k = end;
     }
     return k == steps;

@@ -28,7 +28,7 @@ def built(tmp_path_factory):
         if name.startswith(("dpdr_linear", "dpdr_gated", "dpdr_proj")):
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
-    for name in ("fake_frees", "fake_launches", "fake_syncs"):
+    for name in ("fake_frees", "fake_launches", "fake_syncs", "fake_tiles", "fake_rows"):
         getattr(L, name).restype = ctypes.c_long
     L.fake_wrong.restype = L.fake_message.restype = ctypes.c_char_p
     return L
@@ -145,7 +145,7 @@ def test_many_plans_at_a_time(fake):
         fake.dpdr_proj_destroy(p)
 
 
-@pytest.mark.parametrize("most", [10, 512])
+@pytest.mark.parametrize("most", [10, 128, 256, 512])
 def test_runs_of_a_sum(fake, most):
     """Sums of up to 2^31 elements (2^25 steps of 64; of two chained ones
     2^26) split into runs: none empty or too long, every step in one."""
