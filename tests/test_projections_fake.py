@@ -8,6 +8,7 @@ import subprocess
 import pytest
 
 from paper_2109_12626_gb300 import _native as N
+from proj_tiles import tile_size
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
@@ -151,3 +152,26 @@ def test_runs_of_a_sum(fake, most):
     2^26) split into runs: none empty or too long, every step in one."""
     for steps in [*range(1, 200), 999, 146540, 146541, 160000, (1 << 25) - 1, 1 << 25, 1 << 26]:
         assert fake.fake_runs_fit(steps, most), steps
+
+
+def test_which_kernel_the_tile_tests_reach(fake):
+    """The sizes of test_gpu_projections_tiles.py (on this many SMs, which the
+    fake reports) go to the kernel of tiles: forward, dx and dw."""
+    a = Arrays()
+    rows, n = tile_size(152)
+    for odd in (0, 1, 2, 3):
+        for k in (64, 264, 2500, n):
+            x, w = a.matrix(rows, k), [a.matrix(n + odd, k) for _ in range(2)]
+            y, dx, dw = a.matrix(rows, n + odd), a.matrix(rows, k), [a.matrix(n + odd, k) for _ in range(2)]
+            lin, gat = fake.dpdr_linear_plan(rows, k, n + odd, BF16, BF16, BF16, 4), \
+                fake.dpdr_gated_plan(rows, k, n + odd, BF16, BF16, BF16, 4)
+            assert fake.dpdr_linear(lin, rows, x, w[0], None, None, y, None, None) == 0
+            assert fake.dpdr_gated(gat, rows, x, w[0], w[1], y, None, None) == 0
+            assert (fake.fake_tiles(), fake.fake_rows()) == (2, 0)
+            if k == n:
+                assert fake.dpdr_linear_backward(lin, rows, x, w[0], None, y, None, dx, dw[0], None, None) == 0
+                assert fake.dpdr_gated_backward(gat, rows, x, w[0], w[1], y, None, dx, dw[0], dw[1], None) == 0
+                assert (fake.fake_tiles(), fake.fake_rows()) == (8, 0)
+            fake.dpdr_proj_destroy(lin)
+            fake.dpdr_proj_destroy(gat)
+            fake.fake_reset()
