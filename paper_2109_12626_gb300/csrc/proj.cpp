@@ -261,6 +261,8 @@ EncodeTiled encode_tiled()
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 // TMA's strides are below 2^40 bytes
 constexpr int64_t kFarthest = int64_t(1) << 39;
+// rows of column sums that join_launch takes: as many as column_sum_parts gives
+constexpr int64_t kJoined = 512;
 size_t upto256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
@@ -363,9 +365,11 @@ static bool for_token(int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w0,
 
 // The forward product, or with slope the same product finished as dz (dg, du).
 static int forward(Proj* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w0, const dpdr_matrix& w1,
-                   const void* bias, const Epilogue& e, cudaStream_t s, bool token = false)
+                   const void* bias, const Epilogue& e, cudaStream_t s, bool token = false,
+                   int64_t* sum_parts = nullptr)
 {
     Product p;
+    p.sum_parts = sum_parts;
     p.kind = P->gated ? kPair : kSingle;
     p.M = rows;
     p.N = P->n_out;
@@ -438,11 +442,16 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     const bool as_is = !P->gated && P->act == DPDR_ACT_NONE && !P->out_f32;
     const int64_t ld = padded(N);
     const size_t dz_bytes = as_is ? 0 : upto256(size_t(P->max_rows) * size_t(ld) * 2);
-    const size_t sum_bytes = P->gated ? 0 : upto256(size_t(column_sum_parts(P->max_rows)) * size_t(N) * 4);
-    int rc = DPDR_OK;
-    if (!as_is || c.dbias) rc = hold(P->scratch, n * dz_bytes + sum_bytes, "projection scratch");
-    if (rc) return rc;
     const bool again = !as_is && !c.pre && (P->gated || P->act != DPDR_ACT_NONE);
+    // column sums for the bias: as many rows of them as max_rows rows may come in,
+    // and where those are too many to join at once, their own column sums
+    const int64_t most = std::max<int64_t>(P->act == DPDR_ACT_NONE ? 0 : product_sum_parts(P->max_rows, P->num_sms),
+                                           column_sum_parts(P->max_rows));
+    const size_t sum_bytes = P->gated ? 0 : upto256(size_t(most) * size_t(N) * 4);
+    const size_t more_bytes = P->gated || most <= kJoined ? 0 : upto256(size_t(column_sum_parts(most)) * size_t(N) * 4);
+    int rc = DPDR_OK;
+    if (!as_is || c.dbias) rc = hold(P->scratch, n * dz_bytes + sum_bytes + more_bytes, "projection scratch");
+    if (rc) return rc;
     Operands o;
     const bool need_w = again || c.dx;
     const bool products = c.dx || c.dw0;
@@ -451,8 +460,8 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
     if (rc) return rc;
     dpdr_matrix dz[2] = {{P->scratch, ld, 1}, {P->scratch + dz_bytes, ld, 1}};
     float* sums = reinterpret_cast<float*>(P->scratch + n * dz_bytes);
+    int64_t parts = column_sum_parts(rows);
     Epilogue e = epilogue_of(P);
-    bool summed = false;
     if (as_is) {
         dz[0] = products ? o.dy : *c.dy;
     } else {
@@ -462,7 +471,8 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         e.out2 = static_cast<char*>(dz[1].data);
         e.out_rs = e.out2_rs = ld;
         if (again) {
-            rc = forward(P, rows, o.x, o.w[0], o.w[1], c.bias, e, s);
+            if (c.dbias) e.sums = sums;
+            rc = forward(P, rows, o.x, o.w[0], o.w[1], c.bias, e, s, false, &parts);
         } else {
             if (c.pre) {   // without: no activation, dy is rounded to the operand type
                 e.pre = static_cast<float*>(c.pre->data);
@@ -471,7 +481,6 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
             }
             if (!products) e.out = e.out2 = nullptr;
             rc = slope_launch(e, P->gated, rows, N, c.dbias ? sums : nullptr, s);
-            summed = true;
         }
         if (rc) return rc;
     }
@@ -512,13 +521,20 @@ static int backward(Proj* P, int64_t rows, const Backward& c, cudaStream_t s)
         if (rc) return rc;
     }
     if (c.dbias) {
-        if (!summed) {   // of dz as it was stored, or of dy
+        auto sum_columns = [&](const dpdr_matrix& of, int f32, int64_t height, float* into) {
             Epilogue d = epilogue_of(P);
             d.act = DPDR_ACT_NONE;
-            set_other(d, dz[0], 0);
-            rc = slope_launch(d, false, rows, N, sums, s);
+            set_other(d, of, f32);
+            return slope_launch(d, false, height, N, into, s);
+        };
+        if (as_is) rc = sum_columns(dz[0], 0, rows, sums);
+        if (!rc && parts > kJoined) {
+            float* more = sums + sum_bytes / 4;
+            rc = sum_columns(dpdr_matrix{sums, N, 1}, 1, parts, more);
+            sums = more;
+            parts = column_sum_parts(parts);
         }
-        if (!rc) rc = join_launch(sums, rows, N, c.dbias, P->grad_f32, P->half, s);
+        if (!rc) rc = join_launch(sums, int(parts), N, c.dbias, P->grad_f32, P->half, s);
     }
     return rc;
 }

@@ -46,6 +46,9 @@ struct Epilogue {
     int out_f32 = 0;
     float* pre = nullptr;          // z, or g and, pre_up columns on, u
     int64_t pre_rs = 0, pre_up = 0;
+    // Where the product is finished as a single dz, its column sums before it is
+    // rounded: rows of one float a column, each over some of the rows
+    float* sums = nullptr;
 };
 
 // The tensor cores add to a float32 sum by cutting off, not by rounding, so a
@@ -82,6 +85,7 @@ struct Product {
     int64_t M = 0, N = 0, K = 0;
     Operand a[2] = {}, b[2] = {};
     Epilogue e;
+    int64_t* sum_parts = nullptr;   // given how many rows of e.sums the product fills
 };
 
 constexpr int kPacked = 4;   // x, the weights, dy
@@ -120,11 +124,24 @@ int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int hal
 
 // dz (or dg and du) of at least one row from the kept projections: e.pre and
 // e.other in, e.out (and out2), where given, out.  With `sums` also dz's column
-// sums over column_sum_parts(rows) runs of rows, cols floats each, which
-// join_launch adds up.  No e.pre: z is 0 (of use without an activation).
+// sums over column_sum_parts(rows) runs of rows, cols floats each.  No e.pre: z
+// is 0 (of use without an activation).
 int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, float* sums, cudaStream_t s);
 int column_sum_parts(int64_t rows);
-int join_launch(const float* sums, int64_t rows, int64_t cols, void* out, int out_f32, int half, cudaStream_t s);
+
+// `parts` rows of column sums added up to the gradient of the bias
+int join_launch(const float* sums, int parts, int64_t cols, void* out, int out_f32, int half, cudaStream_t s);
+
+// Rows of column sums that a product of up to `rows` rows may fill: one for every 32
+// rows (tile_launch); one for each CTA down the rows, of 64 rows at least, and of
+// its cluster, of at most eight, with more than one no more in all than two an SM
+// (row_launch).
+constexpr int64_t product_sum_parts(int64_t rows, int num_sms)
+{
+    const int64_t tiles = (rows + 31) / 32, down = (rows + 63) / 64;
+    const int64_t split = 8 * down < 2 * num_sms ? 8 * down : 2 * num_sms;
+    return split > tiles ? split : tiles;
+}
 
 // Copies of 16-bit matrices with unit column stride and rows ld apart, each
 // into a slot of the plan's

@@ -164,9 +164,9 @@ __device__ __forceinline__ float other1(const Epilogue& e, int64_t m, int64_t n)
     return e.other ? load1(e.other, m * e.other_rs + n * e.other_cs, e.other_f32, e.half) : 0.0f;
 }
 
-// One result element from its sum (or pair of sums)
+// One result element from its sum (or pair of sums); its value before rounding
 template <bool PAIR, int FINISH, int ACT>
-__device__ __forceinline__ void put1(const Epilogue& e, char* out, int64_t out_rs, int64_t m, int64_t n, float z,
+__device__ __forceinline__ float put1(const Epilogue& e, char* out, int64_t out_rs, int64_t m, int64_t n, float z,
                                      float u, float bias, float o)
 {
     z += bias;
@@ -178,12 +178,13 @@ __device__ __forceinline__ void put1(const Epilogue& e, char* out, int64_t out_r
     finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
     store1(out, m * out_rs + n, v, e.out_f32, e.half);
     if (PAIR && FINISH == kSlope) store1(e.out2, m * e.out2_rs + n, w, e.out_f32, e.half);
+    return v;
 }
 
-// Four of them side by side
+// Four of them side by side, their values in v
 template <bool PAIR, int FINISH, int ACT>
 __device__ __forceinline__ void put4(const Epilogue& e, char* out, int64_t out_rs, int64_t m, int64_t n, float (&z)[4],
-                                     const float (&u)[4], const float (&bias)[4], const float (&o)[4])
+                                     const float (&u)[4], const float (&bias)[4], const float (&o)[4], float (&v)[4])
 {
 #pragma unroll
     for (int i = 0; i < 4; i++) z[i] += bias[i];
@@ -192,7 +193,7 @@ __device__ __forceinline__ void put4(const Epilogue& e, char* out, int64_t out_r
         if (PAIR)
             *reinterpret_cast<float4*>(e.pre + m * e.pre_rs + e.pre_up + n) = make_float4(u[0], u[1], u[2], u[3]);
     }
-    float v[4], w[4];
+    float w[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         w[i] = 0.0f;

@@ -198,10 +198,10 @@ int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, float
     return launch(kernel, grid, block, 0, 1, s, "projection gradient", e, rows, cols, per, sums);
 }
 
-int join_launch(const float* sums, int64_t rows, int64_t cols, void* out, int out_f32, int half, cudaStream_t s)
+int join_launch(const float* sums, int parts, int64_t cols, void* out, int out_f32, int half, cudaStream_t s)
 {
-    return launch(join_kernel, dim3(unsigned((cols + 31) / 32)), dim3(32, 8), 0, 1, s, "bias gradient", sums,
-                  column_sum_parts(rows), cols, static_cast<char*>(out), out_f32, half);
+    return launch(join_kernel, dim3(unsigned((cols + 31) / 32)), dim3(32, 8), 0, 1, s, "bias gradient", sums, parts,
+                  cols, static_cast<char*>(out), out_f32, half);
 }
 
 int copies_launch(Proj* P, const Copies& c, cudaStream_t s)

@@ -98,6 +98,7 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
         if (e != cudaSuccess) return cuda_fail_c(e, "projection row kernel");
         set = true;
     }
+    if (p.sum_parts) *p.sum_parts = down * split;
     return launch(kernel, dim3(unsigned(across * split), unsigned(down)), dim3(kRowThreads), size_t(smem), split, s,
                   "projection row kernel", t);
 }

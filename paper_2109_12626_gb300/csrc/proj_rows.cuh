@@ -250,6 +250,8 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
     if (t.split > 1) cluster_arrive();
     if (warp == 2) tmem_free<1>(tmem, t.held);
     if (t.split > 1) cluster_wait();
+    constexpr bool kSums = !PAIR && FINISH == kSlope;
+    float down[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // dz's sums over this thread's rows of it
     if (ok) {
         // ------------------------------------------------ results
         // A thread takes four features of a column; the partials of all CTAs
@@ -293,17 +295,37 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
                 for (int b = 0; b < kBatch; b++) {
                     const int64_t m = m0 + c + b * kApart * t.split;
                     if (m >= m0 + cols) break;
+                    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                     if (four)
-                        put4<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n, z[b], u[b], bias, o[b]);
+                        put4<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n, z[b], u[b], bias, o[b], v);
                     else
+#pragma unroll
                         for (int i = 0; i < 4; i++)
                             if (n + i < t.N)
-                                put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[b][i], u[b][i], bias[i], o[b][i]);
+                                v[i] = put1<PAIR, FINISH, ACT>(e, e.out, e.out_rs, m, n + i, z[b][i], u[b][i], bias[i],
+                                                               o[b][i]);
+                    if (kSums)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) down[i] += v[i];
                 }
             }
     }
     __syncwarp();
     if (t.split > 1) cluster_sync();   // the others have read this CTA's partials
+    if (kSums && t.e.sums && ok) {
+        // over the warps, which had every eighth of this CTA's rows of dz, in their
+        // order, where the partials were
+        __syncthreads();
+        *reinterpret_cast<float4*>(part + 4 * threadIdx.x) = make_float4(down[0], down[1], down[2], down[3]);
+        __syncthreads();
+        const int64_t at = n0 + threadIdx.x;
+        if (threadIdx.x < kRowFeatures && at < t.N) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kRowThreads / 32; i++) sum += part[i * kRowFeatures + threadIdx.x];
+            t.e.sums[(int64_t(blockIdx.y) * t.split + rank) * t.N + at] = sum;
+        }
+    }
 }
 
 }  // namespace

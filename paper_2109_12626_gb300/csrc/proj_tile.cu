@@ -59,6 +59,7 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
         if (e != cudaSuccess) return cuda_fail_c(e, "projection tile kernel");
         set = true;
     }
+    if (p.sum_parts) *p.sum_parts = (p.M + 31) / 32;
     const int pairs = t.items < pairs_all ? t.items : pairs_all;
     return launch(kernel, dim3(unsigned(2 * pairs)), dim3(kThreads), kSmem, 2, s, "projection tile kernel", t);
 }

@@ -122,6 +122,21 @@ struct Finisher {
         row = PAIR ? ((lane >> 2) & 1) * 4 + (lane >> 3) : lane / kPer;
     }
 
+    // dz's column sums over a warp's rows, before they are rounded
+    static constexpr bool kSums = !PAIR && FINISH == kSlope;
+
+    // threads kPer apart have the same four columns
+    __device__ __forceinline__ void put_sums(int c0, float (&down)[4])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int d = kPer; d < 32; d *= 2) down[i] += __shfl_xor_sync(0xFFFFFFFFu, down[i], d);
+        if (row == 0 && rows > 0)
+#pragma unroll
+            for (int i = 0; i < 4; i++) t.e.sums[m0 / 32 * t.N + n0 + c0 + 4 * q + i] = down[i];
+    }
+
     // whether a round of fours starts at c0
     __device__ __forceinline__ bool fours(int c0) const { return t.vec && c0 + kCols <= cols; }
 
@@ -181,6 +196,7 @@ struct Finisher {
             }
         }
         const int64_t down = out_rs * kRows * 2, down2 = e.out2_rs * kRows * 2, down_pre = e.pre_rs * kRows;
+        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int b = 0; b < kSteps; b++) {
             const int r = row + b * kRows;
@@ -201,9 +217,13 @@ struct Finisher {
                 }
                 store4(p, 0, 0, HALF, v);
                 if (PAIR && FINISH == kSlope) store4(p2, 0, 0, HALF, w);
+                if (kSums)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) sums[i] += v[i];
             }
             p += down, p2 += down2, pre += down_pre;
         }
+        if (kSums && e.sums) put_sums(c0, sums);
     }
 
     // The same for sums in runs, whatever the results' type, in as few registers as
@@ -214,17 +234,21 @@ struct Finisher {
         const int64_t n = n0 + c0 + 4 * q;
         float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, e.half, bias);
+        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         auto step = [&](int b, const float (&o)[4]) {
             const int r = row + b * kRows;
             if (r >= rows) return;
-            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
             const float4 z4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * (q ^ (r & 7)));
             float z[4] = {z4.x, z4.y, z4.z, z4.w};
             if (PAIR) {
                 const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * ((4 + q) ^ (r & 7)));
                 u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
             }
-            put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o);
+            put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o, v);
+            if (kSums)
+#pragma unroll
+                for (int i = 0; i < 4; i++) sums[i] += v[i];
         };
         if ((!PAIR || FINISH == kSlope) && e.other) {
             for (int b0 = 0; b0 < kSteps; b0 += 4) {
@@ -239,6 +263,7 @@ struct Finisher {
 #pragma unroll
                 for (int b = 0; b < 4; b++) step(b0 + b, o[b]);
             }
+            if (kSums && e.sums) put_sums(c0, sums);
             return;
         }
         const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -261,6 +286,7 @@ struct Finisher {
         const float bias = e.bias ? load1(static_cast<const char*>(e.bias), n, 0, half) : 0.0f;
         char* at = out + (m * out_rs + n) * size;
         const int64_t down = out_rs * kDown * size;
+        float total = 0.0f;   // of a column's dz, which one thread has
         auto step = [&](int r, char* p, float z, float u, float o) {
             if (e.pre) {
                 float* pre = e.pre + ((m0 + r) * e.pre_rs + n);
@@ -270,6 +296,7 @@ struct Finisher {
             float v = 0.0f, w = 0.0f;
             finish1<PAIR, FINISH, ACT>(z, u, o, v, w);
             store1(p, 0, v, f32, half);
+            if (kSums) total += v;
             if (PAIR && FINISH == kSlope) store1(e.out2, (m0 + r) * e.out2_rs + n, w, f32, half);
         };
         auto sum = [&](int r, int side) {
@@ -294,6 +321,7 @@ struct Finisher {
             for (int b = 0; b < kAsk; b++)
                 if (r0 + b * kDown < rows) step(r0 + b * kDown, at + b * down, z[b], u[b], o[b]);
         }
+        if (kSums && e.sums && rows > 0) e.sums[m0 / 32 * t.N + n] = total;
     }
 
     // a round's sums (two halves of its columns), to its results

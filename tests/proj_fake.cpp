@@ -64,6 +64,14 @@ int product(const dpdr::proj::Product& p)
     rows_hold("out", p.e.out, p.e.out_rs, p.M, p.N, es);
     if (p.kind == kTwin || (p.kind == kPair && p.e.finish == kSlope))
         rows_hold("out2", p.e.out2, p.e.out2_rs, p.M, p.N, es);
+    if (p.e.sums) {   // as many rows of sums as the kernels may fill
+        const int64_t parts = product_sum_parts(p.M, 152);
+        if (!p.sum_parts) return wrong("sums, but no count", p.e.sums, 0), DPDR_OK;
+        *p.sum_parts = parts;
+        rows_hold("column sums", p.e.sums, p.N, parts, p.N, 4);
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p.e.sums), z = reinterpret_cast<uintptr_t>(p.e.out);
+        if (at < z + size_t((p.M - 1) * p.e.out_rs + p.N) * es) wrong("sums over dz", p.e.sums, 0);
+    }
     return DPDR_OK;
 }
 
@@ -160,12 +168,18 @@ int slope_launch(const Epilogue& e, bool pair, int64_t rows, int64_t cols, float
     rows_hold("dz", e.out, e.out_rs, rows, cols, 2);
     if (pair) rows_hold("du", e.out2, e.out2_rs, rows, cols, 2);
     if (sums) rows_hold("sums", sums, cols, column_sum_parts(rows), cols, 4);
+    rows_hold("summed", e.other, e.other_rs, rows, cols, e.other_f32 ? 4 : 2);
+    if (e.other_f32 && reinterpret_cast<uintptr_t>(e.other) >= kOwn) {   // sums of sums
+        const uintptr_t a = reinterpret_cast<uintptr_t>(e.other), b = reinterpret_cast<uintptr_t>(sums);
+        if (b < a + size_t(rows) * cols * 4) wrong("sums over those they add up", sums, 0);
+    }
     return DPDR_OK;
 }
-int join_launch(const float* sums, int64_t rows, int64_t cols, void*, int, int, cudaStream_t)
+int join_launch(const float* sums, int parts, int64_t cols, void*, int, int, cudaStream_t)
 {
     B.launches++;
-    rows_hold("joined sums", sums, cols, column_sum_parts(rows), cols, 4);
+    if (parts < 1 || parts > 512) wrong("joined parts", nullptr, parts);
+    rows_hold("joined sums", sums, cols, parts, cols, 4);
     return DPDR_OK;
 }
 int copies_launch(Proj*, const Copies& c, cudaStream_t)
