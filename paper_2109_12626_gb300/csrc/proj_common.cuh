@@ -87,7 +87,8 @@ __device__ __forceinline__ void act_both(float z, float& v, float& d)
     case DPDR_ACT_GELU_TANH: {
         const float s = logistic(kRoot8Pi * (z + kCubic * z * z * z));
         v = z * s;
-        d = s + v * (1.0f - s) * kRoot8Pi * (1.0f + 3.0f * kCubic * z * z);
+        // s is 0 or 1 long before z z is infinite, which would make 0 times it NaN
+        d = s + v * (1.0f - s) * kRoot8Pi * (1.0f + 3.0f * kCubic * fminf(z * z, 1e8f));
         return;
     }
     case DPDR_ACT_SILU: {
