@@ -31,6 +31,7 @@ int fail_c(int status, const char* msg)
 
 int cuda_fail_c(cudaError_t e, const char* what)
 {
+    cudaGetLastError();  // told here: not to be found again by a later call
     g_last = e == cudaErrorMemoryAllocation ? DPDR_ERR_OOM : DPDR_ERR_CUDA;
     std::snprintf(g_msg, sizeof g_msg, "%s: %s", what, cudaGetErrorString(e));
     return g_last;

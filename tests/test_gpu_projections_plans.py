@@ -49,3 +49,28 @@ def test_a_captured_call_is_replayed_after_others(rows, k, n, act):
         for a, b in zip(want, (y, dx, dw)):
             assert torch.equal(a, b)
         assert all(bool((t == 3.0).all()) for t in others)
+
+
+def test_scratch_that_does_not_fit_is_forgotten():
+    """A call whose scratch does not fit fails; the plan and the library's
+    other entry points go on as before."""
+    import ctypes
+    import paper_2109_12626_gb300._native as N
+    g = gen(41)
+    x, w, dy = U.matrix(g, 4, 16, "bfloat16"), U.matrix(g, 8192, 16, "bfloat16"), U.matrix(g, 4, 8192, "bfloat16")
+    dx, y = torch.empty_like(x), torch.empty_like(dy)
+    a = torch.arange(100, dtype=torch.int32, device="cuda")
+    b = torch.empty_like(a)
+    with dpdr.Linear((1 << 31) - 1, 16, 8192, act="silu") as plan:
+        for _ in range(2):   # 35 TB of dz
+            with pytest.raises(dpdr.DpdrError) as e:
+                plan.backward(x, w, dy, dx)
+            assert e.value.status == N.DPDR_ERR_OOM
+            one = (ctypes.c_void_p * 1)
+            rc = N.lib().dpdr_allreduce_schedule_noalloc(1, 100, N.DPDR_INT32, N.DPDR_OP_SUM, 1, one(a.data_ptr()),
+                                                         one(b.data_ptr()), torch.cuda.current_stream().cuda_stream)
+            assert rc == N.DPDR_OK, N.lib().dpdr_last_error_message()
+            assert torch.equal(a, b)
+        plan.forward(x, w, y)
+        plan.sync()
+    U.check_linear(y, x, w, None, None, "silu", "bfloat16")
