@@ -450,10 +450,10 @@ dpdr_proj_t dpdr_gated_plan(int64_t max_rows, int64_t n_in, int64_t n_hidden,
  * pre (float32; z as rows by n_out, or g and u side by side as rows by
  * 2 n_hidden) keeps the projections for the backward call; with a 16-bit
  * result its sums are that result's, of which the tensor cores cut off up to
- * 1e-4 (2e-5 at n_in = 8192).  Asynchronous on
- * stream; the plan's device has to be the current one, for the backward calls
- * too.  Two calls on one plan that overlap on the GPU (two streams) race on
- * its scratch. */
+ * 1e-4 (2e-5 at n_in = 8192).  Asynchronous on stream; the plan's device has
+ * to be the current one, for the backward calls too.  Two calls on one plan
+ * that overlap on the GPU (two streams) race on its scratch, and calls that
+ * need scratch are not thread-safe with respect to one plan. */
 int dpdr_linear(dpdr_proj_t plan, int64_t rows, const dpdr_matrix* x,
                 const dpdr_matrix* w, const void* bias,
                 const dpdr_matrix* residual, const dpdr_matrix* y,

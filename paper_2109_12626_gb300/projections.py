@@ -11,6 +11,7 @@ device memory and streams, and the caller owns every buffer.
 from __future__ import annotations
 
 import ctypes
+import threading
 
 from ._native import (DPDR_BFLOAT16, DPDR_FLOAT16, DPDR_FLOAT32, DpdrError, _check, _stream, lib)
 
@@ -46,11 +47,7 @@ class _Projection:
         self.dtype, self.out, self.grad, self.act = dtype, out, grad, act
         self._operand, self._result, self._gradient = (getattr(torch, t) for t in (dtype, out, grad))
         self._float32 = torch.float32
-        # dpdr_matrix records (address, row stride, column stride) of a call's
-        # arguments, filled in anew by each call
-        self._rec = (ctypes.c_int64 * (3 * self._args))()
-        base = ctypes.addressof(self._rec)
-        self._at = [base + 24 * i for i in range(self._args)]
+        self._local = threading.local()
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -73,16 +70,28 @@ class _Projection:
         """Wait for the stream; raise DpdrError if a kernel's bounded wait expired."""
         _check(lib().dpdr_proj_sync(self._h, _stream(stream)), "dpdr_proj_sync")
 
-    def _matrix(self, i, name, t, rows, cols, dtype):
+    def _records(self):
+        """dpdr_matrix records (address, row stride, column stride) of a call's
+        arguments, filled in anew by each call, and their addresses: this
+        thread's, since a call lets other threads run while it reads them."""
+        try:
+            return self._local.records
+        except AttributeError:
+            r = (ctypes.c_int64 * (3 * self._args))()
+            base = ctypes.addressof(r)
+            self._local.records = r, [base + 24 * i for i in range(self._args)]
+            return self._local.records
+
+    def _matrix(self, records, i, name, t, rows, cols, dtype):
         """Argument number i as a record; its address, 0 for None."""
         if t is None:
             return 0
         if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != self._device:
             self._unfit(name, t, (rows, cols), dtype)
-        r = self._rec
+        r, at = records
         r[3 * i] = t.data_ptr()
         r[3 * i + 1], r[3 * i + 2] = t.stride()
-        return self._at[i]
+        return at[i]
 
     def _vector(self, name, t, n, dtype):
         if t is None:
@@ -122,13 +131,13 @@ class Linear(_Projection):
         """Writes y; y may be the residual.  ``pre`` (float32 [rows, n_out])
         keeps x w^T + bias for the backward call."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
-        m = self._matrix
-        rc = self._forward(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                           m(1, "w", w, n, k, self._operand),
+        m, q = self._matrix, self._records()
+        rc = self._forward(self._h, rows, m(q, 0, "x", x, rows, k, self._operand),
+                           m(q, 1, "w", w, n, k, self._operand),
                            self._vector("bias", bias, n, self._operand),
-                           m(2, "residual", residual, rows, n, self._result),
-                           m(3, "y", y, rows, n, self._result),
-                           m(4, "pre", pre, rows, n, self._float32), _stream(stream))
+                           m(q, 2, "residual", residual, rows, n, self._result),
+                           m(q, 3, "y", y, rows, n, self._result),
+                           m(q, 4, "pre", pre, rows, n, self._float32), _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_linear")
 
@@ -137,14 +146,14 @@ class Linear(_Projection):
         """Writes those of dx, dw and dbias that are given.  Without ``pre``
         the projection is computed again, for which it needs the bias."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
-        m = self._matrix
-        rc = self._backward(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                            m(1, "w", w, n, k, self._operand),
+        m, q = self._matrix, self._records()
+        rc = self._backward(self._h, rows, m(q, 0, "x", x, rows, k, self._operand),
+                            m(q, 1, "w", w, n, k, self._operand),
                             self._vector("bias", bias, n, self._operand),
-                            m(2, "dy", dy, rows, n, self._result),
-                            m(3, "pre", pre, rows, n, self._float32),
-                            m(4, "dx", dx, rows, k, self._gradient),
-                            m(5, "dw", dw, n, k, self._gradient),
+                            m(q, 2, "dy", dy, rows, n, self._result),
+                            m(q, 3, "pre", pre, rows, n, self._float32),
+                            m(q, 4, "dx", dx, rows, k, self._gradient),
+                            m(q, 5, "dw", dw, n, k, self._gradient),
                             self._vector("dbias", dbias, n, self._gradient),
                             _stream(stream))
         if rc:
@@ -167,12 +176,12 @@ class Gated(_Projection):
         """Writes h.  ``pre`` (float32 [rows, 2 n_hidden]) keeps both
         projections, the gate's first, for the backward call."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
-        m = self._matrix
-        rc = self._forward(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                           m(1, "w_gate", w_gate, n, k, self._operand),
-                           m(2, "w_up", w_up, n, k, self._operand),
-                           m(3, "h", h, rows, n, self._result),
-                           m(4, "pre", pre, rows, 2 * n, self._float32), _stream(stream))
+        m, q = self._matrix, self._records()
+        rc = self._forward(self._h, rows, m(q, 0, "x", x, rows, k, self._operand),
+                           m(q, 1, "w_gate", w_gate, n, k, self._operand),
+                           m(q, 2, "w_up", w_up, n, k, self._operand),
+                           m(q, 3, "h", h, rows, n, self._result),
+                           m(q, 4, "pre", pre, rows, 2 * n, self._float32), _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_gated")
 
@@ -181,14 +190,14 @@ class Gated(_Projection):
         """Writes dx, and dw_gate with dw_up, where given.  Without ``pre``
         the projections are computed again."""
         rows, k, n = self._rows(x), self.n_in, self.n_out
-        m = self._matrix
-        rc = self._backward(self._h, rows, m(0, "x", x, rows, k, self._operand),
-                            m(1, "w_gate", w_gate, n, k, self._operand),
-                            m(2, "w_up", w_up, n, k, self._operand),
-                            m(3, "dh", dh, rows, n, self._result),
-                            m(4, "pre", pre, rows, 2 * n, self._float32),
-                            m(5, "dx", dx, rows, k, self._gradient),
-                            m(6, "dw_gate", dw_gate, n, k, self._gradient),
-                            m(7, "dw_up", dw_up, n, k, self._gradient), _stream(stream))
+        m, q = self._matrix, self._records()
+        rc = self._backward(self._h, rows, m(q, 0, "x", x, rows, k, self._operand),
+                            m(q, 1, "w_gate", w_gate, n, k, self._operand),
+                            m(q, 2, "w_up", w_up, n, k, self._operand),
+                            m(q, 3, "dh", dh, rows, n, self._result),
+                            m(q, 4, "pre", pre, rows, 2 * n, self._float32),
+                            m(q, 5, "dx", dx, rows, k, self._gradient),
+                            m(q, 6, "dw_gate", dw_gate, n, k, self._gradient),
+                            m(q, 7, "dw_up", dw_up, n, k, self._gradient), _stream(stream))
         if rc:
             raise DpdrError(rc, "dpdr_gated_backward")
