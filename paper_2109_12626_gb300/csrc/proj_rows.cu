@@ -45,10 +45,9 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.err = P->err;
     const int64_t tiles = across * down;
     // As many CTAs of a cluster as fit beside each other, two an SM, while each
-    // still has four stages to load: 4096 x 4096 weights for one row, 1, 2, 4
-    // and 8 CTAs: 22.2, 14.3, 10.8 and 11.0 us; a pair of 8192 x 4096: 26.3,
-    // 25.8, 28.8 and 35.0 (more than two an SM).  One CTA an SM with twice the
-    // stages is no faster where all fit (4 CTAs: 11.1) and slower where not.
+    // still has four stages to load: two rows of 4096 x 4096 with 1, 2, 4 and 8
+    // CTAs 15.4, 10.6, 8.6 and 8.5 us; eight rows of a pair of 8192 x 4096 24.0,
+    // 23.3, 26.2 and 33.0 (more than two an SM).
     // Clusters leave SMs of their group of SMs unused, and one that finds no
     // place waits for another's whole time, so room is counted for 19/20 of the
     // CTAs with three and four a cluster (16 rows of 4096 x 9728, 76 tiles, 3 and 4:
@@ -70,8 +69,9 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     // Runs with columns of their own, for float32 results of 512 products where two
     // CTAs an SM have tensor memory for them (256 columns each): a power of two, no
     // more than the shortest part's steps.  Where those would be longer than a run
-    // may be, as many runs as it takes, in turn.  Most 16-bit results do without
-    // either: 64 rows of 4096 x 4096 in 9.8 against 12.0 us.
+    // may be, as many runs as it takes, in turn; a fifth more is let pass (384 rows
+    // of 4096 x 4096, 704 products a run, 17.2 against 18.7 us in turn).  The
+    // rounding of most 16-bit results hides what one run loses.
     t.apart = 32;
     while (t.apart < t.columns) t.apart *= 2;
     t.runs = 1;
@@ -79,7 +79,7 @@ int row_launch(Proj* P, const Product& p, cudaStream_t s)
     t.held = t.runs * t.apart;
     t.turns = 0;
     const int most = most_run_steps(p.e.out_f32, p.e.half);
-    if ((mine + t.runs - 1) / t.runs > most) {
+    if (5 * ((mine + t.runs - 1) / t.runs) > 6 * most) {
         t.runs = (mine + most - 1) / most;
         t.turns = 3 * t.apart <= 256 ? 2 : 1;
         t.held = t.turns == 2 ? 4 * t.apart : 256;
