@@ -405,6 +405,9 @@ int dpdr_allreduce_schedule_noalloc(int p, int64_t m, dpdr_dtype dtype,
  * Every value but three is held in float32 until it is stored: dz, dg and du
  * are rounded to the operand type before the products that take them (they
  * are operands of the tensor cores), and results are rounded to their type.
+ * The tensor cores cut sums off: a float32 result of positive products is
+ * about 5e-7 (bfloat16) or 4e-6 (float16) too small, whatever its length, a
+ * 16-bit one by a tenth of what its rounding may be off by.
  *
  * Matrices are given by address and strides in elements, so a transposed or
  * sliced array is passed as it lies.  Operands may have any strides >= 0
@@ -432,7 +435,8 @@ typedef struct {
  * that some calls need (made by the first such call, of the size that
  * max_rows rows need in any call; make that call before any stream capture).
  * Scratch never moves and is freed with the plan, so a captured call can be
- * replayed after calls of any other kind. */
+ * replayed after calls of any other kind.  Plans do not survive
+ * cudaDeviceReset, and none is made after one in the same process. */
 typedef struct dpdr_proj_s* dpdr_proj_t;
 
 /* Plans on the current CUDA device.  max_rows >= 0, the other sizes >= 1,

@@ -8,25 +8,26 @@
 // and CTA r holds the sums of its 128 rows in half of its tensor memory, so
 // that the other half takes the next tile's sums while eight warps finish this
 // one's.  A pair reads 512 rows of operands for 256 x 256 results, half of what
-// two CTAs of 128 x 256 would.  Each operand may have the summed index contiguous or the other one;
-// the tile in shared memory is then laid out the other way and the
-// instruction told so, so that the gradients' products read the same arrays
+// two CTAs of 128 x 256 would.  Each operand may have the summed index contiguous
+// or the other one; the tile in shared memory is then laid out the other way and
+// the instruction told so, so that the gradients' products read the same arrays
 // as the forward product, nothing transposed.  For the gated operator B is the
 // two weights' 128 rows of the same features, one weight a CTA: the pair g, u
 // of an output ends in columns n and n + 128 of one thread's row.
 //
-// Bound by the tensor cores: 4096 x 4096 x 4096 in 72 us (1.90 PFLOP/s, the
-// measured burst), 8192 x 8192 x 4096 in 280 (1.96), the gated operator 8192 x 4096 x
-// 8192 in 535 (2.06); in a long loop the power limit sets the rate.  Short sums are
-// bound by finishing a tile (3.5 us) and by loads: 4096 x 1000 x 4096 in 32 us.
-// Tried and not kept: asking tiles into L2 ahead of their loads (every pair its
-// own: 411 against 299 us; one pair for all: no faster), the last round's tiles summed by several pairs that join
-// their sums (no faster, and 43 against 33 us for short sums).
+// Bound by the tensor cores and, in a long loop, by the power limit: the gated
+// operator 8192 x 4096 x 8192 in 632 to 652 us (1.69 to 1.74 PFLOP/s), in a burst of
+// 24 calls 529; such bursts of 4096 x 4096 x 4096 in 72 us a call (1.91), of 8192 x
+// 4096 x 8192 in 269.  Short sums are bound by finishing a tile (3.5 us) and by
+// loads: 4096 x 1000 x 4096 in 32 us.  Tried and not kept: asking tiles into L2 ahead
+// of their loads (every pair its own: 411 against 299 us; one pair for all: no
+// faster), the last round's tiles summed by several pairs that join their sums (no
+// faster, and 43 against 33 us for short sums).
 //
 // Sums longer than a run (proj.h) are taken in runs (RUNS), and the finishing
 // warps add up the runs in registers, rounded, while the next run's products are
-// at work: float32 results of 4096 x 4096 x 4096 in 82 us instead of 72.  No wait then stands for more than a run, so that
-// none runs out over a sum of any length.
+// at work: float32 results of 4096 x 4096 x 4096 in 79 us instead of 72.  No wait
+// then stands for more than a run, so that none runs out over a sum of any length.
 #pragma once
 
 #include "proj_common.cuh"
