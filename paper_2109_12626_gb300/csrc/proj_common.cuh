@@ -88,7 +88,8 @@ __device__ __forceinline__ void act_both(float z, float& v, float& d)
         const float s = logistic(kRoot8Pi * (z + kCubic * z * z * z));
         v = z * s;
         // s is 0 or 1 long before z z is infinite, which would make 0 times it NaN
-        d = s + v * (1.0f - s) * kRoot8Pi * (1.0f + 3.0f * kCubic * fminf(z * z, 1e8f));
+        const float a = fminf(fabsf(z), 1e9f);
+        d = s + v * (1.0f - s) * kRoot8Pi * (1.0f + 3.0f * kCubic * a * a);
         return;
     }
     case DPDR_ACT_SILU: {
