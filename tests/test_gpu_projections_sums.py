@@ -88,6 +88,21 @@ def test_float32_results_of_long_sums(rows, k, n):
     check_positive("h", h, z * (x.double() @ w2.double().t()), k, 2 * MEAN32, 2 * most32(k) + 2.0 ** -23)
 
 
+@pytest.mark.parametrize("rows,k,n", [(128, 8192, 32768), (48, 40000, 4000), (100, 65536, 256), (1300, 8192, 1500),
+                                      (1300, 40000, 1501)])
+def test_float16_loses_no_more_of_longer_sums(rows, k, n):
+    """Products of float16 have 22 places, which are cut off near the sum's
+    last: 3.4e-6 of a run of 640 is lost (measured over one run; if each of them
+    lost half of the sum's last place it would be 2e-5), and half as much again
+    is allowed, at every length."""
+    x, w = positive(rows, k, "float16", 13, 2.0 ** -4), positive(n, k, "float16", 14, 2.0 ** -4)
+    y = torch.empty(rows, n, device="cuda")
+    with dpdr.Linear(rows, k, n, "float16", out="float32") as lin:
+        lin.forward(x, w, y)
+        lin.sync()
+    check_positive("y", y, x.double() @ w.double().t(), k, 5e-6, 1e-5 + most32(k))
+
+
 @pytest.mark.parametrize("rows,k,n", [(65536, 256, 256), (1 << 20, 64, 130), (300000, 264, 24), (9000, 2000, 2000)])
 def test_float32_weight_gradients_of_long_sums(rows, k, n):
     """dz is dy for the linear operator; for the gated one with w_up's
