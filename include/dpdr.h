@@ -52,7 +52,8 @@ typedef enum {
                             product entry is two rounded products and one
                             rounded sum, never fused                        */
     DPDR_BFLOAT16 = 4,   /* operands of the projections below only           */
-    DPDR_FLOAT16 = 5     /* (IEEE binary16), not of a reduction              */
+    DPDR_FLOAT16 = 5,    /* (IEEE binary16), not of a reduction              */
+    DPDR_INT8 = 6        /* experts' weights, products of 8-bit integers     */
 } dpdr_dtype;
 
 typedef enum {
@@ -491,6 +492,113 @@ int dpdr_proj_sync(dpdr_proj_t plan, dpdr_stream_t stream);
 /* Releases the plan's memory; no call on it may still be running.  NULL is a
  * no-op. */
 void dpdr_proj_destroy(dpdr_proj_t plan);
+
+/* ------------------------------------------------------- 8-bit integers
+ * Products of 8-bit integers with a scale for each row of x (token) and each
+ * row of w (channel), sums exact in 32 bits, and rows rounded to such integers:
+ *
+ *   quantise   scale = a / 127, a the largest size in the row;
+ *              q = 127 x / a rounded to the nearest whole number, halves to even
+ *   product    y = (sum_k x w) x_scale w_scale + bias + residual
+ *
+ * With float32 results a product is one rank's share of a row-parallel product,
+ * which dpdr_allreduce adds up, and the sums of a reduction are what is rounded
+ * for the next product. */
+
+/* x: rows by n of type dtype (DPDR_BFLOAT16, DPDR_FLOAT16 or DPDR_FLOAT32), any
+ * strides >= 0; q: rows by n of int8, col_stride 1; scale: rows, float32.  The
+ * rounding is exact: no other whole number is nearer to 127 x / a.  A row of
+ * zeros gives scale 0 and zeros.  A row with infinities gives an infinite scale,
+ * 127 or -127 for them and 0 for the rest, one with NaN the scale NaN and zeros.
+ * Weights are rounded by the same call, a row a channel.  Needs no plan;
+ * asynchronous on stream, which belongs to the current device. */
+int dpdr_quantise(int64_t rows, int64_t n, dpdr_dtype dtype, const dpdr_matrix* x,
+                  const dpdr_matrix* q, float* scale, dpdr_stream_t stream);
+
+/* Opaque plan of a product of 8-bit integers: sizes, type, scratch. */
+typedef struct dpdr_integer_s* dpdr_integer_t;
+
+/* A plan on the current device.  max_rows >= 0, n_out >= 1, both below 2^31;
+ * 1 <= n_in < 2^17 (sums stay below 2^31).  result: DPDR_BFLOAT16,
+ * DPDR_FLOAT16 or DPDR_FLOAT32, the type of y and the residual.  NULL on error. */
+dpdr_integer_t dpdr_integer_plan(int64_t max_rows, int64_t n_in, int64_t n_out,
+                                 dpdr_dtype result);
+
+/* x: rows by n_in, w: n_out by n_in, int8, any strides >= 0; x_scale: rows,
+ * w_scale: n_out, bias: n_out or NULL, float32 and contiguous; residual: any
+ * strides, or NULL; y: col_stride 1, rows that do not overlap.  y overlaps
+ * nothing else, except that it may be the residual itself.  Up to 64 rows with
+ * rows of w contiguous read w in place once, or for each 32 rows; others widen
+ * both operands to 16 bits, exactly, into the plan's scratch.  Scratch is made
+ * by the first call that needs it, at the size that max_rows rows need, and
+ * stays where it is until the plan goes: make that call before any stream
+ * capture.  0 <= rows <= max_rows; asynchronous on stream; the plan's device
+ * has to be the current one.  Two calls on one plan that overlap on the GPU
+ * race on its scratch, and calls on one plan are not thread-safe. */
+int dpdr_integer_linear(dpdr_integer_t plan, int64_t rows, const dpdr_matrix* x,
+                        const float* x_scale, const dpdr_matrix* w,
+                        const float* w_scale, const float* bias,
+                        const dpdr_matrix* residual, const dpdr_matrix* y,
+                        dpdr_stream_t stream);
+
+/* As dpdr_proj_sync and dpdr_proj_destroy. */
+int dpdr_integer_sync(dpdr_integer_t plan, dpdr_stream_t stream);
+void dpdr_integer_destroy(dpdr_integer_t plan);
+
+/* ------------------------------------------------------------- experts
+ * A layer of experts for a few tokens, or one rank's part of it:
+ *
+ *   l = x router^T;  the `top` largest of a token's l are chosen, equal ones by
+ *   the lower number (NaN counts as the largest);  share = exp(l - max) over the
+ *   sum of these, of the chosen experts (normalise) or of all
+ *   y = sum over the chosen experts e that are here of
+ *       share_e (act(x w_gate_e^T) * (x w_up_e^T)) w_down_e^T
+ *
+ * A rank holds the `local` experts from number `first` on (expert-parallel), or a
+ * slice of every expert's hidden features (n_hidden is then the slice's); either
+ * way y, in float32, is its share of a sum that dpdr_allreduce adds up.  A token
+ * none of whose experts is here gets zeros.  Everything between x and y is held
+ * in float32; hidden values enter the last product with 21 bits. */
+typedef struct {
+    void* data;              /* device memory, aligned to its element       */
+    int64_t stride;          /* elements from one matrix to the next        */
+    int64_t row_stride;
+    int64_t col_stride;
+} dpdr_matrices;
+
+typedef struct dpdr_experts_s* dpdr_experts_t;
+
+/* A plan on the current device, with all its scratch.  1 <= max_rows <= 64;
+ * 1 <= n_model, n_hidden <= 2^20; 1 <= top <= 16, top <= experts <= 512;
+ * 0 <= first, 1 <= local, first + local <= experts.  operands (x, router):
+ * DPDR_BFLOAT16 or DPDR_FLOAT16; weights: the operands' type or DPDR_INT8;
+ * result: the operands' type or DPDR_FLOAT32.  NULL on error. */
+dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, int64_t n_hidden,
+                                 int experts, int top, int first, int local,
+                                 dpdr_dtype operands, dpdr_dtype weights,
+                                 dpdr_dtype result, dpdr_act act, int normalise);
+
+/* x: rows by n_model; router: experts by n_model; both any strides >= 0.
+ * w_gate, w_up: local matrices of n_hidden by n_model, w_down: of n_model by
+ * n_hidden; col_stride 1, other strides >= 0, at any address (multiples of 16
+ * bytes are read faster).  The scales: float32 factors of 8-bit weights' rows,
+ * local by n_hidden (n_model for w_down), contiguous; NULL with 16-bit weights.
+ * y: rows by n_model, col_stride 1.  chosen (int32) and share (float32): rows by
+ * top, contiguous, in the order of their scores; either may be NULL.  Results
+ * overlap nothing.  0 <= rows <= max_rows; asynchronous on stream; the plan's
+ * device has to be the current one.  Two calls on one plan that overlap on the
+ * GPU (two streams, or graphs captured from one plan) race on its scratch. */
+int dpdr_experts(dpdr_experts_t plan, int64_t rows, const dpdr_matrix* x,
+                 const dpdr_matrix* router, const dpdr_matrices* w_gate,
+                 const dpdr_matrices* w_up, const dpdr_matrices* w_down,
+                 const float* gate_scale, const float* up_scale,
+                 const float* down_scale, const dpdr_matrix* y, int32_t* chosen,
+                 float* share, dpdr_stream_t stream);
+
+/* Waits for stream and reports its errors.  No kernel of this operator waits
+ * for another CTA, so none can time out. */
+int dpdr_experts_sync(dpdr_experts_t plan, dpdr_stream_t stream);
+void dpdr_experts_destroy(dpdr_experts_t plan);
 
 /* ------------------------------------------------------------ errors */
 int dpdr_last_error(void);

@@ -20,5 +20,6 @@ from ._native import (DPDR_ERR_CUDA, DPDR_ERR_INVALID,  # noqa: F401
                       Plan,
                       block_count_rule, blocks, lib, tree)
 from .projections import Gated, Linear  # noqa: F401
+from .serving import Experts, Linear8, quantise  # noqa: F401
 
-__all__ = ["Plan", "Linear", "Gated", "DpdrError", "tree", "blocks", "block_count_rule", "lib"]
+__all__ = ["Plan", "Linear", "Gated", "Linear8", "Experts", "quantise", "DpdrError", "tree", "blocks", "block_count_rule", "lib"]

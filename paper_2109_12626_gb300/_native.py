@@ -13,7 +13,7 @@ from typing import Sequence
 import numpy as np
 
 DPDR_INT32, DPDR_FLOAT32, DPDR_MAT2X2_U32, DPDR_MAT2X2_F32 = 0, 1, 2, 3
-DPDR_BFLOAT16, DPDR_FLOAT16 = 4, 5
+DPDR_BFLOAT16, DPDR_FLOAT16, DPDR_INT8 = 4, 5, 6
 DPDR_OP_SUM, DPDR_OP_MATMUL = 0, 1
 (DPDR_OK, DPDR_ERR_INVALID, DPDR_ERR_CUDA, DPDR_ERR_TIMEOUT,
  DPDR_ERR_NOT_COOPERATIVE, DPDR_ERR_OOM) = range(6)
@@ -58,6 +58,15 @@ SIGNATURES = {
     "dpdr_gated_backward": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 9),
     "dpdr_proj_sync": (ctypes.c_int, [_P, _P]),
     "dpdr_proj_destroy": (None, [_P]),
+    "dpdr_quantise": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int] + [_P] * 4),
+    "dpdr_integer_plan": (_P, [ctypes.c_int64] * 3 + [ctypes.c_int]),
+    "dpdr_integer_linear": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 8),
+    "dpdr_integer_sync": (ctypes.c_int, [_P, _P]),
+    "dpdr_integer_destroy": (None, [_P]),
+    "dpdr_experts_plan": (_P, [ctypes.c_int64] * 3 + [ctypes.c_int] * 9),
+    "dpdr_experts": (ctypes.c_int, [_P, ctypes.c_int64] + [_P] * 12),
+    "dpdr_experts_sync": (ctypes.c_int, [_P, _P]),
+    "dpdr_experts_destroy": (None, [_P]),
     "dpdr_last_error": (ctypes.c_int, []),
     "dpdr_last_error_message": (ctypes.c_char_p, []),
     "dpdr_status_string": (ctypes.c_char_p, [ctypes.c_int]),

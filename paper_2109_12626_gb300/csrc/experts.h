@@ -1,0 +1,52 @@
+// experts.h -- what the host side of a layer of experts (experts.cpp) hands to
+// its kernels (experts.cu).  Not part of the public ABI.
+#pragma once
+
+#include "dpdr_internal.h"
+
+namespace dpdr {
+namespace experts {
+
+constexpr int kMostRows = 64;       // tokens: a bit each in an expert's mask
+constexpr int kMostTop = 16;        // of them chosen, a lane each
+constexpr int kMostExperts = 512;   // 16 a lane of a warp
+constexpr int64_t kMostSize = 1 << 20;
+
+struct Layer {
+    int rows, top, total, first, local;
+    int d, h;                      // n_model, n_hidden
+    int64_t d_pad, h_pad;          // a row of the copy of x, of the hidden values
+    int half;                      // operand type: 0 bfloat16, 1 float16
+    int w_int8, act, normalise, out_f32;
+    const char* x;
+    int64_t x_rs, x_cs;
+    const char* router;
+    int64_t router_rs, router_cs;
+    dpdr_matrices w[3];            // gate, up, down
+    const float* scale[3];         // contiguous, channels of an expert after another
+    char* y;
+    int64_t y_rs;
+    int32_t* chosen;               // rows by top, or NULL
+    float* share;
+    // scratch of the plan
+    float* logits;                 // rows by total
+    char* x_copy;                  // rows by d_pad, zero behind d
+    float* hidden;                 // rows top by h_pad, zero behind h
+    float* parts;                  // of units whose sum is split
+    float* z;                      // the experts' results, before they are added up
+    uint32_t* up_count;            // of units, and of blocks of 32 features
+    uint32_t* down_count;
+    int up_ctas[2], down_ctas[2];  // of the product kernels, without and with shifted rows
+};
+
+// the floats of Layer::parts that `ctas` CTAs may fill, and of Layer::z behind
+// those of the pairs of token and expert
+constexpr int64_t parts_floats(int ctas) { return int64_t(ctas) * 32 * 32; }
+
+// makes the product kernels ready and sets how many CTAs each has
+int product_ctas(Layer& l, int num_sms);
+// the whole layer, at least one row
+int launch(const Layer& l, int num_sms, cudaStream_t s);
+
+}  // namespace experts
+}  // namespace dpdr

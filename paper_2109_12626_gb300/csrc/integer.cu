@@ -1,0 +1,376 @@
+// integer.cu -- products of 8-bit integers with a scale for each row and each
+// feature, for few rows, and what goes with them: rows rounded to such integers,
+// matrices laid out anew for the products.
+//
+//   y = (sum_k x w) sx sw + bias + residual
+//
+// Few rows stream the weights past once (stream.cuh): a unit is 32 features and
+// up to 32 rows, its sum split along k over several CTAs where there are fewer
+// units than CTAs, and the sums are whole numbers, so their order does not
+// matter.  Many rows go to the tensor cores' tiles (proj_tile.cuh) as 16-bit
+// values, which hold 8-bit integers exactly: the 8-bit integer instructions of
+// this GPU reach 150 TOP/s, the 16-bit ones twelve times that.
+#include <algorithm>
+
+#include "integer.h"
+#include "stream.cuh"
+
+namespace dpdr {
+namespace integer {
+
+using namespace stream;
+
+namespace {
+
+// ------------------------------------------------------------- few rows
+
+struct RowsArgs {
+    Rows r;
+    int passes, parts, pieces, units;
+};
+
+__device__ __forceinline__ void put(const Finish& f, int64_t m, int64_t n, int sum, float w_scale, float bias)
+{
+    float v = float(sum) * (f.x_scale[m] * w_scale) + bias;
+    if (f.residual) v += proj::load1(f.residual, m * f.residual_rs + n * f.residual_cs, f.out_f32, f.half);
+    proj::store1(f.y, m * f.y_rs + n, v, f.out_f32, f.half);
+}
+
+template <int NT, bool SHIFT>
+__global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant__ RowsArgs a)
+{
+    extern __shared__ __align__(128) char raw[];
+    using S = Stream<kI8, kI8, NT, SHIFT>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Rows& r = a.r;
+    S st(shared_at(raw), warp, lane);
+    float* room = reinterpret_cast<float*>(raw + kWarps * ring_bytes(SHIFT));
+    wait_previous();
+    allow_next();
+    const int all = a.units * a.parts;
+    auto unit = [&](int u, int64_t& n0, int& m0) {
+        const int part = u % a.parts, b = u / a.parts;
+        n0 = int64_t(b / a.passes) * 32;
+        m0 = b % a.passes * (8 * NT);
+        Unit q;
+        q.a[0] = r.w + n0 * r.w_rs;
+        q.a[1] = q.a[0] + 16 * r.w_rs;
+        q.a_stride[0] = q.a_stride[1] = r.w_rs;
+        q.rows_left[0] = int(min(int64_t(16), r.n - n0));
+        q.rows_left[1] = int(max(int64_t(0), min(int64_t(16), r.n - n0 - 16)));
+        q.row_bytes = r.k;
+        q.first = int(int64_t(a.pieces) * part / a.parts);
+        q.last = int(int64_t(a.pieces) * (part + 1) / a.parts);
+        return q;
+    };
+    int loading = int(blockIdx.x) - int(gridDim.x);
+    auto next = [&]() {
+        while (!st.more() && loading + int(gridDim.x) < all) {
+            loading += gridDim.x;
+            int64_t n0;
+            int m0;
+            const Unit q = unit(loading, n0, m0);
+            st.load_from(q, [&](int col) -> const char* { return m0 + col < r.rows ? r.x + (m0 + col) * r.x_rs : nullptr; });
+        }
+    };
+    st.begin(r.x, next);
+    for (int u = blockIdx.x; u < all; u += gridDim.x) {
+        int64_t n0;
+        int m0;
+        const Unit q = unit(u, n0, m0);
+        float sum[2][NT][4];
+        int v[NT];
+        st.sums(q, sum, r.x, next);
+#pragma unroll
+        for (int n = 0; n < NT; n++) v[n] = __float_as_int(join_columns<true>(room, sum[0][n], sum[1][n], warp, lane));
+        if (a.parts > 1) {
+            int32_t* mine = r.parts + int64_t(u) * NT * kThreads + threadIdx.x;
+#pragma unroll
+            for (int n = 0; n < NT; n++) mine[n * kThreads] = v[n];
+            if (!last_to_come(r.count + u / a.parts, a.parts)) continue;
+            const int32_t* from = r.parts + int64_t(u / a.parts) * a.parts * NT * kThreads + threadIdx.x;
+#pragma unroll
+            for (int n = 0; n < NT; n++) v[n] = 0;
+#pragma unroll 4
+            for (int p = 0; p < a.parts; p++)
+#pragma unroll
+                for (int n = 0; n < NT; n++) v[n] += __ldcg(from + (p * NT + n) * kThreads);
+        }
+        const int64_t feature = n0 + lane;
+        if (feature >= r.n) continue;
+        const float w_scale = r.f.w_scale[feature], bias = r.f.bias ? r.f.bias[feature] : 0.0f;
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+            const int m = m0 + n * 8 + warp;
+            if (m < r.rows) put(r.f, m, feature, v[n], w_scale, bias);
+        }
+    }
+}
+
+// --------------------------------------------------------- laid out anew
+
+// Sixteen elements a thread at a time.  Bound by the bytes: 8192 x 4096 to 16
+// bits is 100 MB.
+template <int WIDE>
+__global__ void __launch_bounds__(256) relay_kernel(const __grid_constant__ Relay r)
+{
+    wait_previous();
+    allow_next();
+    const Relay::Job& j = r.job[blockIdx.y];
+    const int64_t across = (j.to + 15) / 16, all = across * j.rows, apart = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += apart) {
+        const int64_t m = i / across, n = (i - m * across) * 16;
+        const int8_t* p = j.src + m * j.rs + n * j.cs;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (j.cs == 1 && n + 16 <= j.cols) {
+            // the aligned words around them
+            const int o = int(reinterpret_cast<uintptr_t>(p) & 3);
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(p - o);
+            if (reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+                const uint4 v = *reinterpret_cast<const uint4*>(p);
+                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+            } else {
+                uint32_t v[5];
+#pragma unroll
+                for (int k = 0; k < 4; k++) v[k] = q[k];
+                v[4] = o ? q[4] : 0u;
+#pragma unroll
+                for (int k = 0; k < 4; k++) w[k] = __funnelshift_r(v[k], v[k + 1], 8 * o);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; k++)
+                if (n + k < j.cols) w[k / 4] |= uint32_t(uint8_t(p[k * j.cs])) << 8 * (k % 4);
+        }
+        if (WIDE == 0) {
+            *reinterpret_cast<uint4*>(j.dst + m * j.ld + n) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            uint32_t v[8];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                if (WIDE == 1) bytes_to_bf16(w[k], v[2 * k], v[2 * k + 1]);
+                else bytes_to_f16(w[k], v[2 * k], v[2 * k + 1]);
+            }
+            char* to = j.dst + (m * j.ld + n) * 2;
+            *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[2], v[3]);
+            if (n + 8 < j.ld) *reinterpret_cast<uint4*>(to + 16) = make_uint4(v[4], v[5], v[6], v[7]);
+        }
+    }
+}
+
+// -------------------------------------------------------------- rounding
+
+__device__ __forceinline__ float value_of(const void* p, int64_t i, int dtype)
+{
+    if (dtype == DPDR_FLOAT32) return static_cast<const float*>(p)[i];
+    return proj::widen(static_cast<const uint16_t*>(p)[i], dtype == DPDR_FLOAT16);
+}
+
+// A row's numbers: what its values are multiplied by before they are rounded,
+// and by what power of two values and largest size are scaled so that nothing in
+// the arithmetic below overflows or loses places.
+struct Rounding {
+    float most, power, by;
+    __device__ __forceinline__ explicit Rounding(float a)
+    {
+        power = a > 1.2676506e30f ? 5.421010862427522e-20f : a < 8.6736174e-19f ? 1.8446744073709552e19f : 1.0f;   // 2^-64, 2^64
+        most = a * power;
+        by = 127.0f / most;
+    }
+};
+
+// 127 v / most, rounded to the nearest whole number, halves to even, exactly.
+// The float32 quotient is off by 1.6e-5 at most, so it decides unless it is near a
+// half; there the sizes of 254 |v| and (2 k + 1) most are compared, each as a float and
+// what that leaves of the product, eight bits more, whose differences are exact.
+__device__ __forceinline__ int rounded(float v, const Rounding& r)
+{
+    const float size = fabsf(v) * r.power, t = size * r.by, low = floorf(t), part = t - low;
+    int q = part > 0.5f ? int(low) + 1 : int(low);
+    if (fabsf(part - 0.5f) < 1e-4f) {
+        const float odd = 2.0f * low + 1.0f;
+        const float a = 254.0f * size, a_rest = fmaf(254.0f, size, -a);
+        const float b = odd * r.most, b_rest = fmaf(odd, r.most, -b);
+        const float d = (a - b) + (a_rest - b_rest);
+        q = d > 0.0f || (d == 0.0f && (int(low) & 1)) ? int(low) + 1 : int(low);
+    }
+    return v < 0.0f ? -q : q;
+}
+
+// Row by row, `share` threads a row, one pass: the values stay in registers (HELD
+// groups of four a thread, kept as they came); longer rows are read twice, from L2
+// the second time.
+template <int DT, int HELD, bool VEC>
+__global__ void __launch_bounds__(256) quantise_kernel(const void* x, int64_t rs, int64_t cs, int8_t* q, int64_t q_rs,
+                                                      float* scale, int64_t rows, int64_t n, int share)
+{
+    __shared__ uint32_t most[8];
+    wait_previous();
+    allow_next();
+    const int per = 256 / share, mine = int(threadIdx.x) / share, at = int(threadIdx.x) % share;
+    const int64_t m = int64_t(blockIdx.x) * per + mine;
+    const bool there = m < rows;
+    const int64_t from = m * rs;
+    const char* row = static_cast<const char*>(x) + from * (DT == DPDR_FLOAT32 ? 4 : 2);
+    const int64_t units = (n + 3) / 4;   // groups of four
+    using Held = typename std::conditional<DT == DPDR_FLOAT32, uint4, uint2>::type;
+    Held held[HELD];
+    auto get = [&](int64_t u) {
+        Held h;
+        if (VEC) {
+            h = reinterpret_cast<const Held*>(row)[u];
+        } else {
+            uint32_t v[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int64_t i = from + (4 * u + k) * cs;
+                if (4 * u + k >= n) v[k] = 0;
+                else if (DT == DPDR_FLOAT32) v[k] = static_cast<const uint32_t*>(x)[i];
+                else v[k] = static_cast<const uint16_t*>(x)[i];
+            }
+            if constexpr (DT == DPDR_FLOAT32) h = make_uint4(v[0], v[1], v[2], v[3]);
+            else h = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
+        }
+        return h;
+    };
+    auto widened = [&](const Held& h, float (&f)[4]) {
+        if constexpr (DT == DPDR_FLOAT32) proj::widen4(h, 1, 0, f);
+        else proj::widen4(make_uint4(h.x, h.y, 0, 0), 0, DT == DPDR_FLOAT16, f);
+    };
+    // sizes as whole numbers, whose order puts NaN above infinity
+    uint32_t high = 0;
+    auto look = [&](const Held& h) {
+        float f[4];
+        widened(h, f);
+#pragma unroll
+        for (int k = 0; k < 4; k++) high = max(high, __float_as_uint(f[k]) & 0x7FFFFFFFu);
+    };
+    const bool whole = units <= int64_t(HELD) * share;
+    if (there) {
+        if (whole) {
+#pragma unroll
+            for (int k = 0; k < HELD; k++) {
+                const int64_t u = at + int64_t(k) * share;
+                if (u < units) held[k] = get(u);
+            }
+#pragma unroll
+            for (int k = 0; k < HELD; k++)
+                if (at + int64_t(k) * share < units) look(held[k]);
+        } else {
+#pragma unroll 4
+            for (int64_t u = at; u < units; u += share) look(get(u));
+        }
+    }
+    high = __reduce_max_sync(0xFFFFFFFFu, high);
+    if (share > 32) {
+        if (threadIdx.x % 32 == 0) most[threadIdx.x / 32] = high;
+        __syncthreads();
+        const int first = mine * (share / 32);
+        for (int w = 0; w < share / 32; w++) high = max(high, most[first + w]);
+    }
+    if (!there) return;
+    const float a = __uint_as_float(high);
+    if (at == 0) scale[m] = a / 127.0f;
+    const bool plain = high > 0 && high < 0x7F800000u;
+    const Rounding r(a);
+    auto put = [&](int64_t u, const Held& h) {
+        float f[4];
+        widened(h, f);
+        int v[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (plain) v[k] = rounded(f[k], r);
+            else v[k] = high == 0x7F800000u && isinf(f[k]) ? (f[k] < 0.0f ? -127 : 127) : 0;
+        }
+        int8_t* to = q + m * q_rs + 4 * u;
+        if (VEC) {
+            *reinterpret_cast<uint32_t*>(to) = uint32_t(v[0] & 255) | uint32_t(v[1] & 255) << 8 |
+                                               uint32_t(v[2] & 255) << 16 | uint32_t(v[3]) << 24;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (4 * u + k < n) to[k] = int8_t(v[k]);
+        }
+    };
+    if (whole) {
+#pragma unroll
+        for (int k = 0; k < HELD; k++) {
+            const int64_t u = at + int64_t(k) * share;
+            if (u < units) put(u, held[k]);
+        }
+    } else {
+#pragma unroll 2
+        for (int64_t u = at; u < units; u += share) put(u, get(u));
+    }
+}
+
+template <int DT>
+int quantise(int64_t rows, int64_t n, const dpdr_matrix& x, const dpdr_matrix& q, float* scale, cudaStream_t s)
+{
+    const int es = DT == DPDR_FLOAT32 ? 4 : 2;
+    const bool vec = x.col_stride == 1 && n % 4 == 0 && reinterpret_cast<uintptr_t>(x.data) % (4 * es) == 0 &&
+                     reinterpret_cast<uintptr_t>(q.data) % 4 == 0 &&
+                     (rows == 1 || (x.row_stride % 4 == 0 && q.row_stride % 4 == 0));
+    const int64_t units = (n + 3) / 4;
+    int share = 32;   // threads a row
+    while (share < 256 && units > share) share *= 2;
+    const int64_t per = 256 / share, ctas = (rows + per - 1) / per;
+    if (ctas > (int64_t(1) << 31) - 1) return fail_c(DPDR_ERR_INVALID, "dpdr_quantise: too many rows");
+    const bool few = units <= 4 * share;
+    auto* kernel = vec ? (few ? quantise_kernel<DT, 4, true> : quantise_kernel<DT, 8, true>)
+                       : (few ? quantise_kernel<DT, 4, false> : quantise_kernel<DT, 8, false>);
+    return proj::launch(kernel, dim3(unsigned(ctas)), dim3(256), 0, 1, s, "quantise kernel", (const void*)x.data,
+                        x.row_stride, x.col_stride, static_cast<int8_t*>(q.data), q.row_stride, scale, rows, n, share);
+}
+
+template <int NT>
+int rows_launch_of(const RowsArgs& a, bool shift, int ctas, cudaStream_t s)
+{
+    auto* kernel = shift ? rows_kernel<NT, true> : rows_kernel<NT, false>;
+    const int bytes = kWarps * ring_bytes(shift) + kJoin * 4;
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return cuda_fail_c(e, "integer rows kernel");
+    return proj::launch(kernel, dim3(unsigned(ctas)), dim3(kThreads), size_t(bytes), 1, s, "integer rows kernel", a);
+}
+
+}  // namespace
+
+int rows_launch(const Rows& r, int num_sms, cudaStream_t s)
+{
+    RowsArgs a;
+    a.r = r;
+    const int nt = r.rows <= 8 ? 1 : r.rows <= 16 ? 2 : 4;
+    a.passes = (r.rows + 8 * nt - 1) / (8 * nt);
+    const int64_t units = (r.n + 31) / 32 * a.passes;
+    a.units = int(units);
+    a.pieces = (r.k + kPiece - 1) / kPiece;
+    const int slots = 2 * num_sms;
+    // as many parts as there are CTAs for, while a warp keeps two pieces
+    a.parts = int(std::max<int64_t>(1, std::min<int64_t>(slots / units, a.pieces / (2 * kWarps))));
+    const int ctas = int(std::min<int64_t>(units * a.parts, slots));
+    const bool shift = reinterpret_cast<uintptr_t>(r.w) % 16 != 0 || (r.n > 1 && r.w_rs % 16 != 0);
+    return nt == 1   ? rows_launch_of<1>(a, shift, ctas, s)
+           : nt == 2 ? rows_launch_of<2>(a, shift, ctas, s)
+                     : rows_launch_of<4>(a, shift, ctas, s);
+}
+
+int relay_launch(const Relay& r, int num_sms, cudaStream_t s)
+{
+    int64_t most = 0;
+    for (int i = 0; i < r.n; i++) most = std::max(most, r.job[i].rows * ((r.job[i].to + 15) / 16));
+    const unsigned blocks = unsigned(std::min<int64_t>((most + 255) / 256, int64_t(num_sms) * 16));
+    auto* kernel = r.wide == 0 ? relay_kernel<0> : r.wide == 1 ? relay_kernel<1> : relay_kernel<2>;
+    return proj::launch(kernel, dim3(blocks, unsigned(r.n)), dim3(256), 0, 1, s, "integer operand copy", r);
+}
+
+int quantise_launch(int dtype, int64_t rows, int64_t n, const dpdr_matrix& x, const dpdr_matrix& q, float* scale,
+                    cudaStream_t s)
+{
+    if (dtype == DPDR_FLOAT32) return quantise<DPDR_FLOAT32>(rows, n, x, q, scale, s);
+    if (dtype == DPDR_FLOAT16) return quantise<DPDR_FLOAT16>(rows, n, x, q, scale, s);
+    return quantise<DPDR_BFLOAT16>(rows, n, x, q, scale, s);
+}
+
+}  // namespace integer
+}  // namespace dpdr

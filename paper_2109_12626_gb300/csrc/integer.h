@@ -1,0 +1,63 @@
+// integer.h -- what the host side of the products of 8-bit integers
+// (integer.cpp) hands to their kernels (integer.cu).  Not part of the public ABI.
+#pragma once
+
+#include "proj.h"
+
+namespace dpdr {
+namespace integer {
+
+// Sums of products of 8-bit integers stay below 2^31
+constexpr int64_t kMostSummed = (int64_t(1) << 17) - 1;
+
+// rows that rows_launch takes
+constexpr int kFewRows = 64;
+// what their elements are a multiple of
+constexpr int kRowsPad = 64;
+
+struct Finish {
+    const float* x_scale;    // of a row, of a feature
+    const float* w_scale;
+    const float* bias;       // or NULL
+    const char* residual;    // result type, or NULL
+    int64_t residual_rs, residual_cs;
+    char* y;
+    int64_t y_rs;
+    int out_f32, half;       // result: float32, or 0 bfloat16, 1 float16
+};
+
+// Few rows: x by rows of whole 64 bytes at multiples of 16 (zero or not there
+// behind k), w with the summed index contiguous at any address and row stride.
+struct Rows {
+    int rows, k;
+    int64_t n;
+    const char* x;
+    int64_t x_rs;
+    const char* w;
+    int64_t w_rs;
+    Finish f;
+    int32_t* parts;          // of units whose sum is split
+    uint32_t* count;
+};
+int rows_launch(const Rows& r, int num_sms, cudaStream_t s);
+constexpr int64_t parts_ints(int num_sms) { return int64_t(2 * num_sms) * 32 * 32; }
+
+// 8-bit matrices laid out anew: by rows ld apart, zero from cols up to `to`, as
+// 8-bit integers (wide 0), bfloat16 (1) or float16 (2)
+struct Relay {
+    struct Job {
+        const int8_t* src;
+        char* dst;
+        int64_t rs, cs, rows, cols, ld, to;
+    };
+    Job job[2];
+    int n = 0, wide = 0;
+};
+int relay_launch(const Relay& r, int num_sms, cudaStream_t s);
+
+// a row's largest size over 127, and the row in units of that, rounded
+int quantise_launch(int dtype, int64_t rows, int64_t n, const dpdr_matrix& x, const dpdr_matrix& q, float* scale,
+                    cudaStream_t s);
+
+}  // namespace integer
+}  // namespace dpdr

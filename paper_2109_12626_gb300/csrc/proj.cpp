@@ -2,11 +2,11 @@
 // and the sequence of kernels of each call.
 #include <algorithm>
 #include <cstdint>
-#include <cstdio>
 #include <mutex>
 #include <new>
 #include <utility>
 
+#include "args.h"
 #include "proj.h"
 
 namespace dpdr {
@@ -15,14 +15,6 @@ namespace proj {
 namespace {
 
 constexpr int64_t kMost = (int64_t(1) << 31) - 1;
-
-// A refusal as "who: what", without allocating.
-int refuse(const char* who, const char* what, const char* more = "")
-{
-    char msg[200];
-    std::snprintf(msg, sizeof msg, "%s: %s%s%s", who, what, *more ? " " : "", more);
-    return fail_c(DPDR_ERR_INVALID, msg);
-}
 
 bool is_half_kind(int t) { return t == DPDR_BFLOAT16 || t == DPDR_FLOAT16; }
 
@@ -111,93 +103,6 @@ Proj* make(bool gated, int64_t max_rows, int64_t n_in, int64_t n_out, int operan
     return P;
 }
 
-// A matrix argument in bytes: which range of memory it touches, and which
-// part of each row of its pitch.
-struct Span {
-    uintptr_t lo = 0, hi = 0, pitch = 0, width = 0;
-};
-
-Span span_of(const dpdr_matrix& m, int64_t rows, int64_t cols, int esize)
-{
-    Span s;
-    if (rows == 0 || cols == 0) return s;
-    s.lo = reinterpret_cast<uintptr_t>(m.data);
-    const uintptr_t last = uintptr_t(rows - 1) * uintptr_t(m.row_stride) + uintptr_t(cols - 1) * uintptr_t(m.col_stride);
-    s.hi = s.lo + (last + 1) * esize;
-    s.pitch = uintptr_t(m.row_stride) * esize;
-    s.width = m.col_stride == 1 ? uintptr_t(cols) * esize : s.pitch;
-    return s;
-}
-
-// Whether two arguments may share a byte.  Column slices of one wider array
-// (equal pitch, disjoint parts of it) do not.
-bool overlap(const Span& a, const Span& b)
-{
-    if (a.lo == a.hi || b.lo == b.hi || a.hi <= b.lo || b.hi <= a.lo) return false;
-    if (a.pitch == b.pitch && a.pitch > 0 && a.width <= a.pitch && b.width <= b.pitch) {
-        const uintptr_t d = b.lo >= a.lo ? (b.lo - a.lo) % a.pitch : (a.pitch - (a.lo - b.lo) % a.pitch) % a.pitch;
-        if (d >= a.width && d + b.width <= a.pitch) return false;
-    }
-    return true;
-}
-
-// The arguments of one call, checked as they are added.
-struct Args {
-    const char* who;
-    Span in[6], out[4];
-    int nin = 0, nout = 0;
-    int rc = DPDR_OK;
-
-    void refuse(const char* name, const char* what)
-    {
-        if (rc == DPDR_OK) rc = proj::refuse(who, name, what);
-    }
-    void input(const char* name, const dpdr_matrix* m, int64_t rows, int64_t cols, int esize)
-    {
-        if (!m) return refuse(name, "is NULL");
-        check(name, *m, rows, cols, esize);
-        if (m->row_stride < 0 || m->col_stride < 0) return refuse(name, "has a negative stride");
-        in[nin++] = span_of(*m, rows, cols, esize);
-    }
-    void output(const char* name, const dpdr_matrix* m, int64_t rows, int64_t cols, int esize)
-    {
-        if (!m) return refuse(name, "is NULL");
-        check(name, *m, rows, cols, esize);
-        if (cols > 1 && m->col_stride != 1) return refuse(name, "needs col_stride 1");
-        if (rows > 1 && m->row_stride < cols) return refuse(name, "has rows that overlap");
-        dpdr_matrix unit = *m;
-        unit.col_stride = 1;
-        out[nout++] = span_of(unit, rows, cols, esize);
-    }
-    void check(const char* name, const dpdr_matrix& m, int64_t rows, int64_t cols, int esize)
-    {
-        if (rows == 0 || cols == 0) return;
-        if (!m.data) return refuse(name, "has no address");
-        if (reinterpret_cast<uintptr_t>(m.data) % uintptr_t(esize)) refuse(name, "is not aligned to its element");
-        // byte offsets stay within 2^62
-        const __int128 far = (__int128)(rows - 1) * m.row_stride + (__int128)(cols - 1) * m.col_stride;
-        if (far > (__int128(1) << 59)) refuse(name, "reaches too far");
-    }
-    void vector(const char* name, const void* p, int64_t n, int esize, bool result)
-    {
-        const dpdr_matrix m{const_cast<void*>(p), n, 1};
-        if (result) output(name, &m, 1, n, esize);
-        else input(name, &m, 1, n, esize);
-    }
-    // no result may touch another argument (but the residual, which is checked
-    // on its own)
-    int done()
-    {
-        for (int i = 0; i < nout && rc == DPDR_OK; i++) {
-            for (int k = 0; k < nin; k++)
-                if (overlap(out[i], in[k])) return rc = proj::refuse(who, "a result overlaps an input");
-            for (int k = 0; k < i; k++)
-                if (overlap(out[i], out[k])) return rc = proj::refuse(who, "two results overlap");
-        }
-        return rc;
-    }
-};
-
 int check_plan(const Proj* P, bool gated, int64_t rows, const char* who)
 {
     if (!P) return refuse(who, "NULL plan");
@@ -275,7 +180,8 @@ bool by_fours(const Epilogue& e)
     const int os = e.out_f32 ? 4 : 2;
     return fits(e.out, e.out_rs, os) && fits(e.out2, e.out2_rs, os) &&
            (!e.other || (e.other_cs == 1 && fits(e.other, e.other_rs, e.other_f32 ? 4 : 2))) &&
-           (!e.pre || (fits(e.pre, e.pre_rs, 4) && e.pre_up % 4 == 0)) && fits(e.bias, 0, 2);
+           (!e.pre || (fits(e.pre, e.pre_rs, 4) && e.pre_up % 4 == 0)) && fits(e.bias, 0, 2) &&
+           fits(e.col_scale, 0, 4) && fits(e.bias32, 0, 4);
 }
 
 int tensor_map(CUtensorMap* map, const Operand& o, int64_t n, int64_t k, int half, int rows, int step)

@@ -30,7 +30,9 @@ enum Kind { kSingle, kPair, kChain, kTwin };
 //   kValue   act(z) + other, or act(g) * u
 //   kSlope   other * act'(z), or other * u * act'(g) -> out and
 //            other * act(g) -> out2
-enum Finish { kValue, kSlope };
+//   kScaled  z row_scale[m] col_scale[n] + bias32 + other, of whole numbers: the
+//            sums of runs are added up as integers (tile_launch, kSingle, no act)
+enum Finish { kValue, kSlope, kScaled };
 
 struct Epilogue {
     int finish = kValue;
@@ -49,6 +51,9 @@ struct Epilogue {
     // Where the product is finished as a single dz, its column sums before it is
     // rounded: rows of one float a column, each over some of the rows
     float* sums = nullptr;
+    const float* row_scale = nullptr;   // kScaled
+    const float* col_scale = nullptr;
+    const float* bias32 = nullptr;
 };
 
 // The tensor cores add to a float32 sum by cutting off, not by rounding, so a
@@ -60,6 +65,9 @@ struct Epilogue {
 // results, for 16-bit ones as long as the loss is below a tenth of what the
 // result's rounding may be off by.
 constexpr int kSumStep = 64;   // products a step
+// Products of 8-bit integers are whole numbers of up to 2^14, whose sums are
+// exact up to 2^24: 16 steps.
+constexpr int kScaledRunSteps = 16;
 constexpr int most_run_steps(int out_f32, int half) { return out_f32 ? 10 : half ? 128 : 256; }
 
 // The runs of a sum, of nearly equal length: next() gives the step behind each,
@@ -100,7 +108,7 @@ struct Proj {
     // copies of operands that the tensor cores' loads cannot take as they lie
     char* packed[kPacked] = {};
     uint32_t* err = nullptr;       // error word, in host memory that kernels write to
-    bool tile_set[2][2][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
+    bool tile_set[2][3][2][2] = {}, row_set[2][2][2][3] = {};   // kernel attributes set
 };
 
 // Tensor-core product of operands that TMA can load: one stride 1, the other

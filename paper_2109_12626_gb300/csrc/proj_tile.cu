@@ -1,7 +1,8 @@
 // proj_tile.cu -- which kernel of proj_tile.cuh a product takes, its tensor
 // maps and launch; the kernels of one product a tile and one run a sum
 // (proj_tile_pair.cu holds the gated operator's, proj_tile_runs.cu and
-// proj_tile_pair_runs.cu those of several runs, compiled beside them).
+// proj_tile_pair_runs.cu those of several runs, proj_tile_scaled.cu the one of
+// scaled whole numbers, compiled beside them).
 #include "proj_tile.cuh"
 
 namespace dpdr {
@@ -11,6 +12,7 @@ TileKernel tile_kernel_single(int finish, int act) { return tile_kernel_of<false
 TileKernel tile_kernel_single_runs(int finish, int act);   // proj_tile_runs.cu
 TileKernel tile_kernel_pair(int finish, int act);          // proj_tile_pair.cu
 TileKernel tile_kernel_pair_runs(int finish, int act);     // proj_tile_pair_runs.cu
+TileKernel tile_kernel_scaled();                           // proj_tile_scaled.cu
 
 int tile_launch(Proj* P, const Product& p, cudaStream_t s)
 {
@@ -19,9 +21,10 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     t.b_mn = p.b[0].ks != 1;
     t.segments = p.kind == kChain ? 2 : 1;
     t.steps = int((p.K + kStep - 1) / kStep);
-    const int most = most_run_steps(p.e.out_f32, p.e.half);
+    const bool scaled = p.e.finish == kScaled;
+    const int most = scaled ? kScaledRunSteps : most_run_steps(p.e.out_f32, p.e.half);
     t.runs = (t.steps * t.segments + most - 1) / most;
-    const bool runs = p.e.out_f32 || t.runs > 1;
+    const bool runs = scaled || p.e.out_f32 || t.runs > 1;
     const int width = p.kind == kPair ? 128 : 256;
     t.tiles_m = int((p.M + 255) / 256);
     t.tiles_n = int((p.N + width - 1) / width);
@@ -50,8 +53,9 @@ int tile_launch(Proj* P, const Product& p, cudaStream_t s)
     }
     if (rc) return rc;
     const TileKernel kernel =
-        p.kind == kPair ? (runs ? tile_kernel_pair_runs : tile_kernel_pair)(p.e.finish, p.e.act)
-                        : (runs ? tile_kernel_single_runs : tile_kernel_single)(p.e.finish, p.e.act);
+        scaled            ? tile_kernel_scaled()
+        : p.kind == kPair ? (runs ? tile_kernel_pair_runs : tile_kernel_pair)(p.e.finish, p.e.act)
+                          : (runs ? tile_kernel_single_runs : tile_kernel_single)(p.e.finish, p.e.act);
     // a plan's activation is fixed, but its gradients' products have none
     bool& set = P->tile_set[p.kind == kPair][p.e.finish][p.e.act != DPDR_ACT_NONE][runs];
     if (!set) {

@@ -235,6 +235,11 @@ struct Finisher {
         const int64_t n = n0 + c0 + 4 * q;
         float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (e.bias) load4(static_cast<const char*>(e.bias), n, 0, e.half, bias);
+        float across[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // the columns' scales
+        if (FINISH == kScaled) {
+            load4(reinterpret_cast<const char*>(e.col_scale), n, 1, 0, across);
+            if (e.bias32) load4(reinterpret_cast<const char*>(e.bias32), n, 1, 0, bias);
+        }
         float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         auto step = [&](int b, const float (&o)[4]) {
             const int r = row + b * kRows;
@@ -246,7 +251,14 @@ struct Finisher {
                 const float4 u4 = *reinterpret_cast<const float4*>(stage + r * 32 + 4 * ((4 + q) ^ (r & 7)));
                 u[0] = u4.x, u[1] = u4.y, u[2] = u4.z, u[3] = u4.w;
             }
-            put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o, v);
+            if constexpr (FINISH == kScaled) {
+                const float scale = e.row_scale[m0 + r];
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = z[i] * (scale * across[i]) + bias[i] + o[i];
+                store4(out, (m0 + r) * out_rs + n, e.out_f32, e.half, v);
+            } else {
+                put4<PAIR, FINISH, ACT>(e, out, out_rs, m0 + r, n, z, u, bias, o, v);
+            }
             if (kSums)
 #pragma unroll
                 for (int i = 0; i < 4; i++) sums[i] += v[i];
@@ -288,7 +300,13 @@ struct Finisher {
         char* at = out + (m * out_rs + n) * size;
         const int64_t down = out_rs * kDown * size;
         float total = 0.0f;   // of a column's dz, which one thread has
+        const float across = FINISH == kScaled ? e.col_scale[n] : 0.0f;
+        const float bias32 = FINISH == kScaled && e.bias32 ? e.bias32[n] : 0.0f;
         auto step = [&](int r, char* p, float z, float u, float o) {
+            if constexpr (FINISH == kScaled) {
+                store1(p, 0, z * (e.row_scale[m0 + r] * across) + bias32 + o, f32, half);
+                return;
+            }
             if (e.pre) {
                 float* pre = e.pre + ((m0 + r) * e.pre_rs + n);
                 *pre = z;
@@ -384,12 +402,20 @@ struct Finisher {
             tmem_load16(v, tmem + (r >> 1) * 2 * kCols + (r & 1) * (PAIR ? sums / 2 : 16));
             tmem_load_wait(v);
 #pragma unroll
-            for (int i = 0; i < 16; i++) sum[r][i] += v[i];
+            for (int i = 0; i < 16; i++) {
+                if (FINISH == kScaled) sum[r][i] = __int_as_float(__float_as_int(sum[r][i]) + __float2int_rn(v[i]));
+                else sum[r][i] += v[i];
+            }
         }
     }
 
-    __device__ __forceinline__ void put_runs(const float (&sum)[8][16], int lane, char* out, int64_t out_rs)
+    __device__ __forceinline__ void put_runs(float (&sum)[8][16], int lane, char* out, int64_t out_rs)
     {
+        if (FINISH == kScaled)   // so far integers
+#pragma unroll
+            for (int r = 0; r < 8; r++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) sum[r][i] = float(__float_as_int(sum[r][i]));
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             const int c0 = turn * kCols + r * 2 * kCols;
