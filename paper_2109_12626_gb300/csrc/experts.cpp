@@ -70,6 +70,8 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
     l.half = operands == DPDR_FLOAT16;
     l.w_int8 = weights == DPDR_INT8;
     l.act = act;
+    l.terms = l.half && !l.w_int8 ? 1 : result == DPDR_FLOAT32 ? 3 : 2;
+    l.pairs = l.rows * top;
     l.normalise = normalise != 0;
     l.out_f32 = result == DPDR_FLOAT32;
     cudaError_t e = cudaGetDevice(&P->device);
@@ -88,7 +90,7 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
             return at;
         };
         const int64_t logits = take(max_rows * experts * 4), x = take(max_rows * l.d_pad * 2),
-                      hidden = take(pairs * l.h_pad * 4), some = take(parts_floats(up_ctas) * 4),
+                      hidden = take(pairs * l.h_pad * (l.terms == 1 ? 4 : 2 * l.terms)), some = take(parts_floats(up_ctas) * 4),
                       z = take(parts * pairs * n_model * 4), up = take(int64_t(up_ctas) * 4), down = take(blocks * 4);
         e = cudaMalloc(&P->scratch, size_t(size));
         // counters at zero, and what lies behind the rows of x and of hidden values
@@ -97,7 +99,7 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
         if (e != cudaSuccess) rc = cuda_fail_c(e, who);
         l.logits = reinterpret_cast<float*>(P->scratch + logits);
         l.x_copy = P->scratch + x;
-        l.hidden = reinterpret_cast<float*>(P->scratch + hidden);
+        l.hidden = P->scratch + hidden;
         l.parts = reinterpret_cast<float*>(P->scratch + some);
         l.z = reinterpret_cast<float*>(P->scratch + z);
         l.up_count = reinterpret_cast<uint32_t*>(P->scratch + up);

@@ -17,8 +17,10 @@
 // order by the last CTA to come.  No CTA waits for another, no sum's order
 // depends on timing.
 //
-// The hidden values stay in float32 (the products split them into two values of
-// 11 bits, stream.cuh), so nothing between x and y is rounded to 16 bits.
+// The hidden values are not rounded to 16 bits: they are kept as terms of bfloat16 that
+// add up to them (two for a 16-bit result: 2^-16 of a value, far below what the
+// result's rounding may be off by; three, which hold all of a float32 value, for a float32
+// result), and for float16 weights as float32.
 #include <algorithm>
 #include <mutex>
 
@@ -36,64 +38,69 @@ constexpr int kScoreWarps = 4;
 
 // ------------------------------------------------------------------ scores
 
-// A warp forms the scores of TOK tokens with one expert, and all warps lay out
-// x's rows.  The products of 16-bit values are exact in float32; a lane sums every
-// 32nd group of 8 and the lanes' sums are added pairwise, so that few roundings
-// lie on top of each other: which experts are chosen hangs on these.
+// A CTA forms the scores of TOK tokens with one expert, and all CTAs lay out x's
+// rows.  The products of 16-bit values are exact in float32; a thread sums every
+// 128th group of 8 and the threads' sums are added pairwise, so that few
+// roundings lie on top of each other: which experts are chosen hangs on these.
+// Bound by a trip to memory: each thread asks for all that it needs at once.
 template <int TOK, bool VEC>
 __global__ void __launch_bounds__(32 * kScoreWarps) scores_kernel(const __grid_constant__ Layer l)
 {
-    const int lane = threadIdx.x & 31;
-    const int groups = (l.rows + TOK - 1) / TOK;
-    const int warps = gridDim.x * kScoreWarps, me = blockIdx.x * kScoreWarps + (threadIdx.x >> 5);
+    __shared__ float part[kScoreWarps][TOK];
+    constexpr int kThreads = 32 * kScoreWarps;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int e = blockIdx.x % l.total, t0 = blockIdx.x / l.total * TOK;
+    const uint16_t* x = reinterpret_cast<const uint16_t*>(l.x);
+    const uint16_t* r = reinterpret_cast<const uint16_t*>(l.router) + e * l.router_rs;
+    if (VEC)   // while the kernel before drains
+        for (int k = 64 * int(threadIdx.x); k < l.d; k += 64 * kThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(r + k));
     wait_previous();
     allow_next();
-    const uint16_t* x = reinterpret_cast<const uint16_t*>(l.x);
-    const uint16_t* router = reinterpret_cast<const uint16_t*>(l.router);
-    for (int unit = me; unit < groups * l.total; unit += warps) {
-        const int e = unit % l.total, t0 = unit / l.total * TOK;
-        const uint16_t* r = router + e * l.router_rs;
-        float acc[TOK] = {};
-        int done = 0;
-        if (VEC) {
-            const int units = l.d / 8;
-            done = units * 8;
-#pragma unroll(TOK == 1 ? 4 : 1)
-            for (int u = lane; u < units; u += 32) {
-                const uint4 a = *reinterpret_cast<const uint4*>(r + 8 * u);
-                float f[2][4];
-                proj::widen4(make_uint4(a.x, a.y, 0, 0), 0, l.half, f[0]);
-                proj::widen4(make_uint4(a.z, a.w, 0, 0), 0, l.half, f[1]);
-                uint4 b[TOK];
+    float acc[TOK] = {};
+    int done = 0;
+    if (VEC) {
+        const int units = l.d / 8;
+        done = units * 8;
+#pragma unroll(TOK == 8 ? 1 : 2)
+        for (int u = threadIdx.x; u < units; u += kThreads) {
+            const uint4 a = *reinterpret_cast<const uint4*>(r + 8 * u);
+            uint4 b[TOK];
 #pragma unroll
-                for (int i = 0; i < TOK; i++)
-                    b[i] = *reinterpret_cast<const uint4*>(x + min(t0 + i, l.rows - 1) * l.x_rs + 8 * u);
+            for (int i = 0; i < TOK; i++)
+                b[i] = *reinterpret_cast<const uint4*>(x + min(t0 + i, l.rows - 1) * l.x_rs + 8 * u);
+            float f[2][4];
+            proj::widen4(make_uint4(a.x, a.y, 0, 0), 0, l.half, f[0]);
+            proj::widen4(make_uint4(a.z, a.w, 0, 0), 0, l.half, f[1]);
 #pragma unroll
-                for (int i = 0; i < TOK; i++) {
-                    float v[2][4];
-                    proj::widen4(make_uint4(b[i].x, b[i].y, 0, 0), 0, l.half, v[0]);
-                    proj::widen4(make_uint4(b[i].z, b[i].w, 0, 0), 0, l.half, v[1]);
+            for (int i = 0; i < TOK; i++) {
+                float v[2][4];
+                proj::widen4(make_uint4(b[i].x, b[i].y, 0, 0), 0, l.half, v[0]);
+                proj::widen4(make_uint4(b[i].z, b[i].w, 0, 0), 0, l.half, v[1]);
 #pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        acc[i] = fmaf(f[0][k], v[0][k], acc[i]);
-                        acc[i] = fmaf(f[1][k], v[1][k], acc[i]);
-                    }
+                for (int k = 0; k < 4; k++) {
+                    acc[i] = fmaf(f[0][k], v[0][k], acc[i]);
+                    acc[i] = fmaf(f[1][k], v[1][k], acc[i]);
                 }
             }
         }
-#pragma unroll(VEC ? 1 : 4)
-        for (int k = done + lane; k < l.d; k += 32) {
-            const float f = proj::widen(r[k * l.router_cs], l.half);
-#pragma unroll
-            for (int i = 0; i < TOK; i++)
-                acc[i] = fmaf(f, proj::widen(x[min(t0 + i, l.rows - 1) * l.x_rs + k * l.x_cs], l.half), acc[i]);
-        }
+    }
+#pragma unroll(VEC || TOK == 8 ? 1 : 4)
+    for (int k = done + int(threadIdx.x); k < l.d; k += kThreads) {
+        const float f = proj::widen(r[k * l.router_cs], l.half);
 #pragma unroll
         for (int i = 0; i < TOK; i++)
+            acc[i] = fmaf(f, proj::widen(x[min(t0 + i, l.rows - 1) * l.x_rs + k * l.x_cs], l.half), acc[i]);
+    }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], o);
-        if (lane == 0)
-            for (int i = 0; i < TOK && t0 + i < l.rows; i++) l.logits[int64_t(t0 + i) * l.total + e] = acc[i];
+    for (int i = 0; i < TOK; i++) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], o);
+        if (lane == 0) part[warp][i] = acc[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < TOK && t0 + int(threadIdx.x) < l.rows) {
+        const int i = threadIdx.x;
+        l.logits[int64_t(t0 + i) * l.total + e] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
     }
     // x by rows of d_pad
     const int64_t units = l.rows * (l.d_pad / 8), apart = int64_t(gridDim.x) * blockDim.x;
@@ -303,18 +310,17 @@ __device__ __forceinline__ void up_units(const Layer& l, const Choice& c, uint32
             int i, row;
             const Unit q = unit(loading, i, row);
             const int n = c.count(i), from = c.from(i);
-            st.load_from(q, [&](int col) -> const char* {
-                return col < n ? l.x_copy + c.order[from + col] / l.top * l.d_pad * size_of(XT) : nullptr;
+            st.load_from(q, [&](int col) {   // columns that there are not repeat the last, for nothing
+                return l.x_copy + c.order[from + min(col, n - 1)] / l.top * l.d_pad * size_of(XT);
             });
         }
     };
-    const char* any = l.x_copy;
-    st.begin(any, next);
+    st.begin(next);
     for (int u = blockIdx.x; u < all; u += gridDim.x) {
         int i, row;
         const Unit q = unit(u, i, row);
         float sum[2][NT][4], v[NT];
-        st.sums(q, sum, any, next);
+        st.sums(q, sum, next);
 #pragma unroll
         for (int n = 0; n < NT; n++) v[n] = join_columns<false>(room, sum[0][n], sum[1][n], warp, lane);
         if (parts > 1) {
@@ -338,17 +344,27 @@ __device__ __forceinline__ void up_units(const Layer& l, const Choice& c, uint32
             const float up = __shfl_down_sync(0xFFFFFFFFu, v[n], 16);
             if (lane < 16 && feature < l.h && col < c.count(i)) {
                 const int pair = c.order[c.from(i) + col];
-                l.hidden[pair * l.h_pad + feature] = act_of(l.act, v[n]) * up * c.share[pair];
+                const float h = act_of(l.act, v[n]) * up * c.share[pair];
+                if (l.terms == 1) {
+                    reinterpret_cast<float*>(l.hidden)[pair * l.h_pad + feature] = h;
+                } else {
+                    uint16_t t[3];
+                    split_bf16(h, l.terms, t);
+                    for (int k = 0; k < l.terms; k++)
+                        reinterpret_cast<uint16_t*>(l.hidden)[(k * int64_t(l.pairs) + pair) * l.h_pad + feature] = t[k];
+                }
             }
         }
     }
 }
 
-template <int WT, int NT, bool SHIFT>
+template <int WT, int NT, bool SHIFT, int TERMS>
 __device__ __forceinline__ void down_units(const Layer& l, const Choice& c, uint32_t ring, float* room, int warp, int lane)
 {
-    using S = Stream<WT, kF32, NT, SHIFT>;
-    S st(ring, warp, lane);
+    // float16 weights take the float32 values, others their terms
+    constexpr int kXT = TERMS == 1 ? kF32 : kBf16;
+    using S = Stream<WT, kXT, NT, SHIFT, TERMS>;
+    S st(ring, warp, lane, l.pairs * l.h_pad * size_of(kXT));
     const int blocks = (l.d + 31) / 32, units = c.entries * blocks;
     const int pieces = (l.h * size_of(WT) + kPiece - 1) / kPiece;
     const int parts = parts_of(units, gridDim.x, pieces), all = units * parts, pairs = l.rows * l.top;
@@ -389,18 +405,17 @@ __device__ __forceinline__ void down_units(const Layer& l, const Choice& c, uint
             int i, row, part;
             const Unit q = unit(loading, i, row, part);
             const int n = c.count(i), from = c.from(i);
-            st.load_from(q, [&](int col) -> const char* {
-                return col < n ? reinterpret_cast<const char*>(l.hidden + c.order[from + col] * l.h_pad) : nullptr;
+            st.load_from(q, [&](int col) {
+                return l.hidden + c.order[from + min(col, n - 1)] * l.h_pad * size_of(kXT);
             });
         }
     };
-    const char* any = reinterpret_cast<const char*>(l.hidden);
-    st.begin(any, next);
+    st.begin(next);
     for (int u = blockIdx.x; u < all; u += gridDim.x) {
         int i, row, part;
         const Unit q = unit(u, i, row, part);
         float sum[2][NT][4];
-        st.sums(q, sum, any, next);
+        st.sums(q, sum, next);
         const int feature = row + lane;
 #pragma unroll
         for (int n = 0; n < NT; n++) {
@@ -451,12 +466,12 @@ __global__ void __launch_bounds__(kThreads, 2) up_kernel(const __grid_constant__
 
 // The choice is made again from the scores, which are there: up_kernel let this
 // kernel start after it had waited for them.
-template <int WT, bool SHIFT>
+template <int WT, bool SHIFT, int TERMS>
 __global__ void __launch_bounds__(kThreads, 2) down_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kMost = WT == kI8 ? 2 : 4;
+    constexpr int kMost = (WT == kI8 ? 2 : 4) / (TERMS == 3 ? 2 : 1);   // eights of columns that the ring has room for
     Choice c(raw + before_choice(SHIFT), l.rows * l.top);
     choose_all(l, c, raw, 8 * kMost, warp, lane);
     if (c.entries == 0) {   // no token chose an expert that is here
@@ -467,9 +482,9 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const __grid_constant
         return;
     }
     float* room = reinterpret_cast<float*>(raw + kWarps * ring_bytes(SHIFT));
-    if (c.columns <= 8) down_units<WT, 1, SHIFT>(l, c, shared_at(raw), room, warp, lane);
-    else if (c.columns <= 16) down_units<WT, 2, SHIFT>(l, c, shared_at(raw), room, warp, lane);
-    else down_units<WT, kMost, SHIFT>(l, c, shared_at(raw), room, warp, lane);
+    if (c.columns <= 8) down_units<WT, 1, SHIFT, TERMS>(l, c, shared_at(raw), room, warp, lane);
+    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS>(l, c, shared_at(raw), room, warp, lane);
+    else down_units<WT, kMost, SHIFT, TERMS>(l, c, shared_at(raw), room, warp, lane);
 }
 
 using Kernel = void (*)(Layer);
@@ -498,12 +513,14 @@ Kernel up_of(const Layer& l, bool shift)
     return shift ? up_kernel<kBf16, kBf16, true> : up_kernel<kBf16, kBf16, false>;
 }
 
-Kernel down_of(const Layer& l, bool shift)
+template <bool SHIFT>
+Kernel down_of(const Layer& l)
 {
-    if (l.w_int8) return shift ? down_kernel<kI8, true> : down_kernel<kI8, false>;
-    if (l.half) return shift ? down_kernel<kF16, true> : down_kernel<kF16, false>;
-    return shift ? down_kernel<kBf16, true> : down_kernel<kBf16, false>;
+    if (l.w_int8) return l.terms == 2 ? down_kernel<kI8, SHIFT, 2> : down_kernel<kI8, SHIFT, 3>;
+    if (l.half) return down_kernel<kF16, SHIFT, 1>;
+    return l.terms == 2 ? down_kernel<kBf16, SHIFT, 2> : down_kernel<kBf16, SHIFT, 3>;
 }
+Kernel down_of(const Layer& l, bool shift) { return shift ? down_of<true>(l) : down_of<false>(l); }
 
 size_t product_smem(const Layer& l, bool shift) { return size_t(before_choice(shift)) + size_t(l.rows) * l.top * 12; }
 
@@ -544,12 +561,12 @@ int launch(const Layer& l, int num_sms, cudaStream_t s)
     const bool vec = l.x_cs == 1 && l.router_cs == 1 && reinterpret_cast<uintptr_t>(l.x) % 16 == 0 &&
                      reinterpret_cast<uintptr_t>(l.router) % 16 == 0 && (l.rows == 1 || l.x_rs % 8 == 0) &&
                      (l.total == 1 || l.router_rs % 8 == 0);
-    const int tok = l.rows == 1 ? 1 : l.rows <= 4 ? 4 : 8;
-    Kernel scores = tok == 1   ? (vec ? scores_kernel<1, true> : scores_kernel<1, false>)
-                    : tok == 4 ? (vec ? scores_kernel<4, true> : scores_kernel<4, false>)
-                               : (vec ? scores_kernel<8, true> : scores_kernel<8, false>);
-    const int units = (l.rows + tok - 1) / tok * l.total;
-    const int grid = std::min((units + kScoreWarps - 1) / kScoreWarps, 8 * num_sms);
+    Kernel scores = nullptr;
+    int tok = 8;
+    if (l.rows == 1) tok = 1, scores = vec ? scores_kernel<1, true> : scores_kernel<1, false>;
+    else if (l.rows <= 16) tok = 4, scores = vec ? scores_kernel<4, true> : scores_kernel<4, false>;
+    else scores = vec ? scores_kernel<8, true> : scores_kernel<8, false>;
+    const int grid = (l.rows + tok - 1) / tok * l.total;
     int rc = proj::launch(scores, dim3(unsigned(grid)), dim3(32 * kScoreWarps), 0, 1, s, "experts' scores", l);
     const bool up = up_shifted(l), down = down_shifted(l);
     if (!rc)

@@ -31,7 +31,10 @@ struct Layer {
     // scratch of the plan
     float* logits;                 // rows by total
     char* x_copy;                  // rows by d_pad, zero behind d
-    float* hidden;                 // rows top by h_pad, zero behind h
+    // rows top by h_pad, zero behind h: terms of bfloat16, an array each of `pairs`
+    // rows (the most that the plan takes), or with terms 1 float32
+    char* hidden;
+    int terms, pairs;
     float* parts;                  // of units whose sum is split
     float* z;                      // the experts' results, before they are added up
     uint32_t* up_count;            // of units, and of blocks of 32 features

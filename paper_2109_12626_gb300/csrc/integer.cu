@@ -70,17 +70,17 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
             int64_t n0;
             int m0;
             const Unit q = unit(loading, n0, m0);
-            st.load_from(q, [&](int col) -> const char* { return m0 + col < r.rows ? r.x + (m0 + col) * r.x_rs : nullptr; });
+            st.load_from(q, [&](int col) { return r.x + min(m0 + col, r.rows - 1) * r.x_rs; });   // past the last, for nothing
         }
     };
-    st.begin(r.x, next);
+    st.begin(next);
     for (int u = blockIdx.x; u < all; u += gridDim.x) {
         int64_t n0;
         int m0;
         const Unit q = unit(u, n0, m0);
         float sum[2][NT][4];
         int v[NT];
-        st.sums(q, sum, r.x, next);
+        st.sums(q, sum, next);
 #pragma unroll
         for (int n = 0; n < NT; n++) v[n] = __float_as_int(join_columns<true>(room, sum[0][n], sum[1][n], warp, lane));
         if (a.parts > 1) {

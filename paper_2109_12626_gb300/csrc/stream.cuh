@@ -23,8 +23,10 @@
 //   8-bit weights and 8-bit columns: both widened to float16; products and sums
 //     below 2^24 are whole numbers that float32 holds exactly, so the sums of 1024
 //     products are added up as integers.
-//   float32 columns: A widened to tf32, exactly, and each column value split into
-//     two of 11 bits (the second cut off, 2^-21 of the value), two products.
+//   columns as terms of bfloat16 that add up to a float32 value: a product each.
+//   float32 columns with float16 weights, which such terms cannot meet: A widened to
+//     tf32, exactly, and each column value split into two of 11 bits (the second
+//     cut off, 2^-21 of the value), two products.
 // SHIFT: rows of A at any address.  The aligned 16 bytes around what a lane needs
 // are loaded, and shifted in registers.  What lies behind the end of a row is
 // never read (cp.async fills up with zeros).
@@ -50,7 +52,6 @@ constexpr int kPiece = 64;              // bytes of a row of A, a stage
 constexpr int ring_bytes(bool shift) { return shift ? 13312 : 12288; }
 
 constexpr int size_of(int kind) { return kind == kI8 ? 1 : kind == kF32 ? 4 : 2; }
-constexpr int elements(int wt) { return kPiece / size_of(wt); }   // of a piece
 
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
 
@@ -58,6 +59,10 @@ __device__ __forceinline__ uint32_t shared_at(const void* p) { return uint32_t(_
 __device__ __forceinline__ void copy16(uint32_t to, const char* from, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const char* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
@@ -117,35 +122,25 @@ __device__ __forceinline__ void bytes_to_bf16(uint32_t v, uint32_t& a, uint32_t&
     b = part(hi);
 }
 
-// and as float32, 2^23 + (v + 128)
-__device__ __forceinline__ void bytes_to_f32(uint32_t v, float (&f)[4])
-{
-    v ^= 0x80808080u;
-    constexpr float off = 8388608.0f + 128.0f;
-    f[0] = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7650)) - off;
-    f[1] = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7651)) - off;
-    f[2] = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7652)) - off;
-    f[3] = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7653)) - off;
-}
-
 // ---------------------------------------------------- matrix instructions
 
+// d = a b + c
 template <int XT>
-__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                      uint32_t b1)
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                      uint32_t b1, float c0, float c1, float c2, float c3)
 {
     if (XT == kBf16)
         asm volatile(
             "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-            "{%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+            "{%10, %11, %12, %13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
     else
         asm volatile(
             "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-            "{%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+            "{%10, %11, %12, %13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
 __device__ __forceinline__ void mma_tf32(float (&c)[4], float a0, float a1, float a2, float a3, float b0, float b1)
@@ -166,115 +161,175 @@ __device__ __forceinline__ void split_tf32(float h, float& hi, float& lo)
     lo = (top & 0x7F800000u) == 0x7F800000u ? 0.0f : h - hi;
 }
 
+// h as bfloat16 values that add up to it: of two terms the first 8 bits and the
+// rest rounded (2^-16 of h), of three all 24 bits.  Infinities and NaN have one.
+__device__ __forceinline__ void split_bf16(float h, int terms, uint16_t (&t)[3])
+{
+    const uint32_t b = __float_as_uint(h);
+    t[0] = uint16_t(b >> 16);
+    t[1] = t[2] = 0;
+    if ((b & 0x7F800000u) == 0x7F800000u) {
+        if (h != h) t[0] |= 0x40;   // the bit that tells may be among those cut off
+        return;
+    }
+    const float r = h - __uint_as_float(b & 0xFFFF0000u);
+    if (terms == 2) {
+        t[1] = __bfloat16_as_ushort(__float2bfloat16_rn(r));
+    } else {
+        const uint32_t c = __float_as_uint(r);
+        t[1] = uint16_t(c >> 16);
+        t[2] = uint16_t(__float_as_uint(r - __uint_as_float(c & 0xFFFF0000u)) >> 16);
+    }
+}
+
 // ---------------------------------------------------------------- a unit
 
 // Where a unit's operands lie.  A's row r (0 .. 31) is row r of the first 16 at
-// a[0], the others at a[1]; rows past rows_left[.] are zero.
+// a[0], the others at a[1].  Rows past rows_left[.] repeat the last, for nothing
+// that is used; of none the others are taken.
 struct Unit {
     const char* a[2];
     int64_t a_stride[2];     // bytes from row to row
-    int rows_left[2];        // rows that there are, of 16
+    int rows_left[2];        // rows that there are, of 16; rows_left[0] >= 1
     int row_bytes;
     int first, last;         // pieces along k
+    __device__ __forceinline__ const char* row(int r) const
+    {
+        const int in = r & 15;
+        if (r >= 16 && rows_left[1] > 0) return a[1] + min(in, rows_left[1] - 1) * a_stride[1];
+        return a[0] + min(in, rows_left[0] - 1) * a_stride[0];
+    }
 };
 
-template <int WT, int XT, int NT, bool SHIFT>
+// TERMS: a column's values are the sums of so many, whose arrays lie `apart`
+// bytes from each other.
+template <int WT, int XT, int NT, bool SHIFT, int TERMS = 1>
 struct Stream {
-    static constexpr int kK = elements(WT);              // of a piece
-    static constexpr int kAPitch = SHIFT ? kPiece + 16 : kPiece;
+    static constexpr int kParts = kPiece / 64;           // a lane has 16 bytes of a row in each
+    static constexpr int kK = 64 / size_of(WT);          // elements of a part
+    static constexpr int kAChunks = kPiece / 16 + SHIFT; // 16-byte chunks of a row
+    static constexpr int kAPitch = 16 * kAChunks;
     static constexpr int kABytes = kRows * kAPitch;
-    static constexpr int kB = kK * size_of(XT);          // bytes of a column, a piece
-    static constexpr int kChunks = kB / 16;              // 16-byte pieces of it
-    static constexpr int kBLoads = 8 * kChunks / 32;     // of a lane, for 8 columns
-    static constexpr int kALoads = SHIFT ? 5 : 4;
-    static constexpr int kStage = kABytes + NT * 8 * kB;
+    static constexpr int kB = kParts * kK * size_of(XT); // bytes of a column, a piece
+    static constexpr int kBChunks = kB / 16;
+    static constexpr int kBLoads = 8 * kBChunks / 32;    // of a lane, for 8 columns
+    static constexpr int kALoads = kAChunks;
+    static constexpr int kBTerm = NT * 8 * kB;
+    static constexpr int kStage = kABytes + TERMS * kBTerm;
     static constexpr int kStages = ring_bytes(SHIFT) / kStage > 5 ? 5 : ring_bytes(SHIFT) / kStage;
     static constexpr int kWarpBytes = kStages * kStage;
     static_assert(kStages >= 2, "the ring holds two stages");
     static constexpr bool kWhole = XT == kI8;            // sums are integers
-    static constexpr int kRun = 1024 / kK;               // pieces whose products float32 sums exactly
+    static constexpr int kRun = 1024 / (kParts * kK);    // pieces whose products float32 sums exactly
 
     const int lane, warp;
     const uint32_t ring;
     // loading side
     const char* a_at[kALoads];
-    int a_left[kALoads];     // bytes of the row from there on; 0: no such row
-    const char* b_at[NT][kBLoads];
-    uint32_t b_there;        // which of them there are
-    int load_piece, load_last, load_stage;
+    const char* b_at[NT * kBLoads];
+    int64_t apart;
+    int load_piece, load_last, load_whole;   // pieces before load_whole are inside every row
+    int load_bytes, load_shift;              // of a row
+    uint32_t load_to, load_end;
     // using side
-    int use_stage;
+    uint32_t use_from_here;
     int shift[2][2];         // of this lane's rows
 
-    __device__ __forceinline__ Stream(uint32_t ring_of_cta, int w, int l)
-        : lane(l), warp(w), ring(ring_of_cta + w * kWarpBytes), load_piece(0), load_last(0), load_stage(0), use_stage(0)
+    __device__ __forceinline__ Stream(uint32_t ring_of_cta, int w, int l, int64_t terms_apart = 0)
+        : lane(l),
+          warp(w),
+          ring(ring_of_cta + w * kWarpBytes),
+          apart(terms_apart),
+          load_piece(0),
+          load_last(0),
+          load_to(ring),
+          load_end(ring + kWarpBytes),
+          use_from_here(ring)
     {
     }
 
-    // The loading side turns to a unit.  column(c): address of column c's values,
-    // nullptr for none; whole pieces of it can be read.
+    // the row and chunk of a lane's i-th 16 bytes of A
+    __device__ __forceinline__ int a_row(int i) const { return (lane + 32 * i) / kAChunks; }
+    __device__ __forceinline__ int a_chunk(int i) const { return (lane + 32 * i) % kAChunks; }
+
+    // The loading side turns to a unit.  column(c): address of column c's values, for
+    // any c; whole pieces of it can be read.
     template <typename Column>
     __device__ __forceinline__ void load_from(const Unit& u, Column column)
     {
+        load_piece = u.first + warp;
+        load_last = u.last;
+        load_bytes = u.row_bytes;
+        load_whole = (u.row_bytes - (SHIFT ? 16 : 0)) / kPiece;
 #pragma unroll
         for (int i = 0; i < kALoads; i++) {
-            const int id = lane + 32 * i, row = SHIFT ? id / 5 : id >> 2, c = SHIFT ? id % 5 : id & 3;
-            const bool second = row >= 16;
-            const int in = row & 15;
-            const char* p = (second ? u.a[1] : u.a[0]) + in * (second ? u.a_stride[1] : u.a_stride[0]);
-            const int o = SHIFT ? int(reinterpret_cast<uintptr_t>(p) & 15) : 0;
-            const bool there = in < (second ? u.rows_left[1] : u.rows_left[0]);
-            a_at[i] = there ? p - o + 16 * c : nullptr;
-            a_left[i] = there ? u.row_bytes - 16 * c + o : 0;
+            const char* p = u.row(a_row(i)) + load_piece * kPiece + 16 * a_chunk(i);
+            a_at[i] = SHIFT ? p - int(reinterpret_cast<uintptr_t>(p) & 15) : p;
         }
-        b_there = 0;
 #pragma unroll
         for (int n = 0; n < NT; n++)
 #pragma unroll
             for (int j = 0; j < kBLoads; j++) {
                 const int id = lane + 32 * j;
-                const char* p = column(n * 8 + id / kChunks);
-                b_at[n][j] = p + 16 * (id % kChunks);
-                if (p) b_there |= 1u << (n * kBLoads + j);
+                b_at[n * kBLoads + j] = column(n * 8 + id / kBChunks) + load_piece * kB + 16 * (id % kBChunks);
             }
-        load_piece = u.first + warp;
-        load_last = u.last;
+        if (SHIFT) {   // what the last pieces have to know of each row
+            load_shift = 0;
+#pragma unroll
+            for (int i = 0; i < kALoads && i < 8; i++)
+                load_shift |= int(reinterpret_cast<uintptr_t>(u.row(a_row(i))) & 15) << 4 * i;
+            if (kALoads > 8) load_last_shift = int(reinterpret_cast<uintptr_t>(u.row(a_row(kALoads - 1))) & 15);
+        }
     }
+    int load_last_shift;
 
     __device__ __forceinline__ bool more() const { return load_piece < load_last; }
 
-    // where chunk c of column row r lies: no bank is met twice by the eight lanes
-    // that a 16-byte access takes together
+    // Where chunk c of column r's piece lies: no bank is met twice by the eight lanes
+    // that a 16-byte access takes together, which have two columns next to each other
+    // and chunks kBChunks / 4 / kParts apart.
     static __device__ __forceinline__ int b_place(int r, int c)
     {
-        if (kChunks == 4) return r * kB + 16 * c;
-        if (kChunks == 8) return r * kB + 16 * (c ^ (r & 1));
+        constexpr int kApart = kBChunks / kParts / 4;   // chunks of a lane in a part
+        if (kApart == 1) return r * kB + 16 * (kParts == 1 ? c : c ^ ((r & 1) << 2));
+        if (kApart == 2) return r * kB + 16 * (c ^ (r & 1));
         return r * kB + 16 * (c ^ ((c >> 3) & 1) ^ ((r & 1) << 1));
     }
-
-    // `any`: an address that can be read, for copies of nothing
-    __device__ __forceinline__ void load(const char* any)
+    static __device__ __forceinline__ int a_place(int r, int c)
     {
-        const uint32_t to = ring + load_stage * kStage;
-        const int off = load_piece * kPiece;
+        return r * kAPitch + 16 * (SHIFT || kParts == 1 ? c : c ^ ((r & 1) << 2));
+    }
+
+    __device__ __forceinline__ void load()
+    {
+        if (load_piece < load_whole) {
 #pragma unroll
-        for (int i = 0; i < kALoads; i++) {
-            const int id = lane + 32 * i, row = SHIFT ? id / 5 : id >> 2, c = SHIFT ? id % 5 : id & 3;
-            const int bytes = max(0, min(16, a_left[i] - off));
-            copy16(to + row * kAPitch + 16 * c, bytes > 0 ? a_at[i] + off : any, bytes);
+            for (int i = 0; i < kALoads; i++) copy16(load_to + a_place(a_row(i), a_chunk(i)), a_at[i]);
+        } else {
+            const int left = load_bytes - load_piece * kPiece;
+#pragma unroll
+            for (int i = 0; i < kALoads; i++) {
+                const int o = SHIFT ? (i < 8 ? load_shift >> 4 * i & 15 : load_last_shift) : 0;
+                const int bytes = max(0, min(16, left + o - 16 * a_chunk(i)));
+                // of none, the address of the row's first bytes in this piece
+                copy16(load_to + a_place(a_row(i), a_chunk(i)), a_at[i] - (bytes > 0 ? 0 : 16 * a_chunk(i)), bytes);
+            }
         }
-        const int64_t b_off = int64_t(load_piece) * kB;
+#pragma unroll
+        for (int i = 0; i < kALoads; i++) a_at[i] += kWarps * kPiece;
 #pragma unroll
         for (int n = 0; n < NT; n++)
 #pragma unroll
             for (int j = 0; j < kBLoads; j++) {
                 const int id = lane + 32 * j;
-                const bool there = b_there >> (n * kBLoads + j) & 1;
-                copy16(to + kABytes + b_place(n * 8 + id / kChunks, id % kChunks), there ? b_at[n][j] + b_off : any,
-                       there ? 16 : 0);
+                const uint32_t to = load_to + kABytes + b_place(n * 8 + id / kBChunks, id % kBChunks);
+#pragma unroll
+                for (int t = 0; t < TERMS; t++) copy16(to + t * kBTerm, b_at[n * kBLoads + j] + t * apart);
+                b_at[n * kBLoads + j] += kWarps * kB;
             }
         load_piece += kWarps;
-        if (++load_stage == kStages) load_stage = 0;
+        load_to += kStage;
+        if (load_to == load_end) load_to = ring;
     }
 
     __device__ __forceinline__ void use_from(const Unit& u)
@@ -284,51 +339,46 @@ struct Stream {
             for (int i = 0; i < 2; i++)
 #pragma unroll
                 for (int h = 0; h < 2; h++)
-                    shift[i][h] = int((reinterpret_cast<uintptr_t>(u.a[i]) + (lane / 4 + 8 * h) * u.a_stride[i]) & 15);
+                    shift[i][h] = int(reinterpret_cast<uintptr_t>(u.row(16 * i + lane / 4 + 8 * h)) & 15);
     }
 
-    __device__ __forceinline__ uint4 a_lane(uint32_t at, int i, int h) const
+    __device__ __forceinline__ uint4 a_lane(uint32_t at, int part, int i, int h) const
     {
-        const uint32_t p = at + (i * 16 + h * 8 + lane / 4) * kAPitch + 16 * (lane & 3);
-        return SHIFT ? shifted(load16(p), load16(p + 16), shift[i][h]) : load16(p);
+        const int r = i * 16 + h * 8 + lane / 4, c = 4 * part + (lane & 3);
+        if (SHIFT) return shifted(load16(at + a_place(r, c)), load16(at + a_place(r, c + 1)), shift[i][h]);
+        return load16(at + a_place(r, c));
     }
 
-    // One piece's products
-    __device__ __forceinline__ void use(float (&acc)[2][NT][4])
+    // One piece's products, added to the sums; of whole numbers to the run's
+    __device__ __forceinline__ void use(float (&sum)[2][NT][4])
     {
-        const uint32_t at = ring + use_stage * kStage, b0 = at + kABytes;
+        const uint32_t at = use_from_here, b0 = at + kABytes;
         const int g = lane / 4, t = lane & 3;
-        if (++use_stage == kStages) use_stage = 0;
+        use_from_here += kStage;
+        if (use_from_here == load_end) use_from_here = ring;
         if constexpr (XT == kF32) {
-            constexpr int kEach = kK / 4;   // elements of a lane
+            // 11 and 11 bits of a column's values, each with sums of its own
+            static_assert(WT == kF16, "other weights take terms of bfloat16");
+            float high[2][NT][4], low[2][NT][4];
 #pragma unroll
-            for (int part = 0; part < kEach / 8; part++) {   // eight elements at a time
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int n = 0; n < NT; n++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) high[i][n][q] = low[i][n][q] = 0.0f;
+#pragma unroll
+            for (int part = 0; part < kParts; part++) {
                 float a[2][2][8];
 #pragma unroll
                 for (int i = 0; i < 2; i++)
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
-                        const uint4 v = a_lane(at, i, h);
-                        if (WT == kI8) {
-                            float f[4];
-                            bytes_to_f32(part ? v.z : v.x, f);
+                        const uint4 v = a_lane(at, part, i, h);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int k = 0; k < 4; k++) a[i][h][k] = f[k];
-                            bytes_to_f32(part ? v.w : v.y, f);
-#pragma unroll
-                            for (int k = 0; k < 4; k++) a[i][h][4 + k] = f[k];
-                        } else {
-                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                            for (int k = 0; k < 4; k++) {
-                                if (WT == kF16) {
-                                    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-                                    a[i][h][2 * k] = p.x, a[i][h][2 * k + 1] = p.y;
-                                } else {
-                                    a[i][h][2 * k] = __uint_as_float(w[k] << 16);
-                                    a[i][h][2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-                                }
-                            }
+                        for (int k = 0; k < 4; k++) {
+                            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                            a[i][h][2 * k] = p.x, a[i][h][2 * k + 1] = p.y;
                         }
                     }
 #pragma unroll
@@ -336,97 +386,129 @@ struct Stream {
                     float hi[8], lo[8];
 #pragma unroll
                     for (int q = 0; q < 2; q++) {
-                        const uint4 v = load16(b0 + b_place(n * 8 + g, kEach / 4 * t + 2 * part + q));
+                        const uint4 v = load16(b0 + b_place(n * 8 + g, 8 * part + 2 * t + q));
                         split_tf32(__uint_as_float(v.x), hi[4 * q], lo[4 * q]);
                         split_tf32(__uint_as_float(v.y), hi[4 * q + 1], lo[4 * q + 1]);
                         split_tf32(__uint_as_float(v.z), hi[4 * q + 2], lo[4 * q + 2]);
                         split_tf32(__uint_as_float(v.w), hi[4 * q + 3], lo[4 * q + 3]);
                     }
 #pragma unroll
-                    for (int i = 0; i < 2; i++)
+                    for (int s = 0; s < 4; s++)
 #pragma unroll
-                        for (int s = 0; s < 4; s++) {
-                            mma_tf32(acc[i][n], a[i][0][2 * s], a[i][1][2 * s], a[i][0][2 * s + 1], a[i][1][2 * s + 1],
+                        for (int i = 0; i < 2; i++) {
+                            mma_tf32(low[i][n], a[i][0][2 * s], a[i][1][2 * s], a[i][0][2 * s + 1], a[i][1][2 * s + 1],
                                      lo[2 * s], lo[2 * s + 1]);
-                            mma_tf32(acc[i][n], a[i][0][2 * s], a[i][1][2 * s], a[i][0][2 * s + 1], a[i][1][2 * s + 1],
+                            mma_tf32(high[i][n], a[i][0][2 * s], a[i][1][2 * s], a[i][0][2 * s + 1], a[i][1][2 * s + 1],
                                      hi[2 * s], hi[2 * s + 1]);
                         }
                 }
             }
-        } else {
-            // words of two elements: four a lane and row, of 8-bit weights eight
-            constexpr int kWords = kK / 8;
-            uint32_t a[2][2][kWords];
 #pragma unroll
             for (int i = 0; i < 2; i++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const uint4 v = a_lane(at, i, h);
-                    if constexpr (WT == kI8) {
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                for (int n = 0; n < NT; n++)
 #pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            if (XT == kBf16) bytes_to_bf16(w[k], a[i][h][2 * k], a[i][h][2 * k + 1]);
-                            else bytes_to_f16(w[k], a[i][h][2 * k], a[i][h][2 * k + 1]);
-                        }
-                    } else {
-                        a[i][h][0] = v.x, a[i][h][1] = v.y, a[i][h][2] = v.z, a[i][h][3] = v.w;
-                    }
-                }
+                    for (int q = 0; q < 4; q++) sum[i][n][q] += high[i][n][q] + low[i][n][q];
+        } else {
+            // words of two elements: four a lane and row, of 8-bit weights eight
+            constexpr int kWords = kK / 8;
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
-                uint32_t b[kWords];
-                if constexpr (XT == kI8) {
-                    const uint4 v = load16(b0 + b_place(n * 8 + g, t));
-                    bytes_to_f16(v.x, b[0], b[1]);
-                    bytes_to_f16(v.y, b[2], b[3]);
-                    bytes_to_f16(v.z, b[4], b[5]);
-                    bytes_to_f16(v.w, b[6], b[7]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < kWords / 4; q++) {
-                        const uint4 v = load16(b0 + b_place(n * 8 + g, kWords / 4 * t + q));
-                        b[4 * q] = v.x, b[4 * q + 1] = v.y, b[4 * q + 2] = v.z, b[4 * q + 3] = v.w;
-                    }
-                }
+            for (int part = 0; part < kParts; part++) {
+                uint32_t a[2][2][kWords];
 #pragma unroll
                 for (int i = 0; i < 2; i++)
 #pragma unroll
-                    for (int s = 0; s < kWords / 2; s++)
-                        mma16<XT>(acc[i][n], a[i][0][2 * s], a[i][1][2 * s], a[i][0][2 * s + 1], a[i][1][2 * s + 1],
-                                  b[2 * s], b[2 * s + 1]);
+                    for (int h = 0; h < 2; h++) {
+                        const uint4 v = a_lane(at, part, i, h);
+                        if constexpr (WT == kI8) {
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int k = 0; k < 4; k++) {
+                                if (XT == kBf16) bytes_to_bf16(w[k], a[i][h][2 * k], a[i][h][2 * k + 1]);
+                                else bytes_to_f16(w[k], a[i][h][2 * k], a[i][h][2 * k + 1]);
+                            }
+                        } else {
+                            a[i][h][0] = v.x, a[i][h][1] = v.y, a[i][h][2] = v.z, a[i][h][3] = v.w;
+                        }
+                    }
+#pragma unroll
+                for (int n = 0; n < NT; n++) {
+                    // a chain of products for each of the two groups of rows
+                    float d[2][4];
+                    bool first = !kWhole;
+#pragma unroll
+                    for (int term = TERMS - 1; term >= 0; term--) {   // the smallest first
+                        uint32_t b[kWords];
+                        if constexpr (XT == kI8) {
+                            const uint4 v = load16(b0 + b_place(n * 8 + g, 4 * part + t));
+                            bytes_to_f16(v.x, b[0], b[1]);
+                            bytes_to_f16(v.y, b[2], b[3]);
+                            bytes_to_f16(v.z, b[4], b[5]);
+                            bytes_to_f16(v.w, b[6], b[7]);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < kWords / 4; q++) {
+                                const uint4 v =
+                                    load16(b0 + term * kBTerm + b_place(n * 8 + g, kWords * part + kWords / 4 * t + q));
+                                b[4 * q] = v.x, b[4 * q + 1] = v.y, b[4 * q + 2] = v.z, b[4 * q + 3] = v.w;
+                            }
+                        }
+#pragma unroll
+                        for (int s = 0; s < kWords / 2; s++)
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                float(&c)[4] = kWhole ? sum[i][n] : d[i];
+                                const bool zero = first && s == 0;
+                                mma16<XT>(c, a[i][0][2 * s], a[i][1][2 * s], a[i][0][2 * s + 1], a[i][1][2 * s + 1],
+                                          b[2 * s], b[2 * s + 1], zero ? 0.0f : c[0], zero ? 0.0f : c[1],
+                                          zero ? 0.0f : c[2], zero ? 0.0f : c[3]);
+                            }
+                        first = false;
+                    }
+                    if (!kWhole)
+#pragma unroll
+                        for (int i = 0; i < 2; i++)
+#pragma unroll
+                            for (int q = 0; q < 4; q++) sum[i][n][q] += d[i][q];
+                }
             }
         }
     }
 
     // This warp's sums over its pieces of unit u.  next(): the loading side turns
-    // to the unit behind the one that it is at, if there is one.
+    // to a unit behind the one that it is at, if there is one with a piece for it.
+    // The instructions cut sums off, so each part's products are summed by
+    // themselves and added up rounded.
     template <typename Next>
-    __device__ __forceinline__ void sums(const Unit& u, float (&total)[2][NT][4], const char* any, Next next)
+    __device__ __forceinline__ void sums(const Unit& u, float (&total)[2][NT][4], Next next)
     {
         use_from(u);
-        float acc[2][NT][4];
+        float run[2][NT][4];   // of whole numbers
 #pragma unroll
         for (int i = 0; i < 2; i++)
 #pragma unroll
             for (int n = 0; n < NT; n++)
 #pragma unroll
-                for (int q = 0; q < 4; q++) acc[i][n][q] = total[i][n][q] = 0.0f;
-        int run = 0;
+                for (int q = 0; q < 4; q++) run[i][n][q] = total[i][n][q] = 0.0f;
+        int done = 0;
         for (int piece = u.first + warp; piece < u.last; piece += kWarps) {
             copies_wait<kStages - 2>();
             __syncwarp();   // every lane's copies are there, and the stage before is free
             if (!more()) next();
-            if (more()) load(any);
+            if (more()) load();
             copies_group();
-            use(acc);
-            if (kWhole && ++run == kRun) run = 0, take(acc, total);
+            if (kWhole) {
+                use(run);
+                if (++done == kRun) done = 0, take(run, total);
+            } else {
+                use(total);
+            }
         }
-        take(acc, total);
+        if (kWhole) take(run, total);
     }
 
-    // sums of a run to the total
-    static __device__ __forceinline__ void take(float (&acc)[2][NT][4], float (&total)[2][NT][4])
+    // whole numbers of a run to the total, which is held as integers
+    static __device__ __forceinline__ void take(float (&run)[2][NT][4], float (&total)[2][NT][4])
     {
 #pragma unroll
         for (int i = 0; i < 2; i++)
@@ -434,23 +516,19 @@ struct Stream {
             for (int n = 0; n < NT; n++)
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
-                    if (kWhole)
-                        total[i][n][q] =
-                            __int_as_float(__float_as_int(total[i][n][q]) + __float2int_rn(acc[i][n][q]));
-                    else
-                        total[i][n][q] += acc[i][n][q];
-                    acc[i][n][q] = 0.0f;
+                    total[i][n][q] = __int_as_float(__float_as_int(total[i][n][q]) + __float2int_rn(run[i][n][q]));
+                    run[i][n][q] = 0.0f;
                 }
     }
 
     // fills the ring ahead of the first unit
     template <typename Next>
-    __device__ __forceinline__ void begin(const char* any, Next next)
+    __device__ __forceinline__ void begin(Next next)
     {
 #pragma unroll
         for (int i = 0; i < kStages - 1; i++) {
             if (!more()) next();
-            if (more()) load(any);
+            if (more()) load();
             copies_group();
         }
     }
