@@ -50,6 +50,11 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
     if (weights != operands && weights != DPDR_INT8) return bad("weights have the operands' type or int8");
     if (result != operands && result != DPDR_FLOAT32) return bad("the result has the operands' type or float32");
     if (act < DPDR_ACT_NONE || act > DPDR_ACT_SIGMOID) return bad("unknown activation");
+    // pieces of 64 bytes that the warps share, counted in 32 bits
+    const int64_t pairs_most = max_rows * top, entries = std::min<int64_t>(local, pairs_most) + pairs_most / 8;
+    if (entries * ((n_hidden + 15) / 16) * (n_model / 32 + 1) > (int64_t(1) << 30) ||
+        entries * ((n_model + 31) / 32) * (n_hidden / 32 + 1) > (int64_t(1) << 30))
+        return bad("more than 2^30 pieces of weights");
     Experts* P = new (std::nothrow) Experts;
     if (!P) {
         fail_c(DPDR_ERR_OOM, "experts plan: host allocation");
@@ -79,10 +84,9 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
     int rc = e == cudaSuccess ? product_ctas(l, P->num_sms) : cuda_fail_c(e, who);
     if (!rc) {
         const int64_t pairs = max_rows * top;
-        // parts that a down unit's sum may be cut into, and results of each
-        const int64_t blocks = (n_model + 31) / 32;
-        const int up_ctas = std::max(l.up_ctas[0], l.up_ctas[1]), down_ctas = std::max(l.down_ctas[0], l.down_ctas[1]);
-        const int64_t parts = std::max<int64_t>(1, down_ctas / blocks);
+        const int64_t up_warps = 8 * std::max(l.up_ctas[0], l.up_ctas[1]), down_warps = 8 * std::max(l.down_ctas[0], l.down_ctas[1]);
+        // two places a warp, of 32 rows by as many columns as an entry may have
+        const int64_t places = 2 * std::max(up_warps, down_warps) * 32 * (max_rows <= 8 ? 8 : max_rows <= 16 ? 16 : 32);
         int64_t size = 0;
         auto take = [&](int64_t bytes) {
             const int64_t at = size;
@@ -90,8 +94,9 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
             return at;
         };
         const int64_t logits = take(max_rows * experts * 4), x = take(max_rows * l.d_pad * 2),
-                      hidden = take(pairs * l.h_pad * (l.terms == 1 ? 4 : 2 * l.terms)), some = take(parts_floats(up_ctas) * 4),
-                      z = take(parts * pairs * n_model * 4), up = take(int64_t(up_ctas) * 4), down = take(blocks * 4);
+                      hidden = take(pairs * l.h_pad * (l.terms == 1 ? 4 : 2 * l.terms)), some = take(places * 4),
+                      z = take(max_rows <= kWholeRows ? 0 : pairs * n_model * 4), expert = take(pairs * 4),
+                      up = take(up_warps * 4), down = take(down_warps * 4);
         e = cudaMalloc(&P->scratch, size_t(size));
         // counters at zero, and what lies behind the rows of x and of hidden values
         if (e == cudaSuccess) e = cudaMemset(P->scratch, 0, size_t(size));
@@ -102,6 +107,7 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
         l.hidden = P->scratch + hidden;
         l.parts = reinterpret_cast<float*>(P->scratch + some);
         l.z = reinterpret_cast<float*>(P->scratch + z);
+        l.expert = reinterpret_cast<int32_t*>(P->scratch + expert);
         l.up_count = reinterpret_cast<uint32_t*>(P->scratch + up);
         l.down_count = reinterpret_cast<uint32_t*>(P->scratch + down);
     }

@@ -11,11 +11,16 @@
 // others waiting for it), then stream the chosen experts' gate and up weights
 // past the tokens that chose them (stream.cuh), a unit being 16 hidden features
 // of an expert; down_kernel does the same with the down weights, a unit being 32
-// features of the result of one expert, and the last CTA of those 32 features
-// adds up what each token's experts gave, in the order of their shares.  Where there are
-// fewer units than CTAs a unit's sum is split along k, and the parts joined in
-// order by the last CTA to come.  No CTA waits for another, no sum's order
-// depends on timing.
+// features of the result.  Up to 8 tokens have a column each there, and the sum runs
+// through all experts; more have their results by expert, which combine_kernel
+// adds up in the order of the shares.
+//
+// All pieces of all units are dealt out to the warps in equal contiguous shares.
+// A unit that lies in several shares is finished by the last of its warps to
+// come, which adds up their sums in order: no warp waits for another, no barrier
+// follows the choice, no sum's order depends on timing.  (A CTA a unit, its sum over
+// eight warps, with two barriers and a fence each: 8 rows of 64 experts of 2048 x
+// 1024 125 us.)
 //
 // The hidden values are not rounded to 16 bits: they are kept as terms of bfloat16 that
 // add up to them (two for a 16-bit result: 2^-16 of a value, far below what the
@@ -262,14 +267,6 @@ __device__ void choose_all(const Layer& l, Choice& c, char* room, int most, int 
 
 // ---------------------------------------------------------------- products
 
-// How many parts a unit's sum is cut into: as many CTAs as there are, while a
-// warp keeps two pieces
-__device__ __forceinline__ int parts_of(int units, int ctas, int pieces)
-{
-    if (units == 0) return 1;
-    return max(1, min(ctas / units, pieces / (2 * kWarps)));
-}
-
 __device__ __forceinline__ float act_of(int act, float z)
 {
     float v = z;
@@ -279,189 +276,284 @@ __device__ __forceinline__ float act_of(int act, float z)
     return v;
 }
 
-template <int WT, int XT, int NT, bool SHIFT>
-__device__ __forceinline__ void up_units(const Layer& l, const Choice& c, uint32_t ring, float* room, int warp, int lane)
+// The warps that share `total` pieces: all, while each has a few
+__device__ __forceinline__ Shares shares_of(int total, int each)
 {
-    using S = Stream<WT, XT, NT, SHIFT>;
-    S st(ring, warp, lane);
-    const int blocks = (l.h + 15) / 16, units = c.entries * blocks;
-    const int pieces = (l.d * size_of(WT) + kPiece - 1) / kPiece;
-    const int parts = parts_of(units, gridDim.x, pieces), all = units * parts;
-    auto unit = [&](int u, int& i, int& row) {
-        const int part = u % parts, b = u / parts;
-        i = b / blocks;
-        row = (b - i * blocks) * 16;
-        Unit q;
-        const int64_t e = c.number(i);
-        for (int k = 0; k < 2; k++)
-            q.a[k] = static_cast<const char*>(l.w[k].data) + (e * l.w[k].stride + row * l.w[k].row_stride) * size_of(WT);
-        q.a_stride[0] = l.w[0].row_stride * size_of(WT);
-        q.a_stride[1] = l.w[1].row_stride * size_of(WT);
-        q.rows_left[0] = q.rows_left[1] = min(16, l.h - row);
-        q.row_bytes = l.d * size_of(WT);
-        q.first = int(int64_t(pieces) * part / parts);
-        q.last = int(int64_t(pieces) * (part + 1) / parts);
-        return q;
-    };
-    int loading = int(blockIdx.x) - int(gridDim.x);
+    return Shares(total, max(1, min(int(gridDim.x) * kWarps, total / kLeast)), each);
+}
+
+// What a warp does with its share: job.part(i) is unit i % ... the i-th run of
+// `each` pieces along k, job.parts of them a unit; job.columns(i) where its columns
+// lie; job.finish(u, sums).
+template <typename S, int NT, typename Job>
+__device__ __forceinline__ void run_share(S& st, const Job& job, int each, const Layer& l, int lane, int id)
+{
+    const Shares s = shares_of(job.units * job.parts * each, job.parts * each);
+    if (id >= s.of) return;
+    int at = s.start(id);
+    const int end = s.start(id + 1);
+    int loading = at;
     auto next = [&]() {
-        while (!st.more() && loading + int(gridDim.x) < all) {
-            loading += gridDim.x;
-            int i, row;
-            const Unit q = unit(loading, i, row);
-            const int n = c.count(i), from = c.from(i);
-            st.load_from(q, [&](int col) {   // columns that there are not repeat the last, for nothing
-                return l.x_copy + c.order[from + min(col, n - 1)] / l.top * l.d_pad * size_of(XT);
-            });
-        }
+        if (loading >= end) return;
+        const int i = loading / each, to = min(end, (i + 1) * each);
+        st.load_from(job.part(i, loading - i * each, to - i * each), job.columns(i));
+        loading = to;
     };
     st.begin(next);
-    for (int u = blockIdx.x; u < all; u += gridDim.x) {
-        int i, row;
-        const Unit q = unit(u, i, row);
-        float sum[2][NT][4], v[NT];
-        st.sums(q, sum, next);
+    while (at < end) {
+        const int u = at / s.each, from = at, to = min(end, (u + 1) * s.each);
+        float sum[2][NT][4];
+        S::clear(sum);
+        while (at < to) {
+            const int i = at / each, there = min(to, (i + 1) * each);
+            const Unit q = job.part(i, at - i * each, there - i * each);
+            if constexpr (Job::kScales) {   // of this part's rows
+                float part[2][NT][4], by[4];
+                S::clear(part);
+                st.sums(q, part, next);
+                job.scales(i, by);
 #pragma unroll
-        for (int n = 0; n < NT; n++) v[n] = join_columns<false>(room, sum[0][n], sum[1][n], warp, lane);
-        if (parts > 1) {
-            float* mine = l.parts + (int64_t(u) * NT) * kThreads + threadIdx.x;
+                for (int k = 0; k < 2; k++)
 #pragma unroll
-            for (int n = 0; n < NT; n++) mine[n * kThreads] = v[n];
-            if (!last_to_come(l.up_count + u / parts, parts)) continue;
-            const float* from = l.parts + (int64_t(u / parts) * parts * NT) * kThreads + threadIdx.x;
+                    for (int n = 0; n < NT; n++)
 #pragma unroll
-            for (int n = 0; n < NT; n++) v[n] = __ldcg(from + n * kThreads);
-            for (int p = 1; p < parts; p++)
-#pragma unroll
-                for (int n = 0; n < NT; n++) v[n] += __ldcg(from + (p * NT + n) * kThreads);
-        }
-        // lanes 0 to 15 have g, the others u of the same features
-        const int feature = row + (lane & 15), e = c.number(i);
-#pragma unroll
-        for (int n = 0; n < NT; n++) {
-            const int col = n * 8 + warp;
-            if (l.scale[0] && feature < l.h) v[n] *= (lane < 16 ? l.scale[0] : l.scale[1])[int64_t(e) * l.h + feature];
-            const float up = __shfl_down_sync(0xFFFFFFFFu, v[n], 16);
-            if (lane < 16 && feature < l.h && col < c.count(i)) {
-                const int pair = c.order[c.from(i) + col];
-                const float h = act_of(l.act, v[n]) * up * c.share[pair];
-                if (l.terms == 1) {
-                    reinterpret_cast<float*>(l.hidden)[pair * l.h_pad + feature] = h;
-                } else {
-                    uint16_t t[3];
-                    split_bf16(h, l.terms, t);
-                    for (int k = 0; k < l.terms; k++)
-                        reinterpret_cast<uint16_t*>(l.hidden)[(k * int64_t(l.pairs) + pair) * l.h_pad + feature] = t[k];
-                }
+                        for (int j = 0; j < 4; j++) sum[k][n][j] += part[k][n][j] * by[2 * k + j / 2];
+            } else {
+                st.sums(q, sum, next);
             }
+            at = there;
         }
+        if (to - from < s.each && !join_parts<NT>(s, id, u, sum, l.parts, job.count, lane)) continue;
+        job.finish(u, sum);
     }
 }
 
-template <int WT, int NT, bool SHIFT, int TERMS>
-__device__ __forceinline__ void down_units(const Layer& l, const Choice& c, uint32_t ring, float* room, int warp, int lane)
+__device__ __forceinline__ void put_hidden(const Layer& l, int pair, int feature, float h)
 {
-    // float16 weights take the float32 values, others their terms
-    constexpr int kXT = TERMS == 1 ? kF32 : kBf16;
-    using S = Stream<WT, kXT, NT, SHIFT, TERMS>;
-    S st(ring, warp, lane, l.pairs * l.h_pad * size_of(kXT));
-    const int blocks = (l.d + 31) / 32, units = c.entries * blocks;
-    const int pieces = (l.h * size_of(WT) + kPiece - 1) / kPiece;
-    const int parts = parts_of(units, gridDim.x, pieces), all = units * parts, pairs = l.rows * l.top;
-    const int64_t stride = l.w[2].row_stride * size_of(WT);
-    auto unit = [&](int u, int& i, int& row, int& part) {
-        part = u % parts;
-        const int b = u / parts;
-        i = b / blocks;
-        row = (b - i * blocks) * 32;
+    if (l.terms == 1) {
+        reinterpret_cast<float*>(l.hidden)[pair * l.h_pad + feature] = h;
+        return;
+    }
+    uint16_t v[3];
+    split_bf16(h, l.terms, v);
+    uint16_t* to = reinterpret_cast<uint16_t*>(l.hidden) + pair * l.h_pad + feature;
+    const int64_t apart = l.pairs * l.h_pad;
+    to[0] = v[0];
+    to[apart] = v[1];
+    if (l.terms == 3) to[2 * apart] = v[2];
+}
+
+// Units of 16 hidden features of an entry
+template <int WT, int XT, int NT>
+struct Up {
+    const Layer& l;
+    const Choice& c;
+    float* tile;
+    const int lane, blocks, units;
+    static constexpr int parts = 1;
+    static constexpr bool kScales = WT == kI8;
+    uint32_t* count;
+
+    __device__ __forceinline__ Up(const Layer& layer, const Choice& choice, float* room, int ln)
+        : l(layer), c(choice), tile(room), lane(ln), blocks((l.h + 15) / 16), units(c.entries * blocks), count(l.up_count)
+    {
+    }
+    __device__ __forceinline__ Unit part(int u, int first, int last) const
+    {
+        const int i = u / blocks, row = (u - i * blocks) * 16;
         Unit q;
-        q.a[0] = static_cast<const char*>(l.w[2].data) + (c.number(i) * l.w[2].stride + row * l.w[2].row_stride) * size_of(WT);
+        const int64_t e = c.number(i);
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            q.a[k] = static_cast<const char*>(l.w[k].data) + (e * l.w[k].stride + row * l.w[k].row_stride) * size_of(WT);
+            q.a_stride[k] = l.w[k].row_stride * size_of(WT);
+        }
+        q.rows_left[0] = q.rows_left[1] = min(16, l.h - row);
+        q.row_bytes = l.d * size_of(WT);
+        q.first = first;
+        q.last = last;
+        return q;
+    }
+    __device__ __forceinline__ auto columns(int u) const
+    {
+        const int i = u / blocks, n = c.count(i), from = c.from(i);
+        return [=](int col) {   // columns that there are not repeat the last, for nothing
+            return l.x_copy + c.order[from + min(col, n - 1)] / l.top * l.d_pad * size_of(XT);
+        };
+    }
+    // the factors of a lane's rows, 8 apart
+    __device__ __forceinline__ void scales(int u, float (&by)[4]) const
+    {
+        const int i = u / blocks, row = (u - i * blocks) * 16 + lane / 4;
+        const int64_t at = int64_t(c.number(i)) * l.h;
+#pragma unroll
+        for (int k = 0; k < 4; k++) by[k] = l.scale[k / 2][at + min(row + 8 * (k % 2), l.h - 1)];
+    }
+    // by way of the warp's tile: rows 0 to 15 of it are g, the others u
+    __device__ __forceinline__ void finish(int u, const float (&sum)[2][NT][4]) const
+    {
+        const int i = u / blocks, feature = (u - i * blocks) * 16 + (lane & 15), n = c.count(i), from = c.from(i);
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            put_tile(tile, sum[0][t], sum[1][t], lane);
+            __syncwarp();
+            if (feature < l.h)
+#pragma unroll 1
+                for (int col = lane >> 4; col < min(8, n - 8 * t); col += 2) {
+                    const int pair = c.order[from + 8 * t + col];
+                    const float* at = tile + col * kJoinPitch + (lane & 15);
+                    put_hidden(l, pair, feature, act_of(l.act, at[0]) * at[16] * c.share[pair]);
+                }
+            __syncwarp();
+        }
+    }
+};
+
+// Of up to 8 tokens: units of 32 features of the result, their sums over all
+// entries one after another, a column a token; one that did not choose an entry has
+// zeros there.  Of more: units of 32 features and an entry, their results to
+// z by pairs.
+template <int WT, int NT, int XT, bool WHOLE>
+struct Down {
+    const Layer& l;
+    const Choice& c;
+    float* tile;
+    const int lane, blocks, parts, units;
+    static constexpr bool kScales = WT == kI8;
+    uint32_t* count;
+
+    __device__ __forceinline__ Down(const Layer& layer, const Choice& choice, float* room, int ln)
+        : l(layer),
+          c(choice),
+          tile(room),
+          lane(ln),
+          blocks((l.d + 31) / 32),
+          parts(WHOLE ? c.entries : 1),
+          units(WHOLE ? blocks : c.entries * blocks),
+          count(l.down_count)
+    {
+    }
+    __device__ __forceinline__ int entry(int p) const { return WHOLE ? p % parts : p / blocks; }
+    __device__ __forceinline__ int block(int p) const { return WHOLE ? p / parts : p % blocks; }
+    __device__ __forceinline__ Unit part(int p, int first, int last) const
+    {
+        const int row = block(p) * 32;
+        const int64_t stride = l.w[2].row_stride * size_of(WT);
+        Unit q;
+        q.a[0] = static_cast<const char*>(l.w[2].data) +
+                 (c.number(entry(p)) * l.w[2].stride + row * l.w[2].row_stride) * size_of(WT);
         q.a[1] = q.a[0] + 16 * stride;
         q.a_stride[0] = q.a_stride[1] = stride;
         q.rows_left[0] = min(16, l.d - row);
         q.rows_left[1] = max(0, min(16, l.d - row - 16));
         q.row_bytes = l.h * size_of(WT);
-        q.first = int(int64_t(pieces) * part / parts);
-        q.last = int(int64_t(pieces) * (part + 1) / parts);
+        q.first = first;
+        q.last = last;
         return q;
-    };
-    // the first unit's weights are asked into L2 while up_kernel drains
-    if (int(blockIdx.x) < all) {
-        int i, row, part;
-        const Unit q = unit(blockIdx.x, i, row, part);
-        const int r = threadIdx.x / 8;
-        if (r % 16 < q.rows_left[r / 16]) {
-            const char* p = q.a[r / 16] + (r % 16) * stride;
-            const int to = min(q.last * kPiece, q.row_bytes), from = q.first * kPiece;
-            for (int k = from + 128 * int(threadIdx.x % 8); k < min(to, from + 4096); k += 1024)
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
-        }
     }
-    wait_previous();
-    int loading = int(blockIdx.x) - int(gridDim.x);
-    auto next = [&]() {
-        while (!st.more() && loading + int(gridDim.x) < all) {
-            loading += gridDim.x;
-            int i, row, part;
-            const Unit q = unit(loading, i, row, part);
-            const int n = c.count(i), from = c.from(i);
-            st.load_from(q, [&](int col) {
-                return l.hidden + c.order[from + min(col, n - 1)] * l.h_pad * size_of(kXT);
-            });
-        }
-    };
-    st.begin(next);
-    for (int u = blockIdx.x; u < all; u += gridDim.x) {
-        int i, row, part;
-        const Unit q = unit(u, i, row, part);
-        float sum[2][NT][4];
-        st.sums(q, sum, next);
-        const int feature = row + lane;
+    __device__ __forceinline__ auto columns(int p) const
+    {
+        const int i = entry(p), n = c.count(i), from = c.from(i);
+        return [=](int col) -> const char* {
+            int pair = c.order[from + min(col, n - 1)];
+            if (WHOLE) {   // the token's, if it chose this entry
+                pair = -1;
+                for (int k = 0; k < n; k++) {
+                    const int p = c.order[from + k];
+                    if (p >= col * l.top && p < (col + 1) * l.top) pair = p;
+                }
+            }
+            return pair < 0 ? nullptr : l.hidden + pair * l.h_pad * size_of(XT);
+        };
+    }
+    __device__ __forceinline__ void scales(int p, float (&by)[4]) const
+    {
+        const int row = block(p) * 32 + lane / 4;
+        const int64_t at = int64_t(c.number(entry(p))) * l.d;
 #pragma unroll
-        for (int n = 0; n < NT; n++) {
-            float v = join_columns<false>(room, sum[0][n], sum[1][n], warp, lane);
-            const int col = n * 8 + warp;
-            if (feature < l.d && col < c.count(i)) {
-                if (l.scale[2]) v *= l.scale[2][int64_t(c.number(i)) * l.d + feature];
-                l.z[(int64_t(part) * pairs + c.order[c.from(i) + col]) * l.d + feature] = v;
-            }
-        }
-        if (!last_to_come(l.down_count + row / 32, uint32_t(c.entries) * parts)) continue;
-        for (int t = warp; t < l.rows; t += kWarps) {
-            if (feature >= l.d) continue;
-            float y = 0.0f;
-            for (int k = 0; k < l.top; k++) {
-                const int pair = t * l.top + k, e = c.expert[pair] - l.first;
-                if (e < 0 || e >= l.local) continue;
-                for (int p = 0; p < parts; p++) y += __ldcg(l.z + (int64_t(p) * pairs + pair) * l.d + feature);
-            }
-            proj::store1(l.y, t * l.y_rs + feature, y, l.out_f32, l.half);
+        for (int k = 0; k < 4; k++) by[k] = l.scale[2][at + min(row + 8 * k, l.d - 1)];
+    }
+    __device__ __forceinline__ void finish(int u, const float (&sum)[2][NT][4]) const
+    {
+        const int feature = (WHOLE ? u : u % blocks) * 32 + lane, i = WHOLE ? 0 : u / blocks;
+        const int n = WHOLE ? l.rows : c.count(i), from = c.from(i);
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            put_tile(tile, sum[0][t], sum[1][t], lane);
+            __syncwarp();
+            if (feature < l.d)
+#pragma unroll 1
+                for (int col = 0; col < min(8, n - 8 * t); col++) {
+                    const float v = tile[col * kJoinPitch + lane];
+                    if (WHOLE) proj::store1(l.y, col * l.y_rs + feature, v, l.out_f32, l.half);
+                    else l.z[int64_t(c.order[from + 8 * t + col]) * l.d + feature] = v;
+                }
+            __syncwarp();
         }
     }
+};
+
+// bytes of shared memory in front of the choice: rings, then tiles
+constexpr int kRings = kWarps * kRing, kBefore = kRings + kJoin * 4;
+
+// Bytes of a row of weights that a stage holds: as many as let the ring hold two
+constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
+{
+    const int stage = kRows * (128 + 16 * shift) + terms * nt * 8 * (128 / size_of(wt)) * size_of(xt);
+    return 5 * stage <= kRing ? 128 : 64;
 }
 
-// Bytes of shared memory in front of the choice
-constexpr int before_choice(bool shift) { return kWarps * ring_bytes(shift) + kJoin * 4; }
+template <int WT, int XT, int NT, bool SHIFT>
+__device__ __forceinline__ void up_units(const Layer& l, const Choice& c, char* raw, int warp, int lane, int id)
+{
+    constexpr int kPiece = piece_of(WT, XT, NT, SHIFT, 1);
+    using S = Stream<WT, XT, NT, SHIFT, 1, kPiece, 1>;
+    S st(shared_at(raw), warp, lane);
+    const Up<WT, XT, NT> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
+    run_share<S, NT>(st, job, (l.d * size_of(WT) + kPiece - 1) / kPiece, l, lane, id);
+}
+
+template <int WT, int NT, bool SHIFT, int TERMS, bool WHOLE>
+__device__ __forceinline__ void down_units(const Layer& l, const Choice& c, char* raw, int warp, int lane, int id)
+{
+    // float16 weights take the float32 values, others their terms
+    constexpr int kXT = TERMS == 1 ? kF32 : kBf16, kPiece = piece_of(WT, kXT, NT, SHIFT, TERMS);
+    using S = Stream<WT, kXT, NT, SHIFT, TERMS, kPiece, 1, WHOLE>;
+    S st(shared_at(raw), warp, lane, l.pairs * l.h_pad * size_of(kXT));
+    const Down<WT, NT, kXT, WHOLE> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
+    const int each = (l.h * size_of(WT) + kPiece - 1) / kPiece;
+    // the first weights are asked into L2 while up_kernel drains
+    const Shares s = shares_of(job.units * job.parts * each, job.parts * each);
+    if (id < s.of) {
+        const int at = s.start(id), i = at / each;
+        const Unit q = job.part(i, at - i * each, each);
+        const char* p = q.row(lane) + q.first * kPiece;
+        const int to = min(min(4, s.start(id + 1) - at) * kPiece, q.row_bytes - q.first * kPiece);
+        for (int k = 0; k < to; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
+    }
+    wait_previous();
+    run_share<S, NT>(st, job, each, l, lane, id);
+}
 
 template <int WT, int XT, bool SHIFT>
 __global__ void __launch_bounds__(kThreads, 2) up_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, id = warp * gridDim.x + blockIdx.x;
     constexpr int kMost = WT == kI8 ? 2 : 4;
-    Choice c(raw + before_choice(SHIFT), l.rows * l.top);
+    Choice c(raw + kBefore, l.rows * l.top);
     wait_previous();
     allow_next();
     choose_all(l, c, raw, 8 * kMost, warp, lane);
     if (blockIdx.x == 0)
         for (int p = threadIdx.x; p < l.rows * l.top; p += kThreads) {
+            l.expert[p] = c.expert[p];
             if (l.chosen) l.chosen[p] = c.expert[p];
             if (l.share) l.share[p] = c.share[p];
         }
-    float* room = reinterpret_cast<float*>(raw + kWarps * ring_bytes(SHIFT));
-    if (c.columns <= 8) up_units<WT, XT, 1, SHIFT>(l, c, shared_at(raw), room, warp, lane);
-    else if (c.columns <= 16) up_units<WT, XT, 2, SHIFT>(l, c, shared_at(raw), room, warp, lane);
-    else up_units<WT, XT, kMost, SHIFT>(l, c, shared_at(raw), room, warp, lane);
+    if (c.columns <= 8) up_units<WT, XT, 1, SHIFT>(l, c, raw, warp, lane, id);
+    else if (c.columns <= 16) up_units<WT, XT, 2, SHIFT>(l, c, raw, warp, lane, id);
+    else up_units<WT, XT, kMost, SHIFT>(l, c, raw, warp, lane, id);
 }
 
 // The choice is made again from the scores, which are there: up_kernel let this
@@ -470,21 +562,45 @@ template <int WT, bool SHIFT, int TERMS>
 __global__ void __launch_bounds__(kThreads, 2) down_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kMost = (WT == kI8 ? 2 : 4) / (TERMS == 3 ? 2 : 1);   // eights of columns that the ring has room for
-    Choice c(raw + before_choice(SHIFT), l.rows * l.top);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, id = warp * gridDim.x + blockIdx.x;
+    // eights of columns that the ring has room for
+    constexpr int kMost = (WT == kI8 ? 2 : 4) / (TERMS == 3 || SHIFT ? 2 : 1);
+    Choice c(raw + kBefore, l.rows * l.top);
+    allow_next();
     choose_all(l, c, raw, 8 * kMost, warp, lane);
     if (c.entries == 0) {   // no token chose an expert that is here
         wait_previous();
-        for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < int64_t(l.rows) * l.d;
+        for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; l.rows <= kWholeRows && i < int64_t(l.rows) * l.d;
              i += int64_t(gridDim.x) * kThreads)
             proj::store1(l.y, i / l.d * l.y_rs + i % l.d, 0.0f, l.out_f32, l.half);
         return;
     }
-    float* room = reinterpret_cast<float*>(raw + kWarps * ring_bytes(SHIFT));
-    if (c.columns <= 8) down_units<WT, 1, SHIFT, TERMS>(l, c, shared_at(raw), room, warp, lane);
-    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS>(l, c, shared_at(raw), room, warp, lane);
-    else down_units<WT, kMost, SHIFT, TERMS>(l, c, shared_at(raw), room, warp, lane);
+    if (l.rows <= kWholeRows) down_units<WT, 1, SHIFT, TERMS, true>(l, c, raw, warp, lane, id);
+    else if (c.columns <= 8) down_units<WT, 1, SHIFT, TERMS, false>(l, c, raw, warp, lane, id);
+    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS, false>(l, c, raw, warp, lane, id);
+    else down_units<WT, kMost, SHIFT, TERMS, false>(l, c, raw, warp, lane, id);
+}
+
+// What each token's experts gave, added up in the order of their shares
+__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Layer l)
+{
+    wait_previous();
+    allow_next();
+    const int t = blockIdx.y;
+    const int feature = blockIdx.x * 256 + threadIdx.x;
+    if (feature >= l.d) return;
+    float v[kMostTop];
+#pragma unroll
+    for (int k = 0; k < kMostTop; k++) {
+        v[k] = 0.0f;
+        if (k >= l.top) continue;
+        const int pair = t * l.top + k, e = l.expert[pair] - l.first;
+        if (e >= 0 && e < l.local) v[k] = l.z[int64_t(pair) * l.d + feature];
+    }
+    float y = v[0];
+#pragma unroll
+    for (int k = 1; k < kMostTop; k++) y += v[k];
+    proj::store1(l.y, t * l.y_rs + feature, y, l.out_f32, l.half);
 }
 
 using Kernel = void (*)(Layer);
@@ -522,7 +638,7 @@ Kernel down_of(const Layer& l)
 }
 Kernel down_of(const Layer& l, bool shift) { return shift ? down_of<true>(l) : down_of<false>(l); }
 
-size_t product_smem(const Layer& l, bool shift) { return size_t(before_choice(shift)) + size_t(l.rows) * l.top * 12; }
+size_t product_smem(const Layer& l) { return size_t(kBefore) + size_t(l.rows) * l.top * 12; }
 
 // The CTAs of a kernel that fit the device at a time, after it may use the shared
 // memory that it takes.  That is only raised: another plan may need more.
@@ -548,7 +664,7 @@ int resident(Kernel k, size_t bytes, int num_sms, int* ctas)
 int product_ctas(Layer& l, int num_sms)
 {
     for (int shift = 0; shift < 2; shift++) {
-        const size_t bytes = product_smem(l, shift);
+        const size_t bytes = product_smem(l);
         int rc = resident(up_of(l, shift), bytes, num_sms, &l.up_ctas[shift]);
         if (!rc) rc = resident(down_of(l, shift), bytes, num_sms, &l.down_ctas[shift]);
         if (rc) return rc;
@@ -570,11 +686,14 @@ int launch(const Layer& l, int num_sms, cudaStream_t s)
     int rc = proj::launch(scores, dim3(unsigned(grid)), dim3(32 * kScoreWarps), 0, 1, s, "experts' scores", l);
     const bool up = up_shifted(l), down = down_shifted(l);
     if (!rc)
-        rc = proj::launch(up_of(l, up), dim3(unsigned(l.up_ctas[up])), dim3(kThreads), product_smem(l, up), 1, s,
+        rc = proj::launch(up_of(l, up), dim3(unsigned(l.up_ctas[up])), dim3(kThreads), product_smem(l), 1, s,
                           "experts' up products", l);
     if (!rc)
-        rc = proj::launch(down_of(l, down), dim3(unsigned(l.down_ctas[down])), dim3(kThreads), product_smem(l, down), 1, s,
+        rc = proj::launch(down_of(l, down), dim3(unsigned(l.down_ctas[down])), dim3(kThreads), product_smem(l), 1, s,
                           "experts' down products", l);
+    if (!rc && l.rows > kWholeRows)
+        rc = proj::launch(combine_kernel, dim3(unsigned((l.d + 255) / 256), unsigned(l.rows)), dim3(256), 0, 1, s,
+                          "experts' sum", l);
     return rc;
 }
 

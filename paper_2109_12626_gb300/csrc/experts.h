@@ -11,6 +11,7 @@ constexpr int kMostRows = 64;       // tokens: a bit each in an expert's mask
 constexpr int kMostTop = 16;        // of them chosen, a lane each
 constexpr int kMostExperts = 512;   // 16 a lane of a warp
 constexpr int64_t kMostSize = 1 << 20;
+constexpr int kWholeRows = 8;       // of which each has a column of its own in the last product
 
 struct Layer {
     int rows, top, total, first, local;
@@ -35,16 +36,13 @@ struct Layer {
     // rows (the most that the plan takes), or with terms 1 float32
     char* hidden;
     int terms, pairs;
-    float* parts;                  // of units whose sum is split
-    float* z;                      // the experts' results, before they are added up
-    uint32_t* up_count;            // of units, and of blocks of 32 features
+    float* parts;                  // sums of units that several warps share
+    float* z;                      // of more than 8 rows, the experts' results by pair
+    int32_t* expert;               // of a pair
+    uint32_t* up_count;            // a counter a warp
     uint32_t* down_count;
     int up_ctas[2], down_ctas[2];  // of the product kernels, without and with shifted rows
 };
-
-// the floats of Layer::parts that `ctas` CTAs may fill, and of Layer::z behind
-// those of the pairs of token and expert
-constexpr int64_t parts_floats(int ctas) { return int64_t(ctas) * 32 * 32; }
 
 // makes the product kernels ready and sets how many CTAs each has
 int product_ctas(Layer& l, int num_sms);

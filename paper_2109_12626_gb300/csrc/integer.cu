@@ -24,6 +24,8 @@ namespace {
 
 // ------------------------------------------------------------- few rows
 
+constexpr int kPiece = 64;
+
 struct RowsArgs {
     Rows r;
     int passes, parts, pieces, units;
@@ -40,11 +42,11 @@ template <int NT, bool SHIFT>
 __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant__ RowsArgs a)
 {
     extern __shared__ __align__(128) char raw[];
-    using S = Stream<kI8, kI8, NT, SHIFT>;
+    using S = Stream<kI8, kI8, NT, SHIFT, 1, kPiece, kWarps>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Rows& r = a.r;
     S st(shared_at(raw), warp, lane);
-    float* room = reinterpret_cast<float*>(raw + kWarps * ring_bytes(SHIFT));
+    float* room = reinterpret_cast<float*>(raw + kWarps * S::kWarpBytes);
     wait_previous();
     allow_next();
     const int all = a.units * a.parts;
@@ -59,7 +61,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
         q.rows_left[0] = int(min(int64_t(16), r.n - n0));
         q.rows_left[1] = int(max(int64_t(0), min(int64_t(16), r.n - n0 - 16)));
         q.row_bytes = r.k;
-        q.first = int(int64_t(a.pieces) * part / a.parts);
+        q.first = int(int64_t(a.pieces) * part / a.parts) + warp;
         q.last = int(int64_t(a.pieces) * (part + 1) / a.parts);
         return q;
     };
@@ -80,6 +82,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
         const Unit q = unit(u, n0, m0);
         float sum[2][NT][4];
         int v[NT];
+        S::clear(sum);
         st.sums(q, sum, next);
 #pragma unroll
         for (int n = 0; n < NT; n++) v[n] = __float_as_int(join_columns<true>(room, sum[0][n], sum[1][n], warp, lane));
@@ -327,7 +330,9 @@ template <int NT>
 int rows_launch_of(const RowsArgs& a, bool shift, int ctas, cudaStream_t s)
 {
     auto* kernel = shift ? rows_kernel<NT, true> : rows_kernel<NT, false>;
-    const int bytes = kWarps * ring_bytes(shift) + kJoin * 4;
+    using S = Stream<kI8, kI8, NT, true, 1, kPiece, kWarps>;
+    using T = Stream<kI8, kI8, NT, false, 1, kPiece, kWarps>;
+    const int bytes = kWarps * (shift ? S::kWarpBytes : T::kWarpBytes) + kJoin * 4;
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return cuda_fail_c(e, "integer rows kernel");

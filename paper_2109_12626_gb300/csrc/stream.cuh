@@ -46,10 +46,7 @@ enum Kind { kBf16, kF16, kI8, kF32 };   // of weights (not kF32) and columns
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kRows = 32;               // of A, a unit
-constexpr int kPiece = 64;              // bytes of a row of A, a stage
-// bytes of a warp's ring: rooms of two CTAs an SM, where the shifted rows of A do
-// not make two stages larger
-constexpr int ring_bytes(bool shift) { return shift ? 13312 : 12288; }
+constexpr int kRing = 12288;            // bytes, a warp: two CTAs an SM
 
 constexpr int size_of(int kind) { return kind == kI8 ? 1 : kind == kF32 ? 4 : 2; }
 
@@ -202,9 +199,11 @@ struct Unit {
 };
 
 // TERMS: a column's values are the sums of so many, whose arrays lie `apart`
-// bytes from each other.
-template <int WT, int XT, int NT, bool SHIFT, int TERMS = 1>
+// bytes from each other.  PIECE: bytes of a row of A, a stage.  STEP: a warp takes
+// every STEP-th piece of a unit.  ZEROS: some columns are zeros.
+template <int WT, int XT, int NT, bool SHIFT, int TERMS, int PIECE, int STEP, bool ZEROS = false>
 struct Stream {
+    static constexpr int kPiece = PIECE;
     static constexpr int kParts = kPiece / 64;           // a lane has 16 bytes of a row in each
     static constexpr int kK = 64 / size_of(WT);          // elements of a part
     static constexpr int kAChunks = kPiece / 16 + SHIFT; // 16-byte chunks of a row
@@ -216,7 +215,7 @@ struct Stream {
     static constexpr int kALoads = kAChunks;
     static constexpr int kBTerm = NT * 8 * kB;
     static constexpr int kStage = kABytes + TERMS * kBTerm;
-    static constexpr int kStages = ring_bytes(SHIFT) / kStage > 5 ? 5 : ring_bytes(SHIFT) / kStage;
+    static constexpr int kStages = kRing / kStage > 5 ? 5 : kRing / kStage;
     static constexpr int kWarpBytes = kStages * kStage;
     static_assert(kStages >= 2, "the ring holds two stages");
     static constexpr bool kWhole = XT == kI8;            // sums are integers
@@ -227,6 +226,7 @@ struct Stream {
     // loading side
     const char* a_at[kALoads];
     const char* b_at[NT * kBLoads];
+    int b_bytes[NT * kBLoads];   // 0: a column of zeros
     int64_t apart;
     int load_piece, load_last, load_whole;   // pieces before load_whole are inside every row
     int load_bytes, load_shift;              // of a row
@@ -248,16 +248,22 @@ struct Stream {
     {
     }
 
-    // the row and chunk of a lane's i-th 16 bytes of A
-    __device__ __forceinline__ int a_row(int i) const { return (lane + 32 * i) / kAChunks; }
-    __device__ __forceinline__ int a_chunk(int i) const { return (lane + 32 * i) % kAChunks; }
+    // the row and chunk of a lane's i-th 16 bytes of A, and where they go
+    __device__ __forceinline__ int a_row(int i) const { return int((unsigned(lane) + 32 * i) / kAChunks); }
+    __device__ __forceinline__ int a_chunk(int i) const { return int((unsigned(lane) + 32 * i) % kAChunks); }
+    __device__ __forceinline__ uint32_t a_to(int i) const
+    {
+        if (SHIFT || kParts == 1) return 16 * lane + 512 * i;
+        return (16 * lane ^ (lane & 8) << 3) + 512 * i;
+    }
 
-    // The loading side turns to a unit.  column(c): address of column c's values, for
-    // any c; whole pieces of it can be read.
+    // The loading side turns to pieces u.first (to u.last) of a unit.  column(c):
+    // address of column c's values, for any c; whole pieces of it can be read.  With
+    // ZEROS nullptr: a column of zeros.
     template <typename Column>
     __device__ __forceinline__ void load_from(const Unit& u, Column column)
     {
-        load_piece = u.first + warp;
+        load_piece = u.first;
         load_last = u.last;
         load_bytes = u.row_bytes;
         load_whole = (u.row_bytes - (SHIFT ? 16 : 0)) / kPiece;
@@ -270,8 +276,13 @@ struct Stream {
         for (int n = 0; n < NT; n++)
 #pragma unroll
             for (int j = 0; j < kBLoads; j++) {
-                const int id = lane + 32 * j;
-                b_at[n * kBLoads + j] = column(n * 8 + id / kBChunks) + load_piece * kB + 16 * (id % kBChunks);
+                const unsigned id = lane + 32 * j;
+                const char* p = column(n * 8 + id / kBChunks);
+                if (ZEROS) {
+                    b_bytes[n * kBLoads + j] = p ? 16 : 0;
+                    if (!p) p = u.a[0] - int(reinterpret_cast<uintptr_t>(u.a[0]) & 15);   // any address
+                }
+                b_at[n * kBLoads + j] = p + load_piece * kB + 16 * (id % kBChunks);
             }
         if (SHIFT) {   // what the last pieces have to know of each row
             load_shift = 0;
@@ -304,7 +315,7 @@ struct Stream {
     {
         if (load_piece < load_whole) {
 #pragma unroll
-            for (int i = 0; i < kALoads; i++) copy16(load_to + a_place(a_row(i), a_chunk(i)), a_at[i]);
+            for (int i = 0; i < kALoads; i++) copy16(load_to + a_to(i), a_at[i]);
         } else {
             const int left = load_bytes - load_piece * kPiece;
 #pragma unroll
@@ -312,22 +323,26 @@ struct Stream {
                 const int o = SHIFT ? (i < 8 ? load_shift >> 4 * i & 15 : load_last_shift) : 0;
                 const int bytes = max(0, min(16, left + o - 16 * a_chunk(i)));
                 // of none, the address of the row's first bytes in this piece
-                copy16(load_to + a_place(a_row(i), a_chunk(i)), a_at[i] - (bytes > 0 ? 0 : 16 * a_chunk(i)), bytes);
+                copy16(load_to + a_to(i), a_at[i] - (bytes > 0 ? 0 : 16 * a_chunk(i)), bytes);
             }
         }
 #pragma unroll
-        for (int i = 0; i < kALoads; i++) a_at[i] += kWarps * kPiece;
+        for (int i = 0; i < kALoads; i++) a_at[i] += STEP * kPiece;
 #pragma unroll
         for (int n = 0; n < NT; n++)
 #pragma unroll
             for (int j = 0; j < kBLoads; j++) {
-                const int id = lane + 32 * j;
+                const unsigned id = lane + 32 * j;
                 const uint32_t to = load_to + kABytes + b_place(n * 8 + id / kBChunks, id % kBChunks);
 #pragma unroll
-                for (int t = 0; t < TERMS; t++) copy16(to + t * kBTerm, b_at[n * kBLoads + j] + t * apart);
-                b_at[n * kBLoads + j] += kWarps * kB;
+                for (int t = 0; t < TERMS; t++) {
+                    const char* from = b_at[n * kBLoads + j] + t * apart;
+                    if (ZEROS) copy16(to + t * kBTerm, from, b_bytes[n * kBLoads + j]);
+                    else copy16(to + t * kBTerm, from);
+                }
+                b_at[n * kBLoads + j] += STEP * kB;
             }
-        load_piece += kWarps;
+        load_piece += STEP;
         load_to += kStage;
         if (load_to == load_end) load_to = ring;
     }
@@ -475,23 +490,18 @@ struct Stream {
         }
     }
 
-    // This warp's sums over its pieces of unit u.  next(): the loading side turns
-    // to a unit behind the one that it is at, if there is one with a piece for it.
+    // The products of the next pieces of a unit, added to `total`.  next(): the
+    // loading side turns to what comes behind the pieces that it is at, if anything.
     // The instructions cut sums off, so each part's products are summed by
-    // themselves and added up rounded.
+    // themselves and added up rounded; whole numbers in `run` first.
     template <typename Next>
     __device__ __forceinline__ void sums(const Unit& u, float (&total)[2][NT][4], Next next)
     {
         use_from(u);
-        float run[2][NT][4];   // of whole numbers
-#pragma unroll
-        for (int i = 0; i < 2; i++)
-#pragma unroll
-            for (int n = 0; n < NT; n++)
-#pragma unroll
-                for (int q = 0; q < 4; q++) run[i][n][q] = total[i][n][q] = 0.0f;
+        float run[2][NT][4];
+        if (kWhole) clear(run);
         int done = 0;
-        for (int piece = u.first + warp; piece < u.last; piece += kWarps) {
+        for (int piece = u.first; piece < u.last; piece += STEP) {
             copies_wait<kStages - 2>();
             __syncwarp();   // every lane's copies are there, and the stage before is free
             if (!more()) next();
@@ -505,6 +515,16 @@ struct Stream {
             }
         }
         if (kWhole) take(run, total);
+    }
+
+    static __device__ __forceinline__ void clear(float (&v)[2][NT][4])
+    {
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) v[i][n][q] = 0.0f;
     }
 
     // whole numbers of a run to the total, which is held as integers
@@ -538,25 +558,31 @@ struct Stream {
 // `threadIdx.x` gets those of row threadIdx.x % 32, column threadIdx.x / 32.  `room`:
 // kJoin floats of shared memory.
 constexpr int kJoinPitch = kRows + 4;                     // floats of a column
-constexpr int kJoin = kWarps * 8 * kJoinPitch;
+constexpr int kTile = 8 * kJoinPitch;                     // of a warp
+constexpr int kJoin = kWarps * kTile;
+
+// A warp's sums of 8 columns to its tile, column by column
+__device__ __forceinline__ void put_tile(float* tile, const float (&first)[4], const float (&second)[4], int lane)
+{
+    const int g = lane / 4, t = lane & 3;
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const int row = g + 8 * (q >> 1), column = 2 * t + (q & 1);
+        tile[column * kJoinPitch + row] = first[q];
+        tile[column * kJoinPitch + 16 + row] = second[q];
+    }
+}
 
 template <bool WHOLE>
 __device__ __forceinline__ float join_columns(float* room, const float (&first)[4], const float (&second)[4], int warp,
                                               int lane)
 {
-    const int g = lane / 4, t = lane & 3;
-    float* mine = room + warp * 8 * kJoinPitch;
-#pragma unroll
-    for (int q = 0; q < 4; q++) {
-        const int row = g + 8 * (q >> 1), column = 2 * t + (q & 1);
-        mine[column * kJoinPitch + row] = first[q];
-        mine[column * kJoinPitch + 16 + row] = second[q];
-    }
+    put_tile(room + warp * kTile, first, second, lane);
     __syncthreads();
     const float* at = room + (threadIdx.x / kRows) * kJoinPitch + threadIdx.x % kRows;
     float v[kWarps];
 #pragma unroll
-    for (int w = 0; w < kWarps; w++) v[w] = at[w * 8 * kJoinPitch];
+    for (int w = 0; w < kWarps; w++) v[w] = at[w * kTile];
     __syncthreads();
     if (WHOLE) {
         int s = __float_as_int(v[0]);
@@ -570,20 +596,100 @@ __device__ __forceinline__ float join_columns(float* room, const float (&first)[
     return s;
 }
 
+// One more on a counter, and what it was: what the thread knows to be written is
+// visible to whoever adds later, and what was written before earlier ones to it.
+__device__ __forceinline__ uint32_t add_in_order(uint32_t* counter)
+{
+    uint32_t was;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(was) : "l"(counter) : "memory");
+    return was;
+}
+
 // Whether this CTA is the last of `all` to come to a counter, which it then sets
 // back to zero; what the others wrote before they came is visible to it.
 __device__ __forceinline__ bool last_to_come(uint32_t* counter, uint32_t all)
 {
     __shared__ uint32_t came;
-    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
-        came = atomicAdd(counter, 1u) + 1u;
+        came = add_in_order(counter) + 1u;
         if (came == all) *counter = 0u;
-        __threadfence();
     }
     __syncthreads();
     return came == all;
+}
+
+// ------------------------------------------------------------ equal shares
+
+// `total` pieces dealt out to `of` warps, each a contiguous share; units of `each`
+// pieces may lie in several.
+constexpr int kLeast = 4;   // pieces a warp, where there are fewer than warps
+struct Shares {
+    int total, of, each;
+    int most, long_ones, behind;   // the first long_ones warps have one more than most, up to piece `behind`
+    __device__ __forceinline__ Shares(int all, int warps, int unit)
+        : total(all), of(warps), each(unit), most(all / warps), long_ones(all - most * warps), behind(long_ones * (most + 1))
+    {
+    }
+    __device__ __forceinline__ int start(int w) const { return w * most + min(w, long_ones); }
+    __device__ __forceinline__ int owner(int piece) const
+    {
+        return piece < behind ? piece / (most + 1) : long_ones + (piece - behind) / most;
+    }
+};
+
+// A warp's sums over a part of a unit, left for the last of the unit's warps to come,
+// which gets them all added up, in the order of the warps, and true.  parts: two
+// places a warp, for the unit that its share starts in and the one that it ends in;
+// count: a counter a warp, zero, used by the unit whose first warp it is.
+template <int NT>
+__device__ __forceinline__ bool join_parts(const Shares& s, int warp_id, int unit, float (&v)[2][NT][4], float* parts,
+                                           uint32_t* count, int lane)
+{
+    constexpr int kPlace = 2 * NT * 4 * 32;
+    const int from = unit * s.each, first = s.owner(from), last = s.owner(from + s.each - 1);
+    auto place = [&](int w) { return parts + (int64_t(w) * 2 + (s.start(w) < from)) * kPlace; };
+    float4* mine = reinterpret_cast<float4*>(place(warp_id)) + lane;
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int n = 0; n < NT; n++) mine[(i * NT + n) * 32] = make_float4(v[i][n][0], v[i][n][1], v[i][n][2], v[i][n][3]);
+    __syncwarp();
+    uint32_t came = 0;
+    if (lane == 0) {
+        came = add_in_order(count + first) + 1u;
+        if (came == uint32_t(last - first + 1)) count[first] = 0u;
+    }
+    came = __shfl_sync(0xFFFFFFFFu, came, 0);
+    if (came != uint32_t(last - first + 1)) return false;
+    // only the first may have begun before the unit
+    const float4* at = reinterpret_cast<const float4*>(place(first)) + lane;
+    const float4* next = reinterpret_cast<const float4*>(parts + (int64_t(first) + 1) * 2 * kPlace) + lane;
+    constexpr int kAhead = NT == 1 ? 4 : 1;   // warps whose sums are asked for together
+    for (int w = first; w <= last; w += kAhead) {
+        float4 p[kAhead][2 * NT];
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+#pragma unroll
+            for (int i = 0; i < 2 * NT; i++)
+                p[k][i] = w + k <= last ? __ldcg(at + i * 32) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            at = next;
+            next += 2 * kPlace / 4;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; k++)
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int n = 0; n < NT; n++) {
+                    const float4 q = p[k][i * NT + n];
+                    if (w + k == first)
+                        v[i][n][0] = q.x, v[i][n][1] = q.y, v[i][n][2] = q.z, v[i][n][3] = q.w;
+                    else
+                        v[i][n][0] += q.x, v[i][n][1] += q.y, v[i][n][2] += q.z, v[i][n][3] += q.w;
+                }
+    }
+    return true;
 }
 
 }  // namespace stream

@@ -233,13 +233,17 @@ def test_equal_scores_take_the_lower_number(pkg):
 
 def test_not_a_number_stays_in_its_row(pkg):
     x, router, w, scale = make(10, 96, 48, 8, 8, "bfloat16", None, 10)
-    whole, chosen, _ = run(pkg, x, router, w, scale, 2, out="float32")
+    _, chosen, _ = run(pkg, x, router, w, scale, 2, out="float32")
+    want, _, _, bound, _ = layer64(x, router, w, scale, 2, 0, "silu", True, chosen)
     for bad in (float("nan"), float("inf")):
         v = x.clone()
         v[3, 5] = bad
         y, c, s = run(pkg, v, router, w, scale, 2, out="float32")
         keep = torch.arange(10, device="cuda") != 3
-        assert torch.equal(y[keep], whole[keep]) and torch.equal(c[keep], chosen[keep])
+        # where the long sums are cut depends on what all tokens chose, and with it
+        # the order of a sum's additions, which the bound allows for
+        U.close("y", y[keep], want[keep], bound[keep], "float32")
+        assert torch.equal(c[keep], chosen[keep])
         assert not bool(torch.isfinite(y[3]).any())
     # an expert that no token chose may hold anything
     _, c, _ = run(pkg, x[:2], router, w, scale, 2)
