@@ -20,6 +20,7 @@ struct Integer {
     char* x_copy = nullptr;     // x of few rows, padded; parts and counters of their sums
     int32_t* parts = nullptr;
     char* wide[2] = {};         // x and w in 16 bits
+    bool set[3][2] = {};        // kernels' attributes set
     proj::Proj* base() const { return reinterpret_cast<proj::Proj*>(tiles); }
 };
 
@@ -45,6 +46,7 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
     r.w = static_cast<const char*>(w.data);
     r.w_rs = P->n_out > 1 ? w.row_stride : P->n_in;
     r.f = f;
+    r.set = P->set;
     int rc = DPDR_OK;
     if (!P->parts) {   // and the counters behind them, at zero
         const int64_t ints = parts_ints(num_sms), all = (ints + 2 * num_sms) * 4;
@@ -58,7 +60,8 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
     r.parts = P->parts;
     r.count = reinterpret_cast<uint32_t*>(P->parts + parts_ints(num_sms));
     // x as it lies where its rows are whole pieces at multiples of 16 bytes
-    if (x.col_stride == 1 && P->n_in == pad && reinterpret_cast<uintptr_t>(x.data) % 16 == 0 &&
+    const bool token = rows <= 4 && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (P->n_out == 1 || r.w_rs % 16 == 0);
+    if (x.col_stride == 1 && (P->n_in == pad || token) && reinterpret_cast<uintptr_t>(x.data) % 16 == 0 &&
         (rows == 1 || x.row_stride % 16 == 0)) {
         r.x = static_cast<const char*>(x.data);
         r.x_rs = x.row_stride;

@@ -110,6 +110,98 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
     }
 }
 
+// -------------------------------------------------------- up to four rows
+
+constexpr int kTokenWarps = 8, kTokenDeep = 4;
+
+// A group of `share` warps takes two features, each lane 16 bytes of both rows of
+// w four times over before it uses the first, and four products at a time on the
+// integer units, which hold whole sums of 32 bits: nothing to widen, and nothing to
+// join beyond the group.  x comes from L1.  From five rows on the reads of x and the
+// products take longer than the weights.
+template <int ROWS>
+__global__ void __launch_bounds__(32 * kTokenWarps) token_kernel(const __grid_constant__ Rows r, int share)
+{
+    __shared__ int parts[kTokenWarps][2 * ROWS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = warp / share, mine = warp % share;
+    const int64_t first = (int64_t(blockIdx.x) * (kTokenWarps / share) + group) * 2;
+    const int64_t second = first + 1 >= r.n ? first : first + 1;   // a last odd feature is taken twice
+    const char *w0 = r.w + first * r.w_rs, *w1 = r.w + second * r.w_rs;
+    // the first loads' lines are asked into L2 while the kernel before drains
+    if (first < r.n)
+        for (int at = 128 * (mine * 32 + lane); at < r.k && at < 16 * 32 * kTokenDeep * share; at += 128 * 32 * share) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(w0 + at));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(w1 + at));
+        }
+    wait_previous();
+    allow_next();
+    int acc[2][ROWS] = {};
+    if (first < r.n) {
+        const int units = r.k / 16, step = 32 * share;
+        auto sum = [&](const uint4& a, const uint4& b, int u) {
+#pragma unroll
+            for (int m = 0; m < ROWS; m++) {
+                const uint4 x = *reinterpret_cast<const uint4*>(r.x + min(m, r.rows - 1) * r.x_rs + 16 * u);
+                acc[0][m] = __dp4a(int(a.x), int(x.x), __dp4a(int(a.y), int(x.y), acc[0][m]));
+                acc[1][m] = __dp4a(int(b.x), int(x.x), __dp4a(int(b.y), int(x.y), acc[1][m]));
+                acc[0][m] = __dp4a(int(a.z), int(x.z), __dp4a(int(a.w), int(x.w), acc[0][m]));
+                acc[1][m] = __dp4a(int(b.z), int(x.z), __dp4a(int(b.w), int(x.w), acc[1][m]));
+            }
+        };
+        const uint4 *p0 = reinterpret_cast<const uint4*>(w0), *p1 = reinterpret_cast<const uint4*>(w1);
+        for (int u0 = mine * 32 + lane; u0 < units; u0 += kTokenDeep * step) {
+            uint4 a[kTokenDeep], b[kTokenDeep];
+#pragma unroll
+            for (int d = 0; d < kTokenDeep; d++)
+                if (u0 + d * step < units) a[d] = __ldcs(p0 + u0 + d * step), b[d] = __ldcs(p1 + u0 + d * step);
+#pragma unroll
+            for (int d = 0; d < kTokenDeep; d++)
+                if (u0 + d * step < units) sum(a[d], b[d], u0 + d * step);
+        }
+        const int k = units * 16 + lane;   // fewer than 16 are left
+        if (mine == 0 && k < r.k) {
+#pragma unroll
+            for (int m = 0; m < ROWS; m++) {
+                const int x = reinterpret_cast<const int8_t*>(r.x)[min(m, r.rows - 1) * r.x_rs + k];
+                acc[0][m] += x * reinterpret_cast<const int8_t*>(w0)[k];
+                acc[1][m] += x * reinterpret_cast<const int8_t*>(w1)[k];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int m = 0; m < ROWS; m++) acc[i][m] = __reduce_add_sync(0xFFFFFFFFu, acc[i][m]);
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int m = 0; m < ROWS; m++) parts[warp][2 * m + i] = acc[i][m];
+    if (share > 1) __syncthreads();
+    else __syncwarp();
+    // lane i finishes feature i % 2 of row i / 2
+    const int m = lane / 2;
+    const int64_t n = first + lane % 2;
+    if (mine != 0 || m >= r.rows || n >= r.n) return;
+    int v = 0;
+    for (int w = 0; w < share; w++) v += parts[warp + w][lane];
+    put(r.f, m, n, v, r.f.w_scale[n], r.f.bias ? r.f.bias[n] : 0.0f);
+}
+
+int token_launch(const Rows& r, int num_sms, cudaStream_t s)
+{
+    // More warps a group where the features alone are too few to keep the memory
+    // busy and each warp keeps four loads a lane
+    const int64_t groups = (r.n + 1) / 2;
+    int share = 1;
+    while (share < 8 && groups * share < 8 * num_sms && r.k >= 4096 * share) share *= 2;
+    const int64_t per = kTokenWarps / share;
+    auto* kernel = r.rows == 1 ? token_kernel<1> : r.rows == 2 ? token_kernel<2> : token_kernel<4>;
+    return proj::launch(kernel, dim3(unsigned((groups + per - 1) / per)), dim3(32 * kTokenWarps), 0, 1, s,
+                        "integer token kernel", r, share);
+}
+
 // --------------------------------------------------------- laid out anew
 
 // Sixteen elements a thread at a time.  Bound by the bytes: 8192 x 4096 to 16
@@ -183,8 +275,8 @@ struct Rounding {
 };
 
 // 127 v / most, rounded to the nearest whole number, halves to even, exactly.
-// The float32 quotient is off by 1.6e-5 at most, so it decides unless it is near a
-// half; there the sizes of 254 |v| and (2 k + 1) most are compared, each as a float and
+// v times the float32 quotient 127 / most is off by 1.6e-5 at most, so it decides unless
+// it is near a half (the caller's fast way); there the sizes of 254 |v| and (2 k + 1) most are compared, each as a float and
 // what that leaves of the product, eight bits more, whose differences are exact.
 __device__ __forceinline__ int rounded(float v, const Rounding& r)
 {
@@ -279,20 +371,36 @@ __global__ void __launch_bounds__(256) quantise_kernel(const void* x, int64_t rs
     auto put = [&](int64_t u, const Held& h) {
         float f[4];
         widened(h, f);
-        int v[4];
+        // t + 1.5 2^23 is t rounded in the low bits; what it was off by tells whether a
+        // half is near
+        uint32_t v[4];
+        float off = plain && r.power == 1.0f ? 0.0f : 1.0f;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            if (plain) v[k] = rounded(f[k], r);
-            else v[k] = high == 0x7F800000u && isinf(f[k]) ? (f[k] < 0.0f ? -127 : 127) : 0;
+            const float y = fmaf(f[k], r.by, 12582912.0f);
+            off = fmaxf(off, fabsf(fmaf(f[k], r.by, 12582912.0f - y)));
+            v[k] = __float_as_uint(y);
         }
+        if (off > 0.4999f)
+#pragma unroll 1
+            for (int k = 0; k < 4; k++) {
+                const float a = k == 0 ? f[0] : k == 1 ? f[1] : k == 2 ? f[2] : f[3];
+                int w = 0;
+                if (plain) w = rounded(a, r);
+                else if (high == 0x7F800000u && isinf(a)) w = a < 0.0f ? -127 : 127;
+                if (k == 0) v[0] = uint32_t(w);
+                else if (k == 1) v[1] = uint32_t(w);
+                else if (k == 2) v[2] = uint32_t(w);
+                else v[3] = uint32_t(w);
+            }
+        const uint32_t all = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
         int8_t* to = q + m * q_rs + 4 * u;
         if (VEC) {
-            *reinterpret_cast<uint32_t*>(to) = uint32_t(v[0] & 255) | uint32_t(v[1] & 255) << 8 |
-                                               uint32_t(v[2] & 255) << 16 | uint32_t(v[3]) << 24;
+            *reinterpret_cast<uint32_t*>(to) = all;
         } else {
 #pragma unroll
             for (int k = 0; k < 4; k++)
-                if (4 * u + k < n) to[k] = int8_t(v[k]);
+                if (4 * u + k < n) to[k] = int8_t(all >> 8 * k);
         }
     };
     if (whole) {
@@ -333,9 +441,13 @@ int rows_launch_of(const RowsArgs& a, bool shift, int ctas, cudaStream_t s)
     using S = Stream<kI8, kI8, NT, true, 1, kPiece, kWarps>;
     using T = Stream<kI8, kI8, NT, false, 1, kPiece, kWarps>;
     const int bytes = kWarps * (shift ? S::kWarpBytes : T::kWarpBytes) + kJoin * 4;
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return cuda_fail_c(e, "integer rows kernel");
+    bool& set = a.r.set[NT == 1 ? 0 : NT == 2 ? 1 : 2][shift];
+    if (!set) {
+        const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != cudaSuccess) return cuda_fail_c(e, "integer rows kernel");
+        set = true;
+    }
     return proj::launch(kernel, dim3(unsigned(ctas)), dim3(kThreads), size_t(bytes), 1, s, "integer rows kernel", a);
 }
 
@@ -343,6 +455,8 @@ int rows_launch_of(const RowsArgs& a, bool shift, int ctas, cudaStream_t s)
 
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s)
 {
+    const bool shift = reinterpret_cast<uintptr_t>(r.w) % 16 != 0 || (r.n > 1 && r.w_rs % 16 != 0);
+    if (r.rows <= 4 && !shift) return token_launch(r, num_sms, s);
     RowsArgs a;
     a.r = r;
     const int nt = r.rows <= 8 ? 1 : r.rows <= 16 ? 2 : 4;
@@ -354,7 +468,6 @@ int rows_launch(const Rows& r, int num_sms, cudaStream_t s)
     // as many parts as there are CTAs for, while a warp keeps two pieces
     a.parts = int(std::max<int64_t>(1, std::min<int64_t>(slots / units, a.pieces / (2 * kWarps))));
     const int ctas = int(std::min<int64_t>(units * a.parts, slots));
-    const bool shift = reinterpret_cast<uintptr_t>(r.w) % 16 != 0 || (r.n > 1 && r.w_rs % 16 != 0);
     return nt == 1   ? rows_launch_of<1>(a, shift, ctas, s)
            : nt == 2 ? rows_launch_of<2>(a, shift, ctas, s)
                      : rows_launch_of<4>(a, shift, ctas, s);

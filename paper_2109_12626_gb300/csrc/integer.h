@@ -38,7 +38,9 @@ struct Rows {
     Finish f;
     int32_t* parts;          // of units whose sum is split
     uint32_t* count;
+    bool (*set)[2];          // of the plan: kernels' attributes set
 };
+// x need not be padded for up to 4 rows of w at multiples of 16 bytes
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s);
 constexpr int64_t parts_ints(int num_sms) { return int64_t(2 * num_sms) * 32 * 32; }
 

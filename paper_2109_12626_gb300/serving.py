@@ -29,30 +29,42 @@ def quantise(x, q, scale, stream=None) -> None:
     the largest size in the row, q = 127 x / a rounded, halves to even.  x
     [rows, n] in bfloat16, float16 or float32, any strides; q int8 [rows, n];
     scale float32 [rows].  Weights are rounded alike, a row a channel."""
-    import torch
+    if _codes is None:
+        _first()
+    code = _codes.get(x.dtype)
+    if code is None:
+        raise TypeError("x is %s, not one of %s" % (x.dtype, ", ".join(RESULTS)))
     if x.dim() != 2:
         raise ValueError("x has %d dimensions, not 2" % x.dim())
-    name = str(x.dtype).split(".")[-1]
-    if name not in RESULTS:
-        raise TypeError("x is %s, not one of %s" % (x.dtype, ", ".join(RESULTS)))
     rows, n = x.shape
-    for what, t, shape, dtype in (("q", q, (rows, n), torch.int8), ("scale", scale, (rows,), torch.float32)):
-        if t.dtype is not dtype:
-            raise TypeError("%s is %s, not %s" % (what, t.dtype, dtype))
-        if tuple(t.shape) != shape:
-            raise ValueError("%s is %s, not %s" % (what, tuple(t.shape), shape))
-    at = torch.cuda.current_device()
-    for what, t in (("x", x), ("q", q), ("scale", scale)):
-        if t.get_device() != at:
-            raise ValueError("%s is not on the current device" % what)
+    if q.dtype is not _int8 or scale.dtype is not _float32:
+        raise TypeError("q is %s and scale %s, not int8 and float32" % (q.dtype, scale.dtype))
+    if q.shape != x.shape or scale.shape != (rows,):
+        raise ValueError("q is %s and scale %s for an x of %s" % (tuple(q.shape), tuple(scale.shape), tuple(x.shape)))
+    at = x.get_device()
+    if at < 0 or at != q.get_device() or at != scale.get_device() or at != _device():
+        raise ValueError("x, q and scale are not all on the current device")
     if rows > 1 and scale.stride(0) != 1:
         raise ValueError("scale: contiguous elements are needed")
-    record = ctypes.c_int64 * 3
-    a, b = record(x.data_ptr(), *x.stride()), record(q.data_ptr(), *q.stride())
-    rc = lib().dpdr_quantise(rows, n, RESULTS[name], ctypes.addressof(a), ctypes.addressof(b), scale.data_ptr(),
-                             _stream(stream))
+    r = _records(x.data_ptr(), *x.stride(), q.data_ptr(), *q.stride())
+    base = ctypes.addressof(r)
+    rc = _quantise(rows, n, code, base, base + 24, scale.data_ptr(), _stream(stream))
     if rc:
         _check(rc, "dpdr_quantise")
+
+
+_records = ctypes.c_int64 * 6   # x and q as dpdr_matrix records
+_codes = _int8 = _float32 = _device = _quantise = None
+
+
+def _first():
+    """What a call looks up once."""
+    global _codes, _int8, _float32, _device, _quantise
+    import torch
+    _quantise = lib().dpdr_quantise
+    _int8, _float32 = torch.int8, torch.float32
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _codes = {getattr(torch, name): code for name, code in RESULTS.items()}
 
 
 class _Serving(_Projection):
