@@ -95,7 +95,8 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
         };
         const int64_t logits = take(max_rows * experts * 4), x = take(max_rows * l.d_pad * 2),
                       hidden = take(pairs * l.h_pad * (l.terms == 1 ? 4 : 2 * l.terms)), some = take(places * 4),
-                      z = take(max_rows <= kWholeRows ? 0 : pairs * n_model * 4), expert = take(pairs * 4),
+                      z = take(max_rows <= kWholeRows ? 0 : pairs * n_model * 4), expert = take(pairs * 4), shares = take(pairs * 4),
+                      scores = take(max_rows * 4),
                       up = take(up_warps * 4), down = take(down_warps * 4);
         e = cudaMalloc(&P->scratch, size_t(size));
         // counters at zero, and what lies behind the rows of x and of hidden values
@@ -108,6 +109,8 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
         l.parts = reinterpret_cast<float*>(P->scratch + some);
         l.z = reinterpret_cast<float*>(P->scratch + z);
         l.expert = reinterpret_cast<int32_t*>(P->scratch + expert);
+        l.shares = reinterpret_cast<float*>(P->scratch + shares);
+        l.score_count = reinterpret_cast<uint32_t*>(P->scratch + scores);
         l.up_count = reinterpret_cast<uint32_t*>(P->scratch + up);
         l.down_count = reinterpret_cast<uint32_t*>(P->scratch + down);
     }

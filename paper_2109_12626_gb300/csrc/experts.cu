@@ -5,11 +5,9 @@
 //   share = exp(l - max) over the sum of these (of the chosen, or of all)
 //   h_e = share_e act(x wg_e^T) (x wu_e^T);  y = sum_e h_e wd_e^T
 //
-// Three kernels, each set up while the one before drains: scores_kernel forms l
-// and lays x out for the products; up_kernel's CTAs all choose the experts for
-// themselves (a few hundred values from L2: less than one CTA doing so and the
-// others waiting for it), then stream the chosen experts' gate and up weights
-// past the tokens that chose them (stream.cuh), a unit being 16 hidden features
+// Three kernels, each set up while the one before drains: scores_kernel forms l,
+// chooses, and lays x out for the products; up_kernel streams the chosen experts'
+// gate and up weights past the tokens that chose them (stream.cuh), a unit being 16 hidden features
 // of an expert; down_kernel does the same with the down weights, a unit being 32
 // features of the result.  Up to 8 tokens have a column each there, and the sum runs
 // through all experts; more have their results by expert, which combine_kernel
@@ -43,10 +41,70 @@ constexpr int kScoreWarps = 4;
 
 // ------------------------------------------------------------------ scores
 
+// Order of scores as whole numbers above 0: NaN highest, -0 as 0
+__device__ __forceinline__ uint32_t rank_of(float v)
+{
+    if (v != v) return 0xFFFFFFFFu;
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// The experts of token t, by a warp: lane j the j-th chosen
+template <int EACH>
+__device__ __forceinline__ void choose(const Layer& l, int t, int lane)
+{
+    constexpr uint32_t kAll = 0xFFFFFFFFu;
+    float v[EACH];
+    uint32_t rank[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; j++) {
+        const int e = lane + 32 * j;
+        v[j] = e < l.total ? __ldcg(l.logits + int64_t(t) * l.total + e) : 0.0f;
+        rank[j] = e < l.total ? rank_of(v[j]) : 0u;
+    }
+    int mine = 0;
+    float score = 0.0f;
+    for (int i = 0; i < l.top; i++) {
+        uint32_t best = 0;
+        int at = 1 << 30;
+        float value = 0.0f;
+#pragma unroll
+        for (int j = 0; j < EACH; j++)
+            if (rank[j] > best) best = rank[j], at = lane + 32 * j, value = v[j];
+        const uint32_t most = __reduce_max_sync(kAll, best);
+        const int who = int(__reduce_min_sync(kAll, uint32_t(best == most ? at : 1 << 30)));
+        value = __shfl_sync(kAll, value, who & 31);
+        if (lane == i) mine = who, score = value;
+#pragma unroll
+        for (int j = 0; j < EACH; j++)
+            if (who == lane + 32 * j) rank[j] = 0u;
+    }
+    const float high = __shfl_sync(kAll, score, 0);
+    const float weight = lane < l.top ? expf(score - high) : 0.0f;
+    float sum = weight;
+    if (!l.normalise) {
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < EACH; j++)
+            if (lane + 32 * j < l.total) sum += expf(v[j] - high);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+    if (lane < l.top) {
+        const int pair = t * l.top + lane;
+        l.expert[pair] = mine;
+        l.shares[pair] = weight / sum;
+        if (l.chosen) l.chosen[pair] = mine;
+        if (l.share) l.share[pair] = weight / sum;
+    }
+}
+
 // A CTA forms the scores of TOK tokens with one expert, and all CTAs lay out x's
 // rows.  The products of 16-bit values are exact in float32; a thread sums every
 // 128th group of 8 and the threads' sums are added pairwise, so that few
-// roundings lie on top of each other: which experts are chosen hangs on these.
+// roundings lie on top of each other: which experts are chosen hangs on these.  The
+// last CTA of the tokens' to come chooses for them: once for all, since a choice in
+// every CTA of the product kernels took those 20 us each with 64 tokens of 128.
 // Bound by a trip to memory: each thread asks for all that it needs at once.
 template <int TOK, bool VEC>
 __global__ void __launch_bounds__(32 * kScoreWarps) scores_kernel(const __grid_constant__ Layer l)
@@ -123,6 +181,13 @@ __global__ void __launch_bounds__(32 * kScoreWarps) scores_kernel(const __grid_c
                                                        v[4] | uint32_t(v[5]) << 16, v[6] | uint32_t(v[7]) << 16);
         }
     }
+    if (last_to_come(l.score_count + blockIdx.x / l.total, uint32_t(l.total)))
+        for (int t = t0 + warp; t < min(t0 + TOK, l.rows); t += kScoreWarps) {
+            if (l.total <= 32) choose<1>(l, t, lane);
+            else if (l.total <= 64) choose<2>(l, t, lane);
+            else if (l.total <= 128) choose<4>(l, t, lane);
+            else choose<16>(l, t, lane);
+        }
 }
 
 // ------------------------------------------------------------------ choice
@@ -153,78 +218,21 @@ struct Choice {
     __device__ __forceinline__ int from(int i) const { return entry[i] >> 17; }
 };
 
-// Order of scores as whole numbers above 0: NaN highest, -0 as 0
-__device__ __forceinline__ uint32_t rank_of(float v)
-{
-    if (v != v) return 0xFFFFFFFFu;
-    const uint32_t b = __float_as_uint(v + 0.0f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-
-// The experts of every eighth token, by this warp: lane j the j-th chosen
-template <int EACH>
-__device__ __forceinline__ void choose(const Layer& l, const Choice& c, int warp, int lane)
-{
-    constexpr uint32_t kAll = 0xFFFFFFFFu;
-    for (int t = warp; t < l.rows; t += kWarps) {
-        float v[EACH];
-        uint32_t rank[EACH];
-#pragma unroll
-        for (int j = 0; j < EACH; j++) {
-            const int e = lane + 32 * j;
-            v[j] = e < l.total ? __ldcg(l.logits + int64_t(t) * l.total + e) : 0.0f;
-            rank[j] = e < l.total ? rank_of(v[j]) : 0u;
-        }
-        int mine = 0;
-        float score = 0.0f;
-        for (int i = 0; i < l.top; i++) {
-            uint32_t best = 0;
-            int at = 1 << 30;
-            float value = 0.0f;
-#pragma unroll
-            for (int j = 0; j < EACH; j++)
-                if (rank[j] > best) best = rank[j], at = lane + 32 * j, value = v[j];
-            const uint32_t most = __reduce_max_sync(kAll, best);
-            const int who = int(__reduce_min_sync(kAll, uint32_t(best == most ? at : 1 << 30)));
-            value = __shfl_sync(kAll, value, who & 31);
-            if (lane == i) mine = who, score = value;
-#pragma unroll
-            for (int j = 0; j < EACH; j++)
-                if (who == lane + 32 * j) rank[j] = 0u;
-        }
-        const float high = __shfl_sync(kAll, score, 0);
-        const float weight = lane < l.top ? expf(score - high) : 0.0f;
-        float sum = weight;
-        if (!l.normalise) {
-            sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < EACH; j++)
-                if (lane + 32 * j < l.total) sum += expf(v[j] - high);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
-        if (lane < l.top) {
-            c.share[t * l.top + lane] = weight / sum;
-            c.expert[t * l.top + lane] = int16_t(mine);
-        }
-    }
-}
-
-// All of it, in every CTA alike.  `room`: shared memory that is free so far, 10
+// The lists of it, in every CTA alike.  `room`: shared memory that is free so far, 10
 // bytes for each local expert.  `most`: pairs of an entry.
-__device__ void choose_all(const Layer& l, Choice& c, char* room, int most, int warp, int lane)
+__device__ void list_all(const Layer& l, Choice& c, char* room, int most, int warp, int lane)
 {
     __shared__ int entries, columns;
     uint64_t* mask = reinterpret_cast<uint64_t*>(room);   // an expert's tokens
     int16_t* from = reinterpret_cast<int16_t*>(mask + l.local);
     const int pairs = l.rows * l.top;
     for (int e = threadIdx.x; e < l.local; e += kThreads) mask[e] = 0;
-    if (l.total <= 32) choose<1>(l, c, warp, lane);
-    else if (l.total <= 64) choose<2>(l, c, warp, lane);
-    else if (l.total <= 128) choose<4>(l, c, warp, lane);
-    else choose<16>(l, c, warp, lane);
-    __syncthreads();
     for (int p = threadIdx.x; p < pairs; p += kThreads) {
+        c.expert[p] = int16_t(__ldcg(l.expert + p));
+        c.share[p] = __ldcg(l.shares + p);
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < pairs; p += kThreads) {   // its own
         const int e = c.expert[p] - l.first;
         if (e >= 0 && e < l.local)
             atomicOr(reinterpret_cast<unsigned long long*>(mask + e), 1ull << (p / l.top));
@@ -544,20 +552,13 @@ __global__ void __launch_bounds__(kThreads, 2) up_kernel(const __grid_constant__
     Choice c(raw + kBefore, l.rows * l.top);
     wait_previous();
     allow_next();
-    choose_all(l, c, raw, 8 * kMost, warp, lane);
-    if (blockIdx.x == 0)
-        for (int p = threadIdx.x; p < l.rows * l.top; p += kThreads) {
-            l.expert[p] = c.expert[p];
-            if (l.chosen) l.chosen[p] = c.expert[p];
-            if (l.share) l.share[p] = c.share[p];
-        }
+    list_all(l, c, raw, 8 * kMost, warp, lane);
     if (c.columns <= 8) up_units<WT, XT, 1, SHIFT>(l, c, raw, warp, lane, id);
     else if (c.columns <= 16) up_units<WT, XT, 2, SHIFT>(l, c, raw, warp, lane, id);
     else up_units<WT, XT, kMost, SHIFT>(l, c, raw, warp, lane, id);
 }
 
-// The choice is made again from the scores, which are there: up_kernel let this
-// kernel start after it had waited for them.
+// The choice is there: up_kernel let this kernel start after it had waited for it.
 template <int WT, bool SHIFT, int TERMS>
 __global__ void __launch_bounds__(kThreads, 2) down_kernel(const __grid_constant__ Layer l)
 {
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const __grid_constant
     constexpr int kMost = (WT == kI8 ? 2 : 4) / (TERMS == 3 || SHIFT ? 2 : 1);
     Choice c(raw + kBefore, l.rows * l.top);
     allow_next();
-    choose_all(l, c, raw, 8 * kMost, warp, lane);
+    list_all(l, c, raw, 8 * kMost, warp, lane);
     if (c.entries == 0) {   // no token chose an expert that is here
         wait_previous();
         for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; l.rows <= kWholeRows && i < int64_t(l.rows) * l.d;

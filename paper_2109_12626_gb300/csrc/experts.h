@@ -38,7 +38,9 @@ struct Layer {
     int terms, pairs;
     float* parts;                  // sums of units that several warps share
     float* z;                      // of more than 8 rows, the experts' results by pair
-    int32_t* expert;               // of a pair
+    int32_t* expert;               // of a pair, and its share
+    float* shares;
+    uint32_t* score_count;         // a counter for some tokens
     uint32_t* up_count;            // a counter a warp
     uint32_t* down_count;
     int up_ctas[2], down_ctas[2];  // of the product kernels, without and with shifted rows
