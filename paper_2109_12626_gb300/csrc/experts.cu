@@ -37,7 +37,9 @@ using namespace stream;
 
 namespace {
 
-constexpr int kScoreWarps = 4;
+// warps of a CTA that forms scores: room beside the product kernels of few tokens,
+// and one for each token whose experts it chooses
+constexpr int score_warps(int tok) { return tok == 8 ? 8 : 4; }
 
 // ------------------------------------------------------------------ scores
 
@@ -101,14 +103,15 @@ __device__ __forceinline__ void choose(const Layer& l, int t, int lane)
 
 // A CTA forms the scores of TOK tokens with one expert, and all CTAs lay out x's
 // rows.  The products of 16-bit values are exact in float32; a thread sums every
-// 128th group of 8 and the threads' sums are added pairwise, so that few
+// 128th or 256th group of 8 and the threads' sums are added pairwise, so that few
 // roundings lie on top of each other: which experts are chosen hangs on these.  The
 // last CTA of the tokens' to come chooses for them: once for all, since a choice in
 // every CTA of the product kernels took those 20 us each with 64 tokens of 128.
 // Bound by a trip to memory: each thread asks for all that it needs at once.
 template <int TOK, bool VEC>
-__global__ void __launch_bounds__(32 * kScoreWarps) scores_kernel(const __grid_constant__ Layer l)
+__global__ void __launch_bounds__(32 * score_warps(TOK), TOK == 8 ? 3 : 8) scores_kernel(const __grid_constant__ Layer l)
 {
+    constexpr int kScoreWarps = score_warps(TOK);
     __shared__ float part[kScoreWarps][TOK];
     constexpr int kThreads = 32 * kScoreWarps;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -163,7 +166,14 @@ __global__ void __launch_bounds__(32 * kScoreWarps) scores_kernel(const __grid_c
     __syncthreads();
     if (threadIdx.x < TOK && t0 + int(threadIdx.x) < l.rows) {
         const int i = threadIdx.x;
-        l.logits[int64_t(t0 + i) * l.total + e] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+        float sum[kScoreWarps];
+#pragma unroll
+        for (int w = 0; w < kScoreWarps; w++) sum[w] = part[w][i];
+#pragma unroll
+        for (int o = kScoreWarps / 2; o > 0; o /= 2)
+#pragma unroll
+            for (int w = 0; w < o; w++) sum[w] += sum[w + o];
+        l.logits[int64_t(t0 + i) * l.total + e] = sum[0];
     }
     // x by rows of d_pad
     const int64_t units = l.rows * (l.d_pad / 8), apart = int64_t(gridDim.x) * blockDim.x;
@@ -226,6 +236,22 @@ __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int wa
     uint64_t* mask = reinterpret_cast<uint64_t*>(room);   // an expert's tokens
     int16_t* from = reinterpret_cast<int16_t*>(mask + l.local);
     const int pairs = l.rows * l.top;
+    if (l.rows == 1) {   // a pair an entry
+        if (warp == 0) {
+            const int e = lane < pairs ? __ldcg(l.expert + lane) - l.first : -1;
+            const float share = lane < pairs ? __ldcg(l.shares + lane) : 0.0f;
+            const bool here = e >= 0 && e < l.local;
+            const uint32_t all = __ballot_sync(0xFFFFFFFFu, here);
+            const int at = __popc(all & ((1u << lane) - 1));
+            if (here) c.entry[at] = Choice::packed(e, 1, at), c.order[at] = int16_t(lane);
+            if (lane < pairs) c.share[lane] = share;
+            if (lane == 0) entries = __popc(all);
+        }
+        __syncthreads();
+        c.entries = entries;
+        c.columns = 1;
+        return;
+    }
     for (int e = threadIdx.x; e < l.local; e += kThreads) mask[e] = 0;
     for (int p = threadIdx.x; p < pairs; p += kThreads) {
         c.expert[p] = int16_t(__ldcg(l.expert + p));
@@ -273,6 +299,20 @@ __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int wa
     __syncthreads();   // `room` is free again
 }
 
+// Whether every row of a stack of matrices starts at a multiple of 16 bytes
+__host__ __device__ bool aligned(const dpdr_matrices& m, int local, int64_t rows, int esize)
+{
+    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows == 1 || m.row_stride * esize % 16 == 0) &&
+           (local == 1 || m.stride * esize % 16 == 0);
+}
+
+__host__ __device__ bool up_shifted(const Layer& l)
+{
+    const int es = l.w_int8 ? 1 : 2;
+    return !aligned(l.w[0], l.local, l.h, es) || !aligned(l.w[1], l.local, l.h, es);
+}
+__host__ __device__ bool down_shifted(const Layer& l) { return !aligned(l.w[2], l.local, l.d, l.w_int8 ? 1 : 2); }
+
 // ---------------------------------------------------------------- products
 
 __device__ __forceinline__ float act_of(int act, float z)
@@ -285,9 +325,27 @@ __device__ __forceinline__ float act_of(int act, float z)
 }
 
 // The warps that share `total` pieces: all, while each has a few
-__device__ __forceinline__ Shares shares_of(int total, int each)
+__device__ __forceinline__ Shares shares_of(int total, int each, int ctas)
 {
-    return Shares(total, max(1, min(int(gridDim.x) * kWarps, total / kLeast)), each);
+    return Shares(total, max(1, min(ctas * kWarps, total / kLeast)), each);
+}
+
+// Asks the first `bytes` of a warp's share of the weights into L2
+template <typename Job>
+__device__ __forceinline__ void ask_share(const Job& job, int each, int piece, int ctas, int bytes, int lane, int id)
+{
+    const Shares s = shares_of(job.units * job.parts * each, job.parts * each, ctas);
+    if (id >= s.of) return;
+    int at = s.start(id);
+    const int end = min(s.start(id + 1), at + bytes / (kRows * piece));
+    while (at < end) {
+        const int i = at / each, there = min(end, (i + 1) * each);
+        const Unit q = job.part(i, at - i * each, there - i * each);
+        const char* p = q.row(lane);
+        const int to = min(q.last * piece, q.row_bytes);
+        for (int k = q.first * piece; k < to; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
+        at = there;
+    }
 }
 
 // What a warp does with its share: job.part(i) is unit i % ... the i-th run of
@@ -296,7 +354,7 @@ __device__ __forceinline__ Shares shares_of(int total, int each)
 template <typename S, int NT, typename Job>
 __device__ __forceinline__ void run_share(S& st, const Job& job, int each, const Layer& l, int lane, int id)
 {
-    const Shares s = shares_of(job.units * job.parts * each, job.parts * each);
+    const Shares s = shares_of(job.units * job.parts * each, job.parts * each, gridDim.x);
     if (id >= s.of) return;
     int at = s.start(id);
     const int end = s.start(id + 1);
@@ -504,6 +562,8 @@ struct Down {
 // bytes of shared memory in front of the choice: rings, then tiles
 constexpr int kRings = kWarps * kRing, kBefore = kRings + kJoin * 4;
 
+constexpr int kAsked = 8192;   // bytes that a warp asks into L2 ahead
+
 // Bytes of a row of weights that a stage holds: as many as let the ring hold two
 constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
 {
@@ -511,7 +571,7 @@ constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
     return 5 * stage <= kRing ? 128 : 64;
 }
 
-template <int WT, int XT, int NT, bool SHIFT>
+template <int WT, int XT, int NT, bool SHIFT, bool FEW>
 __device__ __forceinline__ void up_units(const Layer& l, const Choice& c, char* raw, int warp, int lane, int id)
 {
     constexpr int kPiece = piece_of(WT, XT, NT, SHIFT, 1);
@@ -531,55 +591,52 @@ __device__ __forceinline__ void down_units(const Layer& l, const Choice& c, char
     const Down<WT, NT, kXT, WHOLE> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
     const int each = (l.h * size_of(WT) + kPiece - 1) / kPiece;
     // the first weights are asked into L2 while up_kernel drains
-    const Shares s = shares_of(job.units * job.parts * each, job.parts * each);
-    if (id < s.of) {
-        const int at = s.start(id), i = at / each;
-        const Unit q = job.part(i, at - i * each, each);
-        const char* p = q.row(lane) + q.first * kPiece;
-        const int to = min(min(4, s.start(id + 1) - at) * kPiece, q.row_bytes - q.first * kPiece);
-        for (int k = 0; k < to; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
-    }
+    ask_share(job, each, kPiece, gridDim.x, kAsked, lane, id);
     wait_previous();
     run_share<S, NT>(st, job, each, l, lane, id);
 }
 
-template <int WT, int XT, bool SHIFT>
-__global__ void __launch_bounds__(kThreads, 2) up_kernel(const __grid_constant__ Layer l)
+// FEW: up to 8 tokens.  These kernels hold the code for one eight of columns alone,
+// and leave registers (of 288 threads, in the bounds) for the next call's
+// scores_kernel to be set up beside them.
+constexpr int bound_of(bool few) { return few ? kThreads + 32 : kThreads; }
+
+template <int WT, int XT, bool SHIFT, bool FEW>
+__global__ void __launch_bounds__(bound_of(FEW), 2) up_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, id = warp * gridDim.x + blockIdx.x;
-    constexpr int kMost = WT == kI8 ? 2 : 4;
+    constexpr int kMost = FEW ? 1 : WT == kI8 ? 2 : 4;
     Choice c(raw + kBefore, l.rows * l.top);
     wait_previous();
     allow_next();
     list_all(l, c, raw, 8 * kMost, warp, lane);
-    if (c.columns <= 8) up_units<WT, XT, 1, SHIFT>(l, c, raw, warp, lane, id);
-    else if (c.columns <= 16) up_units<WT, XT, 2, SHIFT>(l, c, raw, warp, lane, id);
-    else up_units<WT, XT, kMost, SHIFT>(l, c, raw, warp, lane, id);
+    if (FEW || c.columns <= 8) up_units<WT, XT, 1, SHIFT, FEW>(l, c, raw, warp, lane, id);
+    else if (c.columns <= 16) up_units<WT, XT, FEW ? 1 : 2, SHIFT, FEW>(l, c, raw, warp, lane, id);
+    else up_units<WT, XT, kMost, SHIFT, FEW>(l, c, raw, warp, lane, id);
 }
 
 // The choice is there: up_kernel let this kernel start after it had waited for it.
-template <int WT, bool SHIFT, int TERMS>
-__global__ void __launch_bounds__(kThreads, 2) down_kernel(const __grid_constant__ Layer l)
+template <int WT, bool SHIFT, int TERMS, bool FEW>
+__global__ void __launch_bounds__(bound_of(FEW), 2) down_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, id = warp * gridDim.x + blockIdx.x;
     // eights of columns that the ring has room for
-    constexpr int kMost = (WT == kI8 ? 2 : 4) / (TERMS == 3 || SHIFT ? 2 : 1);
+    constexpr int kMost = FEW ? 1 : (WT == kI8 ? 2 : 4) / (TERMS == 3 || SHIFT ? 2 : 1);
     Choice c(raw + kBefore, l.rows * l.top);
     allow_next();
     list_all(l, c, raw, 8 * kMost, warp, lane);
     if (c.entries == 0) {   // no token chose an expert that is here
         wait_previous();
-        for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; l.rows <= kWholeRows && i < int64_t(l.rows) * l.d;
+        for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; FEW && i < int64_t(l.rows) * l.d;
              i += int64_t(gridDim.x) * kThreads)
             proj::store1(l.y, i / l.d * l.y_rs + i % l.d, 0.0f, l.out_f32, l.half);
         return;
     }
-    if (l.rows <= kWholeRows) down_units<WT, 1, SHIFT, TERMS, true>(l, c, raw, warp, lane, id);
-    else if (c.columns <= 8) down_units<WT, 1, SHIFT, TERMS, false>(l, c, raw, warp, lane, id);
-    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS, false>(l, c, raw, warp, lane, id);
-    else down_units<WT, kMost, SHIFT, TERMS, false>(l, c, raw, warp, lane, id);
+    if (FEW || c.columns <= 8) down_units<WT, 1, SHIFT, TERMS, FEW>(l, c, raw, warp, lane, id);
+    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS, FEW>(l, c, raw, warp, lane, id);
+    else down_units<WT, kMost, SHIFT, TERMS, FEW>(l, c, raw, warp, lane, id);
 }
 
 // What each token's experts gave, added up in the order of their shares
@@ -606,38 +663,30 @@ __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ La
 
 using Kernel = void (*)(Layer);
 
-// Whether every row of a stack of matrices starts at a multiple of 16 bytes
-bool aligned(const dpdr_matrices& m, int local, int64_t rows, int esize)
+template <bool SHIFT, bool FEW>
+Kernel up_of(const Layer& l)
 {
-    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows == 1 || m.row_stride * esize % 16 == 0) &&
-           (local == 1 || m.stride * esize % 16 == 0);
+    if (l.w_int8) return l.half ? up_kernel<kI8, kF16, SHIFT, FEW> : up_kernel<kI8, kBf16, SHIFT, FEW>;
+    return l.half ? up_kernel<kF16, kF16, SHIFT, FEW> : up_kernel<kBf16, kBf16, SHIFT, FEW>;
+}
+Kernel up_of(const Layer& l, bool shift, bool few)
+{
+    if (few) return shift ? up_of<true, true>(l) : up_of<false, true>(l);
+    return shift ? up_of<true, false>(l) : up_of<false, false>(l);
 }
 
-bool up_shifted(const Layer& l)
-{
-    const int es = l.w_int8 ? 1 : 2;
-    return !aligned(l.w[0], l.local, l.h, es) || !aligned(l.w[1], l.local, l.h, es);
-}
-bool down_shifted(const Layer& l) { return !aligned(l.w[2], l.local, l.d, l.w_int8 ? 1 : 2); }
-
-Kernel up_of(const Layer& l, bool shift)
-{
-    if (l.w_int8) {
-        if (l.half) return shift ? up_kernel<kI8, kF16, true> : up_kernel<kI8, kF16, false>;
-        return shift ? up_kernel<kI8, kBf16, true> : up_kernel<kI8, kBf16, false>;
-    }
-    if (l.half) return shift ? up_kernel<kF16, kF16, true> : up_kernel<kF16, kF16, false>;
-    return shift ? up_kernel<kBf16, kBf16, true> : up_kernel<kBf16, kBf16, false>;
-}
-
-template <bool SHIFT>
+template <bool SHIFT, bool FEW>
 Kernel down_of(const Layer& l)
 {
-    if (l.w_int8) return l.terms == 2 ? down_kernel<kI8, SHIFT, 2> : down_kernel<kI8, SHIFT, 3>;
-    if (l.half) return down_kernel<kF16, SHIFT, 1>;
-    return l.terms == 2 ? down_kernel<kBf16, SHIFT, 2> : down_kernel<kBf16, SHIFT, 3>;
+    if (l.w_int8) return l.terms == 2 ? down_kernel<kI8, SHIFT, 2, FEW> : down_kernel<kI8, SHIFT, 3, FEW>;
+    if (l.half) return down_kernel<kF16, SHIFT, 1, FEW>;
+    return l.terms == 2 ? down_kernel<kBf16, SHIFT, 2, FEW> : down_kernel<kBf16, SHIFT, 3, FEW>;
 }
-Kernel down_of(const Layer& l, bool shift) { return shift ? down_of<true>(l) : down_of<false>(l); }
+Kernel down_of(const Layer& l, bool shift, bool few)
+{
+    if (few) return shift ? down_of<true, true>(l) : down_of<false, true>(l);
+    return shift ? down_of<true, false>(l) : down_of<false, false>(l);
+}
 
 size_t product_smem(const Layer& l) { return size_t(kBefore) + size_t(l.rows) * l.top * 12; }
 
@@ -664,11 +713,17 @@ int resident(Kernel k, size_t bytes, int num_sms, int* ctas)
 
 int product_ctas(Layer& l, int num_sms)
 {
+    const size_t bytes = product_smem(l);
     for (int shift = 0; shift < 2; shift++) {
-        const size_t bytes = product_smem(l);
-        int rc = resident(up_of(l, shift), bytes, num_sms, &l.up_ctas[shift]);
-        if (!rc) rc = resident(down_of(l, shift), bytes, num_sms, &l.down_ctas[shift]);
-        if (rc) return rc;
+        l.up_ctas[shift] = l.down_ctas[shift] = 1 << 30;
+        for (int few = 0; few < 2; few++) {
+            int up = 0, down = 0;
+            int rc = resident(up_of(l, shift, few), bytes, num_sms, &up);
+            if (!rc) rc = resident(down_of(l, shift, few), bytes, num_sms, &down);
+            if (rc) return rc;
+            l.up_ctas[shift] = std::min(l.up_ctas[shift], up);
+            l.down_ctas[shift] = std::min(l.down_ctas[shift], down);
+        }
     }
     return DPDR_OK;
 }
@@ -684,15 +739,15 @@ int launch(const Layer& l, int num_sms, cudaStream_t s)
     else if (l.rows <= 16) tok = 4, scores = vec ? scores_kernel<4, true> : scores_kernel<4, false>;
     else scores = vec ? scores_kernel<8, true> : scores_kernel<8, false>;
     const int grid = (l.rows + tok - 1) / tok * l.total;
-    int rc = proj::launch(scores, dim3(unsigned(grid)), dim3(32 * kScoreWarps), 0, 1, s, "experts' scores", l);
-    const bool up = up_shifted(l), down = down_shifted(l);
+    int rc = proj::launch(scores, dim3(unsigned(grid)), dim3(32 * score_warps(tok)), 0, 1, s, "experts' scores", l);
+    const bool up = up_shifted(l), down = down_shifted(l), few = l.rows <= kWholeRows;
     if (!rc)
-        rc = proj::launch(up_of(l, up), dim3(unsigned(l.up_ctas[up])), dim3(kThreads), product_smem(l), 1, s,
+        rc = proj::launch(up_of(l, up, few), dim3(unsigned(l.up_ctas[up])), dim3(kThreads), product_smem(l), 1, s,
                           "experts' up products", l);
     if (!rc)
-        rc = proj::launch(down_of(l, down), dim3(unsigned(l.down_ctas[down])), dim3(kThreads), product_smem(l), 1, s,
+        rc = proj::launch(down_of(l, down, few), dim3(unsigned(l.down_ctas[down])), dim3(kThreads), product_smem(l), 1, s,
                           "experts' down products", l);
-    if (!rc && l.rows > kWholeRows)
+    if (!rc && !few)
         rc = proj::launch(combine_kernel, dim3(unsigned((l.d + 255) / 256), unsigned(l.rows)), dim3(256), 0, 1, s,
                           "experts' sum", l);
     return rc;
