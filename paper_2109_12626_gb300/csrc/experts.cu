@@ -13,10 +13,10 @@
 // through all experts; more have their results by expert, which combine_kernel
 // adds up in the order of the shares.
 //
-// All pieces of all units are dealt out to the warps in equal contiguous shares.
-// A unit that lies in several shares is finished by the last of its warps to
-// come, which adds up their sums in order: no warp waits for another, no barrier
-// follows the choice, no sum's order depends on timing.  (A CTA a unit, its sum over
+// All pieces of all units are dealt out to the warps in equal contiguous shares, or
+// where units are few each to a team of warps.  A unit that lies in several shares, or
+// a team in several CTAs, is finished by the last of its warps (CTAs) to come, which adds
+// up their sums in order: none waits for another, no sum's order depends on timing.  (A CTA a unit, its sum over
 // eight warps, with two barriers and a fence each: 8 rows of 64 experts of 2048 x
 // 1024 125 us.)
 //
@@ -324,51 +324,37 @@ __device__ __forceinline__ float act_of(int act, float z)
     return v;
 }
 
-// The warps that share `total` pieces: all, while each has a few
-__device__ __forceinline__ Shares shares_of(int total, int each, int ctas)
-{
-    return Shares(total, max(1, min(ctas * kWarps, total / kLeast)), each);
-}
+constexpr int kAsked = 8192;   // bytes that a warp asks into L2 ahead
 
-// Asks the first `bytes` of a warp's share of the weights into L2
-template <typename Job>
-__device__ __forceinline__ void ask_share(const Job& job, int each, int piece, int ctas, int bytes, int lane, int id)
-{
-    const Shares s = shares_of(job.units * job.parts * each, job.parts * each, ctas);
-    if (id >= s.of) return;
-    int at = s.start(id);
-    const int end = min(s.start(id + 1), at + bytes / (kRows * piece));
-    while (at < end) {
-        const int i = at / each, there = min(end, (i + 1) * each);
-        const Unit q = job.part(i, at - i * each, there - i * each);
-        const char* p = q.row(lane);
-        const int to = min(q.last * piece, q.row_bytes);
-        for (int k = q.first * piece; k < to; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
-        at = there;
-    }
-}
-
-// What a warp does with its share: job.part(i) is unit i % ... the i-th run of
-// `each` pieces along k, job.parts of them a unit; job.columns(i) where its columns
-// lie; job.finish(u, sums).
+// What a warp does with its pieces: job.part(i) is the i-th run of `each` pieces along
+// k, job.parts of them a unit; job.columns(i) where its columns lie; job.finish(u,
+// sums).
 template <typename S, int NT, typename Job>
-__device__ __forceinline__ void run_share(S& st, const Job& job, int each, const Layer& l, int lane, int id)
-{
-    const Shares s = shares_of(job.units * job.parts * each, job.parts * each, gridDim.x);
-    if (id >= s.of) return;
-    int at = s.start(id);
-    const int end = s.start(id + 1);
-    int loading = at;
-    auto next = [&]() {
-        if (loading >= end) return;
-        const int i = loading / each, to = min(end, (i + 1) * each);
-        st.load_from(job.part(i, loading - i * each, to - i * each), job.columns(i));
-        loading = to;
-    };
-    st.begin(next);
-    while (at < end) {
-        const int u = at / s.each, from = at, to = min(end, (u + 1) * s.each);
-        float sum[2][NT][4];
+struct Run {
+    S& st;
+    const Job& job;
+    const Layer& l;
+    const int each, lane, warp;
+    float* const room;   // of this warp, NT tiles, once its loads are done
+
+    // Asks the first of pieces [at, end) into L2
+    __device__ __forceinline__ void ask(int at, int end) const
+    {
+        end = min(end, at + kAsked / (kRows * S::kPiece));
+        while (at < end) {
+            const int i = at / each, there = min(end, (i + 1) * each);
+            const Unit q = job.part(i, at - i * each, there - i * each);
+            const char* p = q.row(lane);
+            const int to = min(q.last * S::kPiece, q.row_bytes);
+            for (int k = q.first * S::kPiece; k < to; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
+            at = there;
+        }
+    }
+
+    // Pieces [at, to) of one unit added to `sum`
+    template <typename Next>
+    __device__ __forceinline__ void sums(int at, int to, float (&sum)[2][NT][4], Next next)
+    {
         S::clear(sum);
         while (at < to) {
             const int i = at / each, there = min(to, (i + 1) * each);
@@ -389,10 +375,103 @@ __device__ __forceinline__ void run_share(S& st, const Job& job, int each, const
             }
             at = there;
         }
-        if (to - from < s.each && !join_parts<NT>(s, id, u, sum, l.parts, job.count, lane)) continue;
+    }
+
+    __device__ __forceinline__ auto loads(int& loading, int end)
+    {
+        return [this, &loading, end]() {
+            if (loading >= end) return;
+            const int i = loading / each, to = min(end, (i + 1) * each);
+            st.load_from(job.part(i, loading - i * each, to - i * each), job.columns(i));
+            loading = to;
+        };
+    }
+
+    // Many units: contiguous shares; one that a unit begins or ends in leaves its part.
+    // Warps next to each other are of different CTAs.
+    template <bool ASK>
+    __device__ __forceinline__ void shares()
+    {
+        const int id = warp * gridDim.x + blockIdx.x, per = job.parts * each, total = job.units * per;
+        const Shares s(total, max(1, min(int(gridDim.x) * kWarps, total / kLeast)), per);
+        int at = s.start(min(id, s.of)), loading = at;
+        const int end = s.start(min(id + 1, s.of));
+        if (ASK) {
+            ask(at, end);
+            wait_previous();
+        }
+        auto next = loads(loading, end);
+        st.begin(next);
+        while (at < end) {
+            const int u = at / per, to = min(end, (u + 1) * per);
+            float sum[2][NT][4];
+            sums(at, to, sum, next);
+            const bool some = to - at < per;
+            at = to;
+            if (some) {
+                const int from = u * per, first = s.owner(from), last = s.owner(from + per - 1);
+                auto place = [&](int w) { return l.parts + (int64_t(w) * 2 + (s.start(w) < from)) * (NT * 256); };
+                if (!join_parts<NT>(sum, id, first, last, place, job.count + first, lane)) continue;
+            }
+            job.finish(u, sum);
+        }
+    }
+
+    // Few: teams of warps that follow each other; those of one CTA join their sums in
+    // its shared memory.
+    template <bool ASK>
+    __device__ __forceinline__ void teams()
+    {
+        const int per = job.parts * each;
+        const Teams t{job.units, int(gridDim.x) * kWarps, per};
+        const int base = int(blockIdx.x) * kWarps, id = base + warp;
+        const int u = t.unit(id), begins = t.start(u), size = t.size(u), place_of = id - begins;
+        const bool in = place_of < size;
+        const int from = u * per, at = in ? from + int(int64_t(per) * place_of / size) : 0,
+                  end = in ? from + int(int64_t(per) * (place_of + 1) / size) : 0;
+        if (ASK) {
+            ask(at, end);
+            wait_previous();
+        }
+        int loading = at;
+        auto next = loads(loading, end);
+        st.begin(next);
+        float sum[2][NT][4];
+        sums(at, end, sum, next);
+        // of the team, the warps of this CTA
+        const int low = max(0, begins - base), high = min(kWarps, begins + size - base);
+        if (size > 1) {
+            copies_wait<0>();
+            if (in && warp > low)
+#pragma unroll
+                for (int n = 0; n < NT; n++) put_tile(room + n * kTile, sum[0][n], sum[1][n], lane);
+            __syncwarp();
+        }
+        __syncthreads();
+        if (!in || warp > low) return;
+        for (int w = low + 1; w < high; w++) {
+            const float* other = room + (w - warp) * (S::kWarpBytes / 4);
+#pragma unroll
+            for (int n = 0; n < NT; n++) add_tile(other + n * kTile, sum[0][n], sum[1][n], lane);
+        }
+        if (high - low < size) {   // at most two of a CTA's units reach into others
+            const int first = begins / kWarps, last = (begins + size - 1) / kWarps;
+            auto place = [&](int c) { return l.parts + (int64_t(c) * 2 + (c == first)) * (NT * 256); };
+            if (!join_parts<NT>(sum, int(blockIdx.x), first, last, place, job.count + first, lane)) return;
+        }
         job.finish(u, sum);
     }
-}
+
+    // ASK: the first weights are asked into L2 while the kernel before drains, which is
+    // then waited for
+    template <bool ASK>
+    __device__ __forceinline__ void go()
+    {
+        if (job.units <= 0) return;
+        if (2 * job.units <= int(gridDim.x) * kWarps) teams<ASK>();
+        else shares<ASK>();
+    }
+};
 
 __device__ __forceinline__ void put_hidden(const Layer& l, int pair, int feature, float h)
 {
@@ -562,8 +641,6 @@ struct Down {
 // bytes of shared memory in front of the choice: rings, then tiles
 constexpr int kRings = kWarps * kRing, kBefore = kRings + kJoin * 4;
 
-constexpr int kAsked = 8192;   // bytes that a warp asks into L2 ahead
-
 // Bytes of a row of weights that a stage holds: as many as let the ring hold two
 constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
 {
@@ -572,28 +649,28 @@ constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
 }
 
 template <int WT, int XT, int NT, bool SHIFT, bool FEW>
-__device__ __forceinline__ void up_units(const Layer& l, const Choice& c, char* raw, int warp, int lane, int id)
+__device__ __forceinline__ void up_units(const Layer& l, const Choice& c, char* raw, int warp, int lane)
 {
     constexpr int kPiece = piece_of(WT, XT, NT, SHIFT, 1);
     using S = Stream<WT, XT, NT, SHIFT, 1, kPiece, 1>;
     S st(shared_at(raw), warp, lane);
     const Up<WT, XT, NT> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
-    run_share<S, NT>(st, job, (l.d * size_of(WT) + kPiece - 1) / kPiece, l, lane, id);
+    Run<S, NT, Up<WT, XT, NT>> run{st, job, l, (l.d * size_of(WT) + kPiece - 1) / kPiece, lane, warp,
+                                   reinterpret_cast<float*>(raw + warp * S::kWarpBytes)};
+    run.template go<false>();
 }
 
 template <int WT, int NT, bool SHIFT, int TERMS, bool WHOLE>
-__device__ __forceinline__ void down_units(const Layer& l, const Choice& c, char* raw, int warp, int lane, int id)
+__device__ __forceinline__ void down_units(const Layer& l, const Choice& c, char* raw, int warp, int lane)
 {
     // float16 weights take the float32 values, others their terms
     constexpr int kXT = TERMS == 1 ? kF32 : kBf16, kPiece = piece_of(WT, kXT, NT, SHIFT, TERMS);
     using S = Stream<WT, kXT, NT, SHIFT, TERMS, kPiece, 1, WHOLE>;
     S st(shared_at(raw), warp, lane, l.pairs * l.h_pad * size_of(kXT));
     const Down<WT, NT, kXT, WHOLE> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
-    const int each = (l.h * size_of(WT) + kPiece - 1) / kPiece;
-    // the first weights are asked into L2 while up_kernel drains
-    ask_share(job, each, kPiece, gridDim.x, kAsked, lane, id);
-    wait_previous();
-    run_share<S, NT>(st, job, each, l, lane, id);
+    Run<S, NT, Down<WT, NT, kXT, WHOLE>> run{st, job, l, (l.h * size_of(WT) + kPiece - 1) / kPiece, lane, warp,
+                                             reinterpret_cast<float*>(raw + warp * S::kWarpBytes)};
+    run.template go<true>();
 }
 
 // FEW: up to 8 tokens.  These kernels hold the code for one eight of columns alone,
@@ -605,15 +682,15 @@ template <int WT, int XT, bool SHIFT, bool FEW>
 __global__ void __launch_bounds__(bound_of(FEW), 2) up_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, id = warp * gridDim.x + blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int kMost = FEW ? 1 : WT == kI8 ? 2 : 4;
     Choice c(raw + kBefore, l.rows * l.top);
     wait_previous();
     allow_next();
     list_all(l, c, raw, 8 * kMost, warp, lane);
-    if (FEW || c.columns <= 8) up_units<WT, XT, 1, SHIFT, FEW>(l, c, raw, warp, lane, id);
-    else if (c.columns <= 16) up_units<WT, XT, FEW ? 1 : 2, SHIFT, FEW>(l, c, raw, warp, lane, id);
-    else up_units<WT, XT, kMost, SHIFT, FEW>(l, c, raw, warp, lane, id);
+    if (FEW || c.columns <= 8) up_units<WT, XT, 1, SHIFT, FEW>(l, c, raw, warp, lane);
+    else if (c.columns <= 16) up_units<WT, XT, FEW ? 1 : 2, SHIFT, FEW>(l, c, raw, warp, lane);
+    else up_units<WT, XT, kMost, SHIFT, FEW>(l, c, raw, warp, lane);
 }
 
 // The choice is there: up_kernel let this kernel start after it had waited for it.
@@ -621,7 +698,7 @@ template <int WT, bool SHIFT, int TERMS, bool FEW>
 __global__ void __launch_bounds__(bound_of(FEW), 2) down_kernel(const __grid_constant__ Layer l)
 {
     extern __shared__ __align__(128) char raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, id = warp * gridDim.x + blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // eights of columns that the ring has room for
     constexpr int kMost = FEW ? 1 : (WT == kI8 ? 2 : 4) / (TERMS == 3 || SHIFT ? 2 : 1);
     Choice c(raw + kBefore, l.rows * l.top);
@@ -634,9 +711,9 @@ __global__ void __launch_bounds__(bound_of(FEW), 2) down_kernel(const __grid_con
             proj::store1(l.y, i / l.d * l.y_rs + i % l.d, 0.0f, l.out_f32, l.half);
         return;
     }
-    if (FEW || c.columns <= 8) down_units<WT, 1, SHIFT, TERMS, FEW>(l, c, raw, warp, lane, id);
-    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS, FEW>(l, c, raw, warp, lane, id);
-    else down_units<WT, kMost, SHIFT, TERMS, FEW>(l, c, raw, warp, lane, id);
+    if (FEW || c.columns <= 8) down_units<WT, 1, SHIFT, TERMS, FEW>(l, c, raw, warp, lane);
+    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS, FEW>(l, c, raw, warp, lane);
+    else down_units<WT, kMost, SHIFT, TERMS, FEW>(l, c, raw, warp, lane);
 }
 
 // What each token's experts gave, added up in the order of their shares

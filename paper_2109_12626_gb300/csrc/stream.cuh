@@ -573,6 +573,18 @@ __device__ __forceinline__ void put_tile(float* tile, const float (&first)[4], c
     }
 }
 
+// and those of a tile added to a warp's
+__device__ __forceinline__ void add_tile(const float* tile, float (&first)[4], float (&second)[4], int lane)
+{
+    const int g = lane / 4, t = lane & 3;
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const int row = g + 8 * (q >> 1), column = 2 * t + (q & 1);
+        first[q] += tile[column * kJoinPitch + row];
+        second[q] += tile[column * kJoinPitch + 16 + row];
+    }
+}
+
 template <bool WHOLE>
 __device__ __forceinline__ float join_columns(float* room, const float (&first)[4], const float (&second)[4], int warp,
                                               int lane)
@@ -638,18 +650,24 @@ struct Shares {
     }
 };
 
-// A warp's sums over a part of a unit, left for the last of the unit's warps to come,
-// which gets them all added up, in the order of the warps, and true.  parts: two
-// places a warp, for the unit that its share starts in and the one that it ends in;
-// count: a counter a warp, zero, used by the unit whose first warp it is.
-template <int NT>
-__device__ __forceinline__ bool join_parts(const Shares& s, int warp_id, int unit, float (&v)[2][NT][4], float* parts,
-                                           uint32_t* count, int lane)
+// Fewer units than warps: a team of warps a unit, one after another, teams of equal
+// size (or one more), of no more warps than have a few pieces each.
+struct Teams {
+    int units, of, each;   // units, warps, pieces a unit
+    __device__ __forceinline__ int start(int u) const { return u * of / units; }
+    __device__ __forceinline__ int unit(int w) const { return ((w + 1) * units - 1) / of; }
+    __device__ __forceinline__ int size(int u) const { return min(start(u + 1) - start(u), max(1, each / kLeast)); }
+};
+
+// Sums of a unit that several contributors have parts of -- warps, or CTAs -- added up
+// in the order of these by the last of them to come, which gets true.  Each has two
+// places: place(c) is contributor c's for this unit.  count: the unit's counter,
+// zero.
+template <int NT, typename Place>
+__device__ __forceinline__ bool join_parts(float (&v)[2][NT][4], int me, int first, int last, Place place, uint32_t* count,
+                                           int lane)
 {
-    constexpr int kPlace = 2 * NT * 4 * 32;
-    const int from = unit * s.each, first = s.owner(from), last = s.owner(from + s.each - 1);
-    auto place = [&](int w) { return parts + (int64_t(w) * 2 + (s.start(w) < from)) * kPlace; };
-    float4* mine = reinterpret_cast<float4*>(place(warp_id)) + lane;
+    float4* mine = reinterpret_cast<float4*>(place(me)) + lane;
 #pragma unroll
     for (int i = 0; i < 2; i++)
 #pragma unroll
@@ -657,24 +675,21 @@ __device__ __forceinline__ bool join_parts(const Shares& s, int warp_id, int uni
     __syncwarp();
     uint32_t came = 0;
     if (lane == 0) {
-        came = add_in_order(count + first) + 1u;
-        if (came == uint32_t(last - first + 1)) count[first] = 0u;
+        came = add_in_order(count) + 1u;
+        if (came == uint32_t(last - first + 1)) *count = 0u;
     }
     came = __shfl_sync(0xFFFFFFFFu, came, 0);
     if (came != uint32_t(last - first + 1)) return false;
-    // only the first may have begun before the unit
-    const float4* at = reinterpret_cast<const float4*>(place(first)) + lane;
-    const float4* next = reinterpret_cast<const float4*>(parts + (int64_t(first) + 1) * 2 * kPlace) + lane;
-    constexpr int kAhead = NT == 1 ? 4 : 1;   // warps whose sums are asked for together
-    for (int w = first; w <= last; w += kAhead) {
+    constexpr int kAhead = NT == 1 ? 6 : NT == 2 ? 2 : 1;   // contributors whose sums are asked for together
+#pragma unroll 1
+    for (int c = first; c <= last; c += kAhead) {
         float4 p[kAhead][2 * NT];
 #pragma unroll
         for (int k = 0; k < kAhead; k++) {
+            const float4* at = reinterpret_cast<const float4*>(place(min(c + k, last))) + lane;
 #pragma unroll
             for (int i = 0; i < 2 * NT; i++)
-                p[k][i] = w + k <= last ? __ldcg(at + i * 32) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            at = next;
-            next += 2 * kPlace / 4;
+                p[k][i] = c + k <= last ? __ldcg(at + i * 32) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; k++)
@@ -683,7 +698,7 @@ __device__ __forceinline__ bool join_parts(const Shares& s, int warp_id, int uni
 #pragma unroll
                 for (int n = 0; n < NT; n++) {
                     const float4 q = p[k][i * NT + n];
-                    if (w + k == first)
+                    if (k == 0 && c == first)
                         v[i][n][0] = q.x, v[i][n][1] = q.y, v[i][n][2] = q.z, v[i][n][3] = q.w;
                     else
                         v[i][n][0] += q.x, v[i][n][1] += q.y, v[i][n][2] += q.z, v[i][n][3] += q.w;
