@@ -20,7 +20,7 @@ struct Integer {
     char* x_copy = nullptr;     // x of few rows, padded; parts and counters of their sums
     int32_t* parts = nullptr;
     char* wide[2] = {};         // x and w in 16 bits
-    bool set[3][2] = {};        // kernels' attributes set
+    bool set[3][2] = {}, wide_set[2] = {};   // kernels' attributes set
     proj::Proj* base() const { return reinterpret_cast<proj::Proj*>(tiles); }
 };
 
@@ -76,6 +76,22 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
         r.x_rs = pad;
     }
     return rows_launch(r, num_sms, s);
+}
+
+int some(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, const Finish& f, cudaStream_t s)
+{
+    Wide q;
+    q.rows = int(rows);
+    q.k = int(P->n_in);
+    q.n = P->n_out;
+    q.x = static_cast<const char*>(x.data);
+    q.x_rs = x.row_stride;
+    q.w = static_cast<const char*>(w.data);
+    q.w_rs = w.row_stride;
+    q.f = f;
+    q.set = P->wide_set;
+    q.err = P->base()->err;
+    return wide_launch(q, P->base()->num_sms, s);
 }
 
 int many(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, const Finish& f, cudaStream_t s)
@@ -216,6 +232,9 @@ extern "C" int dpdr_integer_linear(dpdr_integer_t h, int64_t rows, const dpdr_ma
     f.half = P->half;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const bool in_place = w->col_stride == 1 || P->n_in == 1;
+    if (rows > kStreamRows && in_place && (x->col_stride == 1 || P->n_in == 1) &&
+        wide_takes(rows, P->n_out, P->n_in, P->base()->num_sms))
+        return some(P, rows, *x, *w, f, s);
     return rows <= kFewRows && in_place ? few(P, rows, *x, *w, f, s) : many(P, rows, *x, *w, f, s);
 }
 

@@ -12,6 +12,10 @@ constexpr int64_t kMostSummed = (int64_t(1) << 17) - 1;
 
 // rows that rows_launch takes
 constexpr int kFewRows = 64;
+// Rows past which wide_launch is faster where it takes the product.  us of
+// rows_launch and of it, 4096 x 4096 weights: 16 rows 9.3 and 10.2, 32 rows 12.0
+// and 10.6; 24 rows of 1024 x 8192 11.6 and 7.9.
+constexpr int kStreamRows = 16;
 // what their elements are a multiple of
 constexpr int kRowsPad = 64;
 
@@ -43,6 +47,23 @@ struct Rows {
 // x need not be padded for up to 4 rows of w at multiples of 16 bytes
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s);
 constexpr int64_t parts_ints(int num_sms) { return int64_t(2 * num_sms) * 32 * 32; }
+
+// Some rows, both operands widened on their way to the tensor cores: rows of x and w
+// contiguous, at any address and row stride.
+struct Wide {
+    int rows, k;
+    int64_t n;
+    const char* x;
+    int64_t x_rs;
+    const char* w;
+    int64_t w_rs;
+    Finish f;
+    bool* set;               // of the plan: kernels' attributes set
+    uint32_t* err;
+};
+// whether the product's tiles leave SMs for parts of its sum, and tensor memory holds its runs
+bool wide_takes(int64_t rows, int64_t n, int64_t k, int num_sms);
+int wide_launch(const Wide& q, int num_sms, cudaStream_t s);
 
 // 8-bit matrices laid out anew: by rows ld apart, zero from cols up to `to`, as
 // 8-bit integers (wide 0), bfloat16 (1) or float16 (2)
