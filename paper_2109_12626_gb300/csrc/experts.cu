@@ -232,9 +232,7 @@ struct Choice {
 // bytes for each local expert.  `most`: pairs of an entry.
 __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int warp, int lane)
 {
-    __shared__ int entries, columns;
-    uint64_t* mask = reinterpret_cast<uint64_t*>(room);   // an expert's tokens
-    int16_t* from = reinterpret_cast<int16_t*>(mask + l.local);
+    __shared__ int entries, before[kWarps], high[kWarps];
     const int pairs = l.rows * l.top;
     if (l.rows == 1) {   // a pair an entry
         if (warp == 0) {
@@ -252,6 +250,8 @@ __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int wa
         c.columns = 1;
         return;
     }
+    uint64_t* mask = reinterpret_cast<uint64_t*>(room);   // an expert's tokens
+    int16_t* from = reinterpret_cast<int16_t*>(mask + l.local);
     for (int e = threadIdx.x; e < l.local; e += kThreads) mask[e] = 0;
     for (int p = threadIdx.x; p < pairs; p += kThreads) {
         c.expert[p] = int16_t(__ldcg(l.expert + p));
@@ -259,43 +259,48 @@ __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int wa
     }
     __syncthreads();
     for (int p = threadIdx.x; p < pairs; p += kThreads) {   // its own
-        const int e = c.expert[p] - l.first;
-        if (e >= 0 && e < l.local)
-            atomicOr(reinterpret_cast<unsigned long long*>(mask + e), 1ull << (p / l.top));
+        const int e = c.expert[p] - l.first, t = p / l.top;
+        if (e >= 0 && e < l.local) atomicOr(reinterpret_cast<uint32_t*>(mask + e) + t / 32, 1u << t % 32);
     }
     __syncthreads();
-    if (warp == 0) {
-        int pairs_before = 0, entries_before = 0, high = 0;
-        for (int e0 = 0; e0 < l.local; e0 += 32) {
-            const int e = e0 + lane, n = e < l.local ? __popcll(mask[e]) : 0, k = (n + most - 1) / most;
-            int n_to = n, k_to = k;   // up to and with this lane
+    // a thread one or two experts next to each other: their pairs, and their entries above
+    // those, added up over the threads before
+    static_assert(kMostExperts <= 2 * kThreads, "two experts a thread");
+    const int each = l.local > kThreads ? 2 : 1, e0 = each * threadIdx.x;
+    int n[2] = {0, 0}, sum = 0;
+    for (int i = 0; i < each && e0 + i < l.local; i++) {
+        n[i] = __popcll(mask[e0 + i]);
+        sum += n[i] | (n[i] + most - 1) / most << 16;
+    }
+    int to = sum;   // up to and with this thread
 #pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int a = __shfl_up_sync(0xFFFFFFFFu, n_to, o), b = __shfl_up_sync(0xFFFFFFFFu, k_to, o);
-                if (lane >= o) n_to += a, k_to += b;
-            }
-            const int p0 = pairs_before + n_to - n, i0 = entries_before + k_to - k;
-            if (e < l.local) from[e] = int16_t(p0);
-            for (int i = 0; i < k; i++) c.entry[i0 + i] = Choice::packed(e, min(most, n - i * most), p0 + i * most);
-            high = max(high, min(n, most));
-            pairs_before += __shfl_sync(0xFFFFFFFFu, n_to, 31);
-            entries_before += __shfl_sync(0xFFFFFFFFu, k_to, 31);
-        }
-        high = __reduce_max_sync(0xFFFFFFFFu, high);
-        if (lane == 0) entries = entries_before, columns = high;
+    for (int o = 1; o < 32; o *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, to, o);
+        if (lane >= o) to += v;
+    }
+    const int top = __reduce_max_sync(0xFFFFFFFFu, max(n[0], n[1]));
+    if (lane == 31) before[warp] = to, high[warp] = top;
+    __syncthreads();
+    int all = 0;
+    c.columns = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; w++) {
+        if (w < warp) to += before[w];
+        all += before[w];
+        c.columns = max(c.columns, min(most, high[w]));
+    }
+    c.entries = all >> 16;
+    int p0 = (to - sum) & 0xFFFF, i0 = (to - sum) >> 16;
+    for (int i = 0; i < each && e0 + i < l.local; i++) {
+        from[e0 + i] = int16_t(p0);
+        for (int k = 0; k < n[i]; k += most) c.entry[i0++] = Choice::packed(e0 + i, min(most, n[i] - k), p0 + k);
+        p0 += n[i];
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < l.local; e += kThreads) {
-        int at = from[e];
-        for (uint64_t m = mask[e]; m; m &= m - 1) {
-            const int t = __ffsll(m) - 1;
-            int p = t * l.top;
-            while (c.expert[p] != e + l.first) p++;
-            c.order[at++] = int16_t(p);
-        }
+    for (int p = threadIdx.x; p < pairs; p += kThreads) {
+        const int e = c.expert[p] - l.first, t = p / l.top;
+        if (e >= 0 && e < l.local) c.order[from[e] + __popcll(mask[e] & ((1ull << t) - 1))] = int16_t(p);
     }
-    c.entries = entries;
-    c.columns = columns;
     __syncthreads();   // `room` is free again
 }
 

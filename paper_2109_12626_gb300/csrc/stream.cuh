@@ -61,6 +61,12 @@ __device__ __forceinline__ void copy16(uint32_t to, const char* from)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+// The same of a row that is read on from there: what lies beside it goes to L2 too, 256
+// bytes, which DRAM serves at a better rate than 64 (8 rows of 64 experts 113 to 106 us).
+__device__ __forceinline__ void copy16_on(uint32_t to, const char* from)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
 __device__ __forceinline__ void copies_wait()
@@ -315,7 +321,7 @@ struct Stream {
     {
         if (load_piece < load_whole) {
 #pragma unroll
-            for (int i = 0; i < kALoads; i++) copy16(load_to + a_to(i), a_at[i]);
+            for (int i = 0; i < kALoads; i++) copy16_on(load_to + a_to(i), a_at[i]);
         } else {
             const int left = load_bytes - load_piece * kPiece;
 #pragma unroll
