@@ -28,7 +28,8 @@ SOURCES = ["plan.cpp", "api.cpp", "fused.cu", "fused_stream.cu", "fused_tile.cu"
            "proj.cpp", "proj_elem.cu", "proj_tile.cu",
            "proj_tile_pair.cu", "proj_tile_runs.cu", "proj_tile_pair_runs.cu",
            "proj_rows.cu", "proj_rows_pair.cu", "proj_token.cu",
-           "proj_tile_scaled.cu", "experts.cpp", "experts.cu", "integer.cpp", "integer.cu", "integer_rows.cu"]
+           "proj_tile_scaled.cu", "experts.cpp", "experts.cu", "experts_up.cu",
+           "experts_down.cu", "integer.cpp", "integer.cu", "integer_rows.cu"]
 
 
 def nvcc() -> str:

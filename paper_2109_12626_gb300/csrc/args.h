@@ -93,6 +93,7 @@ struct Args {
         check(name, one, rows, cols, esize);
         if (m->stride < 0 || m->row_stride < 0) return refuse(name, "has a negative stride");
         if (cols > 1 && m->col_stride != 1) return refuse(name, "needs col_stride 1");
+        if (rc != DPDR_OK) return;
         const int64_t each = (rows - 1) * m->row_stride + cols;   // elements from the first to the last
         check(name, all, count, each, esize);
         if (rc != DPDR_OK) return;

@@ -27,8 +27,7 @@
 #include <algorithm>
 #include <mutex>
 
-#include "experts.h"
-#include "stream.cuh"
+#include "experts.cuh"
 
 namespace dpdr {
 namespace experts {
@@ -200,527 +199,6 @@ __global__ void __launch_bounds__(32 * score_warps(TOK), TOK == 8 ? 3 : 8) score
         }
 }
 
-// ------------------------------------------------------------------ choice
-
-// What a CTA knows of the choice, in shared memory.  A pair is a token's number
-// times `top` plus the place of one of its experts.
-struct Choice {
-    float* share;         // of a pair
-    uint32_t* entry;      // an expert with up to `most` of its pairs: number among
-                          // the local ones, how many pairs, the first of them in `order`
-    int16_t* expert;      // of a pair
-    int16_t* order;       // pairs, those of an expert together, by token
-    int entries, columns; // the most pairs of an entry
-
-    __device__ __forceinline__ Choice(char* at, int pairs)
-        : share(reinterpret_cast<float*>(at)),
-          entry(reinterpret_cast<uint32_t*>(share + pairs)),
-          expert(reinterpret_cast<int16_t*>(entry + pairs)),
-          order(expert + pairs)
-    {
-    }
-    static __device__ __forceinline__ uint32_t packed(int e, int n, int from)
-    {
-        return uint32_t(e) | uint32_t(n) << 10 | uint32_t(from) << 17;
-    }
-    __device__ __forceinline__ int number(int i) const { return entry[i] & 1023u; }
-    __device__ __forceinline__ int count(int i) const { return entry[i] >> 10 & 127u; }
-    __device__ __forceinline__ int from(int i) const { return entry[i] >> 17; }
-};
-
-// The lists of it, in every CTA alike.  `room`: shared memory that is free so far, 10
-// bytes for each local expert.  `most`: pairs of an entry.
-__device__ void list_all(const Layer& l, Choice& c, char* room, int most, int warp, int lane)
-{
-    __shared__ int entries, before[kWarps], high[kWarps];
-    const int pairs = l.rows * l.top;
-    if (l.rows == 1) {   // a pair an entry
-        if (warp == 0) {
-            const int e = lane < pairs ? __ldcg(l.expert + lane) - l.first : -1;
-            const float share = lane < pairs ? __ldcg(l.shares + lane) : 0.0f;
-            const bool here = e >= 0 && e < l.local;
-            const uint32_t all = __ballot_sync(0xFFFFFFFFu, here);
-            const int at = __popc(all & ((1u << lane) - 1));
-            if (here) c.entry[at] = Choice::packed(e, 1, at), c.order[at] = int16_t(lane);
-            if (lane < pairs) c.share[lane] = share;
-            if (lane == 0) entries = __popc(all);
-        }
-        __syncthreads();
-        c.entries = entries;
-        c.columns = 1;
-        return;
-    }
-    uint64_t* mask = reinterpret_cast<uint64_t*>(room);   // an expert's tokens
-    int16_t* from = reinterpret_cast<int16_t*>(mask + l.local);
-    for (int e = threadIdx.x; e < l.local; e += kThreads) mask[e] = 0;
-    for (int p = threadIdx.x; p < pairs; p += kThreads) {
-        c.expert[p] = int16_t(__ldcg(l.expert + p));
-        c.share[p] = __ldcg(l.shares + p);
-    }
-    __syncthreads();
-    for (int p = threadIdx.x; p < pairs; p += kThreads) {   // its own
-        const int e = c.expert[p] - l.first, t = p / l.top;
-        if (e >= 0 && e < l.local) atomicOr(reinterpret_cast<uint32_t*>(mask + e) + t / 32, 1u << t % 32);
-    }
-    __syncthreads();
-    // a thread one or two experts next to each other: their pairs, and their entries above
-    // those, added up over the threads before
-    static_assert(kMostExperts <= 2 * kThreads, "two experts a thread");
-    const int each = l.local > kThreads ? 2 : 1, e0 = each * threadIdx.x;
-    int n[2] = {0, 0}, sum = 0;
-    for (int i = 0; i < each && e0 + i < l.local; i++) {
-        n[i] = __popcll(mask[e0 + i]);
-        sum += n[i] | (n[i] + most - 1) / most << 16;
-    }
-    int to = sum;   // up to and with this thread
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const int v = __shfl_up_sync(0xFFFFFFFFu, to, o);
-        if (lane >= o) to += v;
-    }
-    const int top = __reduce_max_sync(0xFFFFFFFFu, max(n[0], n[1]));
-    if (lane == 31) before[warp] = to, high[warp] = top;
-    __syncthreads();
-    int all = 0;
-    c.columns = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; w++) {
-        if (w < warp) to += before[w];
-        all += before[w];
-        c.columns = max(c.columns, min(most, high[w]));
-    }
-    c.entries = all >> 16;
-    int p0 = (to - sum) & 0xFFFF, i0 = (to - sum) >> 16;
-    for (int i = 0; i < each && e0 + i < l.local; i++) {
-        from[e0 + i] = int16_t(p0);
-        for (int k = 0; k < n[i]; k += most) c.entry[i0++] = Choice::packed(e0 + i, min(most, n[i] - k), p0 + k);
-        p0 += n[i];
-    }
-    __syncthreads();
-    for (int p = threadIdx.x; p < pairs; p += kThreads) {
-        const int e = c.expert[p] - l.first, t = p / l.top;
-        if (e >= 0 && e < l.local) c.order[from[e] + __popcll(mask[e] & ((1ull << t) - 1))] = int16_t(p);
-    }
-    __syncthreads();   // `room` is free again
-}
-
-// Whether every row of a stack of matrices starts at a multiple of 16 bytes
-__host__ __device__ bool aligned(const dpdr_matrices& m, int local, int64_t rows, int esize)
-{
-    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows == 1 || m.row_stride * esize % 16 == 0) &&
-           (local == 1 || m.stride * esize % 16 == 0);
-}
-
-__host__ __device__ bool up_shifted(const Layer& l)
-{
-    const int es = l.w_int8 ? 1 : 2;
-    return !aligned(l.w[0], l.local, l.h, es) || !aligned(l.w[1], l.local, l.h, es);
-}
-__host__ __device__ bool down_shifted(const Layer& l) { return !aligned(l.w[2], l.local, l.d, l.w_int8 ? 1 : 2); }
-
-// ---------------------------------------------------------------- products
-
-__device__ __forceinline__ float act_of(int act, float z)
-{
-    float v = z;
-#define DPDR_CALL(A) v = proj::act_value<A>(z)
-    DPDR_FOR_ACT(act, DPDR_CALL)
-#undef DPDR_CALL
-    return v;
-}
-
-constexpr int kAsked = 8192;   // bytes that a warp asks into L2 ahead
-
-// What a warp does with its pieces: job.part(i) is the i-th run of `each` pieces along
-// k, job.parts of them a unit; job.columns(i) where its columns lie; job.finish(u,
-// sums).
-template <typename S, int NT, typename Job>
-struct Run {
-    S& st;
-    const Job& job;
-    const Layer& l;
-    const int each, lane, warp;
-    float* const room;   // of this warp, NT tiles, once its loads are done
-
-    // Asks the first of pieces [at, end) into L2
-    __device__ __forceinline__ void ask(int at, int end) const
-    {
-        end = min(end, at + kAsked / (kRows * S::kPiece));
-        while (at < end) {
-            const int i = at / each, there = min(end, (i + 1) * each);
-            const Unit q = job.part(i, at - i * each, there - i * each);
-            const char* p = q.row(lane);
-            const int to = min(q.last * S::kPiece, q.row_bytes);
-            for (int k = q.first * S::kPiece; k < to; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
-            at = there;
-        }
-    }
-
-    // Pieces [at, to) of one unit added to `sum`
-    template <typename Next>
-    __device__ __forceinline__ void sums(int at, int to, float (&sum)[2][NT][4], Next next)
-    {
-        S::clear(sum);
-        while (at < to) {
-            const int i = at / each, there = min(to, (i + 1) * each);
-            const Unit q = job.part(i, at - i * each, there - i * each);
-            if constexpr (Job::kScales) {   // of this part's rows
-                float part[2][NT][4], by[4];
-                S::clear(part);
-                st.sums(q, part, next);
-                job.scales(i, by);
-#pragma unroll
-                for (int k = 0; k < 2; k++)
-#pragma unroll
-                    for (int n = 0; n < NT; n++)
-#pragma unroll
-                        for (int j = 0; j < 4; j++) sum[k][n][j] += part[k][n][j] * by[2 * k + j / 2];
-            } else {
-                st.sums(q, sum, next);
-            }
-            at = there;
-        }
-    }
-
-    __device__ __forceinline__ auto loads(int& loading, int end)
-    {
-        return [this, &loading, end]() {
-            if (loading >= end) return;
-            const int i = loading / each, to = min(end, (i + 1) * each);
-            st.load_from(job.part(i, loading - i * each, to - i * each), job.columns(i));
-            loading = to;
-        };
-    }
-
-    // Many units: contiguous shares; one that a unit begins or ends in leaves its part.
-    // Warps next to each other are of different CTAs.
-    template <bool ASK>
-    __device__ __forceinline__ void shares()
-    {
-        const int id = warp * gridDim.x + blockIdx.x, per = job.parts * each, total = job.units * per;
-        const Shares s(total, max(1, min(int(gridDim.x) * kWarps, total / kLeast)), per);
-        int at = s.start(min(id, s.of)), loading = at;
-        const int end = s.start(min(id + 1, s.of));
-        if (ASK) {
-            ask(at, end);
-            wait_previous();
-        }
-        auto next = loads(loading, end);
-        st.begin(next);
-        while (at < end) {
-            const int u = at / per, to = min(end, (u + 1) * per);
-            float sum[2][NT][4];
-            sums(at, to, sum, next);
-            const bool some = to - at < per;
-            at = to;
-            if (some) {
-                const int from = u * per, first = s.owner(from), last = s.owner(from + per - 1);
-                auto place = [&](int w) { return l.parts + (int64_t(w) * 2 + (s.start(w) < from)) * (NT * 256); };
-                if (!join_parts<NT>(sum, id, first, last, place, job.count + first, lane)) continue;
-            }
-            job.finish(u, sum);
-        }
-    }
-
-    // Few: teams of warps that follow each other; those of one CTA join their sums in
-    // its shared memory.
-    template <bool ASK>
-    __device__ __forceinline__ void teams()
-    {
-        const int per = job.parts * each;
-        const Teams t{job.units, int(gridDim.x) * kWarps, per};
-        const int base = int(blockIdx.x) * kWarps, id = base + warp;
-        const int u = t.unit(id), begins = t.start(u), size = t.size(u), place_of = id - begins;
-        const bool in = place_of < size;
-        const int from = u * per, at = in ? from + int(int64_t(per) * place_of / size) : 0,
-                  end = in ? from + int(int64_t(per) * (place_of + 1) / size) : 0;
-        if (ASK) {
-            ask(at, end);
-            wait_previous();
-        }
-        int loading = at;
-        auto next = loads(loading, end);
-        st.begin(next);
-        float sum[2][NT][4];
-        sums(at, end, sum, next);
-        // of the team, the warps of this CTA
-        const int low = max(0, begins - base), high = min(kWarps, begins + size - base);
-        if (size > 1) {
-            copies_wait<0>();
-            if (in && warp > low)
-#pragma unroll
-                for (int n = 0; n < NT; n++) put_tile(room + n * kTile, sum[0][n], sum[1][n], lane);
-            __syncwarp();
-        }
-        __syncthreads();
-        if (!in || warp > low) return;
-        for (int w = low + 1; w < high; w++) {
-            const float* other = room + (w - warp) * (S::kWarpBytes / 4);
-#pragma unroll
-            for (int n = 0; n < NT; n++) add_tile(other + n * kTile, sum[0][n], sum[1][n], lane);
-        }
-        if (high - low < size) {   // at most two of a CTA's units reach into others
-            const int first = begins / kWarps, last = (begins + size - 1) / kWarps;
-            auto place = [&](int c) { return l.parts + (int64_t(c) * 2 + (c == first)) * (NT * 256); };
-            if (!join_parts<NT>(sum, int(blockIdx.x), first, last, place, job.count + first, lane)) return;
-        }
-        job.finish(u, sum);
-    }
-
-    // ASK: the first weights are asked into L2 while the kernel before drains, which is
-    // then waited for
-    template <bool ASK>
-    __device__ __forceinline__ void go()
-    {
-        if (job.units <= 0) return;
-        if (2 * job.units <= int(gridDim.x) * kWarps) teams<ASK>();
-        else shares<ASK>();
-    }
-};
-
-__device__ __forceinline__ void put_hidden(const Layer& l, int pair, int feature, float h)
-{
-    if (l.terms == 1) {
-        reinterpret_cast<float*>(l.hidden)[pair * l.h_pad + feature] = h;
-        return;
-    }
-    uint16_t v[3];
-    split_bf16(h, l.terms, v);
-    uint16_t* to = reinterpret_cast<uint16_t*>(l.hidden) + pair * l.h_pad + feature;
-    const int64_t apart = l.pairs * l.h_pad;
-    to[0] = v[0];
-    to[apart] = v[1];
-    if (l.terms == 3) to[2 * apart] = v[2];
-}
-
-// Units of 16 hidden features of an entry
-template <int WT, int XT, int NT>
-struct Up {
-    const Layer& l;
-    const Choice& c;
-    float* tile;
-    const int lane, blocks, units;
-    static constexpr int parts = 1;
-    static constexpr bool kScales = WT == kI8;
-    uint32_t* count;
-
-    __device__ __forceinline__ Up(const Layer& layer, const Choice& choice, float* room, int ln)
-        : l(layer), c(choice), tile(room), lane(ln), blocks((l.h + 15) / 16), units(c.entries * blocks), count(l.up_count)
-    {
-    }
-    __device__ __forceinline__ Unit part(int u, int first, int last) const
-    {
-        const int i = u / blocks, row = (u - i * blocks) * 16;
-        Unit q;
-        const int64_t e = c.number(i);
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            q.a[k] = static_cast<const char*>(l.w[k].data) + (e * l.w[k].stride + row * l.w[k].row_stride) * size_of(WT);
-            q.a_stride[k] = l.w[k].row_stride * size_of(WT);
-        }
-        q.rows_left[0] = q.rows_left[1] = min(16, l.h - row);
-        q.row_bytes = l.d * size_of(WT);
-        q.first = first;
-        q.last = last;
-        return q;
-    }
-    __device__ __forceinline__ auto columns(int u) const
-    {
-        const int i = u / blocks, n = c.count(i), from = c.from(i);
-        return [=](int col) {   // columns that there are not repeat the last, for nothing
-            return l.x_copy + c.order[from + min(col, n - 1)] / l.top * l.d_pad * size_of(XT);
-        };
-    }
-    // the factors of a lane's rows, 8 apart
-    __device__ __forceinline__ void scales(int u, float (&by)[4]) const
-    {
-        const int i = u / blocks, row = (u - i * blocks) * 16 + lane / 4;
-        const int64_t at = int64_t(c.number(i)) * l.h;
-#pragma unroll
-        for (int k = 0; k < 4; k++) by[k] = l.scale[k / 2][at + min(row + 8 * (k % 2), l.h - 1)];
-    }
-    // by way of the warp's tile: rows 0 to 15 of it are g, the others u
-    __device__ __forceinline__ void finish(int u, const float (&sum)[2][NT][4]) const
-    {
-        const int i = u / blocks, feature = (u - i * blocks) * 16 + (lane & 15), n = c.count(i), from = c.from(i);
-#pragma unroll
-        for (int t = 0; t < NT; t++) {
-            put_tile(tile, sum[0][t], sum[1][t], lane);
-            __syncwarp();
-            if (feature < l.h)
-#pragma unroll 1
-                for (int col = lane >> 4; col < min(8, n - 8 * t); col += 2) {
-                    const int pair = c.order[from + 8 * t + col];
-                    const float* at = tile + col * kJoinPitch + (lane & 15);
-                    put_hidden(l, pair, feature, act_of(l.act, at[0]) * at[16] * c.share[pair]);
-                }
-            __syncwarp();
-        }
-    }
-};
-
-// Of up to 8 tokens: units of 32 features of the result, their sums over all
-// entries one after another, a column a token; one that did not choose an entry has
-// zeros there.  Of more: units of 32 features and an entry, their results to
-// z by pairs.
-template <int WT, int NT, int XT, bool WHOLE>
-struct Down {
-    const Layer& l;
-    const Choice& c;
-    float* tile;
-    const int lane, blocks, parts, units;
-    static constexpr bool kScales = WT == kI8;
-    uint32_t* count;
-
-    __device__ __forceinline__ Down(const Layer& layer, const Choice& choice, float* room, int ln)
-        : l(layer),
-          c(choice),
-          tile(room),
-          lane(ln),
-          blocks((l.d + 31) / 32),
-          parts(WHOLE ? c.entries : 1),
-          units(WHOLE ? blocks : c.entries * blocks),
-          count(l.down_count)
-    {
-    }
-    __device__ __forceinline__ int entry(int p) const { return WHOLE ? p % parts : p / blocks; }
-    __device__ __forceinline__ int block(int p) const { return WHOLE ? p / parts : p % blocks; }
-    __device__ __forceinline__ Unit part(int p, int first, int last) const
-    {
-        const int row = block(p) * 32;
-        const int64_t stride = l.w[2].row_stride * size_of(WT);
-        Unit q;
-        q.a[0] = static_cast<const char*>(l.w[2].data) +
-                 (c.number(entry(p)) * l.w[2].stride + row * l.w[2].row_stride) * size_of(WT);
-        q.a[1] = q.a[0] + 16 * stride;
-        q.a_stride[0] = q.a_stride[1] = stride;
-        q.rows_left[0] = min(16, l.d - row);
-        q.rows_left[1] = max(0, min(16, l.d - row - 16));
-        q.row_bytes = l.h * size_of(WT);
-        q.first = first;
-        q.last = last;
-        return q;
-    }
-    __device__ __forceinline__ auto columns(int p) const
-    {
-        const int i = entry(p), n = c.count(i), from = c.from(i);
-        return [=](int col) -> const char* {
-            int pair = c.order[from + min(col, n - 1)];
-            if (WHOLE) {   // the token's, if it chose this entry
-                pair = -1;
-                for (int k = 0; k < n; k++) {
-                    const int p = c.order[from + k];
-                    if (p >= col * l.top && p < (col + 1) * l.top) pair = p;
-                }
-            }
-            return pair < 0 ? nullptr : l.hidden + pair * l.h_pad * size_of(XT);
-        };
-    }
-    __device__ __forceinline__ void scales(int p, float (&by)[4]) const
-    {
-        const int row = block(p) * 32 + lane / 4;
-        const int64_t at = int64_t(c.number(entry(p))) * l.d;
-#pragma unroll
-        for (int k = 0; k < 4; k++) by[k] = l.scale[2][at + min(row + 8 * k, l.d - 1)];
-    }
-    __device__ __forceinline__ void finish(int u, const float (&sum)[2][NT][4]) const
-    {
-        const int feature = (WHOLE ? u : u % blocks) * 32 + lane, i = WHOLE ? 0 : u / blocks;
-        const int n = WHOLE ? l.rows : c.count(i), from = c.from(i);
-#pragma unroll
-        for (int t = 0; t < NT; t++) {
-            put_tile(tile, sum[0][t], sum[1][t], lane);
-            __syncwarp();
-            if (feature < l.d)
-#pragma unroll 1
-                for (int col = 0; col < min(8, n - 8 * t); col++) {
-                    const float v = tile[col * kJoinPitch + lane];
-                    if (WHOLE) proj::store1(l.y, col * l.y_rs + feature, v, l.out_f32, l.half);
-                    else l.z[int64_t(c.order[from + 8 * t + col]) * l.d + feature] = v;
-                }
-            __syncwarp();
-        }
-    }
-};
-
-// bytes of shared memory in front of the choice: rings, then tiles
-constexpr int kRings = kWarps * kRing, kBefore = kRings + kJoin * 4;
-
-// Bytes of a row of weights that a stage holds: as many as let the ring hold two
-constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
-{
-    const int stage = kRows * (128 + 16 * shift) + terms * nt * 8 * (128 / size_of(wt)) * size_of(xt);
-    return 5 * stage <= kRing ? 128 : 64;
-}
-
-template <int WT, int XT, int NT, bool SHIFT, bool FEW>
-__device__ __forceinline__ void up_units(const Layer& l, const Choice& c, char* raw, int warp, int lane)
-{
-    constexpr int kPiece = piece_of(WT, XT, NT, SHIFT, 1);
-    using S = Stream<WT, XT, NT, SHIFT, 1, kPiece, 1>;
-    S st(shared_at(raw), warp, lane);
-    const Up<WT, XT, NT> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
-    Run<S, NT, Up<WT, XT, NT>> run{st, job, l, (l.d * size_of(WT) + kPiece - 1) / kPiece, lane, warp,
-                                   reinterpret_cast<float*>(raw + warp * S::kWarpBytes)};
-    run.template go<false>();
-}
-
-template <int WT, int NT, bool SHIFT, int TERMS, bool WHOLE>
-__device__ __forceinline__ void down_units(const Layer& l, const Choice& c, char* raw, int warp, int lane)
-{
-    // float16 weights take the float32 values, others their terms
-    constexpr int kXT = TERMS == 1 ? kF32 : kBf16, kPiece = piece_of(WT, kXT, NT, SHIFT, TERMS);
-    using S = Stream<WT, kXT, NT, SHIFT, TERMS, kPiece, 1, WHOLE>;
-    S st(shared_at(raw), warp, lane, l.pairs * l.h_pad * size_of(kXT));
-    const Down<WT, NT, kXT, WHOLE> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
-    Run<S, NT, Down<WT, NT, kXT, WHOLE>> run{st, job, l, (l.h * size_of(WT) + kPiece - 1) / kPiece, lane, warp,
-                                             reinterpret_cast<float*>(raw + warp * S::kWarpBytes)};
-    run.template go<true>();
-}
-
-// FEW: up to 8 tokens.  These kernels hold the code for one eight of columns alone,
-// and leave registers (of 288 threads, in the bounds) for the next call's
-// scores_kernel to be set up beside them.
-constexpr int bound_of(bool few) { return few ? kThreads + 32 : kThreads; }
-
-template <int WT, int XT, bool SHIFT, bool FEW>
-__global__ void __launch_bounds__(bound_of(FEW), 2) up_kernel(const __grid_constant__ Layer l)
-{
-    extern __shared__ __align__(128) char raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kMost = FEW ? 1 : WT == kI8 ? 2 : 4;
-    Choice c(raw + kBefore, l.rows * l.top);
-    wait_previous();
-    allow_next();
-    list_all(l, c, raw, 8 * kMost, warp, lane);
-    if (FEW || c.columns <= 8) up_units<WT, XT, 1, SHIFT, FEW>(l, c, raw, warp, lane);
-    else if (c.columns <= 16) up_units<WT, XT, FEW ? 1 : 2, SHIFT, FEW>(l, c, raw, warp, lane);
-    else up_units<WT, XT, kMost, SHIFT, FEW>(l, c, raw, warp, lane);
-}
-
-// The choice is there: up_kernel let this kernel start after it had waited for it.
-template <int WT, bool SHIFT, int TERMS, bool FEW>
-__global__ void __launch_bounds__(bound_of(FEW), 2) down_kernel(const __grid_constant__ Layer l)
-{
-    extern __shared__ __align__(128) char raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // eights of columns that the ring has room for
-    constexpr int kMost = FEW ? 1 : (WT == kI8 ? 2 : 4) / (TERMS == 3 || SHIFT ? 2 : 1);
-    Choice c(raw + kBefore, l.rows * l.top);
-    allow_next();
-    list_all(l, c, raw, 8 * kMost, warp, lane);
-    if (c.entries == 0) {   // no token chose an expert that is here
-        wait_previous();
-        for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; FEW && i < int64_t(l.rows) * l.d;
-             i += int64_t(gridDim.x) * kThreads)
-            proj::store1(l.y, i / l.d * l.y_rs + i % l.d, 0.0f, l.out_f32, l.half);
-        return;
-    }
-    if (FEW || c.columns <= 8) down_units<WT, 1, SHIFT, TERMS, FEW>(l, c, raw, warp, lane);
-    else if (c.columns <= 16) down_units<WT, kMost < 2 ? 1 : 2, SHIFT, TERMS, FEW>(l, c, raw, warp, lane);
-    else down_units<WT, kMost, SHIFT, TERMS, FEW>(l, c, raw, warp, lane);
-}
-
 // What each token's experts gave, added up in the order of their shares
 __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Layer l)
 {
@@ -743,32 +221,19 @@ __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ La
     proj::store1(l.y, t * l.y_rs + feature, y, l.out_f32, l.half);
 }
 
-using Kernel = void (*)(Layer);
-
-template <bool SHIFT, bool FEW>
-Kernel up_of(const Layer& l)
+// Whether every row of a stack of matrices starts at a multiple of 16 bytes
+bool aligned(const dpdr_matrices& m, int local, int64_t rows, int esize)
 {
-    if (l.w_int8) return l.half ? up_kernel<kI8, kF16, SHIFT, FEW> : up_kernel<kI8, kBf16, SHIFT, FEW>;
-    return l.half ? up_kernel<kF16, kF16, SHIFT, FEW> : up_kernel<kBf16, kBf16, SHIFT, FEW>;
-}
-Kernel up_of(const Layer& l, bool shift, bool few)
-{
-    if (few) return shift ? up_of<true, true>(l) : up_of<false, true>(l);
-    return shift ? up_of<true, false>(l) : up_of<false, false>(l);
+    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows == 1 || m.row_stride * esize % 16 == 0) &&
+           (local == 1 || m.stride * esize % 16 == 0);
 }
 
-template <bool SHIFT, bool FEW>
-Kernel down_of(const Layer& l)
+bool up_shifted(const Layer& l)
 {
-    if (l.w_int8) return l.terms == 2 ? down_kernel<kI8, SHIFT, 2, FEW> : down_kernel<kI8, SHIFT, 3, FEW>;
-    if (l.half) return down_kernel<kF16, SHIFT, 1, FEW>;
-    return l.terms == 2 ? down_kernel<kBf16, SHIFT, 2, FEW> : down_kernel<kBf16, SHIFT, 3, FEW>;
+    const int es = l.w_int8 ? 1 : 2;
+    return !aligned(l.w[0], l.local, l.h, es) || !aligned(l.w[1], l.local, l.h, es);
 }
-Kernel down_of(const Layer& l, bool shift, bool few)
-{
-    if (few) return shift ? down_of<true, true>(l) : down_of<false, true>(l);
-    return shift ? down_of<true, false>(l) : down_of<false, false>(l);
-}
+bool down_shifted(const Layer& l) { return !aligned(l.w[2], l.local, l.d, l.w_int8 ? 1 : 2); }
 
 size_t product_smem(const Layer& l) { return size_t(kBefore) + size_t(l.rows) * l.top * 12; }
 
