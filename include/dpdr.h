@@ -527,12 +527,12 @@ dpdr_integer_t dpdr_integer_plan(int64_t max_rows, int64_t n_in, int64_t n_out,
 /* x: rows by n_in, w: n_out by n_in, int8, any strides >= 0; x_scale: rows,
  * w_scale: n_out, bias: n_out or NULL, float32 and contiguous; residual: any
  * strides, or NULL; y: col_stride 1, rows that do not overlap.  y overlaps
- * nothing else, except that it may be the residual itself.  Up to 64 rows with
- * rows of w contiguous read w in place once, or for each 32 rows; others widen
- * both operands to 16 bits, exactly, into the plan's scratch.  Scratch is made
- * by the first call that needs it, at the size that max_rows rows need, and
- * stays where it is until the plan goes: make that call before any stream
- * capture.  0 <= rows <= max_rows; asynchronous on stream; the plan's device
+ * nothing else, except that it may be the residual itself.  Few rows (up to
+ * some hundred, as n_out and n_in allow) with rows of x and w contiguous read
+ * both in place; others first widen both to 16 bits, exactly, into the plan's
+ * scratch.  Scratch is made by the first call that needs it, at the size that
+ * max_rows rows need, and stays where it is until the plan goes: make a call of
+ * as many rows, lying alike, before any stream capture.  0 <= rows <= max_rows; asynchronous on stream; the plan's device
  * has to be the current one.  Two calls on one plan that overlap on the GPU
  * race on its scratch, and calls on one plan are not thread-safe. */
 int dpdr_integer_linear(dpdr_integer_t plan, int64_t rows, const dpdr_matrix* x,

@@ -45,7 +45,8 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
         return bad("need 1 <= n_model, n_hidden <= 2^20");
     if (experts < 1 || experts > kMostExperts || top < 1 || top > kMostTop || top > experts)
         return bad("need 1 <= top <= 16 and top <= experts <= 512");
-    if (first < 0 || local < 1 || first > experts - local) return bad("need 0 <= first, 1 <= local, first + local <= experts");
+    if (first < 0 || local < 1 || first > experts - local)
+        return bad("need 0 <= first, 1 <= local, first + local <= experts");
     if (operands != DPDR_BFLOAT16 && operands != DPDR_FLOAT16) return bad("operands are bfloat16 or float16");
     if (weights != operands && weights != DPDR_INT8) return bad("weights have the operands' type or int8");
     if (result != operands && result != DPDR_FLOAT32) return bad("the result has the operands' type or float32");
@@ -84,9 +85,9 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
     int rc = e == cudaSuccess ? product_ctas(l, P->num_sms) : cuda_fail_c(e, who);
     if (!rc) {
         const int64_t pairs = max_rows * top;
-        const int64_t up_warps = 8 * std::max(l.up_ctas[0], l.up_ctas[1]), down_warps = 8 * std::max(l.down_ctas[0], l.down_ctas[1]);
+        const int64_t warps = 8 * int64_t(l.ctas);
         // two places a warp, of 32 rows by as many columns as an entry may have
-        const int64_t places = 2 * std::max(up_warps, down_warps) * 32 * (max_rows <= 8 ? 8 : max_rows <= 16 ? 16 : 32);
+        const int64_t places = 2 * warps * 32 * (max_rows <= 8 ? 8 : max_rows <= 16 ? 16 : 32);
         int64_t size = 0;
         auto take = [&](int64_t bytes) {
             const int64_t at = size;
@@ -94,10 +95,11 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
             return at;
         };
         const int64_t logits = take(max_rows * experts * 4), x = take(max_rows * l.d_pad * 2),
-                      hidden = take(pairs * l.h_pad * (l.terms == 1 ? 4 : 2 * l.terms)), some = take(places * 4),
+                      hidden = take(pairs * l.h_pad * (l.terms == 1 ? 4 : 2 * l.terms)),
+                      some = take(places * 4),
                       z = take(max_rows <= kWholeRows ? 0 : pairs * n_model * 4), expert = take(pairs * 4), shares = take(pairs * 4),
                       scores = take(max_rows * 4),
-                      up = take(up_warps * 4), down = take(down_warps * 4);
+                      up = take(warps * 4), down = take(warps * 4);
         e = cudaMalloc(&P->scratch, size_t(size));
         // counters at zero, and what lies behind the rows of x and of hidden values
         if (e == cudaSuccess) e = cudaMemset(P->scratch, 0, size_t(size));

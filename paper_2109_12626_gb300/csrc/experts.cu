@@ -6,19 +6,28 @@
 //   h_e = share_e act(x wg_e^T) (x wu_e^T);  y = sum_e h_e wd_e^T
 //
 // Three kernels, each set up while the one before drains: scores_kernel forms l,
-// chooses, and lays x out for the products; up_kernel streams the chosen experts'
-// gate and up weights past the tokens that chose them (stream.cuh), a unit being 16 hidden features
-// of an expert; down_kernel does the same with the down weights, a unit being 32
-// features of the result.  Up to 8 tokens have a column each there, and the sum runs
-// through all experts; more have their results by expert, which combine_kernel
-// adds up in the order of the shares.
+// chooses, and lays x out for the products; up_kernel streams the chosen experts' gate
+// and up weights past the tokens that chose them (stream.cuh), a unit being 16 hidden
+// features of an expert; down_kernel does the same with the down weights, a unit being
+// 32 features of the result.  Up to 8 tokens have a column each there, and the sum runs
+// through all experts; more have their results by expert, which combine_kernel adds up
+// in the order of the shares.
 //
 // All pieces of all units are dealt out to the warps in equal contiguous shares, or
-// where units are few each to a team of warps.  A unit that lies in several shares, or
-// a team in several CTAs, is finished by the last of its warps (CTAs) to come, which adds
-// up their sums in order: none waits for another, no sum's order depends on timing.  (A CTA a unit, its sum over
-// eight warps, with two barriers and a fence each: 8 rows of 64 experts of 2048 x
-// 1024 125 us.)
+// where units are few each to a team of warps.  A unit that lies in several shares, or a
+// team in several CTAs, is finished by the last of its warps (CTAs) to come, which adds
+// up their sums in order: none waits for another, and no sum's order depends on timing,
+// though where sums are cut depends on what all tokens chose.  (A CTA a unit, its sum
+// over eight warps, with two barriers and a fence each: 8 rows of 64 experts of 2048 x
+// 1024 125 us instead of 106.)
+//
+// Bound by the weights' bytes from some 50 MB of chosen experts on: 64 rows of 128
+// experts of 2048 x 1024, 8 a token, 1.6 GB in 286 to 291 us (5.5 TB/s), 8 rows of 64
+// such experts 0.5 GB in 103 to 106 (5.1).  One token of 8 experts of 4096 x 1792, 2 a
+// token, 88 MB in 29 us, is a chain: scores and choice 4 us, lists 1, the up weights 11,
+// joining a unit's parts 3, the down weights 5, joining those 3.  8-bit weights are
+// widened in registers, which takes the issue slots to their limit: 16 rows of 64 such
+// experts 0.36 GB in 92 us.
 //
 // The hidden values are not rounded to 16 bits: they are kept as terms of bfloat16 that
 // add up to them (two for a 16-bit result: 2^-16 of a value, far below what the
@@ -108,7 +117,8 @@ __device__ __forceinline__ void choose(const Layer& l, int t, int lane)
 // every CTA of the product kernels took those 20 us each with 64 tokens of 128.
 // Bound by a trip to memory: each thread asks for all that it needs at once.
 template <int TOK, bool VEC>
-__global__ void __launch_bounds__(32 * score_warps(TOK), TOK == 8 ? 3 : 8) scores_kernel(const __grid_constant__ Layer l)
+__global__ void __launch_bounds__(32 * score_warps(TOK), TOK == 8 ? 3 : 8)
+    scores_kernel(const __grid_constant__ Layer l)
 {
     constexpr int kScoreWarps = score_warps(TOK);
     __shared__ float part[kScoreWarps][TOK];
@@ -118,7 +128,8 @@ __global__ void __launch_bounds__(32 * score_warps(TOK), TOK == 8 ? 3 : 8) score
     const uint16_t* x = reinterpret_cast<const uint16_t*>(l.x);
     const uint16_t* r = reinterpret_cast<const uint16_t*>(l.router) + e * l.router_rs;
     if (VEC)   // while the kernel before drains
-        for (int k = 64 * int(threadIdx.x); k < l.d; k += 64 * kThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(r + k));
+        for (int k = 64 * int(threadIdx.x); k < l.d; k += 64 * kThreads)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(r + k));
     wait_previous();
     allow_next();
     float acc[TOK] = {};
@@ -237,41 +248,43 @@ bool down_shifted(const Layer& l) { return !aligned(l.w[2], l.local, l.d, l.w_in
 
 size_t product_smem(const Layer& l) { return size_t(kBefore) + size_t(l.rows) * l.top * 12; }
 
-// The CTAs of a kernel that fit the device at a time, after it may use the shared
-// memory that it takes.  That is only raised: another plan may need more.
-int resident(Kernel k, size_t bytes, int num_sms, int* ctas)
-{
-    const void* f = reinterpret_cast<const void*>(k);
-    static std::mutex hold;
-    std::lock_guard<std::mutex> one(hold);
-    cudaFuncAttributes at;
-    cudaError_t e = cudaFuncGetAttributes(&at, f);
-    if (e == cudaSuccess && size_t(at.maxDynamicSharedSizeBytes) < bytes)
-        e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
-    int each = 0;
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, f, kThreads, bytes);
-    if (e != cudaSuccess) return cuda_fail_c(e, "experts kernel");
-    if (each < 1) return fail_c(DPDR_ERR_CUDA, "experts: a kernel does not fit the device");
-    *ctas = each * num_sms;
-    return DPDR_OK;
-}
-
 }  // namespace
 
+// Every plan's calls may use as much shared memory as the largest plan's, so that it is
+// set once a device.  (Asked of the runtime for each plan, how many CTAs fit took 100
+// of its 300 us.)
 int product_ctas(Layer& l, int num_sms)
 {
-    const size_t bytes = product_smem(l);
-    for (int shift = 0; shift < 2; shift++) {
-        l.up_ctas[shift] = l.down_ctas[shift] = 1 << 30;
-        for (int few = 0; few < 2; few++) {
-            int up = 0, down = 0;
-            int rc = resident(up_of(l, shift, few), bytes, num_sms, &up);
-            if (!rc) rc = resident(down_of(l, shift, few), bytes, num_sms, &down);
-            if (rc) return rc;
-            l.up_ctas[shift] = std::min(l.up_ctas[shift], up);
-            l.down_ctas[shift] = std::min(l.down_ctas[shift], down);
+    static std::mutex hold;
+    static uint64_t set = 0;   // devices, of the first 64
+    int device = 0, an_sm = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&an_sm, cudaDevAttrMaxSharedMemoryPerMultiprocessor, device);
+    if (e == cudaSuccess) {
+        std::lock_guard<std::mutex> one(hold);
+        const uint64_t bit = device < 64 ? 1ull << device : 0;
+        if (!(set & bit)) {
+            Layer q = l;
+            for (int w_int8 = 0; w_int8 < 2; w_int8++)
+                for (int half = 0; half < 2; half++)
+                    for (int terms = 2; terms < 4; terms++)
+                        for (int shift = 0; shift < 2; shift++)
+                            for (int few = 0; few < 2 && e == cudaSuccess; few++) {
+                                q.w_int8 = w_int8, q.half = half, q.terms = terms;
+                                for (Kernel k : {up_of(q, shift, few), down_of(q, shift, few)})
+                                    if (e == cudaSuccess)
+                                        e = cudaFuncSetAttribute(reinterpret_cast<const void*>(k),
+                                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                                 kBefore + kMostRows * kMostTop * 12);
+                            }
+            if (e == cudaSuccess) set |= bit;
         }
     }
+    if (e != cudaSuccess) return cuda_fail_c(e, "experts kernels");
+    // two CTAs an SM, as their registers allow, where it has shared memory for them: with
+    // what the system takes of each and what the kernels hold besides
+    const size_t each = product_smem(l) + 1024 + 512;
+    l.ctas = (2 * each <= size_t(an_sm) ? 2 : 1) * num_sms;
     return DPDR_OK;
 }
 
@@ -289,10 +302,10 @@ int launch(const Layer& l, int num_sms, cudaStream_t s)
     int rc = proj::launch(scores, dim3(unsigned(grid)), dim3(32 * score_warps(tok)), 0, 1, s, "experts' scores", l);
     const bool up = up_shifted(l), down = down_shifted(l), few = l.rows <= kWholeRows;
     if (!rc)
-        rc = proj::launch(up_of(l, up, few), dim3(unsigned(l.up_ctas[up])), dim3(kThreads), product_smem(l), 1, s,
+        rc = proj::launch(up_of(l, up, few), dim3(unsigned(l.ctas)), dim3(kThreads), product_smem(l), 1, s,
                           "experts' up products", l);
     if (!rc)
-        rc = proj::launch(down_of(l, down, few), dim3(unsigned(l.down_ctas[down])), dim3(kThreads), product_smem(l), 1, s,
+        rc = proj::launch(down_of(l, down, few), dim3(unsigned(l.ctas)), dim3(kThreads), product_smem(l), 1, s,
                           "experts' down products", l);
     if (!rc && !few)
         rc = proj::launch(combine_kernel, dim3(unsigned((l.d + 255) / 256), unsigned(l.rows)), dim3(256), 0, 1, s,

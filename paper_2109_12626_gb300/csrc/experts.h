@@ -43,10 +43,10 @@ struct Layer {
     uint32_t* score_count;         // a counter for some tokens
     uint32_t* up_count;            // a counter a warp
     uint32_t* down_count;
-    int up_ctas[2], down_ctas[2];  // of the product kernels, without and with shifted rows
+    int ctas;                      // of either product kernel
 };
 
-// makes the product kernels ready and sets how many CTAs each has
+// makes the product kernels ready and sets how many CTAs each has, of l's rows and top
 int product_ctas(Layer& l, int num_sms);
 // the whole layer, at least one row
 int launch(const Layer& l, int num_sms, cudaStream_t s);

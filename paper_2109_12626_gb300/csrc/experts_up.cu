@@ -35,7 +35,13 @@ struct Up {
     uint32_t* count;
 
     __device__ __forceinline__ Up(const Layer& layer, const Choice& choice, float* room, int ln)
-        : l(layer), c(choice), tile(room), lane(ln), blocks((l.h + 15) / 16), units(c.entries * blocks), count(l.up_count)
+        : l(layer),
+          c(choice),
+          tile(room),
+          lane(ln),
+          blocks((l.h + 15) / 16),
+          units(c.entries * blocks),
+          count(l.up_count)
     {
     }
     __device__ __forceinline__ Unit part(int u, int first, int last) const
@@ -45,7 +51,8 @@ struct Up {
         const int64_t e = c.number(i);
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-            q.a[k] = static_cast<const char*>(l.w[k].data) + (e * l.w[k].stride + row * l.w[k].row_stride) * size_of(WT);
+            q.a[k] =
+                static_cast<const char*>(l.w[k].data) + (e * l.w[k].stride + row * l.w[k].row_stride) * size_of(WT);
             q.a_stride[k] = l.w[k].row_stride * size_of(WT);
         }
         q.rows_left[0] = q.rows_left[1] = min(16, l.h - row);

@@ -69,7 +69,8 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
         rc = hold(P->x_copy, most * pad, "integer product: operand copy");
         if (rc) return rc;
         Relay c;
-        c.job[c.n++] = {static_cast<const int8_t*>(x.data), P->x_copy, x.row_stride, x.col_stride, rows, P->n_in, pad, pad};
+        c.job[c.n++] = {static_cast<const int8_t*>(x.data), P->x_copy, x.row_stride, x.col_stride, rows, P->n_in,
+                        pad, pad};
         rc = relay_launch(c, num_sms, s);
         if (rc) return rc;
         r.x = P->x_copy;
@@ -103,8 +104,9 @@ int many(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, c
     if (rc) return rc;
     Relay c;
     c.wide = 1 + P->half;
-    c.job[c.n++] = {static_cast<const int8_t*>(x.data), P->wide[0], x.row_stride, x.col_stride, rows, P->n_in, ld, P->n_in};
-    c.job[c.n++] = {static_cast<const int8_t*>(w.data), P->wide[1], w.row_stride, w.col_stride, P->n_out, P->n_in, ld, P->n_in};
+    const int64_t k = P->n_in;
+    c.job[c.n++] = {static_cast<const int8_t*>(x.data), P->wide[0], x.row_stride, x.col_stride, rows, k, ld, k};
+    c.job[c.n++] = {static_cast<const int8_t*>(w.data), P->wide[1], w.row_stride, w.col_stride, P->n_out, k, ld, k};
     rc = relay_launch(c, B->num_sms, s);
     if (rc) return rc;
     proj::Product p;
@@ -211,7 +213,8 @@ extern "C" int dpdr_integer_linear(dpdr_integer_t h, int64_t rows, const dpdr_ma
     if (bias) a.vector("bias", bias, P->n_out, 4, false);
     // y may be the residual itself: each element is read by the thread that
     // then writes it
-    const bool same = residual && y && residual->data == y->data && (rows < 2 || residual->row_stride == y->row_stride) &&
+    const bool same = residual && y && residual->data == y->data &&
+                      (rows < 2 || residual->row_stride == y->row_stride) &&
                       (P->n_out < 2 || residual->col_stride == y->col_stride);
     if (residual && !same) a.input("residual", residual, rows, P->n_out, es);
     a.output("y", y, rows, P->n_out, es);

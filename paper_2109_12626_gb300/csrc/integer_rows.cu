@@ -39,7 +39,7 @@ constexpr int kStep = 2 * kHalf;           // and of a stage
 constexpr int kRunSteps = kScaledRunSteps * kSumStep / kStep;
 constexpr int kWideners = 16;              // warps
 constexpr int kThreads = 32 * kWideners + 32;
-constexpr int kAhead = 2;                  // steps whose loads are under way
+constexpr int kAhead = 2;                  // steps whose loads are under way; three gained nothing
 constexpr int kMostStages = 3;
 // CTAs of a cluster.  Clusters of eight do not all find a place at a time: 48 rows of
 // 5120 x 2048 17.8 us with them, 12.0 with four
@@ -277,11 +277,12 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             const float by = f.x_scale[m];
             float o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, y[4];
             if (f.residual) {
-                if (four) load4(f.residual, m * f.residual_rs + n, f.out_f32, f.half, o);
+                const int64_t at_m = m * f.residual_rs;
+                if (four) load4(f.residual, at_m + n, f.out_f32, f.half, o);
                 else
 #pragma unroll
                     for (int i = 0; i < 4; i++)
-                        if (n + i < a.n) o[i] = load1(f.residual, m * f.residual_rs + (n + i) * f.residual_cs, f.out_f32, f.half);
+                        if (n + i < a.n) o[i] = load1(f.residual, at_m + (n + i) * f.residual_cs, f.out_f32, f.half);
             }
 #pragma unroll
             for (int i = 0; i < 4; i++) y[i] = float(sum[i]) * (by * scale[i]) + bias[i] + o[i];
@@ -353,23 +354,27 @@ int wide_launch(const Wide& q, int num_sms, cudaStream_t s)
     a.sets = c.sets;
     a.held = c.held;
     const int stage = kWBytes + a.columns * kStep * 2;
-    a.stages = a.columns > 64 ? 2 : kMostStages;   // 128 rows of 4096 x 4096 with 2 and 3: 13.9 and 14.2 us, 32 rows 10.8 and 10.6
-    auto fits = [](const void* p, int64_t rs, int unit) { return reinterpret_cast<uintptr_t>(p) % unit == 0 && rs % unit == 0; };
+    // 128 rows of 4096 x 4096 with 2 and 3 stages 13.9 and 14.2 us, 32 rows 10.8 and 10.6
+    a.stages = a.columns > 64 ? 2 : kMostStages;
+    auto fits = [](const void* p, int64_t rs, int unit) {
+        return reinterpret_cast<uintptr_t>(p) % unit == 0 && rs % unit == 0;
+    };
     const int os = q.f.out_f32 ? 4 : 2;
     a.vec = fits(q.f.y, q.f.y_rs * os, 4 * os) &&
             (!q.f.residual || (q.f.residual_cs == 1 && fits(q.f.residual, q.f.residual_rs * os, 4 * os)));
     const bool aligned = fits(q.x, q.rows > 1 ? q.x_rs : 0, 16) && fits(q.w, q.n > 1 ? q.w_rs : 0, 16);
     auto* kernel = aligned ? wide_kernel<true> : wide_kernel<false>;
     const int bytes = 1024 + kMostStages * (kWBytes + 64 * kStep * 2);
-    static_assert(kMostStages * (kWBytes + 64 * kStep * 2) >= 2 * (kWBytes + 128 * kStep * 2), "either number of stages fits");
+    static_assert(kMostStages * (kWBytes + 64 * kStep * 2) >= 2 * (kWBytes + 128 * kStep * 2),
+                  "either number of stages fits");
     if (!q.set[aligned]) {
         const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                    cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess) return cuda_fail_c(e, "integer wide kernel");
         q.set[aligned] = true;
     }
-    return launch(kernel, dim3(unsigned(c.across * a.split), unsigned(c.down)), dim3(kThreads), size_t(1024 + a.stages * stage),
-                  a.split, s, "integer wide kernel", a);
+    return launch(kernel, dim3(unsigned(c.across * a.split), unsigned(c.down)), dim3(kThreads),
+                  size_t(1024 + a.stages * stage), a.split, s, "integer wide kernel", a);
 }
 
 }  // namespace integer

@@ -4,13 +4,11 @@
 // D[row][column] = sum_k A[row][k] B[column][k] for 32 rows of A (weights: 32 of
 // one matrix, or 16 of either of two) and 8 NT columns (tokens).  With so few
 // columns the weights' bytes are the bound, and what matters is that some 100 KB
-// an SM are always under way.  Each warp of a CTA takes every eighth piece of 64
-// bytes along k and loads it into a ring of its own by cp.async, four bytes of
-// A's rows beside the columns that go with them, several pieces ahead, across
-// the CTA's units of work; no warp waits for another until a unit's eight partial
-// sums are joined, in the order of the warps.  (Rows copied by cp.async.bulk
-// instead reached 4.1 TB/s with 1 KB a copy, an issuing warp making one in 70
-// cycles.)
+// an SM are always under way.  Each warp loads pieces of 64 bytes along k of its rows,
+// beside the columns that go with them, into a ring of its own by cp.async, several
+// pieces ahead and across the ends of units, and no warp waits for another until its
+// sums are done.  (Rows copied by cp.async.bulk instead reached 4.1 TB/s with 1 KB a
+// copy, an issuing warp making one in 70 cycles.)
 //
 // The products are legacy matrix instructions (m16n8k16 of 16-bit operands,
 // m16n8k8 of tf32), which at 600 and 300 TFLOP/s are far from the bound for up
@@ -646,7 +644,12 @@ struct Shares {
     int total, of, each;
     int most, long_ones, behind;   // the first long_ones warps have one more than most, up to piece `behind`
     __device__ __forceinline__ Shares(int all, int warps, int unit)
-        : total(all), of(warps), each(unit), most(all / warps), long_ones(all - most * warps), behind(long_ones * (most + 1))
+        : total(all),
+          of(warps),
+          each(unit),
+          most(all / warps),
+          long_ones(all - most * warps),
+          behind(long_ones * (most + 1))
     {
     }
     __device__ __forceinline__ int start(int w) const { return w * most + min(w, long_ones); }
@@ -670,14 +673,15 @@ struct Teams {
 // places: place(c) is contributor c's for this unit.  count: the unit's counter,
 // zero.
 template <int NT, typename Place>
-__device__ __forceinline__ bool join_parts(float (&v)[2][NT][4], int me, int first, int last, Place place, uint32_t* count,
-                                           int lane)
+__device__ __forceinline__ bool join_parts(float (&v)[2][NT][4], int me, int first, int last, Place place,
+                                           uint32_t* count, int lane)
 {
     float4* mine = reinterpret_cast<float4*>(place(me)) + lane;
 #pragma unroll
     for (int i = 0; i < 2; i++)
 #pragma unroll
-        for (int n = 0; n < NT; n++) mine[(i * NT + n) * 32] = make_float4(v[i][n][0], v[i][n][1], v[i][n][2], v[i][n][3]);
+        for (int n = 0; n < NT; n++)
+            mine[(i * NT + n) * 32] = make_float4(v[i][n][0], v[i][n][1], v[i][n][2], v[i][n][3]);
     __syncwarp();
     uint32_t came = 0;
     if (lane == 0) {

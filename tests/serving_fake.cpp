@@ -63,14 +63,14 @@ int quantise_launch(int, int64_t, int64_t, const dpdr_matrix&, const dpdr_matrix
 namespace experts {
 int product_ctas(Layer& l, int num_sms)
 {
-    for (int i = 0; i < 2; i++) l.up_ctas[i] = l.down_ctas[i] = ctas_an_sm * num_sms;
+    l.ctas = ctas_an_sm * num_sms;
     return DPDR_OK;
 }
 int launch(const Layer& l, int, cudaStream_t)
 {
     B.launches++;
     layers++;
-    const int64_t pairs = int64_t(l.rows) * l.top, warps = 8 * int64_t(l.up_ctas[0]);
+    const int64_t pairs = int64_t(l.rows) * l.top, warps = 8 * int64_t(l.ctas);
     const int64_t columns = l.rows <= 8 ? 8 : l.rows <= 16 ? 16 : 32;
     if (pairs > l.pairs) wrong("pairs", nullptr, pairs);
     holds("scores", l.logits, size_t(l.rows) * l.total * 4);
