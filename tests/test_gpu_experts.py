@@ -355,3 +355,21 @@ def test_refusals(pkg):
         w8 = [v.to(torch.int8) for v in w]
         with pytest.raises(pkg.DpdrError):                 # and the other way round
             plan.forward(x, router, *w8, y)
+
+
+@pytest.mark.parametrize("ranks,tokens", [(1, 3), (4, 1), (4, 40), (2, 64)])
+def test_the_example_runs(ranks, tokens):
+    """examples/expert_parallel_tokens.py: sums of some hundred products in float32,
+    2^-24 a step at most, of values of one size."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import expert_parallel_tokens as example
+    block = example.SplitTokens(ranks, tokens, 256, 128, 8, 2)
+    x = torch.randn(tokens, 256, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    for _ in range(2):
+        block.forward(x)
+        block.sync()
+    errors = example.worst(block, x)
+    assert max(errors.values()) < 512 * 2.0 ** -24, errors
+    block.close()
