@@ -251,8 +251,7 @@ size_t product_smem(const Layer& l) { return size_t(kBefore) + size_t(l.rows) * 
 }  // namespace
 
 // Every plan's calls may use as much shared memory as the largest plan's, so that it is
-// set once a device.  (Asked of the runtime for each plan, how many CTAs fit took 100
-// of its 300 us.)
+// set once a device.
 int product_ctas(Layer& l, int num_sms)
 {
     static std::mutex hold;

@@ -39,7 +39,7 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
 {
     const int num_sms = P->base()->num_sms;
     const int64_t pad = upto(P->n_in, kRowsPad), most = std::min<int64_t>(P->max_rows, kFewRows);
-    Rows r;
+    Rows r{};
     r.rows = int(rows);
     r.k = int(P->n_in);
     r.n = P->n_out;
@@ -48,19 +48,26 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
     r.f = f;
     r.set = P->set;
     int rc = DPDR_OK;
-    if (!P->parts) {   // and the counters behind them, at zero
+    const bool token = rows <= kTokenRows && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 &&
+                       (P->n_out == 1 || r.w_rs % 16 == 0);
+    if (!P->parts && !token) {   // and the counters behind them, at zero
         const int64_t ints = parts_ints(num_sms), all = (ints + 2 * num_sms) * 4;
         rc = hold(P->parts, all, "integer product: parts");
         if (!rc) {
             const cudaError_t e = cudaMemsetAsync(P->parts + ints, 0, size_t(2 * num_sms) * 4, s);
-            if (e != cudaSuccess) rc = cuda_fail_c(e, "integer product: counters");
+            if (e != cudaSuccess) {   // none, for the next call to make
+                rc = cuda_fail_c(e, "integer product: counters");
+                cudaFree(P->parts);
+                P->parts = nullptr;
+            }
         }
         if (rc) return rc;
     }
-    r.parts = P->parts;
-    r.count = reinterpret_cast<uint32_t*>(P->parts + parts_ints(num_sms));
+    if (!token) {
+        r.parts = P->parts;
+        r.count = reinterpret_cast<uint32_t*>(P->parts + parts_ints(num_sms));
+    }
     // x as it lies where its rows are whole pieces at multiples of 16 bytes
-    const bool token = rows <= 4 && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (P->n_out == 1 || r.w_rs % 16 == 0);
     if (x.col_stride == 1 && (P->n_in == pad || token) && reinterpret_cast<uintptr_t>(x.data) % 16 == 0 &&
         (rows == 1 || x.row_stride % 16 == 0)) {
         r.x = static_cast<const char*>(x.data);

@@ -300,147 +300,203 @@ __device__ __forceinline__ int rounded(float v, const Rounding& r)
     return v < 0.0f ? -q : q;
 }
 
-// Row by row, `share` threads a row, one pass: the values stay in registers (HELD
-// groups of four a thread, kept as they came); longer rows are read twice, from L2
-// the second time.  Bound by the bytes, and nearly so by instructions: 8192 x 8192
-// float32, 336 MB, in 57 us (5.9 TB/s; with the exact comparison for every value 79).
-template <int DT, int HELD, bool VEC>
-__global__ void __launch_bounds__(256) quantise_kernel(const void* x, int64_t rs, int64_t cs, int8_t* q, int64_t q_rs,
-                                                      float* scale, int64_t rows, int64_t n, int share)
+// What a row's largest size makes of its values: `plain` rounding, or none (zeros,
+// infinities, NaN)
+struct Row {
+    uint32_t high;   // the size's bits
+    Rounding r;
+    bool plain;
+    __device__ __forceinline__ Row(uint32_t bits, float size)
+        : high(bits), r(size), plain(bits > 0 && bits < 0x7F800000u)
+    {
+    }
+};
+
+// four values of it, each by itself
+__device__ __noinline__ uint32_t round4_apart(float f0, float f1, float f2, float f3, uint32_t high, float size)
 {
-    __shared__ uint32_t most[8];
+    const Row w(high, size);
+    auto one = [&](float f) {
+        if (w.plain) return uint32_t(rounded(f, w.r) & 255);
+        if (w.high == 0x7F800000u && isinf(f)) return f < 0.0f ? 129u : 127u;
+        return 0u;
+    };
+    return one(f0) | one(f1) << 8 | one(f2) << 16 | one(f3) << 24;
+}
+
+// t + 1.5 2^23 is t rounded in the low bits; what it was off by tells whether a half
+// is near
+__device__ __forceinline__ uint32_t round4(const float (&f)[4], const Row& w)
+{
+    uint32_t v[4];
+    float off = w.plain && w.r.power == 1.0f ? 0.0f : 1.0f;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const float y = fmaf(f[k], w.r.by, 12582912.0f);
+        off = fmaxf(off, fabsf(fmaf(f[k], w.r.by, 12582912.0f - y)));
+        v[k] = __float_as_uint(y);
+    }
+    if (off > 0.4999f) return round4_apart(f[0], f[1], f[2], f[3], w.high, __uint_as_float(w.high));
+    return __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
+}
+
+// The largest of a row's threads' `high`; all threads of the CTA come here
+template <int SHARE, int THREADS>
+__device__ __forceinline__ uint32_t row_high(uint32_t high)
+{
+    __shared__ uint32_t most[THREADS / 32];
+    high = __reduce_max_sync(0xFFFFFFFFu, high);
+    if (SHARE > 32) {
+        if (threadIdx.x % 32 == 0) most[threadIdx.x / 32] = high;
+        __syncthreads();
+        const int first = threadIdx.x / SHARE * (SHARE / 32);
+#pragma unroll
+        for (int w = 0; w < SHARE / 32; w++) high = max(high, most[first + w]);
+    }
+    return high;
+}
+
+// Rows that lie at multiples of 16 bytes, and are such long: SHARE threads a row, one
+// pass.  The values stay in registers, HELD groups of 16 bytes a thread, kept as they
+// came (as few as let several rows an SM be under way); longer rows are read twice, from
+// L2 the second time.  Bound by the bytes, and by some ten instructions a value: 8192 x
+// 8192 float32, 336 MB, in 52 us (6.4 TB/s; with 256 threads a row 60, with the exact
+// comparison for every value 79), 4096 x 4096 bfloat16, 50 MB, in 13.3.
+template <int DT, int HELD, int SHARE>
+__global__ void __launch_bounds__(SHARE < 256 ? 256 : SHARE)
+    quantise_kernel(const char* x, int64_t x_bytes, int8_t* q, int64_t q_rs, float* scale, int64_t rows, int units)
+{
+    constexpr int kThreads = SHARE < 256 ? 256 : SHARE, kEach = DT == DPDR_FLOAT32 ? 4 : 8;   // values of a group
     wait_previous();
     allow_next();
-    const int per = 256 / share, mine = int(threadIdx.x) / share, at = int(threadIdx.x) % share;
-    const int64_t m = int64_t(blockIdx.x) * per + mine;
+    const int at = int(threadIdx.x) % SHARE;
+    const int64_t m = int64_t(blockIdx.x) * (kThreads / SHARE) + threadIdx.x / SHARE;
     const bool there = m < rows;
-    const int64_t from = m * rs;
-    const char* row = static_cast<const char*>(x) + from * (DT == DPDR_FLOAT32 ? 4 : 2);
-    const int64_t units = (n + 3) / 4;   // groups of four
-    using Held = typename std::conditional<DT == DPDR_FLOAT32, uint4, uint2>::type;
-    Held held[HELD];
-    auto get = [&](int64_t u) {
-        Held h;
-        if (VEC) {
-            h = reinterpret_cast<const Held*>(row)[u];
-        } else {
-            uint32_t v[4];
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const int64_t i = from + (4 * u + k) * cs;
-                if (4 * u + k >= n) v[k] = 0;
-                else if (DT == DPDR_FLOAT32) v[k] = static_cast<const uint32_t*>(x)[i];
-                else v[k] = static_cast<const uint16_t*>(x)[i];
-            }
-            if constexpr (DT == DPDR_FLOAT32) h = make_uint4(v[0], v[1], v[2], v[3]);
-            else h = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
-        }
-        return h;
-    };
-    auto widened = [&](const Held& h, float (&f)[4]) {
-        if constexpr (DT == DPDR_FLOAT32) proj::widen4(h, 1, 0, f);
-        else proj::widen4(make_uint4(h.x, h.y, 0, 0), 0, DT == DPDR_FLOAT16, f);
-    };
-    // sizes as whole numbers, whose order puts NaN above infinity
+    const uint4* from = reinterpret_cast<const uint4*>(x + m * x_bytes) + at;
+    // Sizes as whole numbers, whose order puts NaN above infinity: of 16-bit types two at a
+    // time
     uint32_t high = 0;
-    auto look = [&](const Held& h) {
-        float f[4];
-        widened(h, f);
+    auto look = [&](const uint4& h) {
+        const uint32_t w[4] = {h.x, h.y, h.z, h.w};
 #pragma unroll
-        for (int k = 0; k < 4; k++) high = max(high, __float_as_uint(f[k]) & 0x7FFFFFFFu);
+        for (int k = 0; k < 4; k++) {
+            if (DT == DPDR_FLOAT32) high = max(high, w[k] & 0x7FFFFFFFu);
+            else high = __vmaxu2(high, w[k] & 0x7FFF7FFFu);
+        }
     };
-    const bool whole = units <= int64_t(HELD) * share;
+    uint4 held[HELD];
+    const bool whole = units <= HELD * SHARE;
     if (there) {
         if (whole) {
 #pragma unroll
-            for (int k = 0; k < HELD; k++) {
-                const int64_t u = at + int64_t(k) * share;
-                if (u < units) held[k] = get(u);
-            }
+            for (int k = 0; k < HELD; k++)
+                if (at + k * SHARE < units) held[k] = from[k * SHARE];
 #pragma unroll
             for (int k = 0; k < HELD; k++)
-                if (at + int64_t(k) * share < units) look(held[k]);
+                if (at + k * SHARE < units) look(held[k]);
         } else {
 #pragma unroll 4
-            for (int64_t u = at; u < units; u += share) look(get(u));
+            for (int u = 0; u < units - at; u += SHARE) look(from[u]);
         }
     }
-    high = __reduce_max_sync(0xFFFFFFFFu, high);
-    if (share > 32) {
-        if (threadIdx.x % 32 == 0) most[threadIdx.x / 32] = high;
-        __syncthreads();
-        const int first = mine * (share / 32);
-        for (int w = 0; w < share / 32; w++) high = max(high, most[first + w]);
+    if (DT != DPDR_FLOAT32) {
+        high = max(high >> 16, high & 0xFFFFu);
+        high = __float_as_uint(proj::widen(uint16_t(high), DT == DPDR_FLOAT16));
     }
+    high = row_high<SHARE, kThreads>(high);
+    const Row w(high, __uint_as_float(high));
     if (!there) return;
-    const float a = __uint_as_float(high);
-    if (at == 0) scale[m] = a / 127.0f;
-    const bool plain = high > 0 && high < 0x7F800000u;
-    const Rounding r(a);
-    auto put = [&](int64_t u, const Held& h) {
+    if (at == 0) scale[m] = __uint_as_float(w.high) / 127.0f;
+    int8_t* to = q + m * q_rs + at * kEach;
+    auto put = [&](int u, const uint4& h) {
         float f[4];
-        widened(h, f);
-        // t + 1.5 2^23 is t rounded in the low bits; what it was off by tells whether a
-        // half is near
-        uint32_t v[4];
-        float off = plain && r.power == 1.0f ? 0.0f : 1.0f;
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const float y = fmaf(f[k], r.by, 12582912.0f);
-            off = fmaxf(off, fabsf(fmaf(f[k], r.by, 12582912.0f - y)));
-            v[k] = __float_as_uint(y);
-        }
-        if (off > 0.4999f)
-#pragma unroll 1
-            for (int k = 0; k < 4; k++) {
-                const float a = k == 0 ? f[0] : k == 1 ? f[1] : k == 2 ? f[2] : f[3];
-                int w = 0;
-                if (plain) w = rounded(a, r);
-                else if (high == 0x7F800000u && isinf(a)) w = a < 0.0f ? -127 : 127;
-                if (k == 0) v[0] = uint32_t(w);
-                else if (k == 1) v[1] = uint32_t(w);
-                else if (k == 2) v[2] = uint32_t(w);
-                else v[3] = uint32_t(w);
-            }
-        const uint32_t all = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
-        int8_t* to = q + m * q_rs + 4 * u;
-        if (VEC) {
-            *reinterpret_cast<uint32_t*>(to) = all;
+        if (DT == DPDR_FLOAT32) {
+            proj::widen4(h, 1, 0, f);
+            *reinterpret_cast<uint32_t*>(to + u * kEach) = round4(f, w);
         } else {
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-                if (4 * u + k < n) to[k] = int8_t(all >> 8 * k);
+            uint2 v;
+            proj::widen4(make_uint4(h.x, h.y, 0, 0), 0, DT == DPDR_FLOAT16, f);
+            v.x = round4(f, w);
+            proj::widen4(make_uint4(h.z, h.w, 0, 0), 0, DT == DPDR_FLOAT16, f);
+            v.y = round4(f, w);
+            *reinterpret_cast<uint2*>(to + u * kEach) = v;
         }
     };
     if (whole) {
 #pragma unroll
-        for (int k = 0; k < HELD; k++) {
-            const int64_t u = at + int64_t(k) * share;
-            if (u < units) put(u, held[k]);
-        }
+        for (int k = 0; k < HELD; k++)
+            if (at + k * SHARE < units) put(k * SHARE, held[k]);
     } else {
 #pragma unroll 2
-        for (int64_t u = at; u < units; u += share) put(u, get(u));
+        for (int u = 0; u < units - at; u += SHARE) put(u, from[u]);
+    }
+}
+
+// Rows that lie otherwise: a CTA a row, value by value, read twice
+template <int DT>
+__global__ void __launch_bounds__(256)
+    quantise_any_kernel(const void* x, int64_t rs, int64_t cs, int8_t* q, int64_t q_rs, float* scale, int64_t n)
+{
+    constexpr int kDeep = 8;   // values of a thread under way
+    wait_previous();
+    allow_next();
+    const int64_t m = blockIdx.x, from = m * rs;
+    auto get = [&](int64_t k) {
+        if (DT == DPDR_FLOAT32) return static_cast<const float*>(x)[from + k * cs];
+        return proj::widen(static_cast<const uint16_t*>(x)[from + k * cs], DT == DPDR_FLOAT16);
+    };
+    uint32_t high = 0;
+    for (int64_t k0 = threadIdx.x; k0 < n; k0 += kDeep * 256) {
+        float f[kDeep];
+#pragma unroll
+        for (int d = 0; d < kDeep; d++) f[d] = k0 + d * 256 < n ? get(k0 + d * 256) : 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDeep; d++) high = max(high, __float_as_uint(f[d]) & 0x7FFFFFFFu);
+    }
+    high = row_high<256, 256>(high);
+    const Row w(high, __uint_as_float(high));
+    if (threadIdx.x == 0) scale[m] = __uint_as_float(w.high) / 127.0f;
+    int8_t* to = q + m * q_rs;
+    for (int64_t k0 = threadIdx.x; k0 < n; k0 += kDeep * 256) {
+        float f[kDeep];
+#pragma unroll
+        for (int d = 0; d < kDeep; d++) f[d] = k0 + d * 256 < n ? get(k0 + d * 256) : 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDeep; d += 4) {
+            const uint32_t v = round4(reinterpret_cast<const float(&)[4]>(f[d]), w);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (k0 + (d + i) * 256 < n) to[k0 + (d + i) * 256] = int8_t(v >> 8 * i);
+        }
     }
 }
 
 template <int DT>
 int quantise(int64_t rows, int64_t n, const dpdr_matrix& x, const dpdr_matrix& q, float* scale, cudaStream_t s)
 {
-    const int es = DT == DPDR_FLOAT32 ? 4 : 2;
-    const bool vec = x.col_stride == 1 && n % 4 == 0 && reinterpret_cast<uintptr_t>(x.data) % (4 * es) == 0 &&
-                     reinterpret_cast<uintptr_t>(q.data) % 4 == 0 &&
-                     (rows == 1 || (x.row_stride % 4 == 0 && q.row_stride % 4 == 0));
-    const int64_t units = (n + 3) / 4;
-    int share = 32;   // threads a row
-    while (share < 256 && units > share) share *= 2;
-    const int64_t per = 256 / share, ctas = (rows + per - 1) / per;
-    if (ctas > (int64_t(1) << 31) - 1) return fail_c(DPDR_ERR_INVALID, "dpdr_quantise: too many rows");
-    const bool few = units <= 4 * share;
-    auto* kernel = vec ? (few ? quantise_kernel<DT, 4, true> : quantise_kernel<DT, 8, true>)
-                       : (few ? quantise_kernel<DT, 4, false> : quantise_kernel<DT, 8, false>);
-    return proj::launch(kernel, dim3(unsigned(ctas)), dim3(256), 0, 1, s, "quantise kernel", (const void*)x.data,
-                        x.row_stride, x.col_stride, static_cast<int8_t*>(q.data), q.row_stride, scale, rows, n, share);
+    const char* what = "quantise kernel";
+    const int es = DT == DPDR_FLOAT32 ? 4 : 2, each = 16 / es;
+    auto fits = [&](const void* p, int64_t bytes, int unit) {
+        return reinterpret_cast<uintptr_t>(p) % unit == 0 && (rows == 1 || bytes % unit == 0);
+    };
+    if ((x.col_stride != 1 && n > 1) || n % each || !fits(x.data, x.row_stride * es, 16) ||
+        !fits(q.data, q.row_stride, each))
+        return proj::launch(quantise_any_kernel<DT>, dim3(unsigned(rows)), dim3(256), 0, 1, s, what,
+                            (const void*)x.data, x.row_stride, x.col_stride, static_cast<int8_t*>(q.data), q.row_stride,
+                            scale, n);
+    const int units = int(n / each);
+    auto run = [&](auto* kernel, int share) {
+        const int threads = share < 256 ? 256 : share, per = threads / share;
+        return proj::launch(kernel, dim3(unsigned((rows + per - 1) / per)), dim3(unsigned(threads)), 0, 1, s, what,
+                            (const char*)x.data, x.row_stride * es, static_cast<int8_t*>(q.data), q.row_stride, scale,
+                            rows, units);
+    };
+    if (units <= 4 * 32) return run(quantise_kernel<DT, 4, 32>, 32);
+    if (units <= 4 * 128) return run(quantise_kernel<DT, 4, 128>, 128);
+    if (units <= 4 * 256) return run(quantise_kernel<DT, 4, 256>, 256);
+    if (units <= 4 * 512) return run(quantise_kernel<DT, 4, 512>, 512);
+    if (units <= 8 * 512) return run(quantise_kernel<DT, 8, 512>, 512);
+    return run(quantise_kernel<DT, 8, 1024>, 1024);
 }
 
 template <int NT>
@@ -465,7 +521,7 @@ int rows_launch_of(const RowsArgs& a, bool shift, int ctas, cudaStream_t s)
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s)
 {
     const bool shift = reinterpret_cast<uintptr_t>(r.w) % 16 != 0 || (r.n > 1 && r.w_rs % 16 != 0);
-    if (r.rows <= 4 && !shift) return token_launch(r, num_sms, s);
+    if (r.rows <= kTokenRows && !shift) return token_launch(r, num_sms, s);
     RowsArgs a;
     a.r = r;
     const int nt = r.rows <= 8 ? 1 : r.rows <= 16 ? 2 : 4;

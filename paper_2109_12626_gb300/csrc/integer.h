@@ -12,6 +12,8 @@ constexpr int64_t kMostSummed = (int64_t(1) << 17) - 1;
 
 // rows that rows_launch takes
 constexpr int kFewRows = 64;
+// and of these the ones that its kernel for tokens takes, of w at multiples of 16 bytes
+constexpr int kTokenRows = 4;
 // Rows past which wide_launch is faster where it takes the product.  us of
 // rows_launch and of it, 4096 x 4096 weights: 16 rows 9.3 and 10.2, 32 rows 12.0
 // and 10.6; 24 rows of 1024 x 8192 11.6 and 7.9.
@@ -44,7 +46,7 @@ struct Rows {
     uint32_t* count;
     bool (*set)[2];          // of the plan: kernels' attributes set
 };
-// x need not be padded for up to 4 rows of w at multiples of 16 bytes
+// (that kernel needs neither parts nor padded rows of x)
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s);
 constexpr int64_t parts_ints(int num_sms) { return int64_t(2 * num_sms) * 32 * 32; }
 

@@ -24,11 +24,13 @@ int rows_launch(const Rows& r, int num_sms, cudaStream_t)
 {
     B.launches++;
     streamed++;
-    const bool token = r.rows <= 4 && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (r.n == 1 || r.w_rs % 16 == 0);
+    const bool token = r.rows <= kTokenRows && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (r.n == 1 || r.w_rs % 16 == 0);
     if (r.rows < 1 || r.rows > kFewRows) wrong("rows", nullptr, r.rows);
     // whole pieces of 64 values, but for up to four rows
     holds("x", r.x, size_t(r.rows - 1) * r.x_rs + (token ? r.k : (r.k + 63) / 64 * 64));
     if (reinterpret_cast<uintptr_t>(r.x) % 16 || (r.rows > 1 && r.x_rs % 16)) wrong("x at", r.x, 0);
+    if (token) return DPDR_OK;
+    if (!r.parts || !r.count) wrong("no parts", nullptr, 0);
     holds("parts", r.parts, size_t(parts_ints(num_sms)) * 4);
     holds("counters", r.count, size_t(2 * num_sms) * 4);
     if (reinterpret_cast<char*>(r.count) < reinterpret_cast<char*>(r.parts + parts_ints(num_sms)))
