@@ -357,6 +357,23 @@ def test_refusals(pkg):
             plan.forward(x, router, *w8, y)
 
 
+def test_two_plans_on_two_streams(pkg):
+    """Calls of different plans may overlap: each has scratch of its own."""
+    cases = [make(rows, 320, 160, 24, 24, "bfloat16", weights, rows) for rows, weights in ((1, None), (30, None), (8, "int8"))]
+    plans = [pkg.Experts(c[0].shape[0], 320, 160, 24, 4, out="float32", weights=w) for c, w in zip(cases, (None, None, "int8"))]
+    want = [run(pkg, *c, 4, out="float32", plan=p)[0] for c, p in zip(cases, plans)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[torch.empty_like(w) for _ in range(6)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for (x, router, w, scale), plan, stream, y in zip(cases, plans, streams, got):
+            plan.forward(x, router, *w, y[i], gate_scale=scale[0], up_scale=scale[1], down_scale=scale[2], stream=stream)
+    for plan, stream in zip(plans, streams):
+        plan.sync(stream)
+        plan.close()
+    assert all(torch.equal(y, w) for ys, w in zip(got, want) for y in ys)
+
+
 @pytest.mark.parametrize("ranks,tokens", [(1, 3), (4, 1), (4, 40), (2, 64)])
 def test_the_example_runs(ranks, tokens):
     """examples/expert_parallel_tokens.py: sums of some hundred products in float32,

@@ -148,6 +148,37 @@ def test_scales_without_a_value_stay_in_their_place(pkg):
         assert torch.equal(y, plain)
 
 
+@pytest.mark.parametrize("rows", [2, 12, 100, 700])
+def test_scales_and_bias_at_any_place(pkg, rows):
+    """Vectors that start at odd elements of their arrays, and results whose rows do."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, w = bytes_(g, rows, 320), bytes_(g, 1000, 320)
+    xs, ws = scales(g, rows + 1)[1:], scales(g, 1003)[3:]
+    bias = torch.randn(1001, device="cuda", generator=g)[1:]
+    residual = torch.randn(rows, 1001, device="cuda", generator=g).bfloat16()[:, 1:]
+    check(pkg, x, xs, w, ws, "bfloat16", bias, residual)
+    check(pkg, x, xs, w, ws, "float32", bias, residual.float())
+
+
+def test_two_plans_on_two_streams(pkg):
+    """Calls of different plans may overlap: each has scratch of its own."""
+    g = torch.Generator(device="cuda").manual_seed(10)
+    w, ws = bytes_(g, 768, 704), scales(g, 768)
+    xs = [(bytes_(g, rows, 704), scales(g, rows)) for rows in (1, 9, 90, 2000)]
+    plans = [pkg.Linear8(x.shape[0], 704, 768, out="float32") for x, _ in xs]
+    want = [check(pkg, x, s, w, ws, "float32", plan=p) for (x, s), p in zip(xs, plans)]
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[torch.empty_like(v) for _ in range(6)] for v in want]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for (x, s), plan, stream, y in zip(xs, plans, streams, got):
+            plan.forward(x, s, w, ws, y[i], stream=stream)
+    for plan, stream in zip(plans, streams):
+        plan.sync(stream)
+        plan.close()
+    assert all(torch.equal(y, v) for ys, v in zip(got, want) for y in ys)
+
+
 def test_one_plan_many_calls(pkg):
     g = torch.Generator(device="cuda").manual_seed(4)
     k, n = 2000, 150
