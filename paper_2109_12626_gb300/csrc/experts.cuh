@@ -271,7 +271,10 @@ struct Run {
     __device__ __forceinline__ void go()
     {
         if (job.units <= 0) return;
-        if (2 * job.units <= int(gridDim.x) * kWarps) teams<ASK>();
+        // Teams of two and three warps are 3 to 2, which is less than joining shares costs
+        // while a piece's columns are few: 16 rows of 8 experts of 4096 x 1792 with teams
+        // of two or more, and of four or more, 81.0 and 83.6 us, 64 rows 128.9 and 118.7.
+        if ((NT > 2 ? 4 : 2) * job.units <= int(gridDim.x) * kWarps) teams<ASK>();
         else shares<ASK>();
     }
 };
