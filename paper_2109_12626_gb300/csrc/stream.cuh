@@ -79,6 +79,17 @@ __device__ __forceinline__ uint4 load16(uint32_t at)
     return v;
 }
 
+// 16 bytes at any place
+__device__ __forceinline__ uint4 load16_at(uint32_t at)
+{
+    const uint32_t p = at & ~3u, b = 8 * (at & 3u);
+    uint32_t w[5];
+#pragma unroll
+    for (int i = 0; i < 5; i++) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(p + 4 * i));
+    return make_uint4(__funnelshift_r(w[0], w[1], b), __funnelshift_r(w[1], w[2], b), __funnelshift_r(w[2], w[3], b),
+                      __funnelshift_r(w[3], w[4], b));
+}
+
 // bytes o .. o + 15 of the 32 in lo and hi, 0 <= o < 16
 __device__ __forceinline__ uint4 shifted(const uint4& lo, const uint4& hi, int o)
 {
@@ -364,7 +375,7 @@ struct Stream {
     __device__ __forceinline__ uint4 a_lane(uint32_t at, int part, int i, int h) const
     {
         const int r = i * 16 + h * 8 + lane / 4, c = 4 * part + (lane & 3);
-        if (SHIFT) return shifted(load16(at + a_place(r, c)), load16(at + a_place(r, c + 1)), shift[i][h]);
+        if (SHIFT) return load16_at(at + a_place(r, c) + shift[i][h]);
         return load16(at + a_place(r, c));
     }
 
