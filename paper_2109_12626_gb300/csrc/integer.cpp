@@ -48,8 +48,7 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
     r.f = f;
     r.set = P->set;
     int rc = DPDR_OK;
-    const bool token = rows <= kTokenRows && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 &&
-                       (P->n_out == 1 || r.w_rs % 16 == 0);
+    const bool token = for_tokens(r);
     if (!P->parts && !token) {   // and the counters behind them, at zero
         const int64_t ints = parts_ints(num_sms), all = (ints + 2 * num_sms) * 4;
         rc = hold(P->parts, all, "integer product: parts");
@@ -67,9 +66,10 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
         r.parts = P->parts;
         r.count = reinterpret_cast<uint32_t*>(P->parts + parts_ints(num_sms));
     }
-    // x as it lies where its rows are whole pieces at multiples of 16 bytes
-    if (x.col_stride == 1 && (P->n_in == pad || token) && reinterpret_cast<uintptr_t>(x.data) % 16 == 0 &&
-        (rows == 1 || x.row_stride % 16 == 0)) {
+    // x as it lies where its rows are whole pieces at multiples of 16 bytes, and wherever
+    // they are for tokens and weights at any address
+    const bool at_16 = reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && (rows == 1 || x.row_stride % 16 == 0);
+    if (x.col_stride == 1 && (P->n_in == pad || token) && (at_16 || (token && !aligned_weights(r)))) {
         r.x = static_cast<const char*>(x.data);
         r.x_rs = x.row_stride;
     } else {

@@ -125,9 +125,13 @@ constexpr int kTokenWarps = 8, kTokenDeep = 4;
 // integer units, which hold whole sums of 32 bits: nothing to widen, and nothing to
 // join beyond the group.  x comes from L1.  From five rows on the reads of x and the
 // products take longer than the weights.
-template <int ROWS>
+// ALIGNED: rows of w and x at multiples of 16 bytes.  Others are loaded by the aligned 16
+// bytes that what is wanted begins and ends in, and shifted, which binds: one row of 4001 x
+// 4003 9.0 us (1.8 TB/s), aligned of 4096 x 4096 5.2.
+template <int ROWS, bool ALIGNED>
 __global__ void __launch_bounds__(32 * kTokenWarps) token_kernel(const __grid_constant__ Rows r, int share)
 {
+    constexpr int kDeep = ALIGNED ? kTokenDeep : 2, kParts = ALIGNED ? 1 : 2;
     __shared__ int parts[kTokenWarps][2 * ROWS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = warp / share, mine = warp % share;
@@ -145,25 +149,45 @@ __global__ void __launch_bounds__(32 * kTokenWarps) token_kernel(const __grid_co
     int acc[2][ROWS] = {};
     if (first < r.n) {
         const int units = r.k / 16, step = 32 * share;
+        // 16 bytes from p on, all of them of one row, as they are loaded and as they are meant
+        auto load = [](const char* p, uint4 (&v)[kParts]) {
+            const int o = ALIGNED ? 0 : int(reinterpret_cast<uintptr_t>(p) & 15);
+            const uint4* q = reinterpret_cast<const uint4*>(p - o);
+            v[0] = __ldcs(q);
+            if (!ALIGNED) v[kParts - 1] = o ? __ldcs(q + 1) : v[0];
+        };
+        auto meant = [](const char* p, const uint4 (&v)[kParts]) {
+            return ALIGNED ? v[0] : shifted(v[0], v[kParts - 1], int(reinterpret_cast<uintptr_t>(p) & 15));
+        };
         auto sum = [&](const uint4& a, const uint4& b, int u) {
 #pragma unroll
             for (int m = 0; m < ROWS; m++) {
-                const uint4 x = *reinterpret_cast<const uint4*>(r.x + min(m, r.rows - 1) * r.x_rs + 16 * u);
+                const char* p = r.x + min(m, r.rows - 1) * r.x_rs + 16 * u;
+                uint4 v[kParts];
+                const int o = ALIGNED ? 0 : int(reinterpret_cast<uintptr_t>(p) & 15);
+                const uint4* q = reinterpret_cast<const uint4*>(p - o);
+                v[0] = q[0];
+                if (!ALIGNED) v[kParts - 1] = o ? q[1] : v[0];
+                const uint4 x = meant(p, v);
                 acc[0][m] = __dp4a(int(a.x), int(x.x), __dp4a(int(a.y), int(x.y), acc[0][m]));
                 acc[1][m] = __dp4a(int(b.x), int(x.x), __dp4a(int(b.y), int(x.y), acc[1][m]));
                 acc[0][m] = __dp4a(int(a.z), int(x.z), __dp4a(int(a.w), int(x.w), acc[0][m]));
                 acc[1][m] = __dp4a(int(b.z), int(x.z), __dp4a(int(b.w), int(x.w), acc[1][m]));
             }
         };
-        const uint4 *p0 = reinterpret_cast<const uint4*>(w0), *p1 = reinterpret_cast<const uint4*>(w1);
-        for (int u0 = mine * 32 + lane; u0 < units; u0 += kTokenDeep * step) {
-            uint4 a[kTokenDeep], b[kTokenDeep];
+        for (int u0 = mine * 32 + lane; u0 < units; u0 += kDeep * step) {
+            uint4 a[kDeep][kParts], b[kDeep][kParts];
 #pragma unroll
-            for (int d = 0; d < kTokenDeep; d++)
-                if (u0 + d * step < units) a[d] = __ldcs(p0 + u0 + d * step), b[d] = __ldcs(p1 + u0 + d * step);
+            for (int d = 0; d < kDeep; d++)
+                if (u0 + d * step < units) {
+                    load(w0 + 16 * (u0 + d * step), a[d]);
+                    load(w1 + 16 * (u0 + d * step), b[d]);
+                }
 #pragma unroll
-            for (int d = 0; d < kTokenDeep; d++)
-                if (u0 + d * step < units) sum(a[d], b[d], u0 + d * step);
+            for (int d = 0; d < kDeep; d++) {
+                const int u = u0 + d * step;
+                if (u < units) sum(meant(w0 + 16 * u, a[d]), meant(w1 + 16 * u, b[d]), u);
+            }
         }
         const int k = units * 16 + lane;   // fewer than 16 are left
         if (mine == 0 && k < r.k) {
@@ -203,7 +227,10 @@ int token_launch(const Rows& r, int num_sms, cudaStream_t s)
     int share = 1;
     while (share < 8 && groups * share < 8 * num_sms && r.k >= 4096 * share) share *= 2;
     const int64_t per = kTokenWarps / share;
-    auto* kernel = r.rows == 1 ? token_kernel<1> : r.rows == 2 ? token_kernel<2> : token_kernel<4>;
+    const bool aligned = aligned_weights(r);
+    auto* kernel = r.rows == 1   ? (aligned ? token_kernel<1, true> : token_kernel<1, false>)
+                   : r.rows == 2 ? (aligned ? token_kernel<2, true> : token_kernel<2, false>)
+                                 : token_kernel<4, true>;
     return proj::launch(kernel, dim3(unsigned((groups + per - 1) / per)), dim3(32 * kTokenWarps), 0, 1, s,
                         "integer token kernel", r, share);
 }
@@ -520,8 +547,8 @@ int rows_launch_of(const RowsArgs& a, bool shift, int ctas, cudaStream_t s)
 
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s)
 {
-    const bool shift = reinterpret_cast<uintptr_t>(r.w) % 16 != 0 || (r.n > 1 && r.w_rs % 16 != 0);
-    if (r.rows <= kTokenRows && !shift) return token_launch(r, num_sms, s);
+    if (for_tokens(r)) return token_launch(r, num_sms, s);
+    const bool shift = !aligned_weights(r);
     RowsArgs a;
     a.r = r;
     const int nt = r.rows <= 8 ? 1 : r.rows <= 16 ? 2 : 4;

@@ -12,8 +12,13 @@ constexpr int64_t kMostSummed = (int64_t(1) << 17) - 1;
 
 // rows that rows_launch takes
 constexpr int kFewRows = 64;
-// and of these the ones that its kernel for tokens takes, of w at multiples of 16 bytes
-constexpr int kTokenRows = 4;
+// and of these the ones that its kernel for tokens takes: of w and x at multiples of 16
+// bytes, and of both at any address
+constexpr int kTokenRows = 4, kAnyTokenRows = 2;
+// Weights up to which it is faster than the streams for rows at any address.  us of it
+// and of them, one or two rows: 4001 x 4003 9.0 and 12.5, 14,336 x 4096 29 and 23; three
+// rows of 4001 x 4003 12.5 and 12.4.
+constexpr int64_t kAnyTokenMost = int64_t(1) << 25;
 // Rows past which wide_launch is faster where it takes the product.  us of
 // rows_launch and of it, 4096 x 4096 weights: 16 rows 9.3 and 10.2, 32 rows 12.0
 // and 10.6; 24 rows of 1024 x 8192 11.6 and 7.9.
@@ -48,6 +53,14 @@ struct Rows {
 };
 // (that kernel needs neither parts nor padded rows of x)
 int rows_launch(const Rows& r, int num_sms, cudaStream_t s);
+inline bool aligned_weights(const Rows& r)
+{
+    return reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (r.n == 1 || r.w_rs % 16 == 0);
+}
+inline bool for_tokens(const Rows& r)
+{
+    return aligned_weights(r) ? r.rows <= kTokenRows : r.rows <= kAnyTokenRows && r.n <= kAnyTokenMost / r.k;
+}
 constexpr int64_t parts_ints(int num_sms) { return int64_t(2 * num_sms) * 32 * 32; }
 
 // Some rows, both operands widened on their way to the tensor cores: rows of x and w

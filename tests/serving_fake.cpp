@@ -24,11 +24,12 @@ int rows_launch(const Rows& r, int num_sms, cudaStream_t)
 {
     B.launches++;
     streamed++;
-    const bool token = r.rows <= kTokenRows && reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (r.n == 1 || r.w_rs % 16 == 0);
+    const bool aligned = reinterpret_cast<uintptr_t>(r.w) % 16 == 0 && (r.n == 1 || r.w_rs % 16 == 0);
+    const bool token = aligned ? r.rows <= 4 : r.rows <= 2 && r.n * r.k <= 1 << 25;
     if (r.rows < 1 || r.rows > kFewRows) wrong("rows", nullptr, r.rows);
     // whole pieces of 64 values, but for up to four rows
     holds("x", r.x, size_t(r.rows - 1) * r.x_rs + (token ? r.k : (r.k + 63) / 64 * 64));
-    if (reinterpret_cast<uintptr_t>(r.x) % 16 || (r.rows > 1 && r.x_rs % 16)) wrong("x at", r.x, 0);
+    if ((aligned || !token) && (reinterpret_cast<uintptr_t>(r.x) % 16 || (r.rows > 1 && r.x_rs % 16))) wrong("x at", r.x, 0);
     if (token) return DPDR_OK;
     if (!r.parts || !r.count) wrong("no parts", nullptr, 0);
     holds("parts", r.parts, size_t(parts_ints(num_sms)) * 4);

@@ -89,6 +89,18 @@ def test_operands_as_they_lie(pkg, rows, how_x, how_w):
         check(pkg, lay(x, how_x), scales(g, rows), lay(w, how_w), scales(g, n), "float32")
 
 
+@pytest.mark.parametrize("rows", [1, 2, 3])
+@pytest.mark.parametrize("k", [1, 15, 16, 17, 32, 1003, 9000])
+def test_tokens_at_any_address(pkg, rows, k):
+    """Every place of x and w within 16 bytes, and others' values on both sides."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    n = 9
+    with pkg.Linear8(rows, k, n, out="float32") as plan:
+        for at in range(16):
+            x, w = bytes_(g, rows, k + 37)[:, 5 * at % 16:][:, :k], bytes_(g, n, k + 37 - at % 3)[:, at:at + k]
+            check(pkg, x, scales(g, rows), w, scales(g, n), "float32", plan=plan)
+
+
 @pytest.mark.parametrize("rows", [1, 5, 12, 40, 80, 300])
 @pytest.mark.parametrize("k", [512, 1024, 4096, 16384, 131071])
 def test_sums_are_exact(pkg, rows, k):

@@ -142,6 +142,8 @@ def test_which_kernel_a_product_takes(fake):
 
     assert call(1) == call(16) == (1, 0, 0, 0)
     assert call(3, "odd") == call(16, "turned") == (1, 0, 0, 1)
+    assert call(1, "odd", "odd") == call(2, "odd", "odd") == (1, 0, 0, 0)
+    assert call(3, "odd", "odd") == (1, 0, 0, 1)
     assert call(17) == call(200) == call(40, "odd", "odd") == (0, 1, 0, 0)
     assert call(9000) == call(5, "plain", "turned") == call(100, "turned") == (0, 0, 1, 1)
     fake.dpdr_integer_destroy(plan)
