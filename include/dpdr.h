@@ -530,11 +530,12 @@ dpdr_integer_t dpdr_integer_plan(int64_t max_rows, int64_t n_in, int64_t n_out,
  * nothing else, except that it may be the residual itself.  Few rows (up to
  * some hundred, as n_out and n_in allow) with rows of x and w contiguous read
  * both in place; others first widen both to 16 bits, exactly, into the plan's
- * scratch.  Scratch is made by the first call that needs it, at the size that
+ * scratch.  That is made by the first call that needs it, at the size that
  * max_rows rows need, and stays where it is until the plan goes: make a call of
- * as many rows, lying alike, before any stream capture.  0 <= rows <= max_rows; asynchronous on stream; the plan's device
- * has to be the current one.  Two calls on one plan that overlap on the GPU
- * race on its scratch, and calls on one plan are not thread-safe. */
+ * as many rows, lying alike, before any stream capture.  0 <= rows <= max_rows;
+ * asynchronous on stream; the plan's device has to be the current one.  Two
+ * calls on one plan that overlap on the GPU race on its scratch, and calls on
+ * one plan are not thread-safe. */
 int dpdr_integer_linear(dpdr_integer_t plan, int64_t rows, const dpdr_matrix* x,
                         const float* x_scale, const dpdr_matrix* w,
                         const float* w_scale, const float* bias,

@@ -17,8 +17,8 @@ struct Integer {
     dpdr_proj_t tiles = nullptr;
     int64_t max_rows = 0, n_in = 0, n_out = 0;
     int out_f32 = 0, half = 0;
-    char* x_copy = nullptr;     // x of few rows, padded; parts and counters of their sums
-    int32_t* parts = nullptr;
+    char* x_copy = nullptr;     // x of few rows, padded
+    int32_t* parts = nullptr;   // of their sums, and counters
     char* wide[2] = {};         // x and w in 16 bits
     bool set[3][2] = {}, wide_set[2] = {};   // kernels' attributes set
     proj::Proj* base() const { return reinterpret_cast<proj::Proj*>(tiles); }
@@ -47,25 +47,9 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
     r.w_rs = P->n_out > 1 ? w.row_stride : P->n_in;
     r.f = f;
     r.set = P->set;
-    int rc = DPDR_OK;
     const bool token = for_tokens(r);
-    if (!P->parts && !token) {   // and the counters behind them, at zero
-        const int64_t ints = parts_ints(num_sms), all = (ints + 2 * num_sms) * 4;
-        rc = hold(P->parts, all, "integer product: parts");
-        if (!rc) {
-            const cudaError_t e = cudaMemsetAsync(P->parts + ints, 0, size_t(2 * num_sms) * 4, s);
-            if (e != cudaSuccess) {   // none, for the next call to make
-                rc = cuda_fail_c(e, "integer product: counters");
-                cudaFree(P->parts);
-                P->parts = nullptr;
-            }
-        }
-        if (rc) return rc;
-    }
-    if (!token) {
-        r.parts = P->parts;
-        r.count = reinterpret_cast<uint32_t*>(P->parts + parts_ints(num_sms));
-    }
+    r.parts = P->parts;
+    r.count = reinterpret_cast<uint32_t*>(P->parts + parts_ints(num_sms));
     // x as it lies where its rows are whole pieces at multiples of 16 bytes, and wherever
     // they are for tokens and weights at any address
     const bool at_16 = reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && (rows == 1 || x.row_stride % 16 == 0);
@@ -73,7 +57,7 @@ int few(Integer* P, int64_t rows, const dpdr_matrix& x, const dpdr_matrix& w, co
         r.x = static_cast<const char*>(x.data);
         r.x_rs = x.row_stride;
     } else {
-        rc = hold(P->x_copy, most * pad, "integer product: operand copy");
+        int rc = hold(P->x_copy, most * pad, "integer product: operand copy");
         if (rc) return rc;
         Relay c;
         c.job[c.n++] = {static_cast<const int8_t*>(x.data), P->x_copy, x.row_stride, x.col_stride, rows, P->n_in,
@@ -194,6 +178,19 @@ extern "C" dpdr_integer_t dpdr_integer_plan(int64_t max_rows, int64_t n_in, int6
     P->tiles = dpdr_linear_plan(max_rows, n_in, n_out, wide, result, wide, DPDR_ACT_NONE);
     if (!P->tiles) {
         delete P;
+        return nullptr;
+    }
+    // counters at zero before any call: a call's own clearing, captured, would wait for its replay
+    const int num_sms = P->base()->num_sms;
+    const int64_t ints = parts_ints(num_sms), counters = 2 * num_sms * 4;
+    int rc = hold(P->parts, ints * 4 + counters, who);
+    if (!rc) {
+        cudaError_t e = cudaMemset(P->parts + ints, 0, size_t(counters));
+        if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
+        if (e != cudaSuccess) rc = cuda_fail_c(e, who);
+    }
+    if (rc) {
+        dpdr_integer_destroy(reinterpret_cast<dpdr_integer_t>(P));
         return nullptr;
     }
     return reinterpret_cast<dpdr_integer_t>(P);

@@ -228,4 +228,9 @@ def test_memory_that_runs_out(fake):
     fake.dpdr_integer_destroy(lin)
     fake.fake_refuse_mallocs(1)
     assert not fake.dpdr_experts_plan(4, 64, 32, 4, 2, 0, 4, BF16, BF16, BF16, 4, 1)
+    lived = fake.fake_live()
+    fake.fake_refuse_mallocs(1)
+    assert not fake.dpdr_integer_plan(4, 64, 32, BF16)
+    fake.fake_refuse_mallocs(0)
+    assert fake.fake_live() == lived
     assert fake.fake_live() == 0 and fake.fake_wrong() == b""
