@@ -14,7 +14,7 @@
 // twelve times that.
 //
 // One row of 4096 x 4096 5.5 us from memory (3.1 TB/s), 16 rows 9.3; 8192 rows of 4096 x
-// 8192 with bias and residual 380 to 393 (1.4 PFLOP/s), 32 of them the copies.
+// 8192 with bias and residual 380 to 397 (1.4 PFLOP/s), 32 of them the copies.
 #include <algorithm>
 
 #include "integer.h"
