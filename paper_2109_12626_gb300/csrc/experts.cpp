@@ -70,11 +70,10 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
     l.local = local;
     l.d = int(n_model);
     l.h = int(n_hidden);
-    // a piece of 64 bytes of a row of weights has at most 64 elements
-    l.d_pad = upto(n_model, 64);
-    l.h_pad = upto(n_hidden, 64);
     l.half = operands == DPDR_FLOAT16;
     l.w_int8 = weights == DPDR_INT8;
+    l.d_pad = upto(n_model, l.w_int8 ? kPad8 : kPad);
+    l.h_pad = upto(n_hidden, kPad);
     l.act = act;
     l.terms = l.half && !l.w_int8 ? 1 : result == DPDR_FLOAT32 ? 3 : 2;
     l.pairs = l.rows * top;

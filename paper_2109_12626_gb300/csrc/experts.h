@@ -12,11 +12,15 @@ constexpr int kMostTop = 16;        // of them chosen, a lane each
 constexpr int kMostExperts = 512;   // 16 a lane of a warp
 constexpr int64_t kMostSize = 1 << 20;
 constexpr int kWholeRows = 8;       // of which each has a column of its own in the last product
+// Columns of the products (x, hidden values) are read by whole pieces of the rows of
+// weights, so a row of them is a multiple of the elements that a piece has at most: in
+// the up products of 8-bit weights 128, else 64 (checked where the pieces are chosen).
+constexpr int kPad = 64, kPad8 = 128;
 
 struct Layer {
     int rows, top, total, first, local;
     int d, h;                      // n_model, n_hidden
-    int64_t d_pad, h_pad;          // a row of the copy of x, of the hidden values
+    int64_t d_pad, h_pad;          // a row of the copy of x, of the hidden values (kPad)
     int half;                      // operand type: 0 bfloat16, 1 float16
     int w_int8, act, normalise, out_f32;
     const char* x;

@@ -97,6 +97,7 @@ __device__ __forceinline__ void down_units(const Layer& l, const Choice& c, char
 {
     // float16 weights take the float32 values, others their terms
     constexpr int kXT = TERMS == 1 ? kF32 : kBf16, kPiece = piece_of(WT, kXT, NT, SHIFT, TERMS);
+    static_assert(kPad % (kPiece / size_of(WT)) == 0, "a piece stays in its row of hidden values");
     using S = Stream<WT, kXT, NT, SHIFT, TERMS, kPiece, 1, WHOLE>;
     S st(shared_at(raw), warp, lane, l.pairs * l.h_pad * size_of(kXT));
     const Down<WT, NT, kXT, WHOLE> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);

@@ -100,6 +100,7 @@ template <int WT, int XT, int NT, bool SHIFT, bool FEW>
 __device__ __forceinline__ void up_units(const Layer& l, const Choice& c, char* raw, int warp, int lane)
 {
     constexpr int kPiece = piece_of(WT, XT, NT, SHIFT, 1);
+    static_assert((WT == kI8 ? kPad8 : kPad) % (kPiece / size_of(WT)) == 0, "a piece stays in its row of x");
     using S = Stream<WT, XT, NT, SHIFT, 1, kPiece, 1>;
     S st(shared_at(raw), warp, lane);
     const Up<WT, XT, NT> job(l, c, reinterpret_cast<float*>(raw + kRings) + warp * kTile, lane);
