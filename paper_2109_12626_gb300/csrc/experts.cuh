@@ -19,7 +19,8 @@ namespace {
 struct Choice {
     float* share;         // of a pair
     uint32_t* entry;      // an expert with up to `most` of its pairs: number among
-                          // the local ones, how many pairs, the first of them in `order`
+                          // the local ones, how many pairs, the first of them in `order`,
+                          // which of the first 8 tokens chose it
     int16_t* expert;      // of a pair
     int16_t* order;       // pairs, those of an expert together, by token
     int entries, columns; // the most pairs of an entry
@@ -31,13 +32,15 @@ struct Choice {
           order(expert + pairs)
     {
     }
-    static __device__ __forceinline__ uint32_t packed(int e, int n, int from)
+    static __device__ __forceinline__ uint32_t packed(int e, int n, int from, uint32_t tokens)
     {
-        return uint32_t(e) | uint32_t(n) << 10 | uint32_t(from) << 17;
+        static_assert(kMostExperts <= 1 << 9 && kMostRows * kMostTop <= 1 << 10 && kWholeRows <= 8, "9, 5, 10 and 8 bits");
+        return uint32_t(e) | uint32_t(n - 1) << 9 | uint32_t(from) << 14 | tokens << 24;
     }
-    __device__ __forceinline__ int number(int i) const { return entry[i] & 1023u; }
-    __device__ __forceinline__ int count(int i) const { return entry[i] >> 10 & 127u; }
-    __device__ __forceinline__ int from(int i) const { return entry[i] >> 17; }
+    __device__ __forceinline__ int number(int i) const { return entry[i] & 511u; }
+    __device__ __forceinline__ int count(int i) const { return (entry[i] >> 9 & 31u) + 1; }
+    __device__ __forceinline__ int from(int i) const { return entry[i] >> 14 & 1023u; }
+    __device__ __forceinline__ uint32_t chose(int i) const { return entry[i] >> 24; }
 };
 
 // The lists of it, in every CTA alike.  `room`: shared memory that is free so far, 10
@@ -53,7 +56,7 @@ __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int wa
             const bool here = e >= 0 && e < l.local;
             const uint32_t all = __ballot_sync(0xFFFFFFFFu, here);
             const int at = __popc(all & ((1u << lane) - 1));
-            if (here) c.entry[at] = Choice::packed(e, 1, at), c.order[at] = int16_t(lane);
+            if (here) c.entry[at] = Choice::packed(e, 1, at, 1u), c.order[at] = int16_t(lane);
             if (lane < pairs) c.share[lane] = share;
             if (lane == 0) entries = __popc(all);
         }
@@ -105,7 +108,7 @@ __device__ void list_all(const Layer& l, Choice& c, char* room, int most, int wa
     int p0 = (to - sum) & 0xFFFF, i0 = (to - sum) >> 16;
     for (int i = 0; i < each && e0 + i < l.local; i++) {
         from[e0 + i] = int16_t(p0);
-        for (int k = 0; k < n[i]; k += most) c.entry[i0++] = Choice::packed(e0 + i, min(most, n[i] - k), p0 + k);
+        for (int k = 0; k < n[i]; k += most) c.entry[i0++] = Choice::packed(e0 + i, min(most, n[i] - k), p0 + k, uint32_t(mask[e0 + i]));
         p0 += n[i];
     }
     __syncthreads();
@@ -172,7 +175,8 @@ struct Run {
 #pragma unroll
                     for (int n = 0; n < NT; n++)
 #pragma unroll
-                        for (int j = 0; j < 4; j++) sum[k][n][j] += part[k][n][j] * by[2 * k + j / 2];
+                        for (int j = 0; j < 4; j++)
+                            if (!S::kZeros || st.counts[j & 1]) sum[k][n][j] += part[k][n][j] * by[2 * k + j / 2];
             } else {
                 st.sums(q, sum, next);
             }

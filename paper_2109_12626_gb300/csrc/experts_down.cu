@@ -9,8 +9,9 @@ using namespace stream;
 namespace {
 
 // Of up to 8 tokens: units of 32 features of the result, their sums over all
-// entries one after another, a column a token; one that did not choose an entry has
-// zeros there.  Of more: units of 32 features and an entry, their results to
+// entries one after another, a column a token.  One that did not choose an entry has
+// zeros there, whose sums are left out: an infinity or NaN among the entry's weights or
+// scales would make them NaN.  Of more: units of 32 features and an entry, their results to
 // z by pairs.
 template <int WT, int NT, int XT, bool WHOLE>
 struct Down {
@@ -48,6 +49,7 @@ struct Down {
         q.row_bytes = l.h * size_of(WT);
         q.first = first;
         q.last = last;
+        if (WHOLE) q.counts = c.chose(entry(p));
         return q;
     }
     __device__ __forceinline__ auto columns(int p) const

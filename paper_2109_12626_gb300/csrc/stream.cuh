@@ -206,6 +206,7 @@ struct Unit {
     int rows_left[2];        // rows that there are, of 16; rows_left[0] >= 1
     int row_bytes;
     int first, last;         // pieces along k
+    uint32_t counts = 0;     // with ZEROS: bits of the columns whose sums are wanted
     __device__ __forceinline__ const char* row(int r) const
     {
         const int in = r & 15;
@@ -216,10 +217,12 @@ struct Unit {
 
 // TERMS: a column's values are the sums of so many, whose arrays lie `apart`
 // bytes from each other.  PIECE: bytes of a row of A, a stage.  STEP: a warp takes
-// every STEP-th piece of a unit.  ZEROS: some columns are zeros.
+// every STEP-th piece of a unit.  ZEROS: some columns are zeros, whose sums with
+// infinities and NaN among the weights are left out.
 template <int WT, int XT, int NT, bool SHIFT, int TERMS, int PIECE, int STEP, bool ZEROS = false>
 struct Stream {
     static constexpr int kPiece = PIECE;
+    static constexpr bool kZeros = ZEROS;
     static constexpr int kParts = kPiece / 64;           // a lane has 16 bytes of a row in each
     static constexpr int kK = 64 / size_of(WT);          // elements of a part
     static constexpr int kAChunks = kPiece / 16 + SHIFT; // 16-byte chunks of a row
@@ -250,6 +253,7 @@ struct Stream {
     // using side
     uint32_t use_from_here;
     int shift[2][2];         // of this lane's rows
+    bool counts[2];          // this lane's columns
 
     __device__ __forceinline__ Stream(uint32_t ring_of_cta, int w, int l, int64_t terms_apart = 0)
         : lane(l),
@@ -365,6 +369,11 @@ struct Stream {
 
     __device__ __forceinline__ void use_from(const Unit& u)
     {
+        if (ZEROS) {
+            static_assert(!ZEROS || NT == 1, "a bit a column");
+            counts[0] = u.counts >> 2 * (lane & 3) & 1u;
+            counts[1] = u.counts >> 2 * (lane & 3) & 2u;
+        }
         if (SHIFT)
 #pragma unroll
             for (int i = 0; i < 2; i++)
@@ -439,7 +448,8 @@ struct Stream {
 #pragma unroll
                 for (int n = 0; n < NT; n++)
 #pragma unroll
-                    for (int q = 0; q < 4; q++) sum[i][n][q] += high[i][n][q] + low[i][n][q];
+                    for (int q = 0; q < 4; q++)
+                        if (!ZEROS || counts[q & 1]) sum[i][n][q] += high[i][n][q] + low[i][n][q];
         } else {
             // words of two elements: four a lane and row, of 8-bit weights eight
             constexpr int kWords = kK / 8;
@@ -500,7 +510,8 @@ struct Stream {
 #pragma unroll
                         for (int i = 0; i < 2; i++)
 #pragma unroll
-                            for (int q = 0; q < 4; q++) sum[i][n][q] += d[i][q];
+                            for (int q = 0; q < 4; q++)
+                                if (!ZEROS || counts[q & 1]) sum[i][n][q] += d[i][q];
                 }
             }
         }
