@@ -559,7 +559,8 @@ void dpdr_integer_destroy(dpdr_integer_t plan);
  * slice of every expert's hidden features (n_hidden is then the slice's); either
  * way y, in float32, is its share of a sum that dpdr_allreduce adds up.  A token
  * none of whose experts is here gets zeros.  Everything between x and y is held
- * in float32; hidden values enter the last product with 21 bits. */
+ * in float32; hidden values enter the last product with 24 bits, past float16
+ * weights with 21. */
 typedef struct {
     void* data;              /* device memory, aligned to its element       */
     int64_t stride;          /* elements from one matrix to the next        */

@@ -75,7 +75,7 @@ extern "C" dpdr_experts_t dpdr_experts_plan(int64_t max_rows, int64_t n_model, i
     l.d_pad = upto(n_model, l.w_int8 ? kPad8 : kPad);
     l.h_pad = upto(n_hidden, kPad);
     l.act = act;
-    l.terms = l.half && !l.w_int8 ? 1 : result == DPDR_FLOAT32 ? 3 : 2;
+    l.terms = l.half && !l.w_int8 ? 1 : 3;
     l.pairs = l.rows * top;
     l.normalise = normalise != 0;
     l.out_f32 = result == DPDR_FLOAT32;

@@ -36,7 +36,7 @@ struct Layer {
     // scratch of the plan
     float* logits;                 // rows by total
     char* x_copy;                  // rows by d_pad, zero behind d
-    // rows top by h_pad, zero behind h: terms of bfloat16, an array each of `pairs`
+    // rows top by h_pad, zero behind h: three terms of bfloat16, an array each of `pairs`
     // rows (the most that the plan takes), or with terms 1 float32
     char* hidden;
     int terms, pairs;

@@ -134,9 +134,8 @@ __global__ void __launch_bounds__(bound_of(FEW), 2) down_kernel(const __grid_con
 template <bool SHIFT, bool FEW>
 Kernel down_of(const Layer& l)
 {
-    if (l.w_int8) return l.terms == 2 ? down_kernel<kI8, SHIFT, 2, FEW> : down_kernel<kI8, SHIFT, 3, FEW>;
-    if (l.half) return down_kernel<kF16, SHIFT, 1, FEW>;
-    return l.terms == 2 ? down_kernel<kBf16, SHIFT, 2, FEW> : down_kernel<kBf16, SHIFT, 3, FEW>;
+    if (l.w_int8) return down_kernel<kI8, SHIFT, 3, FEW>;
+    return l.half ? down_kernel<kF16, SHIFT, 1, FEW> : down_kernel<kBf16, SHIFT, 3, FEW>;
 }
 
 }  // namespace

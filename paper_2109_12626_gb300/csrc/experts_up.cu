@@ -15,12 +15,12 @@ __device__ __forceinline__ void put_hidden(const Layer& l, int pair, int feature
         return;
     }
     uint16_t v[3];
-    split_bf16(h, l.terms, v);
+    split_bf16(h, v);
     uint16_t* to = reinterpret_cast<uint16_t*>(l.hidden) + pair * l.h_pad + feature;
     const int64_t apart = l.pairs * l.h_pad;
     to[0] = v[0];
     to[apart] = v[1];
-    if (l.terms == 3) to[2 * apart] = v[2];
+    to[2 * apart] = v[2];
 }
 
 // Units of 16 hidden features of an entry

@@ -174,9 +174,9 @@ __device__ __forceinline__ void split_tf32(float h, float& hi, float& lo)
     lo = (top & 0x7F800000u) == 0x7F800000u ? 0.0f : h - hi;
 }
 
-// h as bfloat16 values that add up to it: of two terms the first 8 bits and the
-// rest rounded (2^-16 of h), of three all 24 bits.  Infinities and NaN have one.
-__device__ __forceinline__ void split_bf16(float h, int terms, uint16_t (&t)[3])
+// h as three bfloat16 values of 8 bits each that add up to it.  Infinities and NaN
+// have one.
+__device__ __forceinline__ void split_bf16(float h, uint16_t (&t)[3])
 {
     const uint32_t b = __float_as_uint(h);
     t[0] = uint16_t(b >> 16);
@@ -186,13 +186,9 @@ __device__ __forceinline__ void split_bf16(float h, int terms, uint16_t (&t)[3])
         return;
     }
     const float r = h - __uint_as_float(b & 0xFFFF0000u);
-    if (terms == 2) {
-        t[1] = __bfloat16_as_ushort(__float2bfloat16_rn(r));
-    } else {
-        const uint32_t c = __float_as_uint(r);
-        t[1] = uint16_t(c >> 16);
-        t[2] = uint16_t(__float_as_uint(r - __uint_as_float(c & 0xFFFF0000u)) >> 16);
-    }
+    const uint32_t c = __float_as_uint(r);
+    t[1] = uint16_t(c >> 16);
+    t[2] = uint16_t(__float_as_uint(r - __uint_as_float(c & 0xFFFF0000u)) >> 16);
 }
 
 // ---------------------------------------------------------------- a unit
