@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
         S::clear(sum);
         st.sums(q, sum, next);
 #pragma unroll
-        for (int n = 0; n < NT; n++) v[n] = __float_as_int(join_columns<true>(room, sum[0][n], sum[1][n], warp, lane));
+        for (int n = 0; n < NT; n++) v[n] = join_columns(room, sum[0][n], sum[1][n], warp, lane);
         if (a.parts > 1) {
             int32_t* mine = r.parts + int64_t(u) * NT * kThreads + threadIdx.x;
 #pragma unroll

@@ -233,6 +233,7 @@ struct Stream {
     static constexpr int kStages = kRing / kStage > 5 ? 5 : kRing / kStage;
     static constexpr int kWarpBytes = kStages * kStage;
     static_assert(kStages >= 2, "the ring holds two stages");
+    static_assert(!SHIFT || kALoads <= 8, "four bits a load");
     static constexpr bool kWhole = XT == kI8;            // sums are integers
     static constexpr int kRun = 1024 / (kParts * kK);    // pieces whose products float32 sums exactly
 
@@ -244,7 +245,7 @@ struct Stream {
     int b_bytes[NT * kBLoads];   // 0: a column of zeros
     int64_t apart;
     int load_piece, load_last, load_whole;   // pieces before load_whole are inside every row
-    int load_bytes, load_shift;              // of a row
+    int load_bytes, load_shift;              // of a row; of the loads, four bits each
     uint32_t load_to, load_end;
     // using side
     uint32_t use_from_here;
@@ -303,12 +304,10 @@ struct Stream {
         if (SHIFT) {   // what the last pieces have to know of each row
             load_shift = 0;
 #pragma unroll
-            for (int i = 0; i < kALoads && i < 8; i++)
+            for (int i = 0; i < kALoads; i++)
                 load_shift |= int(reinterpret_cast<uintptr_t>(u.row(a_row(i))) & 15) << 4 * i;
-            if (kALoads > 8) load_last_shift = int(reinterpret_cast<uintptr_t>(u.row(a_row(kALoads - 1))) & 15);
         }
     }
-    int load_last_shift;
 
     __device__ __forceinline__ bool more() const { return load_piece < load_last; }
 
@@ -318,9 +317,9 @@ struct Stream {
     static __device__ __forceinline__ int b_place(int r, int c)
     {
         constexpr int kApart = kBChunks / kParts / 4;   // chunks of a lane in a part
+        static_assert(kApart == 1 || kApart == 2, "one or two");
         if (kApart == 1) return r * kB + 16 * (kParts == 1 ? c : c ^ ((r & 1) << 2));
-        if (kApart == 2) return r * kB + 16 * (c ^ (r & 1));
-        return r * kB + 16 * (c ^ ((c >> 3) & 1) ^ ((r & 1) << 1));
+        return r * kB + 16 * (c ^ (r & 1));
     }
     static __device__ __forceinline__ int a_place(int r, int c)
     {
@@ -336,7 +335,7 @@ struct Stream {
             const int left = load_bytes - load_piece * kPiece;
 #pragma unroll
             for (int i = 0; i < kALoads; i++) {
-                const int o = SHIFT ? (i < 8 ? load_shift >> 4 * i & 15 : load_last_shift) : 0;
+                const int o = SHIFT ? load_shift >> 4 * i & 15 : 0;
                 const int bytes = max(0, min(16, left + o - 16 * a_chunk(i)));
                 // of none, the address of the row's first bytes in this piece
                 copy16(load_to + a_to(i), a_at[i] - (bytes > 0 ? 0 : 16 * a_chunk(i)), bytes);
@@ -577,9 +576,6 @@ struct Stream {
     }
 };
 
-// The eight warps' sums of 8 columns, joined in the order of the warps: thread
-// `threadIdx.x` gets those of row threadIdx.x % 32, column threadIdx.x / 32.  `room`:
-// kJoin floats of shared memory.
 constexpr int kJoinPitch = kRows + 4;                     // floats of a column
 constexpr int kTile = 8 * kJoinPitch;                     // of a warp
 constexpr int kJoin = kWarps * kTile;
@@ -608,9 +604,11 @@ __device__ __forceinline__ void add_tile(const float* tile, float (&first)[4], f
     }
 }
 
-template <bool WHOLE>
-__device__ __forceinline__ float join_columns(float* room, const float (&first)[4], const float (&second)[4], int warp,
-                                              int lane)
+// The eight warps' sums of 8 columns, held as integers, added up: thread `threadIdx.x` gets
+// those of row threadIdx.x % 32, column threadIdx.x / 32.  `room`: kJoin floats of shared
+// memory.
+__device__ __forceinline__ int join_columns(float* room, const float (&first)[4], const float (&second)[4], int warp,
+                                            int lane)
 {
     put_tile(room + warp * kTile, first, second, lane);
     __syncthreads();
@@ -619,15 +617,9 @@ __device__ __forceinline__ float join_columns(float* room, const float (&first)[
 #pragma unroll
     for (int w = 0; w < kWarps; w++) v[w] = at[w * kTile];
     __syncthreads();
-    if (WHOLE) {
-        int s = __float_as_int(v[0]);
+    int s = __float_as_int(v[0]);
 #pragma unroll
-        for (int w = 1; w < kWarps; w++) s += __float_as_int(v[w]);
-        return __int_as_float(s);
-    }
-    float s = v[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; w++) s += v[w];
+    for (int w = 1; w < kWarps; w++) s += __float_as_int(v[w]);
     return s;
 }
 
