@@ -499,7 +499,7 @@ void dpdr_proj_destroy(dpdr_proj_t plan);
  *
  *   quantise   scale = a / 127, a the largest size in the row;
  *              q = 127 x / a rounded to the nearest whole number, halves to even
- *   product    y = (sum_k x w) x_scale w_scale + bias + residual
+ *   product    y = (sum_k x w) (x_scale w_scale) + bias + residual
  *
  * With float32 results a product is one rank's share of a row-parallel product,
  * which dpdr_allreduce adds up, and the sums of a reduction are what is rounded
@@ -527,10 +527,14 @@ dpdr_integer_t dpdr_integer_plan(int64_t max_rows, int64_t n_in, int64_t n_out,
 /* x: rows by n_in, w: n_out by n_in, int8, any strides >= 0; x_scale: rows,
  * w_scale: n_out, bias: n_out or NULL, float32 and contiguous; residual: any
  * strides, or NULL; y: col_stride 1, rows that do not overlap.  y overlaps
- * nothing else, except that it may be the residual itself.  Few rows (up to
- * some hundred, as n_out and n_in allow) with rows of x and w contiguous read
- * both in place; others first widen both to 16 bits, exactly, into the plan's
- * scratch.  That is made by the first call that needs it, at the size that
+ * nothing else, except that it may be the residual itself.  The scales' product
+ * is formed first, in float32, and has to be a normal number or 0 (1.2e-38 to
+ * 3.4e38): below, y loses places, past it sums of 0 give NaN.  Where w's rows are
+ * contiguous up to 64 rows read both operands in place, where x's are too also
+ * more, as many as leave the GPU room for parts of the sum (on 152 SMs up to 128
+ * rows of 9728 features, 256 of 4864, 384 of 3200; n_in from 385 on, up to 8192
+ * at least); others first widen both to 16 bits, exactly, into the plan's scratch
+ * (2 bytes for each of (max_rows + n_out) n_in elements).  That is made by the first call that needs it, at the size that
  * max_rows rows need, and stays where it is until the plan goes: make a call of
  * as many rows, lying alike, before any stream capture.  0 <= rows <= max_rows;
  * asynchronous on stream; the plan's device has to be the current one.  Two
@@ -560,7 +564,9 @@ void dpdr_integer_destroy(dpdr_integer_t plan);
  * way y, in float32, is its share of a sum that dpdr_allreduce adds up.  A token
  * none of whose experts is here gets zeros.  Everything between x and y is held
  * in float32; hidden values enter the last product with 24 bits, past float16
- * weights with 21. */
+ * weights with 21.  Infinities and NaN of a token, and of an expert's weights and
+ * scales, reach that token's result, and those of the tokens that chose the expert,
+ * alone; an infinity among w_down gives them infinities or NaN. */
 typedef struct {
     void* data;              /* device memory, aligned to its element       */
     int64_t stride;          /* elements from one matrix to the next        */

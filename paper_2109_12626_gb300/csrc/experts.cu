@@ -22,12 +22,13 @@
 // 1024 125 us instead of 106.)
 //
 // Bound by the weights' bytes from some 50 MB of chosen experts on: 64 rows of 128
-// experts of 2048 x 1024, 8 a token, 1.6 GB in 286 to 291 us (5.5 TB/s), 8 rows of 64
-// such experts 0.5 GB in 103 to 106 (5.1).  One token of 8 experts of 4096 x 1792, 2 a
-// token, 88 MB in 29 us, is a chain: scores and choice 4 us, lists 1, the up weights 11,
-// joining a unit's parts 3, the down weights 5, joining those 3.  8-bit weights are
+// experts of 2048 x 1024, 8 a token, 1.6 GB in 282 to 298 us (5.4 TB/s), 8 rows of 64
+// such experts 0.5 GB in 100 to 106 (5.1).  One token of 8 experts of 4096 x 1792, 2 a
+// token, 88 MB in 30 us, is a chain: scores and choice 4 us, lists 1, the up weights 11,
+// joining a unit's parts 3, the down weights 5, joining those 3, the rest the ends and
+// beginnings of kernels.  8-bit weights are
 // widened in registers, which takes the issue slots to their limit: 16 rows of 64 such
-// experts 0.36 GB in 92 us.
+// experts 0.36 GB in 90 us.
 //
 // The hidden values are not rounded to 16 bits: they are kept as three terms of bfloat16,
 // which hold all of a float32 value, and for float16 weights as float32, of which the
@@ -280,8 +281,9 @@ int product_ctas(Layer& l, int num_sms)
         }
     }
     if (e != cudaSuccess) return cuda_fail_c(e, "experts kernels");
-    // two CTAs an SM, as their registers allow, where it has shared memory for them: with
-    // what the system takes of each and what the kernels hold besides
+    // Two CTAs an SM, as their registers allow, where it has shared memory for them: with
+    // what the system takes of each and what the kernels hold besides.  That is up to 640
+    // pairs of the plan's largest call; plans for more run every call on one an SM.
     const size_t each = product_smem(l) + 1024 + 512;
     l.ctas = (2 * each <= size_t(an_sm) ? 2 : 1) * num_sms;
     return DPDR_OK;

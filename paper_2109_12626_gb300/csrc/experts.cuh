@@ -288,8 +288,8 @@ constexpr int kRings = kWarps * kRing, kBefore = kRings + kJoin * 4;
 
 // Bytes of a row of weights that a stage holds.  Where widening binds (8-bit weights,
 // tf32) 128 bytes save turns of the loop, if the ring holds two such stages; else more
-// and smaller ones keep more under way.  With 64 and 128: 16 rows of 64 experts in 8
-// bits 91 and 89 us, 8 rows in 16 bits 100.7 and 102.3.
+// and smaller ones keep more under way.  With 64 and 128, on one GPU: 16 rows of 64
+// experts in 8 bits 91 and 89 us, 8 rows in 16 bits 100.7 and 102.3.
 constexpr int piece_of(int wt, int xt, int nt, bool shift, int terms)
 {
     const int stage = kRows * (128 + 16 * shift) + terms * nt * 8 * (128 / size_of(wt)) * size_of(xt);

@@ -459,7 +459,8 @@ __global__ void __launch_bounds__(SHARE < 256 ? 256 : SHARE)
     }
 }
 
-// Rows that lie otherwise: a CTA a row, value by value, read twice
+// Rows that lie otherwise: a CTA a row, value by value, read twice: 8192 x 8191 float32 in
+// 100 us (of 8192 values 52), 4096 x 4095 bfloat16 in 32 (15)
 template <int DT>
 __global__ void __launch_bounds__(256)
     quantise_any_kernel(const void* x, int64_t rs, int64_t cs, int8_t* q, int64_t q_rs, float* scale, int64_t n)

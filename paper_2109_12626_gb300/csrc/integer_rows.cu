@@ -19,7 +19,9 @@
 // by 128 values, of which the products are 512).  4096 x 4096 weights: 32 rows 10.6 us,
 // 128 rows 13.9, 256 rows 20.1 (two tiles of columns), where widened copies and the
 // tiles take 26.  From where tiles leave no SMs for parts of the sum these are faster:
-// 512 rows 27.5 and 32.7 us.
+// 512 rows 27.5 and 32.7 us.  Features past some thousand go that way too from 65 rows on (128
+// rows of 8192 to 28,672 210 us, of which the bytes take 35); this kernel unsplit is not
+// measured there.
 #include "integer.h"
 #include "proj_common.cuh"
 #include "proj_launch.cuh"

@@ -108,7 +108,8 @@ __device__ __forceinline__ uint4 shifted(const uint4& lo, const uint4& hi, int o
 
 // ------------------------------------------------------- 8 bits widened
 
-// Four 8-bit integers as float16: 1024 + (v + 128) has v + 128 in its low bits
+// Four 8-bit integers as float16, by the known way of putting a whole number into the
+// low bits of a float whose last bit counts one: 1024 + (v + 128) has v + 128 there
 __device__ __forceinline__ void bytes_to_f16(uint32_t v, uint32_t& a, uint32_t& b)
 {
     v ^= 0x80808080u;

@@ -103,7 +103,8 @@ class Linear8(_Serving):
     int8 [n_out, n_in], x_scale [rows], w_scale and bias [n_out] in float32.
 
     ``out`` is the type of y and the residual ("bfloat16", "float16",
-    "float32").  Sums are exact.  x, w and the residual may have any strides."""
+    "float32").  Sums are exact.  x, w and the residual may have any strides.
+    x_scale w_scale has to be a normal float32 number or 0."""
 
     _end = ("dpdr_integer_sync", "dpdr_integer_destroy")
     _args = 4
